@@ -46,13 +46,15 @@ typedef enum {
     GRAFT_ERR_STATE = 5        /* call order: TDES tables or SABA parameters not set */
 } graft_status;
 
-typedef enum { GRAFT_F32 = 0, GRAFT_BF16 = 1 } graft_dtype;
+typedef enum { GRAFT_F32 = 0, GRAFT_BF16 = 1, GRAFT_E4M3 = 2 /* entries of a graft_cache only */ } graft_dtype;
 
 /* per-sequence bits written to d_status */
 #define GRAFT_ST_BAD_LOGITS 1     /* a logits row holds NaN or +inf, or no finite entry (entries below -1e9 may count as none): root-only tree */
 #define GRAFT_ST_TAU_CLAMPED 2    /* SABA: phi . s_t fell below tau_min and was clamped */
 #define GRAFT_ST_FRONTIER_EMPTY 4 /* fewer reachable prefixes than the budget */
 #define GRAFT_ST_INTERNAL 8       /* a bounded device-side wait ran out (should never happen) */
+#define GRAFT_ST_BAD_CACHE 16     /* a slot that is needed lies beyond the table or in a page outside the cache, or a count is out of range */
+#define GRAFT_ST_BAD_TREE 32      /* n_nodes outside [1, rows] */
 
 typedef struct {
     int32_t V;          /* vocabulary size */
@@ -246,6 +248,89 @@ graft_status graft_accept(graft_ctx* ctx, int32_t batch, const graft_tree_out* t
  * d_hist argument of the next graft_build_trees.  w in [1, 64]; w = 0 (pointers ignored) switches it off.
  * Host-only call; the buffers are borrowed until it is called again or the context is destroyed. */
 graft_status graft_set_hist_window(graft_ctx* ctx, int32_t w, int32_t* d_window, int32_t* d_count, float* d_hist);
+
+/* ---- verification of the trees -----------------------------------------------------------------------------------------
+ * What a target model needs of this library between graft_build_trees and the next round: a paged key/value cache, attention of
+ * the trees' nodes over it, the walk that keeps the target's distribution, and the accepted nodes' entries moved up.  (The paper
+ * leaves the verifier to the reader; its tree attention is the mask of Sec. 3.1.)
+ *
+ * A cache of `layers` layers.  Sequence b's slot s (s = 0, 1, ... in token order) lives in page d_table[b, s / page_size], place
+ * s % page_size; d_table [batch, table_width] int32, device.  In every call below row i of sequence b belongs to slot
+ * d_prefix_len[b] - 1 + i, as d_position of graft_build_trees says of the root (row 0, the last committed token) and of chains; a
+ * tree's nodes stand in node order.  Prompts start with d_prefix_len = 1.
+ *
+ * GRAFT_BF16: entries as they come.  GRAFT_E4M3: a row x (one token, one head, K or V) is held as e4m3 numbers y = x 2^-e, rounded
+ * to nearest even, and e + 127 in a byte, e the smallest whole number with max |x| <= 448 2^e, at least -120.  A power of two costs
+ * no precision (what is not below 2^-13 of its row's largest keeps its four bits) and makes reading back exact in bf16.  A row with a NaN or an infinity: byte 255, reads back as NaN.
+ *
+ * A sequence that would touch a slot beyond its table or a page outside [0, n_pages), or whose prefix length is below 1 or whose
+ * count is negative or above `rows`, is left out of the call as a whole: nothing of it is read or written, and d_status[b] (may be
+ * NULL; overwritten, 0 when all is well) is GRAFT_ST_BAD_CACHE.  Entries of the table behind the slots in use are not read.
+ * Pages may be shared between sequences as long as no call writes to them.
+ * Limits: head_dim 64 or 128, page_size a power of two from 16 to 1024, kv_heads * n_pages * page_size < 2^31, d_k, d_v, and rows of
+ * q, key, value and out 16-byte aligned, batch <= cfg.max_batch. */
+typedef struct graft_cache {
+    int32_t layers, n_pages, kv_heads, page_size, head_dim;
+    graft_dtype dtype;        /* GRAFT_BF16 or GRAFT_E4M3 */
+    void* d_k;                /* [layers, n_pages, kv_heads, page_size, head_dim] */
+    void* d_v;                /* the same */
+    uint8_t* d_k_exp;         /* E4M3: [layers, n_pages, kv_heads, page_size]; else NULL */
+    uint8_t* d_v_exp;
+    const int32_t* d_table;   /* [batch, table_width] */
+    int32_t table_width;
+} graft_cache;
+
+/* New entries of one layer: d_key, d_value [batch, rows, kv_heads, head_dim] bf16, a row `stride` elements behind the one before (a
+ * multiple of 8; kv_heads * head_dim when dense, more for slices of a fused projection; sequences rows * stride apart).
+ * d_count [batch]: rows in use (n_nodes of the trees); the others are neither read nor written. */
+graft_status graft_cache_write(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer,
+                               const int32_t* d_prefix_len, const int32_t* d_count, int32_t rows, int64_t stride, const void* d_key,
+                               const void* d_value, int32_t* d_status, void* stream);
+/* The entries of the same slots back, as bf16 [batch, rows, kv_heads, head_dim] dense; rows behind the count are left as they were. */
+graft_status graft_cache_read(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer,
+                              const int32_t* d_prefix_len, const int32_t* d_count, int32_t rows, void* d_key, void* d_value,
+                              int32_t* d_status, void* stream);
+/* After the walk: entry d_prefix_len[b] - 1 + d_accept_path[b, k] becomes entry d_prefix_len[b] + k for every k < d_accept_len[b], in all
+ * layers, as if all were read before one is written; the cache then holds the committed tokens and the next round's root (the bonus
+ * token) is its next row.  d_accept_path [batch, L].  d_next_prefix [batch] or NULL: d_prefix_len + d_accept_len + 1 (may be the same
+ * array as d_prefix_len); a sequence with GRAFT_ST_BAD_CACHE (an accepted length outside [0, L], a node below 0 also give it) keeps its
+ * prefix length. */
+graft_status graft_cache_keep(graft_ctx* ctx, int32_t batch, const graft_cache* cache, const int32_t* d_prefix_len,
+                              const int32_t* d_accept_len, const int32_t* d_accept_path, int32_t* d_next_prefix, int32_t* d_status,
+                              void* stream);
+
+/* Attention of the rows of a call over the cache of one layer, their own entries (graft_cache_write) among it.
+ *   d_q [batch, rows, q_heads, head_dim] bf16, row stride q_stride (as `stride` above); query head h reads key head
+ *   h / (q_heads / kv_heads).  Row i < d_count[b] sees every slot before d_prefix_len[b] - 1 and of the new slots j < d_count[b] those with
+ *   bit j of d_mask[b, i] set (d_mask [batch, Nmax, W] as graft_build_trees emits it; then rows <= Nmax), or those with j <= i where
+ *   d_mask is NULL (single tokens, chains, chunks of a prompt).
+ *   d_out [batch, rows, q_heads, head_dim] bf16 dense: sum_j p_j v_j, p = softmax(scale q . k_j); d_lse [batch, rows, q_heads] fp32 or
+ *   NULL: log sum_j exp(scale q . k_j).  A row that sees nothing: 0 and -inf.  Rows behind the count are left as they were.
+ *   shared: the first `shared` slots (a multiple of page_size; 0: none) are the same pages in every sequence's table (sequence 0's
+ *   are read) and are gone through once for the rows of all sequences; every prefix_len is above `shared` (else GRAFT_ST_BAD_CACHE).
+ * Scores, statistics and sums are fp32; the weights p enter the second product as bf16, as a bf16 cache's values do. */
+graft_status graft_tree_attention(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer, int32_t q_heads,
+                                  int32_t rows, int64_t q_stride, const void* d_q, float scale, const int32_t* d_prefix_len,
+                                  const int32_t* d_count, const uint32_t* d_mask, int32_t shared, void* d_out, float* d_lse,
+                                  int32_t* d_status, void* stream);
+
+/* The acceptance walk for a target that samples (graft_accept is the one for a target that takes its likeliest token).  The tree's
+ * tokens are the drafter's best, not draws, so a child is kept with the target's own probability and what is left of the target's
+ * distribution is sampled when none is: the committed tokens are distributed as the target's, whatever the tree.
+ *   d_target_logits [batch, rows, V] (V of the context, rows <= Nmax, dtype given): the target's logits behind every node; n_nodes <= rows.
+ *   d_temperature [batch] fp32 or NULL (1 everywhere); 0: the likeliest token (lowest id among equals), as graft_accept.
+ *   d_uniform [batch, Nmax] fp32 in [0, 1): entry i > 0 decides on node i, entry 0 draws the bonus token.
+ * At a node, with w_v = exp((z_v - max z) / T): its children c in index order are taken in turn; c is accepted iff
+ * u_c (sum of w without the tokens of earlier children) < w(token of c).  The first accepted child is the next node; without one the
+ * bonus token is the first v in id order with sum_{v' <= v} w' > u_0 sum w', w' = w without the children's tokens.  Only the rows of
+ * visited nodes are read.  Sums that decide are good to 1e-13 where it matters: a comparison closer than 1e-5 is made again from a
+ * sum in fp64, and the bonus token comes from fp64 sums.
+ *   d_accept_len, d_accept_path, d_bonus_token as graft_accept; the acceptance history (graft_set_hist_window) is kept too.
+ *   d_status [batch] or NULL (overwritten): GRAFT_ST_BAD_LOGITS when a visited row holds NaN or +inf or no finite entry, or a
+ *   temperature is negative, NaN or infinite: the walk ends there and the bonus token is -1; GRAFT_ST_BAD_TREE: accepted length 0, bonus -1. */
+graft_status graft_verify(graft_ctx* ctx, int32_t batch, const graft_tree_out* trees, int32_t rows, graft_dtype logits_dtype,
+                          const void* d_target_logits, const float* d_temperature, const float* d_uniform, int32_t* d_accept_len,
+                          int32_t* d_accept_path, int32_t* d_bonus_token, int32_t* d_status, void* stream);
 
 /* TDES training objective, forward and backward (Sec. 3.2 "Training", Eq. 7-12), on traces resident on the device.
  * Every pointer of graft_tdes_traces is a DEVICE pointer (borrowed for the call); a list with n = 0 may be NULL.

@@ -15,13 +15,14 @@ import torch
 
 from . import build as _build
 
-F32, BF16 = 0, 1
-ST_BAD_LOGITS, ST_TAU_CLAMPED, ST_FRONTIER_EMPTY, ST_INTERNAL = 1, 2, 4, 8
+F32, BF16, E4M3 = 0, 1, 2
+ST_BAD_LOGITS, ST_TAU_CLAMPED, ST_FRONTIER_EMPTY, ST_INTERNAL, ST_BAD_CACHE, ST_BAD_TREE = 1, 2, 4, 8, 16, 32
 
 ENTRY_POINTS = [
     "graft_create", "graft_destroy", "graft_nmax", "graft_mask_words", "graft_set_saba", "graft_set_tdes_tables",
     "graft_tdes_precompute", "graft_build_trees", "graft_vocab_pass", "graft_vocab_pass_static", "graft_tdes_edges",
     "graft_accept", "graft_tdes_loss", "graft_saba_fit", "graft_set_edge_rows", "graft_edge_rows", "graft_set_hist_window", "graft_vocab_pass_partial", "graft_vocab_merge",
+    "graft_cache_write", "graft_cache_read", "graft_cache_keep", "graft_tree_attention", "graft_verify",
     "graft_build_trees_host", "graft_launch_count", "graft_set_timing", "graft_read_timing", "graft_status_str",
     "graft_version",
 ]
@@ -63,6 +64,12 @@ class _TdesTraces(C.Structure):
 class _TdesLossConfig(C.Structure):
     _fields_ = [("gamma", C.c_float), ("w1", C.c_float), ("lambda_kl", C.c_float), ("lambda_pair", C.c_float),
                 ("lambda_bce", C.c_float)]
+
+
+class _Cache(C.Structure):
+    _fields_ = [("layers", C.c_int32), ("n_pages", C.c_int32), ("kv_heads", C.c_int32), ("page_size", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int), ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_exp", C.c_void_p),
+                ("d_v_exp", C.c_void_p), ("d_table", C.c_void_p), ("table_width", C.c_int32)]
 
 
 _lib = None
@@ -108,6 +115,12 @@ def load_library():
     lib.graft_accept.argtypes = [vp, C.c_int32, C.POINTER(_TreeOut), vp, vp, vp, vp, vp]
     lib.graft_tdes_loss.argtypes = [vp, C.POINTER(_TdesTraces), C.POINTER(_TdesLossConfig), vp, vp, vp, vp, vp, vp, vp]
     lib.graft_saba_fit.argtypes = [vp, C.c_int64, vp, vp, vp, vp, vp, vp, vp]
+    i32, i64, pc = C.c_int32, C.c_int64, C.POINTER(_Cache)
+    lib.graft_cache_write.argtypes = [vp, i32, pc, i32, vp, vp, i32, i64, vp, vp, vp, vp]
+    lib.graft_cache_read.argtypes = [vp, i32, pc, i32, vp, vp, i32, vp, vp, vp, vp]
+    lib.graft_cache_keep.argtypes = [vp, i32, pc, vp, vp, vp, vp, vp, vp]
+    lib.graft_tree_attention.argtypes = [vp, i32, pc, i32, i32, i32, i64, vp, C.c_float, vp, vp, vp, i32, vp, vp, vp, vp]
+    lib.graft_verify.argtypes = [vp, i32, C.POINTER(_TreeOut), i32, C.c_int, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.graft_launch_count.argtypes = [vp]
     lib.graft_launch_count.restype = C.c_uint64
     lib.graft_set_timing.argtypes = [vp, C.c_int32]
@@ -147,6 +160,68 @@ def _stream():
     if torch.cuda.is_initialized():
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return torch.cuda.current_stream().cuda_stream
+
+
+def _shaped(name, t, dtype, shape):
+    """The pointer of a dense tensor of this type and shape on the current device (None: NULL)."""
+    if t is None:
+        return None
+    if t.shape != shape:
+        raise GraftError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
+        raise GraftError(f"{name} is on another device than the current one")
+    return _ptr(t, dtype)
+
+
+def _token_rows(name, t, heads, head_dim):
+    """[batch, rows, heads, head_dim] bf16, whose tokens may stand further apart than dense (slices of a fused projection): pointer,
+    rows, numbers from one token to the next."""
+    if t.dim() != 4 or t.shape[2] != heads or t.shape[3] != head_dim:
+        raise GraftError(f"{name} must be [batch, rows, {heads}, {head_dim}], got {tuple(t.shape)}")
+    if t.dtype is not torch.bfloat16 or not t.is_cuda:
+        raise GraftError(f"{name} must be a bfloat16 CUDA tensor")
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise GraftError(f"{name} is on another device than the current one")
+    batch, rows = t.shape[:2]
+    if t.is_contiguous():
+        return t.data_ptr(), rows, heads * head_dim
+    sb, st, sh, sd = t.stride()
+    stride = st if rows > 1 else sb if batch > 1 else heads * head_dim
+    if sd != 1 or (heads > 1 and sh != head_dim) or (batch > 1 and sb != rows * stride):
+        raise GraftError(f"{name}: heads and numbers of a token must be dense, tokens evenly spaced; got strides {t.stride()}")
+    return t.data_ptr(), rows, stride
+
+
+@dataclass
+class KVCache:
+    """Caller-owned tensors of a paged cache (graft_cache in include/graft.h): k, v [layers, n_pages, kv_heads, page_size, head_dim],
+    bfloat16, or float8_e4m3fn with a uint8 exponent a row, k_exp, v_exp [layers, n_pages, kv_heads, page_size]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_exp: torch.Tensor | None = None
+    v_exp: torch.Tensor | None = None
+
+    @classmethod
+    def alloc(cls, layers, n_pages, kv_heads, page_size, head_dim, dtype=BF16):
+        shape = (layers, n_pages, kv_heads, page_size, head_dim)
+        dt = torch.float8_e4m3fn if dtype == E4M3 else torch.bfloat16
+        e = lambda: torch.zeros(shape[:-1], dtype=torch.uint8, device="cuda") if dtype == E4M3 else None  # noqa: E731
+        return cls(torch.zeros(shape, dtype=dt, device="cuda"), torch.zeros(shape, dtype=dt, device="cuda"), e(), e())
+
+    def _c(self, table, batch):
+        if self.k.dim() != 5 or self.k.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise GraftError("a cache is [layers, n_pages, kv_heads, page_size, head_dim], bfloat16 or float8_e4m3fn")
+        if table.dim() != 2:
+            raise GraftError(f"table must be [batch, pages], got {tuple(table.shape)}")
+        shape, q8 = self.k.shape, self.k.dtype is torch.float8_e4m3fn
+        if q8 != (self.k_exp is not None) or q8 != (self.v_exp is not None):
+            raise GraftError("an e4m3 cache has exponents, a bfloat16 one has none")
+        layers, n_pages, heads, page, dim = shape
+        u8 = torch.uint8
+        return _Cache(layers, n_pages, heads, page, dim, E4M3 if q8 else BF16, _shaped("k", self.k, self.k.dtype, shape),
+                      _shaped("v", self.v, self.k.dtype, shape), _shaped("k_exp", self.k_exp, u8, shape[:-1]),
+                      _shaped("v_exp", self.v_exp, u8, shape[:-1]), _shaped("table", table, torch.int32, (batch, table.shape[1])),
+                      table.shape[1])
 
 
 def vocab_pass_static(logits, K, topk_id, topk_lp, lse, row_status):
@@ -346,6 +421,81 @@ class Graft:
         _check(self.lib, self.lib.graft_accept(self._ctx, batch, C.byref(oc), _ptr(target_next, i32),
                                                _ptr(accept_len, i32), _ptr(accept_path, i32),
                                                _ptr(bonus_token, i32), _stream()), "graft_accept")
+
+    # ---- verification of the trees
+    def cache_write(self, cache: KVCache, layer, table, prefix_len, count, key, value, status=None):
+        """Row i < count[b] of key and value [batch, rows, kv_heads, head_dim] into slot prefix_len[b] - 1 + i of the layer."""
+        batch, i32 = key.shape[0], torch.int32
+        cc = cache._c(table, batch)
+        kp, rows, stride = _token_rows("key", key, cc.kv_heads, cc.head_dim)
+        vp, v_rows, v_stride = _token_rows("value", value, cc.kv_heads, cc.head_dim)
+        if value.shape[0] != batch or v_rows != rows or v_stride != stride:
+            raise GraftError("key and value must be laid out alike")
+        _check(self.lib, self.lib.graft_cache_write(
+            self._ctx, batch, C.byref(cc), int(layer), _shaped("prefix_len", prefix_len, i32, (batch,)),
+            _shaped("count", count, i32, (batch,)), rows, stride, kp, vp, _shaped("status", status, i32, (batch,)), _stream()),
+            "graft_cache_write")
+
+    def cache_read(self, cache: KVCache, layer, table, prefix_len, count, key, value, status=None):
+        """The entries of the same slots back into dense key and value; rows behind the count are left as they were."""
+        batch, i32 = key.shape[0], torch.int32
+        cc = cache._c(table, batch)
+        if key.dim() != 4:
+            raise GraftError(f"key must be [batch, rows, {cc.kv_heads}, {cc.head_dim}], got {tuple(key.shape)}")
+        shape = (batch, key.shape[1], cc.kv_heads, cc.head_dim)
+        _check(self.lib, self.lib.graft_cache_read(
+            self._ctx, batch, C.byref(cc), int(layer), _shaped("prefix_len", prefix_len, i32, (batch,)),
+            _shaped("count", count, i32, (batch,)), key.shape[1], _shaped("key", key, torch.bfloat16, shape),
+            _shaped("value", value, torch.bfloat16, shape), _shaped("status", status, i32, (batch,)), _stream()), "graft_cache_read")
+
+    def cache_keep(self, cache: KVCache, table, prefix_len, accept_len, accept_path, next_prefix=None, status=None):
+        """The accepted nodes' entries move up behind the prefix, in all layers; next_prefix (may be prefix_len): the new lengths."""
+        batch, i32 = accept_len.shape[0], torch.int32
+        cc = cache._c(table, batch)
+        one = (batch,)
+        _check(self.lib, self.lib.graft_cache_keep(
+            self._ctx, batch, C.byref(cc), _shaped("prefix_len", prefix_len, i32, one), _shaped("accept_len", accept_len, i32, one),
+            _shaped("accept_path", accept_path, i32, (batch, self.cfg.L)), _shaped("next_prefix", next_prefix, i32, one),
+            _shaped("status", status, i32, one), _stream()), "graft_cache_keep")
+
+    def tree_attention(self, cache: KVCache, layer, table, q, prefix_len, count, mask, out, lse=None, scale=None, shared=0, status=None):
+        """Attention of q [batch, rows, q_heads, head_dim] over one layer of the cache: the prefix, and of the rows' own entries those
+        that mask [batch, nmax, mask_words] (None: a chain) lets a row see.  scale: head_dim ** -0.5 unless given.  shared: the first
+        slots that are the same pages for all sequences."""
+        batch, i32 = q.shape[0], torch.int32
+        cc = cache._c(table, batch)
+        if q.dim() != 4:
+            raise GraftError(f"q must be [batch, rows, heads, {cc.head_dim}], got {tuple(q.shape)}")
+        heads = q.shape[2]
+        qp, rows, stride = _token_rows("q", q, heads, cc.head_dim)
+        _check(self.lib, self.lib.graft_tree_attention(
+            self._ctx, batch, C.byref(cc), int(layer), heads, rows, stride, qp, cc.head_dim ** -0.5 if scale is None else scale,
+            _shaped("prefix_len", prefix_len, i32, (batch,)), _shaped("count", count, i32, (batch,)),
+            _shaped("mask", mask, i32, (batch, self.nmax, self.mask_words)), int(shared),
+            _shaped("out", out, torch.bfloat16, (batch, rows, heads, cc.head_dim)),
+            _shaped("lse", lse, torch.float32, (batch, rows, heads)), _shaped("status", status, i32, (batch,)), _stream()),
+            "graft_tree_attention")
+
+    def verify(self, trees: TreeOut, target_logits, temperature, uniform, accept_len, accept_path, bonus_token, status=None):
+        """The acceptance walk for a target that samples: target_logits [batch, rows, V] bfloat16 or float32, temperature [batch] or
+        None (1), uniform [batch, nmax] in [0, 1); outputs as accept()."""
+        i32, f32 = torch.int32, torch.float32
+        if target_logits.dim() != 3 or target_logits.shape[2] != self.cfg.V:
+            raise GraftError(f"target_logits must be [batch, rows, {self.cfg.V}], got {tuple(target_logits.shape)}")
+        if target_logits.dtype not in (torch.bfloat16, f32):
+            raise GraftError(f"target_logits must be bfloat16 or float32, got {target_logits.dtype}")
+        batch, rows = target_logits.shape[:2]
+        one, nodes = (batch,), (batch, self.nmax)
+        oc = _TreeOut()
+        oc.d_n_nodes = _shaped("n_nodes", trees.n_nodes, i32, one)
+        oc.d_token = _shaped("token", trees.token, i32, nodes)
+        oc.d_parent = _shaped("parent", trees.parent, i32, nodes)
+        _check(self.lib, self.lib.graft_verify(
+            self._ctx, batch, C.byref(oc), rows, F32 if target_logits.dtype is f32 else BF16,
+            _shaped("target_logits", target_logits, None, target_logits.shape), _shaped("temperature", temperature, f32, one),
+            _shaped("uniform", uniform, f32, nodes), _shaped("accept_len", accept_len, i32, one),
+            _shaped("accept_path", accept_path, i32, (batch, self.cfg.L)), _shaped("bonus_token", bonus_token, i32, one),
+            _shaped("status", status, i32, one), _stream()), "graft_verify")
 
     def tdes_loss(self, groups, pairs, edges, gamma, w1, lambda_kl, lambda_pair, lambda_bce, loss, skipped=None,
                   gP=None, gC=None, gu=None, gs=None):

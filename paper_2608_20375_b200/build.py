@@ -23,6 +23,9 @@ SOURCES = {
     "tree.cu": ALL_HEADERS,
     "tdes_train.cu": ["common.cuh", "internal.h", GRAFT_H],
     "saba_fit.cu": ["common.cuh", "internal.h", GRAFT_H],
+    "cache.cu": ["common.cuh", "internal.h", "cache.cuh", GRAFT_H],
+    "tree_attn.cu": ["common.cuh", "internal.h", "cache.cuh", "umma.cuh", GRAFT_H],
+    "verify.cu": ["common.cuh", "internal.h", "umma.cuh", GRAFT_H],
     "tables_mma.cu": ["common.cuh", "internal.h", "umma.cuh", GRAFT_H],
 }
 # no --use_fast_math: the fp64 pieces (log-sum-exp fold, SABA) and the fp32 divisions must stay IEEE

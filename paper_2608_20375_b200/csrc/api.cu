@@ -467,6 +467,102 @@ graft_status graft_accept(graft_ctx* ctx, int32_t batch, const graft_tree_out* t
     return GRAFT_OK;
 }
 
+// Arguments that the calls on a cache have in common.
+static graft_status check_cache(const graft_ctx* ctx, int32_t batch, const graft_cache* c, int32_t layer) {
+    if (!ctx || !c || !c->d_k || !c->d_v || !c->d_table) return GRAFT_ERR_INVALID_ARG;
+    if (batch < 1 || batch > ctx->cfg.max_batch) return GRAFT_ERR_INVALID_ARG;
+    if (c->dtype != GRAFT_BF16 && c->dtype != GRAFT_E4M3) return GRAFT_ERR_INVALID_ARG;
+    if ((c->dtype == GRAFT_E4M3) != (c->d_k_exp != nullptr) || (c->dtype == GRAFT_E4M3) != (c->d_v_exp != nullptr))
+        return GRAFT_ERR_INVALID_ARG;
+    if (c->layers < 1 || c->n_pages < 1 || c->kv_heads < 1 || c->table_width < 1) return GRAFT_ERR_INVALID_ARG;
+    if (layer < 0 || layer >= c->layers) return GRAFT_ERR_INVALID_ARG;
+    if (((uintptr_t)c->d_k | (uintptr_t)c->d_v) & 15) return GRAFT_ERR_INVALID_ARG;
+    if (c->head_dim != 64 && c->head_dim != 128) return GRAFT_ERR_UNSUPPORTED;
+    if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return GRAFT_ERR_UNSUPPORTED;
+    if ((double)c->kv_heads * c->n_pages * c->page_size >= 2147483648.0) return GRAFT_ERR_UNSUPPORTED;
+    if ((long long)c->table_width * c->page_size > 2147483647LL - 65536) return GRAFT_ERR_UNSUPPORTED;
+    int dev = -1;  // the context's scratch and kernels belong to its device
+    if (cudaGetDevice(&dev) != cudaSuccess) {
+        cudaGetLastError();
+        return GRAFT_ERR_CUDA;
+    }
+    return dev == ctx->device ? GRAFT_OK : GRAFT_ERR_INVALID_ARG;
+}
+// rows a call brings or takes: `heads` of them a token, `stride` numbers from one token's to the next's
+static graft_status check_rows(const graft_cache* c, int32_t rows, int32_t heads, int64_t stride) {
+    if (rows < 1 || stride < (int64_t)heads * c->head_dim || stride % 8) return GRAFT_ERR_INVALID_ARG;
+    if ((double)rows * heads * 2 >= 2147483648.0 || stride > (1LL << 40)) return GRAFT_ERR_UNSUPPORTED;
+    return GRAFT_OK;
+}
+
+graft_status graft_cache_write(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer, const int32_t* d_prefix_len,
+                               const int32_t* d_count, int32_t rows, int64_t stride, const void* d_key, const void* d_value,
+                               int32_t* d_status, void* stream) {
+    graft_status gs = check_cache(ctx, batch, cache, layer);
+    if (gs != GRAFT_OK) return gs;
+    if (!d_prefix_len || !d_count || !d_key || !d_value || (((uintptr_t)d_key | (uintptr_t)d_value) & 15)) return GRAFT_ERR_INVALID_ARG;
+    if ((gs = check_rows(cache, rows, cache->kv_heads, stride)) != GRAFT_OK) return gs;
+    return cache_rows_launch(ctx, true, batch, cache, layer, d_prefix_len, d_count, rows, stride, d_key, d_value, d_status,
+                             (cudaStream_t)stream) == cudaSuccess ? GRAFT_OK : GRAFT_ERR_CUDA;
+}
+
+graft_status graft_cache_read(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer, const int32_t* d_prefix_len,
+                              const int32_t* d_count, int32_t rows, void* d_key, void* d_value, int32_t* d_status, void* stream) {
+    graft_status gs = check_cache(ctx, batch, cache, layer);
+    if (gs != GRAFT_OK) return gs;
+    if (!d_prefix_len || !d_count || !d_key || !d_value || (((uintptr_t)d_key | (uintptr_t)d_value) & 15)) return GRAFT_ERR_INVALID_ARG;
+    const int64_t stride = (int64_t)cache->kv_heads * cache->head_dim;
+    if ((gs = check_rows(cache, rows, cache->kv_heads, stride)) != GRAFT_OK) return gs;
+    return cache_rows_launch(ctx, false, batch, cache, layer, d_prefix_len, d_count, rows, stride, d_key, d_value, d_status,
+                             (cudaStream_t)stream) == cudaSuccess ? GRAFT_OK : GRAFT_ERR_CUDA;
+}
+
+graft_status graft_cache_keep(graft_ctx* ctx, int32_t batch, const graft_cache* cache, const int32_t* d_prefix_len,
+                              const int32_t* d_accept_len, const int32_t* d_accept_path, int32_t* d_next_prefix, int32_t* d_status,
+                              void* stream) {
+    const graft_status gs = check_cache(ctx, batch, cache, 0);
+    if (gs != GRAFT_OK) return gs;
+    if (!d_prefix_len || !d_accept_len || !d_accept_path) return GRAFT_ERR_INVALID_ARG;
+    if ((double)2 * cache->kv_heads * cache->layers >= 2147483648.0) return GRAFT_ERR_UNSUPPORTED;
+    return cache_keep_launch(ctx, batch, cache, d_prefix_len, d_accept_len, d_accept_path, d_next_prefix, d_status,
+                             (cudaStream_t)stream) == cudaSuccess ? GRAFT_OK : GRAFT_ERR_CUDA;
+}
+
+graft_status graft_tree_attention(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer, int32_t q_heads, int32_t rows,
+                                  int64_t q_stride, const void* d_q, float scale, const int32_t* d_prefix_len, const int32_t* d_count,
+                                  const uint32_t* d_mask, int32_t shared, void* d_out, float* d_lse, int32_t* d_status, void* stream) {
+    graft_status gs = check_cache(ctx, batch, cache, layer);
+    if (gs != GRAFT_OK) return gs;
+    if (!d_q || !d_prefix_len || !d_count || !d_out || (((uintptr_t)d_q | (uintptr_t)d_out) & 15)) return GRAFT_ERR_INVALID_ARG;
+    if (q_heads < 1 || q_heads % cache->kv_heads || !(scale == scale) || scale - scale != 0.0f) return GRAFT_ERR_INVALID_ARG;
+    if ((gs = check_rows(cache, rows, q_heads, q_stride)) != GRAFT_OK) return gs;
+    if (d_mask && rows > ctx->nmax) return GRAFT_ERR_INVALID_ARG;
+    if (shared < 0 || shared % cache->page_size || shared > cache->table_width * cache->page_size) return GRAFT_ERR_INVALID_ARG;
+    return tree_attn_launch(ctx, batch, cache, layer, q_heads, rows, q_stride, d_q, scale, d_prefix_len, d_count, d_mask, shared, d_out,
+                            d_lse, d_status, (cudaStream_t)stream) == cudaSuccess ? GRAFT_OK : GRAFT_ERR_CUDA;
+}
+
+graft_status graft_verify(graft_ctx* ctx, int32_t batch, const graft_tree_out* trees, int32_t rows, graft_dtype logits_dtype,
+                          const void* d_target_logits, const float* d_temperature, const float* d_uniform, int32_t* d_accept_len,
+                          int32_t* d_accept_path, int32_t* d_bonus_token, int32_t* d_status, void* stream) {
+    if (!ctx || !trees || !d_target_logits || !d_uniform || !d_accept_len || !d_accept_path || !d_bonus_token)
+        return GRAFT_ERR_INVALID_ARG;
+    if (!trees->d_n_nodes || !trees->d_token || !trees->d_parent) return GRAFT_ERR_INVALID_ARG;
+    if (batch < 1 || batch > ctx->cfg.max_batch || rows < 1 || rows > ctx->nmax) return GRAFT_ERR_INVALID_ARG;
+    if (logits_dtype != GRAFT_F32 && logits_dtype != GRAFT_BF16) return GRAFT_ERR_INVALID_ARG;
+    if ((uintptr_t)d_target_logits % (logits_dtype == GRAFT_BF16 ? 2 : 4)) return GRAFT_ERR_INVALID_ARG;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) {
+        cudaGetLastError();
+        return GRAFT_ERR_CUDA;
+    }
+    if (dev != ctx->device) return GRAFT_ERR_INVALID_ARG;
+    if (verify_launch(ctx, batch, trees, rows, logits_dtype, d_target_logits, d_temperature, d_uniform, d_accept_len, d_accept_path,
+                      d_bonus_token, d_status, (cudaStream_t)stream) != cudaSuccess)
+        return GRAFT_ERR_CUDA;
+    return GRAFT_OK;
+}
+
 static_assert(sizeof(graft_vocab_partial) == 280, "the Python binding gathers partials as 280-byte records");
 
 graft_status graft_vocab_pass_partial(graft_ctx* ctx, int32_t batch, const void* d_logits_shard,

@@ -1,0 +1,71 @@
+// What the kernels that read and write a paged key/value cache share.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+
+#include "common.cuh"
+#include "internal.h"
+
+namespace graft {
+
+// A graft_cache as the kernels see it: one layer of it (cache_keep: all), addresses in entries.
+struct CacheView {
+    uint8_t* k;
+    uint8_t* v;
+    uint8_t* k_exp;  // NULL: bf16
+    uint8_t* v_exp;
+    const int32_t* table;  // [batch, width]
+    int width, n_pages, kv_heads, page_shift, head_dim;
+    int row_bytes;  // of an entry (one token, one head)
+};
+
+CacheView cache_view(const graft_cache* c, int layer);  // csrc/cache.cu
+
+// row (token, head) of a layer that slot `at` of a page holds
+__device__ __forceinline__ size_t cache_row(const CacheView& c, int page, int head, int at) {
+    return ((((size_t)page * c.kv_heads + head) << c.page_shift) + at);
+}
+
+// Whether slots [first, end) of the sequence lie within its table and in pages of the cache; a whole warp calls it.
+__device__ __forceinline__ bool cache_slots_ok(const CacheView& c, const int32_t* table, long long first, long long end) {
+    if (first < 0 || end > ((long long)c.width << c.page_shift)) return false;
+    bool ok = true;
+    if (end > first)
+        for (int p = (int)(first >> c.page_shift) + lane_id(); p <= (int)((end - 1) >> c.page_shift); p += 32)
+            ok = ok && (unsigned)table[p] < (unsigned)c.n_pages;
+    return __all_sync(0xFFFFFFFFu, ok);
+}
+
+// two e4m3 numbers (the low 16 bits) -> bf16 times 2^-120: their exponent and mantissa bits in the places of bf16's; exact
+__device__ __forceinline__ uint32_t e4m3x2_to_bf16x2_small(uint32_t two_in_bytes_1_and_3) {
+    return ((two_in_bytes_1_and_3 >> 4) & 0x07F007F0u) | (two_in_bytes_1_and_3 & 0x80008000u);
+}
+__device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// Factors that take what e4m3x2_to_bf16x2_small gives to the numbers that it stands for, as pairs of bf16: 2^(e + 120) with
+// e = byte - 127.  Up to 2^127 one factor holds it and the second is 1; byte 255 is NaN.
+__device__ __forceinline__ void e4m3_factors(uint32_t byte, uint32_t& f, uint32_t& more) {
+    int x = (int)byte - 7;  // e + 120
+    const int y = x > 127 ? x - 127 : 0;
+    x = x > 127 ? 127 : (x < -126 ? -126 : x);
+    const uint32_t a = byte == 255 ? 0x7FC0u : (uint32_t)(x + 127) << 7;
+    f = a | (a << 16);
+    const uint32_t b = (uint32_t)(y + 127) << 7;
+    more = b | (b << 16);
+}
+// four e4m3 numbers -> two pairs of bf16
+__device__ __forceinline__ uint2 e4m3x4_to_bf16(uint32_t w, uint32_t f, uint32_t more) {
+    uint2 r;
+    r.x = bf16x2_mul(e4m3x2_to_bf16x2_small(__byte_perm(w, 0, 0x1404)), f);
+    r.y = bf16x2_mul(e4m3x2_to_bf16x2_small(__byte_perm(w, 0, 0x3424)), f);
+    if (more != 0x3F803F80u) {
+        r.x = bf16x2_mul(r.x, more);
+        r.y = bf16x2_mul(r.y, more);
+    }
+    return r;
+}
+
+}  // namespace graft

@@ -194,6 +194,19 @@ size_t saba_fit_doubles();                         // graft_ctx::w_fit
 cudaError_t saba_fit_launch(graft_ctx* ctx, long long n, const float* d_state, const int32_t* d_budget,
                             const float* d_gain, const int32_t* d_prefix, const float* d_latency, double* d_out,
                             cudaStream_t st);
+// verification of the trees (csrc/cache.cu, csrc/tree_attn.cu, csrc/verify.cu)
+cudaError_t cache_rows_launch(graft_ctx* ctx, bool write, int batch, const graft_cache* cache, int layer, const int32_t* d_prefix_len,
+                              const int32_t* d_count, int rows, long long stride, const void* d_key, const void* d_value,
+                              int32_t* d_status, cudaStream_t st);
+cudaError_t cache_keep_launch(graft_ctx* ctx, int batch, const graft_cache* cache, const int32_t* d_prefix_len,
+                              const int32_t* d_accept_len, const int32_t* d_accept_path, int32_t* d_next_prefix, int32_t* d_status,
+                              cudaStream_t st);
+cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache, int layer, int q_heads, int rows, long long q_stride,
+                             const void* d_q, float scale, const int32_t* d_prefix_len, const int32_t* d_count, const uint32_t* d_mask,
+                             int shared, void* d_out, float* d_lse, int32_t* d_status, cudaStream_t st);
+cudaError_t verify_launch(graft_ctx* ctx, int batch, const graft_tree_out* trees, int rows, graft_dtype dt, const void* d_logits,
+                          const float* d_temperature, const float* d_uniform, int32_t* d_accept_len, int32_t* d_accept_path,
+                          int32_t* d_bonus, int32_t* d_status, cudaStream_t st);
 size_t tree_smem_bytes(const graft_config& cfg);
 bool tree_ordered(const graft_ctx* ctx, int batch);  // the edge-score kernel gives the order of the trees
 bool tree_lazy_fits(const graft_config& cfg);  // edge scores are computed inside the tree kernel
