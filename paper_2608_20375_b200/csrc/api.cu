@@ -18,7 +18,6 @@ using namespace graft;
 namespace {
 
 constexpr int kTimingRing = 64;
-constexpr int kMaxOldTables = 16;  // (each at least twice the one before)
 
 struct Timing {
     cudaEvent_t ev[kTimingRing][4];
@@ -51,27 +50,23 @@ struct CtxExtra {
     char* d_in = nullptr;
     char* d_out = nullptr;
     size_t in_bytes = 0, out_bytes = 0;
-    // scratch of the table precompute that became too small
-    void* old_tables[kMaxOldTables];
-    int n_old_tables = 0;
 };
 
 CtxExtra* extra_of(graft_ctx* ctx) { return (CtxExtra*)ctx->stage; }
 
-// Scratch of the tensor-core table precompute, `need` bytes at least, or NULL if there is no memory for it.  It comes with
-// the first call that needs it, be it under stream capture: the allocation is made outside of any capture.  A captured call
-// keeps the address, so scratch that has become too small lives on until the context goes; a new piece is at least twice
-// the size of the last, so that all the old ones together are smaller than the one in use.
-void* tables_scratch(graft_ctx* ctx, size_t need) {
-    if (ctx->tables_scratch_bytes >= need) return ctx->tables_scratch;
-    CtxExtra* ex = extra_of(ctx);
-    if (ctx->tables_scratch && ex->n_old_tables == kMaxOldTables) return nullptr;
+// Scratch of a call, `need` bytes at least, or NULL if there is no memory for it.  It comes with the first call that needs
+// it, be it under stream capture: the allocation is made outside of any capture.  A captured call keeps the address, so
+// scratch that has become too small lives on until the context goes; a new piece is at least twice the size of the last, so
+// that all the old ones together are smaller than the one in use.
+void* grown(Grown& g, size_t need) {
+    if (g.bytes >= need) return g.p;
+    if (g.p && g.n_old == kMaxOld) return nullptr;
     cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
     if (cudaThreadExchangeStreamCaptureMode(&mode) != cudaSuccess) {
         cudaGetLastError();
         return nullptr;
     }
-    const size_t bytes = need > 2 * ctx->tables_scratch_bytes ? need : 2 * ctx->tables_scratch_bytes;
+    const size_t bytes = need > 2 * g.bytes ? need : 2 * g.bytes;
     void* buf = nullptr;
     if (cudaMalloc(&buf, bytes) != cudaSuccess) {
         cudaGetLastError();
@@ -79,10 +74,14 @@ void* tables_scratch(graft_ctx* ctx, size_t need) {
     }
     cudaThreadExchangeStreamCaptureMode(&mode);
     if (buf == nullptr) return nullptr;
-    if (ctx->tables_scratch) ex->old_tables[ex->n_old_tables++] = ctx->tables_scratch;
-    ctx->tables_scratch = buf;
-    ctx->tables_scratch_bytes = bytes;
+    if (g.p) g.old[g.n_old++] = g.p;
+    g.p = buf;
+    g.bytes = bytes;
     return buf;
+}
+void free_grown(Grown& g) {
+    for (int i = 0; i < g.n_old; ++i) cudaFree(g.old[i]);
+    if (g.p) cudaFree(g.p);
 }
 
 }  // namespace
@@ -158,7 +157,7 @@ graft_status graft_create(const graft_config* cfg, graft_ctx** out) {
     const size_t o_id = take(B * L * K * 4), o_lp = take(B * L * K * 4), o_lse = take(B * L * 4);
     const size_t o_rs = take(B * L * 4), o_edge = take(B * L * K * K * 4);
     const size_t o_es = take(B * L * K * K * 4), o_ei = take(B * L * K * K);
-    const size_t o_u = take(L * (size_t)cfg->m * 4), o_err = take(256), o_cos = take(B * L * 8), o_saba = take(B * sizeof(SabaResult)), o_fit = take(saba_fit_doubles() * 8), o_loss = take(tdes_loss_bytes(*cfg)), o_order = take(B * 4), o_ordn = take(256);
+    const size_t o_u = take(L * (size_t)cfg->m * 4), o_err = take(256), o_cos = take(B * L * 8), o_saba = take(B * sizeof(SabaResult)), o_fit = take(saba_fit_doubles() * 8), o_loss = take(tdes_loss_bytes(*cfg)), o_order = take(B * 4), o_ordn = take(256), o_attn = take(256);
     ctx->ws_bytes = off;
     if (cudaMalloc(&ctx->ws, ctx->ws_bytes) != cudaSuccess) {
         cudaGetLastError();
@@ -191,8 +190,6 @@ graft_status graft_create(const graft_config* cfg, graft_ctx** out) {
     ctx->w_esort = (float*)(base + o_es);
     ctx->w_eidx = (uint8_t*)(base + o_ei);
     ctx->d_u = (float*)(base + o_u);
-    ctx->tables_scratch = nullptr;
-    ctx->tables_scratch_bytes = 0;
     ctx->hist_w = 0;
     ctx->hist_window = nullptr;
     ctx->hist_count = nullptr;
@@ -205,6 +202,7 @@ graft_status graft_create(const graft_config* cfg, graft_ctx** out) {
     ctx->w_loss = (double*)(base + o_loss);
     ctx->w_order = (int32_t*)(base + o_order);
     ctx->w_order_n = (int*)(base + o_ordn);
+    ctx->w_attn_n = (int*)(base + o_attn);
     *out = ctx;
     return GRAFT_OK;
 }
@@ -218,10 +216,10 @@ graft_status graft_destroy(graft_ctx* ctx) {
                 for (int j = 0; j < 4; ++j) cudaEventDestroy(ex->timing.ev[i][j]);
         if (ex->d_in) cudaFree(ex->d_in);
         if (ex->d_out) cudaFree(ex->d_out);
-        for (int i = 0; i < ex->n_old_tables; ++i) cudaFree(ex->old_tables[i]);
         delete ex;
     }
-    if (ctx->tables_scratch) cudaFree(ctx->tables_scratch);
+    free_grown(ctx->tables_scratch);
+    free_grown(ctx->attn_scratch);
     if (ctx->ws) cudaFree(ctx->ws);
     delete ctx;
     return GRAFT_OK;
@@ -293,7 +291,7 @@ graft_status graft_tdes_precompute(graft_ctx* ctx, const void* d_emb, graft_dtyp
     if (emb_dtype != GRAFT_F32 && emb_dtype != GRAFT_BF16) return GRAFT_ERR_INVALID_ARG;
     // the tensor cores (16-bit parts of the inputs, exact products), where the rows fit and their scratch is to be had
     if (tables_mma_fits(ctx->num_sms, ctx->cfg.V, d_emb, emb_dtype, E, ctx->cfg.m, d_out)) {
-        void* scratch = tables_scratch(ctx, tables_mma_scratch_bytes(ctx->num_sms, ctx->cfg.V, E, ctx->cfg.m, emb_dtype));
+        void* scratch = grown(ctx->tables_scratch, tables_mma_scratch_bytes(ctx->num_sms, ctx->cfg.V, E, ctx->cfg.m, emb_dtype));
         if (scratch != nullptr) {
             if (tables_mma_launch(ctx, d_emb, emb_dtype, E, d_W, d_b, d_out, scratch, (cudaStream_t)stream) == cudaSuccess)
                 return GRAFT_OK;
@@ -538,8 +536,14 @@ graft_status graft_tree_attention(graft_ctx* ctx, int32_t batch, const graft_cac
     if ((gs = check_rows(cache, rows, q_heads, q_stride)) != GRAFT_OK) return gs;
     if (d_mask && rows > ctx->nmax) return GRAFT_ERR_INVALID_ARG;
     if (shared < 0 || shared % cache->page_size || shared > cache->table_width * cache->page_size) return GRAFT_ERR_INVALID_ARG;
-    return tree_attn_launch(ctx, batch, cache, layer, q_heads, rows, q_stride, d_q, scale, d_prefix_len, d_count, d_mask, shared, d_out,
-                            d_lse, d_status, (cudaStream_t)stream) == cudaSuccess ? GRAFT_OK : GRAFT_ERR_CUDA;
+    void* scratch = grown(ctx->attn_scratch, tree_attn_scratch_bytes(ctx, batch, cache, q_heads, rows, shared));
+    if (scratch == nullptr) return GRAFT_ERR_WORKSPACE;
+    if (tree_attn_launch(ctx, batch, cache, layer, q_heads, rows, q_stride, d_q, scale, d_prefix_len, d_count, d_mask, shared, d_out,
+                         d_lse, d_status, scratch, (cudaStream_t)stream) != cudaSuccess) {
+        cudaGetLastError();
+        return GRAFT_ERR_CUDA;
+    }
+    return GRAFT_OK;
 }
 
 graft_status graft_verify(graft_ctx* ctx, int32_t batch, const graft_tree_out* trees, int32_t rows, graft_dtype logits_dtype,

@@ -57,6 +57,15 @@ struct SabaResult {
     float state[4];  // conf, degen, hist, tau
 };
 
+// Scratch that grows with the calls: the piece in use and the ones before it, which captured calls may still hold.
+constexpr int kMaxOld = 16;  // (each at least twice the one before)
+struct Grown {
+    void* p;
+    size_t bytes;
+    void* old[kMaxOld];
+    int n_old;
+};
+
 }  // namespace graft
 
 struct graft_ctx {
@@ -98,10 +107,11 @@ struct graft_ctx {
     double* w_loss;               // graft_tdes_loss: [kLossSums] sums and arrival counter, then shares of gu; zero between calls
     int32_t* w_errflag;           // [1] device-side internal error flag
     graft::VpPlan vp_plan;
-    // scratch of the tensor-core table precompute (allocated on its first use: pieces of split tiles, W's parts,
-    // flags of rows)
-    void* tables_scratch;
-    size_t tables_scratch_bytes;
+    // scratch that comes with the first call that needs it (api.cu, grown): of the tensor-core table precompute (pieces of split
+    // tiles, W's parts, flags of rows) and of graft_tree_attention (the plan, pieces of units that were cut)
+    graft::Grown tables_scratch, attn_scratch;
+    int attn_ready;  // variants of the attention kernel that may use their shared memory
+    int* w_attn_n;   // graft_tree_attention: arrivals, zero between calls
     // host-buffer staging (allocated on first use of graft_build_trees_host)
     void* stage;
     size_t stage_bytes;
@@ -203,7 +213,8 @@ cudaError_t cache_keep_launch(graft_ctx* ctx, int batch, const graft_cache* cach
                               cudaStream_t st);
 cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache, int layer, int q_heads, int rows, long long q_stride,
                              const void* d_q, float scale, const int32_t* d_prefix_len, const int32_t* d_count, const uint32_t* d_mask,
-                             int shared, void* d_out, float* d_lse, int32_t* d_status, cudaStream_t st);
+                             int shared, void* d_out, float* d_lse, int32_t* d_status, void* scratch, cudaStream_t st);
+size_t tree_attn_scratch_bytes(const graft_ctx* ctx, int batch, const graft_cache* cache, int q_heads, int rows, int shared);
 cudaError_t verify_launch(graft_ctx* ctx, int batch, const graft_tree_out* trees, int rows, graft_dtype dt, const void* d_logits,
                           const float* d_temperature, const float* d_uniform, int32_t* d_accept_len, int32_t* d_accept_path,
                           int32_t* d_bonus, int32_t* d_status, cudaStream_t st);

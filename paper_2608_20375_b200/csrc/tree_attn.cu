@@ -1,13 +1,54 @@
-// Attention of the trees' nodes over a paged cache (graft_tree_attention).
+// Attention of the trees' nodes over a paged cache (graft_tree_attention), on the tcgen05 tensor cores.
+//
+// For a node i and a query head h:  o = sum_j p_j v_j,  p = softmax(scale q . k_j)  over the slots j that i sees.  All query heads of a
+// key head and all nodes of a sequence are rows of one matrix product against the same keys, so the prefix is gone through once for a
+// whole tree; with a shared prefix, once for the nodes of all sequences.
+//
+// Units and pieces.  A unit is a sequence (or, for the shared prefix, all of them), a key head and up to 256 rows (two row tiles
+// of 128), against all key tiles of 128 slots.  The units' key tiles stand in one line, weighted by the row tiles that they feed, and every
+// CTA takes an equal stretch of it: lengths and trees may be as unlike as they want, and one sequence's prefix spreads over all SMs.  A
+// unit that is cut leaves unnormalised sums with their maximum and denominator behind, which a second kernel joins.
+//
+// Inside a CTA two groups of four warps (`streams`) hold a row tile each and take turns on the tensor cores: while one stream's
+// exponentials are worked out, the other's products run.  A unit of one row tile gives the streams the even and the odd key tiles
+// instead, joined at the end.  Scores and sums stay in TMEM: S of 128 columns a stream, overwritten in place by the weights p in bf16
+// (which are the second product's first operand from there), and O of head_dim columns.  One thread has one row, so maxima and sums need no
+// exchange.  O is rescaled only when a row's maximum has grown by more than 2^8 since it was last taken: weights are then up to 256,
+// which fp32 sums and bf16 hold as well as those up to 1.
+#include <cuda.h>
 #include <float.h>
 
 #include "cache.cuh"
+#include "umma.cuh"
 
 namespace graft {
 
 namespace {
 
-struct AttnParams {
+constexpr int kTile = 128;      // slots of a key tile, rows of a row tile
+constexpr int kUnitRows = 256;
+
+// What the plan says of a sequence (entry 0: the shared prefix with the rows of all of them; entry b + 1: sequence b).
+struct __align__(16) PlanSeq {
+    int n;       // rows in use (nodes); 0: none, or left out
+    int base;    // slots before the first row's (shared prefix: its length)
+    int node0;   // nodes of the sequences before
+    int unit0;   // units before
+    long long cost0;  // key tiles before, each times its row tiles
+    int kt;      // key tiles
+    int pad;
+};
+struct PlanStart {
+    int s, h, mt, k;
+};
+struct PlanHead {
+    long long total;
+    int parts;  // CTAs that the line is cut for
+    int pad;
+};
+
+struct __align__(64) AttnParams {
+    CUtensorMap map_k, map_v;
     CacheView c;
     const uint8_t* q;
     long long q_stride;
@@ -17,89 +58,1123 @@ struct AttnParams {
     __nv_bfloat16* out;
     float* lse;
     int32_t* status;
-    float scale;
-    int rows, q_heads, shared, nmax, words;
+    float c2;            // |scale| log2(e)
+    uint32_t q_flip;     // a negative scale: the sign of q
+    uint32_t q_keep;     // 0: a scale of zero
+    int rows, q_heads, group, shared, nmax, words, batch;
+    int box_rows;        // slots of a page that one copy brings
+    PlanHead* head;
+    PlanSeq* seq;        // [batch + 1]
+    PlanStart* start;    // [gridDim of the attention kernel]
+    int ctas, min_cost;
+    int* arrivals;       // zero between calls
+    float* part_o;       // [slots][256][D]
+    float2* part_ml;     // [slots][256]: maximum (log2 domain), sum
 };
 
-// A warp a (row, query head): 32 slots at a time, a lane a slot for the scores, a lane head_dim / 32 numbers for the sums.
-template <int D, bool Q8>
-__global__ void __launch_bounds__(128) tree_attn_kernel(const AttnParams p) {
+// ---- the plan ------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ int row_tiles2(int R) { return (R + kUnitRows - 1) / kUnitRows; }  // units of R rows
+__device__ __forceinline__ int unit_weight(int R, int mt) { return R - mt * kUnitRows > kTile ? 2 : 1; }
+__device__ __forceinline__ long long head_cost(int R, int kt) {
+    const int u = row_tiles2(R);
+    return u == 0 ? 0 : (long long)kt * (2 * (u - 1) + unit_weight(R, u - 1));
+}
+
+// first position of CTA c's stretch
+__device__ __forceinline__ long long part_first(long long total, int parts, int c) { return (c * total + parts - 1) / parts; }
+
+constexpr int kPlanThreads = 128;
+__global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const AttnParams p) {
     pdl_launch_dependents();
     pdl_wait();
     const CacheView& c = p.c;
-    __shared__ float qs[4][D];
-    const int lane = lane_id(), w = threadIdx.x >> 5, b = blockIdx.y;
-    const long long item = (long long)blockIdx.x * 4 + w;
-    const int row = (int)(item / p.q_heads), h = (int)(item % p.q_heads), hk = h / (p.q_heads / c.kv_heads);
-    const int n = p.count[b], base = p.prefix_len[b] - 1;
-    const int32_t* table = c.table + (size_t)b * c.width;
-    const bool ok = n >= 0 && n <= p.rows && base >= 0 && base >= p.shared && cache_slots_ok(c, table, 0, (long long)base + n);
-    if (item == 0 && lane == 0 && p.status) p.status[b] = ok ? 0 : GRAFT_ST_BAD_CACHE;
-    if (!ok || row >= n) return;
-    const uint16_t* q = (const uint16_t*)p.q + ((long long)b * p.rows + row) * p.q_stride + h * D;
-    for (int i = lane; i < D; i += 32) qs[w][i] = __uint_as_float((uint32_t)q[i] << 16) * p.scale;
-    __syncwarp();
-    float m = -INFINITY, l = 0.0f, o[D / 32] = {};
-    for (int s0 = 0; s0 < base + n; s0 += 32) {
-        const int s = s0 + lane, j = s - base;
-        bool seen = s < base + n;
-        if (seen && j >= 0) seen = p.mask ? (p.mask[((size_t)b * p.nmax + row) * p.words + (j >> 5)] >> (j & 31)) & 1 : j <= row;
-        float x = -INFINITY;
-        if (seen) {
-            const size_t at = cache_row(c, table[s >> c.page_shift], hk, s & ((1 << c.page_shift) - 1));
-            const uint8_t* k = c.k + at * c.row_bytes;
-            uint32_t f = 0, more = 0;
-            if (Q8) e4m3_factors(c.k_exp[at], f, more);
-            x = 0.0f;
-            for (int i = 0; i < D; i += 4) {
-                uint2 y;
-                if (Q8)
-                    y = e4m3x4_to_bf16(*(const uint32_t*)(k + i), f, more);
-                else
-                    y = *(const uint2*)(k + 2 * i);
-                x += qs[w][i] * __uint_as_float(y.x << 16) + qs[w][i + 1] * __uint_as_float(y.x & 0xFFFF0000u) +
-                     qs[w][i + 2] * __uint_as_float(y.y << 16) + qs[w][i + 3] * __uint_as_float(y.y & 0xFFFF0000u);
+    __shared__ int fine[kPlanThreads / 32], last;
+    __shared__ long long sums[3][kPlanThreads / 32];
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    {
+        const int n = p.count[b], base = p.prefix_len[b] - 1;
+        const int32_t* table = c.table + (size_t)b * c.width;
+        const long long end = (long long)base + n;
+        bool ok = n >= 0 && n <= p.rows && base >= 0 && base >= p.shared && end <= ((long long)c.width << c.page_shift);
+        if (ok && n > 0)
+            for (int i = tid; i <= (int)((end - 1) >> c.page_shift); i += kPlanThreads) {
+                ok = ok && (unsigned)table[i] < (unsigned)c.n_pages;
+                // (the shared pages are read from the first sequence's table)
+                if (i < p.shared >> c.page_shift) ok = ok && (unsigned)c.table[i] < (unsigned)c.n_pages;
+            }
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (lane == 0) fine[warp] = ok;
+        __syncthreads();
+        if (tid == 0) {
+            ok = true;
+            for (int w = 0; w < kPlanThreads / 32; ++w) ok = ok && fine[w];
+            if (p.status) p.status[b] = ok ? 0 : GRAFT_ST_BAD_CACHE;
+            p.seq[b + 1].n = ok ? n : 0;
+            p.seq[b + 1].base = base;
+            last = atom_add_acq_rel(p.arrivals, 1) == (int)gridDim.x - 1;
+        }
+        __syncthreads();
+        if (!last) return;
+    }
+    // the last block adds up: nodes, units, cost
+    const int Hk = c.kv_heads;
+    long long run[3] = {0, 0, 0};
+    for (int b0 = 0; b0 < p.batch; b0 += kPlanThreads) {
+        const int i = b0 + tid;
+        int n = 0, kt = 0;
+        if (i < p.batch) {
+            n = ((volatile PlanSeq*)p.seq)[i + 1].n;
+            kt = n > 0 ? (((volatile PlanSeq*)p.seq)[i + 1].base + n - p.shared + kTile - 1) / kTile : 0;
+        }
+        const int R = n * p.group;
+        const long long mine[3] = {n, (long long)Hk * row_tiles2(R), Hk * head_cost(R, kt)};
+        long long upto[3];
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            long long x = mine[q];
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+                if (lane >= o) x += y;
+            }
+            upto[q] = x;
+            if (lane == 31) sums[q][warp] = x;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            long long before = run[q];
+            for (int w = 0; w < kPlanThreads / 32; ++w) {
+                if (w < warp) before += sums[q][w];
+                run[q] += sums[q][w];
+            }
+            upto[q] += before - mine[q];
+        }
+        if (i < p.batch) {
+            p.seq[i + 1].node0 = (int)upto[0];
+            p.seq[i + 1].unit0 = (int)upto[1];
+            p.seq[i + 1].cost0 = upto[2];
+            p.seq[i + 1].kt = kt;
+        }
+        __syncthreads();
+    }
+    // the shared prefix goes first
+    const int nodes = (int)run[0], Rs = p.shared > 0 ? nodes * p.group : 0, kts = (p.shared + kTile - 1) / kTile;
+    const int us = Hk * row_tiles2(Rs);
+    const long long cs = Hk * head_cost(Rs, kts);
+    for (int i = tid; i < p.batch; i += kPlanThreads) {
+        p.seq[i + 1].unit0 += us;
+        p.seq[i + 1].cost0 += cs;
+    }
+    const long long total = run[2] + cs;
+    long long parts = (total + p.min_cost - 1) / p.min_cost;
+    parts = parts > p.ctas ? p.ctas : parts;
+    if (tid == 0) {
+        PlanSeq s = {};
+        s.n = Rs > 0 ? nodes : 0;
+        s.base = p.shared;
+        s.kt = kts;
+        p.seq[0] = s;
+        p.head->total = total;
+        p.head->parts = (int)parts;
+        *p.arrivals = 0;
+    }
+    __syncthreads();
+    // where every CTA begins
+    for (int i = tid; i < (int)parts; i += kPlanThreads) {
+        const long long x = part_first(total, (int)parts, i);
+        int lo = 0, hi = p.batch;  // the last entry whose cost0 is not above x and that has any
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (((volatile PlanSeq*)p.seq)[mid].cost0 <= x)
+                lo = mid;
+            else
+                hi = mid - 1;
+        }
+        const int n = ((volatile PlanSeq*)p.seq)[lo].n, R = n * p.group, kt = ((volatile PlanSeq*)p.seq)[lo].kt;
+        const long long hc = head_cost(R, kt), local = x - ((volatile PlanSeq*)p.seq)[lo].cost0;
+        PlanStart st = {lo, 0, 0, 0};
+        if (hc > 0) {
+            st.h = (int)(local / hc);
+            long long rem = local % hc;
+            const int u = row_tiles2(R);
+            st.mt = (int)(rem / (2 * (long long)kt));
+            st.mt = st.mt < u - 1 ? st.mt : u - 1;
+            rem -= 2 * (long long)kt * st.mt;
+            const int w = unit_weight(R, st.mt);
+            st.k = (int)((rem + w - 1) / w);  // may be kt: the next unit's first
+        }
+        p.start[i] = st;
+    }
+}
+
+// ---- walking along a CTA's stretch -----------------------------------------------------------------------------------
+struct Piece {
+    int s, h, mt, k0, k1;  // entry of the plan, key head, unit of the head, key tiles
+    int n, base, node0, unit, kt, R;
+    int rows;  // rows of the unit
+};
+struct Walk {
+    const PlanSeq* seq;
+    int last_s, Hk, group;
+    long long x, x1;
+    int s, h, mt, k;
+    PlanSeq q;
+    __device__ __forceinline__ void load() {
+        const int4* a = (const int4*)(seq + s);
+        ((int4*)&q)[0] = __ldcg(a);
+        ((int4*)&q)[1] = __ldcg(a + 1);
+    }
+    __device__ __forceinline__ void begin(const AttnParams& p, int cta) {
+        seq = p.seq;
+        last_s = p.batch;
+        Hk = p.c.kv_heads;
+        group = p.group;
+        const long long total = __ldcg(&p.head->total);
+        const int parts = __ldcg(&p.head->parts);
+        x = x1 = 0;
+        if (cta >= parts) return;
+        x1 = part_first(total, parts, cta + 1);
+        const int4 st = __ldcg((const int4*)(p.start + cta));
+        s = st.x, h = st.y, mt = st.z, k = st.w;
+        load();
+        const int R = q.n * group;
+        x = q.cost0 + h * head_cost(R, q.kt) + 2LL * q.kt * mt + (long long)k * unit_weight(R, mt);
+    }
+    __device__ __forceinline__ bool next(Piece& pc) {
+        if (x >= x1) return false;
+        int R = q.n * group;
+        while (q.n == 0 || k >= q.kt) {  // the next unit
+            k = 0;
+            mt += 1;
+            if (q.n == 0 || mt >= row_tiles2(R)) {
+                mt = 0;
+                h += 1;
+                if (q.n == 0 || h >= Hk) {
+                    h = 0;
+                    s += 1;
+                    if (s > last_s) return false;
+                    load();
+                    R = q.n * group;
+                }
             }
         }
-        float mm = x;
-        for (int d = 16; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xFFFFFFFFu, mm, d));
-        mm = fmaxf(mm, m);
-        const float keep = m > -INFINITY ? expf(m - mm) : 0.0f, e = seen && mm > -INFINITY ? expf(x - mm) : 0.0f;
-        float sum = e;
-        for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-        l = l * keep + sum;
-        m = mm;
-        for (int i = 0; i < D / 32; ++i) o[i] *= keep;
-        for (int t = 0; t < 32 && s0 + t < base + n; ++t) {
-            const float pe = __shfl_sync(0xFFFFFFFFu, e, t);
-            if (pe == 0.0f) continue;
-            const size_t at = cache_row(c, table[(s0 + t) >> c.page_shift], hk, (s0 + t) & ((1 << c.page_shift) - 1));
-            const uint8_t* v = c.v + at * c.row_bytes;
-            for (int i = 0; i < D / 32; ++i) {
-                const int d = lane + 32 * i;
-                float y;
-                if (Q8) {
-                    uint32_t f, more;
-                    e4m3_factors(c.v_exp[at], f, more);
-                    y = __uint_as_float(e4m3x4_to_bf16(v[d], f, more).x << 16);
-                } else
-                    y = __uint_as_float((uint32_t)((const uint16_t*)v)[d] << 16);
-                o[i] += pe * y;
+        const int w = unit_weight(R, mt);
+        const long long left = (x1 - x + w - 1) / w;
+        pc.s = s, pc.h = h, pc.mt = mt, pc.k0 = k;
+        pc.k1 = left < q.kt - k ? k + (int)left : q.kt;
+        pc.n = q.n, pc.base = q.base, pc.node0 = q.node0, pc.kt = q.kt, pc.R = R;
+        pc.unit = q.unit0 + h * row_tiles2(R) + mt;
+        pc.rows = min(kUnitRows, R - mt * kUnitRows);
+        x += (long long)(pc.k1 - pc.k0) * w;
+        k = pc.k1;
+        return true;
+    }
+};
+
+// the sequence, node and query head of row r of an entry's rows
+__device__ __forceinline__ void row_of(const AttnParams& p, int s, int r, int& b, int& node, int& g) {
+    const int f = r / p.group;
+    g = r - f * p.group;
+    b = s - 1;
+    node = f;
+    if (s == 0) {  // all sequences' nodes in a row: the last sequence whose first node is not behind f
+        int lo = 1, hi = p.batch;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (__ldcg(&p.seq[mid].node0) <= f)
+                lo = mid;
+            else
+                hi = mid - 1;
+        }
+        b = lo - 1;
+        node = f - __ldcg(&p.seq[lo].node0);
+    }
+}
+
+// which of the 32 slots from `slot` on row `node` sees; end: slots there are
+__device__ __forceinline__ uint32_t seen_word(const uint32_t* mask_row, int words, int node, int n, int base, int end, int slot) {
+    const int left = end - slot;
+    if (left <= 0) return 0;
+    const uint32_t in = left >= 32 ? 0xFFFFFFFFu : (1u << left) - 1;
+    const int j0 = slot - base;  // new row of the first slot
+    if (j0 <= -32) return in;
+    const uint32_t prefix = j0 < 0 ? (1u << -j0) - 1 : 0;
+    uint32_t tree;
+    if (mask_row == nullptr) {
+        const int upto = node - j0;  // slots up to this one
+        tree = upto < 0 ? 0 : upto >= 31 ? 0xFFFFFFFFu : (2u << upto) - 1;
+    } else if (j0 < 0) {
+        tree = mask_row[0] << -j0;
+    } else {
+        const int w = j0 >> 5, sh = j0 & 31;
+        const uint32_t lo = w < words ? mask_row[w] : 0, hi = sh && w + 1 < words ? mask_row[w + 1] : 0;
+        tree = __funnelshift_r(lo, hi, sh);
+    }
+    return in & (prefix | (tree & ~prefix));
+}
+
+// ---- the attention kernel ------------------------------------------------------------------------------------------
+template <int D, bool Q8>
+struct Shape {
+    static constexpr int kHalf = kTile * 128;                 // 128 rows of 128 bytes: 64 numbers of a row, in the 128-byte swizzle
+    static constexpr int kTileBytes = kTile * D * 2;          // a tile of Q, K or V in bf16
+    static constexpr int kRawBytes = kTile * D;               // a tile of e4m3 numbers
+    static constexpr int kStages = Q8 ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 10);
+    static constexpr int kRaw = Q8 ? (D == 128 ? 4 : 8) : 0;
+    static constexpr int kThreads = Q8 ? 448 : 320;
+    static constexpr int kConvWarps = Q8 ? 4 : 0;
+    static constexpr size_t kSmem = 1024 + 2 * kTileBytes + (size_t)kStages * kTileBytes + (size_t)kRaw * kRawBytes + 512;
+};
+
+// D (+)= A B with both operands in shared memory, a CTA by itself
+__device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate, uint32_t lead) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u), "r"(lead)
+        : "memory");
+}
+// V as the second operand of P V: rows (slots) of 64 numbers of head_dim side by side, so head_dim is the contiguous direction.  In the
+// 128-byte swizzle: blocks of 64 numbers kHalf apart, groups of eight slots 1024 bytes apart.
+__device__ __forceinline__ uint64_t desc_v(uint32_t addr, uint32_t half) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(half >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
+           ((uint64_t)2 << 61);
+}
+// 32 columns of the lane's row
+__device__ __forceinline__ void tmem_ld_32x32(uint32_t taddr, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, "
+        "%26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr));
+}
+// the same 32 registers, known to have arrived: nothing that reads them is moved ahead of the wait
+__device__ __forceinline__ void tmem_arrived(uint32_t (&r)[32]) {
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ bool not_finite2(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+
+// log(2^m sum); m = -inf: nothing seen, or nothing but what is not a number
+__device__ __forceinline__ float log_sum(float m, float sum) {
+    return sum == 0.0f ? -INFINITY : (m > -INFINITY ? m * 0.69314718f : 0.0f) + logf(sum);
+}
+
+// Entries of the ring are used in the order K0 V0 K1 V1 ... (two row tiles against every key tile), or K0 K1 V0 K2 V1 K3 ... (one row tile:
+// a stream's product with K(t + 2) follows its product with V(t)); T key tiles are 2 T entries either way.
+__device__ __forceinline__ int v_entry(bool two, int T, int t) { return two ? 1 + 2 * t : t <= T - 2 ? 2 + 2 * t : 2 * T - 1; }
+
+// What a row sees of new slots whose V is not a number, which was taken out of the products: added to its O in TMEM, with scores of
+// its own.  Key tiles t0, t0 + dt, .. of the piece; a whole warp calls it, `sums` are the rows that see anything, m their maxima.
+template <int D, bool Q8>
+__device__ __noinline__ void add_spoilt(const AttnParams& p, const Piece& pc, uint32_t tO, bool sums, int b, int node, int head, int t0,
+                                        int dt, int kv0, int end, float m) {
+    const CacheView& c = p.c;
+    const int32_t* table = c.table + (size_t)b * c.width;
+    const uint32_t* mask_row = p.mask ? p.mask + ((size_t)b * p.nmax + node) * p.words : nullptr;
+    const uint16_t* q = (const uint16_t*)p.q + ((long long)b * p.rows + node) * p.q_stride + (long long)head * D;
+    for (int t = t0; t < pc.k1 - pc.k0; t += dt) {
+        const int first = kv0 + (pc.k0 + t) * kTile;
+        for (int slot = max(first, pc.base); slot < min(end, first + kTile); ++slot) {
+            const size_t at = cache_row(c, __ldg(c.table + (size_t)(pc.s - 1) * c.width + (slot >> c.page_shift)), pc.h,
+                                        slot & ((1 << c.page_shift) - 1));
+            const auto entry = [&](const uint8_t* x, const uint8_t* exps, int d) {  // four numbers from d on
+                if (!Q8) return *(const uint2*)(x + at * c.row_bytes + 2 * d);
+                uint32_t f, more;
+                e4m3_factors(exps[at], f, more);
+                return e4m3x4_to_bf16(*(const uint32_t*)(x + at * c.row_bytes + d), f, more);
+            };
+            bool bad = false;  // the same in all lanes: a piece's rows have one sequence where there are new slots
+            for (int d = 0; d < D; d += 4) {
+                const uint2 v = entry(c.v, c.v_exp, d);
+                bad = bad || not_finite2(v.x) || not_finite2(v.y);
+            }
+            if (!bad) continue;
+            const bool mine = sums && (seen_word(mask_row, p.words, node, pc.n, pc.base, end, slot) & 1);
+            float s = 0.0f;
+            if (mine)
+                for (int d = 0; d < D; d += 4) {
+                    const uint2 k = entry(c.k, c.k_exp, d);
+                    for (int y = 0; y < 4; ++y) {
+                        const uint32_t qw = (((uint32_t)q[d + y] << 16) ^ (p.q_flip & 0xFFFF0000u)) & p.q_keep, kw = y < 2 ? k.x : k.y;
+                        s += __uint_as_float(qw) * __uint_as_float(y & 1 ? kw & 0xFFFF0000u : kw << 16);
+                    }
+                }
+            const float e = mine ? ex2_approx((s - m) * p.c2) : 0.0f;
+            for (int d = 0; d < D; d += 4) {
+                const uint2 v = entry(c.v, c.v_exp, d);
+                const uint32_t vw[4] = {v.x << 16, v.x & 0xFFFF0000u, v.y << 16, v.y & 0xFFFF0000u};
+                uint32_t o[4];
+                asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3])
+                             : "r"(tO + d));
+                tmem_wait_ld();
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    asm volatile("" : "+r"(o[y]));
+                    if (mine) o[y] = __float_as_uint(__uint_as_float(o[y]) + e * __uint_as_float(vw[y]));
+                }
+                asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tO + d), "r"(o[0]), "r"(o[1]), "r"(o[2]),
+                             "r"(o[3])
+                             : "memory");
+                tmem_wait_st();
             }
         }
     }
-    const size_t oat = ((size_t)b * p.rows + row) * p.q_heads + h;
-    for (int i = 0; i < D / 32; ++i) p.out[oat * D + lane + 32 * i] = __float2bfloat16(l > 0.0f ? o[i] / l : o[i]);
-    if (p.lse && lane == 0) p.lse[oat] = m > -INFINITY ? m + logf(l) : -INFINITY;
+}
+
+template <int D, bool Q8>
+__global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(const __grid_constant__ AttnParams p) {
+    using S = Shape<D, Q8>;
+    constexpr int NS = S::kStages, NR = S::kRaw > 0 ? S::kRaw : 1;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base_addr = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* const smem = smem_raw + (base_addr - smem_u32(smem_raw));
+    const uint32_t q_addr = base_addr, kv_addr = q_addr + 2 * S::kTileBytes, raw_addr = kv_addr + NS * S::kTileBytes;
+    uint8_t* const raw_ptr = smem + (raw_addr - base_addr);
+    uint64_t* bars = (uint64_t*)(raw_ptr + S::kRaw * S::kRawBytes);
+    const uint32_t bar0 = smem_u32(bars);
+    const auto kv_full = [&](int i) { return bar0 + 8 * i; };
+    const auto kv_empty = [&](int i) { return bar0 + 8 * (NS + i); };
+    const auto raw_full = [&](int i) { return bar0 + 8 * (2 * NS + i); };
+    const auto raw_empty = [&](int i) { return bar0 + 8 * (2 * NS + NR + i); };
+    const uint32_t q_full = bar0 + 8 * (2 * NS + 2 * NR), s_full0 = q_full + 8, p_full0 = q_full + 24, pair = q_full + 40;
+    volatile int* const gave_up = (volatile int*)(bars + 2 * NS + 2 * NR + 6);
+    volatile int* const spoilt = gave_up + 1;  // [2] the last piece (counted from 1) with a row of V that was taken out
+    uint32_t* const tmem_at = (uint32_t*)(gave_up + 3);
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int i = 0; i < NS; ++i) {
+            mbar_init(kv_full(i), Q8 ? S::kConvWarps : 1);
+            mbar_init(kv_empty(i), 1);
+        }
+        for (int i = 0; i < NR; ++i) {
+            mbar_init(raw_full(i), 1);
+            mbar_init(raw_empty(i), S::kConvWarps > 0 ? S::kConvWarps : 1);
+        }
+        mbar_init(q_full, 8);
+        mbar_init(pair, 8);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(s_full0 + 8 * i, 1);
+            mbar_init(p_full0 + 8 * i, 4);
+        }
+        *gave_up = 0;
+        spoilt[0] = spoilt[1] = 0;
+        mbar_fence_init();
+    }
+    if (warp == 8) tmem_alloc<false>(smem_u32(tmem_at), 512);
+    pdl_launch_dependents();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_at;
+    pdl_wait();
+
+    Walk walk;
+    walk.begin(p, blockIdx.x);
+    Piece pc;
+    const CacheView& c = p.c;
+
+    if (warp == 9) {
+        // ---- copies: K and V tiles page by page, into the ring (bf16) or to where the conversion takes them from (e4m3)
+        constexpr int N = Q8 ? NR : NS;
+        constexpr int kParts = Q8 ? 1 : D / 64;  // copies a page and tile
+        uint32_t it = 0;
+        bool ok = true;
+        const int box = p.box_rows, shift = c.page_shift, low = (1 << shift) - 1;
+        while (ok && walk.next(pc)) {
+            const int T = pc.k1 - pc.k0;
+            const bool two = pc.rows > kTile;
+            const int kv0 = pc.s == 0 ? 0 : p.shared, end = pc.s == 0 ? p.shared : pc.base + pc.n;
+            const int32_t* table = c.table + (pc.s == 0 ? 0 : (size_t)(pc.s - 1) * c.width);
+            const auto bring = [&](int t, bool is_v) {
+                const int first = kv0 + (pc.k0 + t) * kTile, upto = min(end, first + kTile);
+                const int copies = (upto - first + box - 1) / box;  // boxes with a slot in use
+                const int i = lane / kParts, part = lane % kParts;
+                int page = 0, at = 0;
+                if (i < copies) {
+                    const int slot = first + i * box;
+                    page = __ldg(table + (slot >> shift));
+                    at = slot & low;
+                }
+                const uint32_t st = it % N, full = Q8 ? raw_full(st) : kv_full(st), empty = Q8 ? raw_empty(st) : kv_empty(st);
+                if (!mbar_wait_bounded(empty, ((it / N) & 1) ^ 1, gave_up)) return false;
+                const uint32_t to = Q8 ? raw_addr + st * S::kRawBytes : kv_addr + st * S::kTileBytes;
+                if (lane == 0) mbar_arrive_expect_tx(full, copies * box * D * (Q8 ? 1 : 2));
+                __syncwarp();
+                if (i < copies)
+                    tma_load_2d(to + (Q8 ? i * box * D : part * S::kHalf + i * box * 128), is_v ? &p.map_v : &p.map_k, Q8 ? 0 : part * 64,
+                                (int)cache_row(c, page, pc.h, at), full);
+                it += 1;
+                return true;
+            };
+            if (two) {
+                for (int t = 0; ok && t < T; ++t) ok = bring(t, false) && bring(t, true);
+            } else {
+                ok = bring(0, false);
+                if (T > 1) ok = ok && bring(1, false);
+                for (int t = 0; ok && t < T; ++t) {
+                    ok = bring(t, true);
+                    if (t + 2 < T) ok = ok && bring(t + 2, false);
+                }
+            }
+        }
+        // (after a wait that ran out: what is on its way arrives before the CTA ends)
+        if (!ok && lane == 0)
+            for (uint32_t i = it > (uint32_t)N ? it - N : 0; i < it; ++i)
+                for (int w = 0; w < (1 << 16) && !mbar_try_wait(Q8 ? raw_full(i % N) : kv_full(i % N), (i / N) & 1); ++w) {
+                }
+        __syncwarp();
+    } else if (warp == 8) {
+        // ---- products
+        constexpr uint32_t id_s = umma_idesc(128, 128, true), id_o = umma_idesc(128, D, true) | (1u << 16);
+        const uint32_t lead = lane == 0;
+        uint32_t it = 0, n_piece = 0, n_p[2] = {0, 0};
+        bool ok = true;
+        const auto qk = [&](int i, bool two, uint32_t entry) {
+            const uint32_t a = q_addr + (two ? i : 0) * S::kTileBytes, b = kv_addr + (entry % NS) * S::kTileBytes;
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks)
+                umma_ss(tmem + i * 128, umma_desc_sw128(a + (ks >> 2) * S::kHalf + (ks & 3) * 32),
+                        umma_desc_sw128(b + (ks >> 2) * S::kHalf + (ks & 3) * 32), id_s, ks > 0, lead);
+        };
+        const auto pv = [&](int i, bool first, uint32_t entry) {
+            const uint32_t b = kv_addr + (entry % NS) * S::kTileBytes;
+#pragma unroll
+            for (int ks = 0; ks < kTile / 16; ++ks)
+                umma_ts(tmem + 256 + i * 128, tmem + i * 128 + ks * 8, desc_v(b + ks * 2048, S::kHalf), id_o, !first || ks > 0, lead);
+        };
+        const auto wait_kv = [&](uint32_t entry) {
+            const bool r = mbar_wait_bounded(kv_full(entry % NS), (entry / NS) & 1, gave_up);
+            tc_fence_after();
+            return r;
+        };
+        const auto wait_p = [&](int i) {
+            const bool r = mbar_wait_bounded(p_full0 + 8 * i, n_p[i] & 1, gave_up);
+            n_p[i] += 1;
+            tc_fence_after();
+            return r;
+        };
+        while (ok && walk.next(pc)) {
+            const int T = pc.k1 - pc.k0;
+            const bool two = pc.rows > kTile;
+            ok = mbar_wait_bounded(q_full, n_piece & 1, gave_up);
+            n_piece += 1;
+            if (!ok) break;
+            if (two) {
+                if (!(ok = wait_kv(it))) break;
+                for (int i = 0; i < 2; ++i) {
+                    qk(i, true, it);
+                    umma_commit_by(s_full0 + 8 * i, lead);
+                }
+                umma_commit_by(kv_empty(it % NS), lead);
+                for (int t = 0; ok && t < T; ++t) {
+                    const uint32_t ev = it + 1 + 2 * t, ek = ev + 1;
+                    for (int i = 0; ok && i < 2; ++i) {
+                        ok = wait_p(i) && (i == 1 || wait_kv(ev));
+                        if (!ok) break;
+                        pv(i, t == 0, ev);
+                        if (i == 1) umma_commit_by(kv_empty(ev % NS), lead);
+                        if (t + 1 < T) {
+                            if (i == 0 && !(ok = wait_kv(ek))) break;
+                            qk(i, true, ek);
+                            if (i == 1) umma_commit_by(kv_empty(ek % NS), lead);
+                        }
+                        umma_commit_by(s_full0 + 8 * i, lead);
+                    }
+                }
+            } else {
+                for (int i = 0; ok && i < min(T, 2); ++i) {
+                    if (!(ok = wait_kv(it + i))) break;
+                    qk(i, false, it + i);
+                    umma_commit_by(kv_empty((it + i) % NS), lead);
+                    umma_commit_by(s_full0 + 8 * i, lead);
+                }
+                for (int t = 0; ok && t < T; ++t) {
+                    const int i = t & 1;
+                    const uint32_t ev = it + v_entry(false, T, t), ek = ev + 1;
+                    if (!(ok = wait_p(i) && wait_kv(ev))) break;
+                    pv(i, t < 2, ev);
+                    umma_commit_by(kv_empty(ev % NS), lead);
+                    if (t + 2 < T) {
+                        if (!(ok = wait_kv(ek))) break;
+                        qk(i, false, ek);
+                        umma_commit_by(kv_empty(ek % NS), lead);
+                    }
+                    umma_commit_by(s_full0 + 8 * i, lead);
+                }
+            }
+            it += 2 * T;
+        }
+    } else if (warp < 8) {
+        // ---- softmax: a thread a row
+        const int i = warp >> 2, row_in_tile = tid & 127;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the lanes
+        const uint32_t tS = tmem + lanes + i * 128, tO = tmem + lanes + 256 + i * 128;
+        uint32_t it = 0, n_s = 0, n_piece = 0, n_pair = 0;
+        bool ok = true;
+        const float c2 = p.c2;
+        const auto both = [&]() {  // the two streams meet
+            __syncwarp();
+            if (lane == 0) mbar_arrive(pair);
+            const bool r = mbar_wait_bounded(pair, n_pair & 1, gave_up);
+            n_pair += 1;
+            return r;
+        };
+        const auto wait_s = [&]() {
+            const bool r = mbar_wait_bounded(s_full0 + 8 * i, n_s & 1, gave_up);
+            n_s += 1;
+            tc_fence_after();
+            return r;
+        };
+        while (ok && walk.next(pc)) {
+            n_piece += 1;
+            const int T = pc.k1 - pc.k0;
+            const bool two = pc.rows > kTile;
+            const int kv0 = pc.s == 0 ? 0 : p.shared, end = pc.s == 0 ? p.shared : pc.base + pc.n;
+            const int r = (two ? i * kTile : 0) + row_in_tile;  // row of the unit
+            const bool live = r < pc.rows;
+            int b = 0, node = 0, g = 0;
+            if (live) row_of(p, pc.s, pc.mt * kUnitRows + r, b, node, g);
+            const int head = pc.h * p.group + g;
+            const size_t q_row = (size_t)b * p.rows + node;
+            const uint32_t* mask_row = p.mask ? p.mask + ((size_t)b * p.nmax + node) * p.words : nullptr;
+            if (two || i == 0) {
+                const uint32_t to = q_addr + i * S::kTileBytes + row_in_tile * 128;
+                const uint4* from = (const uint4*)(p.q + 2 * ((long long)q_row * p.q_stride + (long long)head * D));
+#pragma unroll
+                for (int x = 0; x < D / 8; ++x) {
+                    uint4 u = live ? __ldg(from + x) : make_uint4(0, 0, 0, 0);
+                    u.x = (u.x ^ p.q_flip) & p.q_keep, u.y = (u.y ^ p.q_flip) & p.q_keep;
+                    u.z = (u.z ^ p.q_flip) & p.q_keep, u.w = (u.w ^ p.q_flip) & p.q_keep;
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (x >> 3) * S::kHalf +
+                                                                                  ((((uint32_t)x & 7) ^ (row_in_tile & 7)) << 4)),
+                                 "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w)
+                                 : "memory");
+                }
+                fence_proxy_async();
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full);
+            const bool warp_live = __any_sync(0xFFFFFFFFu, live);
+            float m = -INFINITY, l = 0.0f;  // maximum of the raw scores, sum of 2^(c2 (s - m))
+            bool any = false;               // this stream has had a tile
+            for (int t = two ? 0 : i; t < T; t += two ? 1 : 2) {
+                if (!(ok = wait_s())) break;
+                const int first = kv0 + (pc.k0 + t) * kTile;
+                const bool masked = first + kTile > pc.base;  // new slots, or slots that are not there (the shared prefix: base is its end)
+                if (warp_live) {
+                    uint32_t u[32];
+                    uint32_t sees[4] = {0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu};
+                    if (masked)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            sees[x] = live ? seen_word(mask_row, p.words, node, pc.n, pc.base, end, first + 32 * x) : 0;
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        tmem_ld_32x32(tS + 32 * x, u);
+                        tmem_arrived(u);
+                        if (masked) {
+#pragma unroll
+                            for (int y = 0; y < 32; ++y) mx = fmaxf(mx, (sees[x] >> y) & 1 ? __uint_as_float(u[y]) : -INFINITY);
+                        } else {
+#pragma unroll
+                            for (int y = 0; y < 32; ++y) mx = fmaxf(mx, __uint_as_float(u[y]));
+                        }
+                    }
+                    // (m = -inf: nothing seen so far, and what O holds is zero)
+                    const bool grown = mx > m && !((mx - m) * c2 <= 8.0f);
+                    if (__any_sync(0xFFFFFFFFu, grown)) {
+                        const float now = fmaxf(mx, m), f = m > -INFINITY ? ex2_approx((m - now) * c2) : 1.0f;
+                        if (any) {
+#pragma unroll
+                            for (int x = 0; x < D / 32; ++x) {
+                                tmem_ld_32x32(tO + 32 * x, u);
+                                tmem_arrived(u);
+#pragma unroll
+                                for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(__uint_as_float(u[y]) * f);
+                                tmem_st_32x32(tO + 32 * x, u);
+                            }
+                        }
+                        l *= f;
+                        m = now;
+                    }
+                    const float mc = m > -INFINITY ? m * c2 : 0.0f;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        uint32_t w[32];
+                        float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            tmem_ld_32x32(tS + 64 * x + 32 * z, u);
+                            tmem_arrived(u);
+                            if (masked) {
+#pragma unroll
+                                for (int y = 0; y < 32; ++y)
+                                    u[y] = (sees[2 * x + z] >> y) & 1 ? u[y] : 0xFF800000u;
+                            }
+#pragma unroll
+                            for (int y = 0; y < 32; y += 2) {
+                                const float e0 = ex2_approx(fmaf(__uint_as_float(u[y]), c2, -mc));
+                                const float e1 = ex2_approx(fmaf(__uint_as_float(u[y + 1]), c2, -mc));
+                                part[y >> 1 & 3] += e0 + e1;
+                                w[16 * z + (y >> 1)] = pack_bf16(e0, e1);
+                            }
+                        }
+                        tmem_st_32x32(tS + 32 * x, w);
+                        l += (part[0] + part[1]) + (part[2] + part[3]);
+                    }
+                    tmem_wait_st();
+                }
+                // Slots that are not there hold anything, and new slots may hold what is not a number and is not for every row: weights of zero do
+                // not keep it out of the sums.  Their rows of V are cleared (a thread a slot); rows that see such a slot get it in the end.
+                if (masked && (i == 0 || !two)) {
+                    const uint32_t entry = it + v_entry(two, T, t);
+                    if (!(ok = mbar_wait_bounded(kv_full(entry % NS), (entry / NS) & 1, gave_up))) break;
+                    const int slot = first + row_in_tile;
+                    if (slot >= pc.base) {
+                        const uint32_t at = kv_addr + (entry % NS) * S::kTileBytes + row_in_tile * 128;
+                        bool clear = slot >= end;
+                        if (!clear)
+#pragma unroll
+                            for (int x = 0; x < D / 8; ++x) {
+                                uint32_t a0, a1, a2, a3;
+                                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                             : "=r"(a0), "=r"(a1), "=r"(a2), "=r"(a3)
+                                             : "r"(at + (x >> 3) * S::kHalf + (x & 7) * 16)
+                                             : "memory");
+                                clear = clear || not_finite2(a0) || not_finite2(a1) || not_finite2(a2) || not_finite2(a3);
+                            }
+                        if (clear) {
+#pragma unroll
+                            for (int x = 0; x < D / 8; ++x)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + (x >> 3) * S::kHalf + (x & 7) * 16), "r"(0)
+                                             : "memory");
+                            if (slot < end) spoilt[i] = (int)n_piece;
+                        }
+                    }
+                    fence_proxy_async();
+                }
+                any = true;
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full0 + 8 * i);
+            }
+            if (!ok) break;
+            it += 2 * T;
+            if (any)
+                ok = wait_s();  // the last product is done
+            else
+                ok = mbar_wait_bounded(q_full, (n_piece - 1) & 1, gave_up);  // (nor does a stream without a tile run ahead)
+            if (!ok) break;
+
+            // ---- the end of a piece: O as far as it goes
+            if (spoilt[two ? 0 : i] == (int)n_piece)
+                add_spoilt<D, Q8>(p, pc, tO, live && m > -INFINITY, b, node, head, two ? 0 : i, two ? 1 : 2, kv0, end, m);
+            const bool whole = pc.k0 == 0 && pc.k1 == pc.kt && p.shared == 0;
+            const size_t slot = p.shared > 0 ? (size_t)pc.unit + blockIdx.x : 2 * (size_t)blockIdx.x + (pc.k0 == 0 ? 1 : 0);
+            const size_t out_row = q_row * p.q_heads + head;
+            const auto put = [&](int d0, const uint32_t (&u)[32], float inv) {
+                if (!live) return;
+                if (whole) {
+                    uint4* to = (uint4*)(p.out + out_row * D + d0);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int y = 0; y < 4; ++y)
+                            w[y] = pack_bf16(__uint_as_float(u[8 * x + 2 * y]) * inv, __uint_as_float(u[8 * x + 2 * y + 1]) * inv);
+                        to[x] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                } else {
+                    float4* to = (float4*)(p.part_o + (slot * kUnitRows + r) * D + d0);
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)
+                        to[x] = make_float4(__uint_as_float(u[4 * x]), __uint_as_float(u[4 * x + 1]), __uint_as_float(u[4 * x + 2]),
+                                            __uint_as_float(u[4 * x + 3]));
+                }
+            };
+            const auto put_sums = [&](float mm, float ll) {
+                if (!live) return;
+                if (!whole)
+                    p.part_ml[slot * kUnitRows + r] = make_float2(mm > -INFINITY ? mm * c2 : -INFINITY, ll);
+                else if (p.lse)
+                    p.lse[out_row] = log_sum(mm > -INFINITY ? mm * c2 : -INFINITY, ll);
+            };
+            uint32_t u[32];
+            if (two || T == 1) {
+                if (two || i == 0) {
+                    const float inv = l != 0.0f ? 1.0f / l : 1.0f;  // (a row that sees nothing: O is zero)
+#pragma unroll
+                    for (int x = 0; x < D / 32; ++x) {
+                        tmem_ld_32x32(tO + 32 * x, u);
+                        tmem_arrived(u);
+                        put(32 * x, u, inv);
+                    }
+                    put_sums(m, l);
+                }
+            } else {
+                // the streams' halves are joined: the second one's goes through the shared memory of the row tile that is not there
+                float* const tmp = (float*)(smem + S::kTileBytes);  // [D / 2 columns][128 rows]
+                float m1 = 0.0f, l1 = 0.0f, f0 = 1.0f, f1 = 0.0f, ms = 0.0f, ls = 0.0f, inv = 1.0f;
+#pragma unroll
+                for (int half = 0; half < 2 && ok; ++half) {
+                    // maximum and sum of the second stream go ahead of its sums
+                    if (half == 0) {
+                        if (i == 1) {
+                            tmp[row_in_tile] = m;
+                            tmp[128 + row_in_tile] = l;
+                        }
+                        if (!(ok = both())) break;
+                        if (i == 0) {
+                            m1 = tmp[row_in_tile];
+                            l1 = tmp[128 + row_in_tile];
+                            ms = fmaxf(m, m1);
+                            f0 = m > -INFINITY ? ex2_approx((m - ms) * c2) : 0.0f;
+                            f1 = m1 > -INFINITY ? ex2_approx((m1 - ms) * c2) : 0.0f;
+                            ls = l * f0 + l1 * f1;
+                            inv = ls != 0.0f ? 1.0f / ls : 1.0f;
+                        }
+                        if (!(ok = both())) break;
+                    }
+                    if (i == 1) {
+#pragma unroll
+                        for (int x = 0; x < D / 64; ++x) {
+                            const int d0 = half * (D / 2) + 32 * x;
+                            tmem_ld_32x32(tO + d0, u);
+                            tmem_arrived(u);
+#pragma unroll
+                            for (int y = 0; y < 32; ++y) tmp[(32 * x + y) * 128 + row_in_tile] = __uint_as_float(u[y]);
+                        }
+                    }
+                    if (!(ok = both())) break;
+                    if (i == 0) {
+#pragma unroll
+                        for (int x = 0; x < D / 64; ++x) {
+                            const int d0 = half * (D / 2) + 32 * x;
+                            tmem_ld_32x32(tO + d0, u);
+                            tmem_arrived(u);
+#pragma unroll
+                            for (int y = 0; y < 32; ++y)
+                                u[y] = __float_as_uint(__uint_as_float(u[y]) * f0 + tmp[(32 * x + y) * 128 + row_in_tile] * f1);
+                            put(d0, u, inv);
+                        }
+                    }
+                    ok = both();
+                }
+                if (i == 0 && ok) put_sums(ms, ls);
+            }
+            tc_fence_before();  // what follows in TMEM follows these reads
+        }
+    } else if (Q8) {
+        // ---- e4m3 tiles to bf16 tiles in the 128-byte swizzle: sixteen numbers a thread and step
+        const int ct = tid - 320;  // 0 .. 127
+        constexpr int kPer = D / 16, kRowsStep = 128 / kPer, kSteps = kTile / kRowsStep;
+        const int col = ct % kPer, row0 = ct / kPer;
+        uint32_t it = 0;
+        bool ok = true;
+        const int shift = c.page_shift, low = (1 << shift) - 1;
+        while (ok && walk.next(pc)) {
+            const int T = pc.k1 - pc.k0;
+            const bool two = pc.rows > kTile;
+            const int kv0 = pc.s == 0 ? 0 : p.shared, end = pc.s == 0 ? p.shared : pc.base + pc.n;
+            const int32_t* table = c.table + (pc.s == 0 ? 0 : (size_t)(pc.s - 1) * c.width);
+            const auto convert = [&](int t, bool is_v) {
+                const int first = kv0 + (pc.k0 + t) * kTile;
+                uint32_t exps[kSteps];
+                const uint8_t* from = is_v ? c.v_exp : c.k_exp;
+#pragma unroll
+                for (int x = 0; x < kSteps; ++x) {
+                    const int slot = first + x * kRowsStep + row0;
+                    exps[x] = slot < end ? __ldg(from + cache_row(c, __ldg(table + (slot >> shift)), pc.h, slot & low)) : 127;
+                }
+                const uint32_t rs = it % NR, ks = it % NS;
+                if (!mbar_wait_bounded(raw_full(rs), (it / NR) & 1, gave_up)) return false;
+                if (!mbar_wait_bounded(kv_empty(ks), ((it / NS) & 1) ^ 1, gave_up)) return false;
+                const uint8_t* raw = raw_ptr + rs * S::kRawBytes;
+                const uint32_t to = kv_addr + ks * S::kTileBytes + (col >> 2) * S::kHalf;
+#pragma unroll
+                for (int x = 0; x < kSteps; ++x) {
+                    const int row = x * kRowsStep + row0;
+                    const uint4 y = *(const uint4*)(raw + row * D + col * 16);
+                    uint32_t f, more;
+                    e4m3_factors(exps[x], f, more);
+                    const uint2 a = e4m3x4_to_bf16(y.x, f, more), d = e4m3x4_to_bf16(y.y, f, more);
+                    const uint2 e = e4m3x4_to_bf16(y.z, f, more), h = e4m3x4_to_bf16(y.w, f, more);
+                    const uint4 lo = make_uint4(a.x, a.y, d.x, d.y), hi = make_uint4(e.x, e.y, h.x, h.y);
+                    // (the second half of a row's threads store their second piece first: eight threads then use all banks)
+                    const uint32_t chunk = (col & 3) * 2, at = to + row * 128, swap = D == 128 ? (uint32_t)col >> 2 : 0u;
+                    const uint4 w0 = swap ? hi : lo, w1 = swap ? lo : hi;
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((chunk + swap) ^ (row & 7)) << 4)), "r"(w0.x),
+                                 "r"(w0.y), "r"(w0.z), "r"(w0.w)
+                                 : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((chunk + 1 - swap) ^ (row & 7)) << 4)), "r"(w1.x),
+                                 "r"(w1.y), "r"(w1.z), "r"(w1.w)
+                                 : "memory");
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(raw_empty(rs));
+                    mbar_arrive(kv_full(ks));
+                }
+                it += 1;
+                return true;
+            };
+            if (two) {
+                for (int t = 0; ok && t < T; ++t) ok = convert(t, false) && convert(t, true);
+            } else {
+                ok = convert(0, false);
+                if (T > 1) ok = ok && convert(1, false);
+                for (int t = 0; ok && t < T; ++t) {
+                    ok = convert(t, true);
+                    if (t + 2 < T) ok = ok && convert(t + 2, false);
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (*gave_up && p.status)
+        for (int i = tid; i < p.batch; i += blockDim.x) atomicOr(p.status + i, GRAFT_ST_INTERNAL);
+    if (warp == 8) tmem_free<false>(tmem, 512);
+}
+
+// ---- joining the pieces ----------------------------------------------------------------------------------------------
+// pieces of a unit: CTAs that have tiles of it
+struct UnitAt {
+    long long x0;  // position of its first tile
+    int w, kt;
+};
+__device__ __forceinline__ UnitAt unit_at(const PlanSeq& q, int group, int h, int mt) {
+    const int R = q.n * group;
+    UnitAt u;
+    u.x0 = q.cost0 + h * head_cost(R, q.kt) + 2LL * q.kt * mt;
+    u.w = unit_weight(R, mt);
+    u.kt = q.kt;
+    return u;
+}
+// first tile of the unit that is not ahead of CTA c's stretch
+__device__ __forceinline__ int first_tile(const UnitAt& u, long long total, int parts, int c) {
+    const long long d = part_first(total, parts, c) - u.x0;
+    if (d <= 0) return 0;
+    const long long k = (d + u.w - 1) / u.w;
+    return k < u.kt ? (int)k : u.kt;
+}
+__device__ __forceinline__ int cta_of(long long x, long long total, int parts) { return (int)(x * parts / total); }
+
+template <int D>
+struct Joined {
+    static constexpr int kPer = D / 32;
+    float m, l, o[kPer];
+    __device__ __forceinline__ void clear() {
+        m = -INFINITY, l = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) o[i] = 0.0f;
+    }
+    // a piece's row; the whole warp
+    __device__ __forceinline__ void add(const AttnParams& p, size_t slot, int r, int lane) {
+        const float2 ml = __ldcg(p.part_ml + slot * kUnitRows + r);
+        const float* from = p.part_o + (slot * kUnitRows + r) * D + lane * kPer;
+        float x[kPer];
+        if (kPer == 4) {
+            const float4 v = __ldcg((const float4*)from);
+            x[0] = v.x, x[1] = v.y, x[2 % kPer] = v.z, x[3 % kPer] = v.w;
+        } else {
+            const float2 v = __ldcg((const float2*)from);
+            x[0] = v.x, x[1] = v.y;
+        }
+        const float now = fmaxf(m, ml.x);
+        const float f0 = m > -INFINITY ? ex2_approx(m - now) : 0.0f, f1 = ml.x > -INFINITY ? ex2_approx(ml.x - now) : 0.0f;
+        m = now;
+        l = l * f0 + ml.y * f1;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) o[i] = o[i] * f0 + x[i] * f1;
+    }
+    __device__ __forceinline__ void store(const AttnParams& p, size_t out_row, int lane) {
+        const float inv = l != 0.0f ? 1.0f / l : 1.0f;
+        uint32_t* to = (uint32_t*)(p.out + out_row * D) + lane * (kPer / 2);
+        if (kPer == 4)
+            *(uint2*)to = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2 % kPer] * inv, o[3 % kPer] * inv));
+        else
+            *to = pack_bf16(o[0] * inv, o[1] * inv);
+        if (p.lse && lane == 0) p.lse[out_row] = log_sum(m, l);
+    }
+};
+
+constexpr int kJoinThreads = 256;
+
+// Units that were cut, without a shared prefix: a block row a boundary between CTAs; the first boundary inside a unit joins it.
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_constant__ AttnParams p) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int c = blockIdx.y + 1, lane = lane_id();
+    const long long total = __ldcg(&p.head->total);
+    const int parts = __ldcg(&p.head->parts);
+    if (c >= parts) return;
+    const int4 st = __ldcg((const int4*)(p.start + c));
+    PlanSeq q;
+    ((int4*)&q)[0] = __ldcg((const int4*)(p.seq + st.x));
+    ((int4*)&q)[1] = __ldcg((const int4*)(p.seq + st.x) + 1);
+    if (st.w == 0 || st.w >= q.kt) return;  // the stretch begins with a unit
+    const UnitAt u = unit_at(q, p.group, st.y, st.z);
+    const int f = cta_of(u.x0, total, parts);
+    const int k1f = first_tile(u, total, parts, f + 1);
+    // tiles before this CTA's are those of the unit's first CTA: nobody joins it ahead of this one (CTAs without a tile have none to join)
+    if (k1f != st.w) return;
+    if (first_tile(u, total, parts, c + 1) <= st.w) return;
+    const int l = cta_of(u.x0 + (long long)(u.kt - 1) * u.w, total, parts);
+    const int R = q.n * p.group, rows = min(kUnitRows, R - st.z * kUnitRows);
+    for (int r = blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5); r < rows; r += gridDim.x * (kJoinThreads / 32)) {
+        int b, node, g;
+        row_of(p, st.x, st.z * kUnitRows + r, b, node, g);
+        Joined<D> j;
+        j.clear();
+        j.add(p, 2 * (size_t)f + 1, r, lane);
+        for (int d = f + 1; d <= l; ++d)
+            if (first_tile(u, total, parts, d + 1) > first_tile(u, total, parts, d)) j.add(p, 2 * (size_t)d, r, lane);
+        j.store(p, ((size_t)b * p.rows + node) * p.q_heads + st.y * p.group + g, lane);
+    }
+}
+
+// Behind a shared prefix every row has pieces of two units: a warp a row.
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) attn_join_shared_kernel(const __grid_constant__ AttnParams p) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int b = blockIdx.y, lane = lane_id();
+    PlanSeq q[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int4* a = (const int4*)(p.seq + (i == 0 ? 0 : b + 1));
+        ((int4*)&q[i])[0] = __ldcg(a);
+        ((int4*)&q[i])[1] = __ldcg(a + 1);
+    }
+    const long long total = __ldcg(&p.head->total);
+    const int parts = __ldcg(&p.head->parts);
+    const int rows = q[1].n * p.q_heads;
+    for (int x = blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5); x < rows; x += gridDim.x * (kJoinThreads / 32)) {
+        const int node = x / p.q_heads, head = x - node * p.q_heads, h = head / p.group, g = head - h * p.group;
+        Joined<D> j;
+        j.clear();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = ((i == 0 ? q[1].node0 : 0) + node) * p.group + g, mt = r / kUnitRows;
+            const UnitAt u = unit_at(q[i], p.group, h, mt);
+            const int unit = q[i].unit0 + h * row_tiles2(q[i].n * p.group) + mt;
+            const int f = cta_of(u.x0, total, parts), l = cta_of(u.x0 + (long long)(u.kt - 1) * u.w, total, parts);
+            for (int d = f; d <= l; ++d)
+                if (first_tile(u, total, parts, d + 1) > first_tile(u, total, parts, d)) j.add(p, (size_t)unit + d, r - mt * kUnitRows, lane);
+        }
+        j.store(p, ((size_t)b * p.rows + node) * p.q_heads + head, lane);
+    }
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled() {
+    static const EncodeTiledFn fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            return (EncodeTiledFn) nullptr;
+        }
+        return (EncodeTiledFn)f;
+    }();
+    return fn;
+}
+// Entries of one layer as rows: boxes of 64 bf16 numbers in the 128-byte swizzle, or of whole rows of e4m3 numbers as they are.
+bool encode_map(CUtensorMap* map, const void* base, bool q8, int D, uint64_t rows, int box_rows) {
+    const cuuint64_t dims[2] = {(cuuint64_t)D, rows}, strides[1] = {(cuuint64_t)D * (q8 ? 1 : 2)};
+    const cuuint32_t box[2] = {(cuuint32_t)(q8 ? D : 64), (cuuint32_t)box_rows}, step[2] = {1, 1};
+    return encode_tiled()(map, q8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
+                          strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, q8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct AttnSizes {
+    size_t o_seq, o_start, o_ml, o_o, total;
+};
+AttnSizes attn_sizes(const graft_ctx* ctx, int batch, int kv_heads, int head_dim, int group, int rows, int shared) {
+    const auto units = [&](long long nodes) { return (size_t)kv_heads * (size_t)((nodes * group + kUnitRows - 1) / kUnitRows); };
+    const size_t slots = shared > 0 ? units((long long)batch * rows) + (size_t)batch * units(rows) + ctx->num_sms : 2 * (size_t)ctx->num_sms;
+    AttnSizes z;
+    size_t off = 256;
+    const auto take = [&](size_t bytes) {
+        const size_t o = off;
+        off = (off + bytes + 255) / 256 * 256;
+        return o;
+    };
+    z.o_seq = take((size_t)(batch + 1) * sizeof(PlanSeq));
+    z.o_start = take((size_t)ctx->num_sms * sizeof(PlanStart));
+    z.o_ml = take(slots * kUnitRows * sizeof(float2));
+    z.o_o = take(slots * kUnitRows * head_dim * sizeof(float));
+    z.total = off;
+    return z;
+}
+
+template <int D, bool Q8>
+cudaError_t launch_attn(graft_ctx* ctx, const AttnParams& p, cudaStream_t st) {
+    using S = Shape<D, Q8>;
+    constexpr int kReady = 1 << ((D == 128) + 2 * Q8);
+    cudaError_t e;
+    if (!(ctx->attn_ready & kReady)) {
+        e = allow_smem((const void*)tree_attn_kernel<D, Q8>, S::kSmem);
+        if (e != cudaSuccess) return e;
+        ctx->attn_ready |= kReady;
+    }
+    e = launch_pdl(attn_plan_kernel, dim3(p.batch), dim3(kPlanThreads), 0, st, p);
+    if (e != cudaSuccess) return e;
+    ctx->launches += 1;
+    e = launch_pdl(tree_attn_kernel<D, Q8>, dim3(p.ctas), dim3(S::kThreads), S::kSmem, st, p);
+    if (e != cudaSuccess) return e;
+    ctx->launches += 1;
+    if (p.shared > 0) {
+        const long long warps = (long long)p.rows * p.q_heads;
+        const int blocks = (int)min((warps + kJoinThreads / 32 - 1) / (kJoinThreads / 32), 1024LL);
+        e = launch_pdl(attn_join_shared_kernel<D>, dim3(blocks, p.batch), dim3(kJoinThreads), 0, st, p);
+    } else if (p.ctas > 1) {
+        const int rows = min((long long)kUnitRows, (long long)p.rows * p.group);
+        e = launch_pdl(attn_join_kernel<D>, dim3((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32), p.ctas - 1), dim3(kJoinThreads), 0, st, p);
+    }
+    ctx->launches += 1;
+    return e;
 }
 
 }  // namespace
 
+size_t tree_attn_scratch_bytes(const graft_ctx* ctx, int batch, const graft_cache* cache, int q_heads, int rows, int shared) {
+    return attn_sizes(ctx, batch, cache->kv_heads, cache->head_dim, q_heads / cache->kv_heads, rows, shared).total;
+}
+
 cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache, int layer, int q_heads, int rows, long long q_stride,
                              const void* d_q, float scale, const int32_t* d_prefix_len, const int32_t* d_count, const uint32_t* d_mask,
-                             int shared, void* d_out, float* d_lse, int32_t* d_status, cudaStream_t st) {
+                             int shared, void* d_out, float* d_lse, int32_t* d_status, void* scratch, cudaStream_t st) {
+    if (encode_tiled() == nullptr) return cudaErrorNotSupported;
     AttnParams p;
     p.c = cache_view(cache, layer);
+    const bool q8 = cache->dtype == GRAFT_E4M3;
+    p.box_rows = cache->page_size < kTile ? cache->page_size : kTile;
+    const uint64_t cache_rows = (uint64_t)cache->n_pages * cache->kv_heads * cache->page_size;
+    if (!encode_map(&p.map_k, p.c.k, q8, cache->head_dim, cache_rows, p.box_rows) ||
+        !encode_map(&p.map_v, p.c.v, q8, cache->head_dim, cache_rows, p.box_rows))
+        return cudaErrorInvalidValue;
     p.q = (const uint8_t*)d_q;
     p.q_stride = q_stride;
     p.prefix_len = d_prefix_len;
@@ -108,19 +1183,28 @@ cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache
     p.out = (__nv_bfloat16*)d_out;
     p.lse = d_lse;
     p.status = d_status;
-    p.scale = scale;
+    p.c2 = scale == 0.0f ? kLog2e : fabsf(scale) * kLog2e;
+    p.q_flip = scale < 0.0f ? 0x80008000u : 0u;
+    p.q_keep = scale == 0.0f ? 0u : 0xFFFFFFFFu;
     p.rows = rows;
     p.q_heads = q_heads;
+    p.group = q_heads / cache->kv_heads;
     p.shared = shared;
     p.nmax = ctx->nmax;
     p.words = ctx->mask_words;
-    const dim3 grid((unsigned)(((long long)rows * q_heads + 3) / 4), batch);
-    const bool q8 = cache->dtype == GRAFT_E4M3;
-    const auto kernel = cache->head_dim == 128 ? (q8 ? tree_attn_kernel<128, true> : tree_attn_kernel<128, false>)
-                                               : (q8 ? tree_attn_kernel<64, true> : tree_attn_kernel<64, false>);
-    const cudaError_t e = launch_pdl(kernel, grid, dim3(128), 0, st, p);
-    ctx->launches += 1;
-    return e != cudaSuccess ? e : cudaGetLastError();
+    p.batch = batch;
+    p.ctas = ctx->num_sms;
+    p.min_cost = 2;
+    const AttnSizes z = attn_sizes(ctx, batch, cache->kv_heads, cache->head_dim, p.group, rows, shared);
+    uint8_t* base = (uint8_t*)scratch;
+    p.head = (PlanHead*)base;
+    p.seq = (PlanSeq*)(base + z.o_seq);
+    p.start = (PlanStart*)(base + z.o_start);
+    p.part_ml = (float2*)(base + z.o_ml);
+    p.part_o = (float*)(base + z.o_o);
+    p.arrivals = ctx->w_attn_n;
+    return cache->head_dim == 128 ? (q8 ? launch_attn<128, true>(ctx, p, st) : launch_attn<128, false>(ctx, p, st))
+                                  : (q8 ? launch_attn<64, true>(ctx, p, st) : launch_attn<64, false>(ctx, p, st));
 }
 
 }  // namespace graft
