@@ -474,7 +474,7 @@ static graft_status check_cache(const graft_ctx* ctx, int32_t batch, const graft
         return GRAFT_ERR_INVALID_ARG;
     if (c->layers < 1 || c->n_pages < 1 || c->kv_heads < 1 || c->table_width < 1) return GRAFT_ERR_INVALID_ARG;
     if (layer < 0 || layer >= c->layers) return GRAFT_ERR_INVALID_ARG;
-    if (((uintptr_t)c->d_k | (uintptr_t)c->d_v) & 15) return GRAFT_ERR_INVALID_ARG;
+    if (((uintptr_t)c->d_k | (uintptr_t)c->d_v | (uintptr_t)c->d_k_exp | (uintptr_t)c->d_v_exp) & 15) return GRAFT_ERR_INVALID_ARG;
     if (c->head_dim != 64 && c->head_dim != 128) return GRAFT_ERR_UNSUPPORTED;
     if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return GRAFT_ERR_UNSUPPORTED;
     if ((double)c->kv_heads * c->n_pages * c->page_size >= 2147483648.0) return GRAFT_ERR_UNSUPPORTED;
@@ -536,6 +536,10 @@ graft_status graft_tree_attention(graft_ctx* ctx, int32_t batch, const graft_cac
     if ((gs = check_rows(cache, rows, q_heads, q_stride)) != GRAFT_OK) return gs;
     if (d_mask && rows > ctx->nmax) return GRAFT_ERR_INVALID_ARG;
     if (shared < 0 || shared % cache->page_size || shared > cache->table_width * cache->page_size) return GRAFT_ERR_INVALID_ARG;
+    // positions in the line of key tiles are 32-bit numbers (a tile of 128 rows against 128 slots is one)
+    const double row_tiles = (double)batch * ((double)rows * (q_heads / cache->kv_heads) / 128 + 2);
+    if (2 * row_tiles * cache->kv_heads * ((double)cache->table_width * cache->page_size / 128 + 2) >= 2147483648.0) return GRAFT_ERR_UNSUPPORTED;
+    if (cache->kv_heads > 65535 || batch > 65535) return GRAFT_ERR_UNSUPPORTED;
     void* scratch = grown(ctx->attn_scratch, tree_attn_scratch_bytes(ctx, batch, cache, q_heads, rows, shared));
     if (scratch == nullptr) return GRAFT_ERR_WORKSPACE;
     if (tree_attn_launch(ctx, batch, cache, layer, q_heads, rows, q_stride, d_q, scale, d_prefix_len, d_count, d_mask, shared, d_out,

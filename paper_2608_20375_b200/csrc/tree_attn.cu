@@ -34,17 +34,17 @@ struct __align__(16) PlanSeq {
     int base;    // slots before the first row's (shared prefix: its length)
     int node0;   // nodes of the sequences before
     int unit0;   // units before
-    long long cost0;  // key tiles before, each times its row tiles
+    int cost0;   // key tiles before, each times its row tiles
     int kt;      // key tiles
-    int pad;
+    int pad[2];
 };
-struct PlanStart {
-    int s, h, mt, k;
+struct __align__(16) PlanStart {
+    int s, h, mt, k;   // where a CTA begins: entry, key head, unit of the head, key tile (may be one behind the unit's last)
+    int x, x1, pad[2]; // that tile's position in the line, and where the CTA's stretch ends
 };
 struct PlanHead {
-    long long total;
-    int parts;  // CTAs that the line is cut for
-    int pad;
+    int total;  // length of the line
+    int parts;  // CTAs that it is cut for
 };
 
 struct __align__(64) AttnParams {
@@ -68,35 +68,45 @@ struct __align__(64) AttnParams {
     PlanStart* start;    // [gridDim of the attention kernel]
     int ctas, min_cost;
     int* arrivals;       // zero between calls
-    float* part_o;       // [slots][256][D]
+    float* part_o;       // [slots][D / 4][256][4]
     float2* part_ml;     // [slots][256]: maximum (log2 domain), sum
 };
+
+__device__ __forceinline__ void load_seq(PlanSeq& q, const PlanSeq* from) {
+    ((int4*)&q)[0] = __ldcg((const int4*)from);
+    ((int4*)&q)[1] = __ldcg((const int4*)from + 1);
+}
 
 // ---- the plan ------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ int row_tiles2(int R) { return (R + kUnitRows - 1) / kUnitRows; }  // units of R rows
 __device__ __forceinline__ int unit_weight(int R, int mt) { return R - mt * kUnitRows > kTile ? 2 : 1; }
-__device__ __forceinline__ long long head_cost(int R, int kt) {
+__device__ __forceinline__ int head_cost(int R, int kt) {
     const int u = row_tiles2(R);
-    return u == 0 ? 0 : (long long)kt * (2 * (u - 1) + unit_weight(R, u - 1));
+    return u == 0 ? 0 : kt * (2 * (u - 1) + unit_weight(R, u - 1));
 }
 
-// first position of CTA c's stretch
-__device__ __forceinline__ long long part_first(long long total, int parts, int c) { return (c * total + parts - 1) / parts; }
+// first position of CTA c's stretch: ceil(c total / parts)
+__device__ __forceinline__ int part_first(int total, int parts, int c) {
+    const int q = total / parts;
+    return c * q + (c * (total - q * parts) + parts - 1) / parts;
+}
 
-constexpr int kPlanThreads = 128;
-__global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const AttnParams p) {
+constexpr int kPlanThreads = 256;
+constexpr int kPlanSeqs = 512;  // sequences whose positions are searched in shared memory; more are in global memory
+__global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const __grid_constant__ AttnParams p) {
     pdl_launch_dependents();
     pdl_wait();
+    constexpr int kWarps = kPlanThreads / 32;
     const CacheView& c = p.c;
-    __shared__ int fine[kPlanThreads / 32], last;
-    __shared__ long long sums[3][kPlanThreads / 32];
+    __shared__ int fine[kWarps], last;
+    __shared__ int sums[3][kWarps], at[kPlanSeqs + 1];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int n0 = p.count[b], base0 = p.prefix_len[b] - 1;
     {
-        const int n = p.count[b], base = p.prefix_len[b] - 1;
         const int32_t* table = c.table + (size_t)b * c.width;
-        const long long end = (long long)base + n;
-        bool ok = n >= 0 && n <= p.rows && base >= 0 && base >= p.shared && end <= ((long long)c.width << c.page_shift);
-        if (ok && n > 0)
+        const long long end = (long long)base0 + n0;
+        bool ok = n0 >= 0 && n0 <= p.rows && base0 >= 0 && base0 >= p.shared && end <= ((long long)c.width << c.page_shift);
+        if (ok && n0 > 0)
             for (int i = tid; i <= (int)((end - 1) >> c.page_shift); i += kPlanThreads) {
                 ok = ok && (unsigned)table[i] < (unsigned)c.n_pages;
                 // (the shared pages are read from the first sequence's table)
@@ -105,35 +115,37 @@ __global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const AttnParam
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (lane == 0) fine[warp] = ok;
         __syncthreads();
+        for (int w = 0; w < kWarps; ++w) ok = ok && fine[w];
+        n0 = ok ? n0 : 0;
         if (tid == 0) {
-            ok = true;
-            for (int w = 0; w < kPlanThreads / 32; ++w) ok = ok && fine[w];
             if (p.status) p.status[b] = ok ? 0 : GRAFT_ST_BAD_CACHE;
-            p.seq[b + 1].n = ok ? n : 0;
-            p.seq[b + 1].base = base;
-            last = atom_add_acq_rel(p.arrivals, 1) == (int)gridDim.x - 1;
+            *(int2*)&p.seq[b + 1] = make_int2(n0, base0);
+            last = gridDim.x == 1 || atom_add_acq_rel(p.arrivals, 1) == (int)gridDim.x - 1;
         }
         __syncthreads();
         if (!last) return;
     }
     // the last block adds up: nodes, units, cost
     const int Hk = c.kv_heads;
-    long long run[3] = {0, 0, 0};
+    int run[3] = {0, 0, 0};
     for (int b0 = 0; b0 < p.batch; b0 += kPlanThreads) {
         const int i = b0 + tid;
-        int n = 0, kt = 0;
-        if (i < p.batch) {
-            n = ((volatile PlanSeq*)p.seq)[i + 1].n;
-            kt = n > 0 ? (((volatile PlanSeq*)p.seq)[i + 1].base + n - p.shared + kTile - 1) / kTile : 0;
+        int n = 0, base = 0;
+        if (gridDim.x == 1) {
+            if (i == 0) n = n0, base = base0;
+        } else if (i < p.batch) {
+            const int2 v = __ldcg((const int2*)&p.seq[i + 1]);
+            n = v.x, base = v.y;
         }
+        const int kt = n > 0 ? (base + n - p.shared + kTile - 1) / kTile : 0;
         const int R = n * p.group;
-        const long long mine[3] = {n, (long long)Hk * row_tiles2(R), Hk * head_cost(R, kt)};
-        long long upto[3];
+        const int mine[3] = {n, Hk * row_tiles2(R), Hk * head_cost(R, kt)};
+        int upto[3];
 #pragma unroll
         for (int q = 0; q < 3; ++q) {
-            long long x = mine[q];
+            int x = mine[q];
             for (int o = 1; o < 32; o <<= 1) {
-                const long long y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+                const int y = __shfl_up_sync(0xFFFFFFFFu, x, o);
                 if (lane >= o) x += y;
             }
             upto[q] = x;
@@ -142,32 +154,30 @@ __global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const AttnParam
         __syncthreads();
 #pragma unroll
         for (int q = 0; q < 3; ++q) {
-            long long before = run[q];
-            for (int w = 0; w < kPlanThreads / 32; ++w) {
+            int before = run[q];
+            for (int w = 0; w < kWarps; ++w) {
                 if (w < warp) before += sums[q][w];
                 run[q] += sums[q][w];
             }
             upto[q] += before - mine[q];
         }
         if (i < p.batch) {
-            p.seq[i + 1].node0 = (int)upto[0];
-            p.seq[i + 1].unit0 = (int)upto[1];
-            p.seq[i + 1].cost0 = upto[2];
-            p.seq[i + 1].kt = kt;
+            PlanSeq s = {n, base, upto[0], upto[1], upto[2], kt, {0, 0}};
+            p.seq[i + 1] = s;
+            if (i < kPlanSeqs) at[i + 1] = upto[2];
         }
         __syncthreads();
     }
     // the shared prefix goes first
-    const int nodes = (int)run[0], Rs = p.shared > 0 ? nodes * p.group : 0, kts = (p.shared + kTile - 1) / kTile;
-    const int us = Hk * row_tiles2(Rs);
-    const long long cs = Hk * head_cost(Rs, kts);
-    for (int i = tid; i < p.batch; i += kPlanThreads) {
-        p.seq[i + 1].unit0 += us;
-        p.seq[i + 1].cost0 += cs;
-    }
-    const long long total = run[2] + cs;
-    long long parts = (total + p.min_cost - 1) / p.min_cost;
-    parts = parts > p.ctas ? p.ctas : parts;
+    const int nodes = run[0], Rs = p.shared > 0 ? nodes * p.group : 0, kts = (p.shared + kTile - 1) / kTile;
+    const int us = Hk * row_tiles2(Rs), cs = Hk * head_cost(Rs, kts);
+    if (us > 0)
+        for (int i = tid; i < p.batch; i += kPlanThreads) {
+            p.seq[i + 1].unit0 += us;
+            p.seq[i + 1].cost0 += cs;
+            if (i < kPlanSeqs) at[i + 1] += cs;
+        }
+    const int total = run[2] + cs, parts = min(p.ctas, (total + p.min_cost - 1) / p.min_cost);
     if (tid == 0) {
         PlanSeq s = {};
         s.n = Rs > 0 ? nodes : 0;
@@ -175,34 +185,35 @@ __global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const AttnParam
         s.kt = kts;
         p.seq[0] = s;
         p.head->total = total;
-        p.head->parts = (int)parts;
+        p.head->parts = parts;
         *p.arrivals = 0;
     }
     __syncthreads();
     // where every CTA begins
-    for (int i = tid; i < (int)parts; i += kPlanThreads) {
-        const long long x = part_first(total, (int)parts, i);
-        int lo = 0, hi = p.batch;  // the last entry whose cost0 is not above x and that has any
+    for (int i = tid; i < parts; i += kPlanThreads) {
+        PlanStart st = {};
+        st.x = part_first(total, parts, i);
+        st.x1 = part_first(total, parts, i + 1);
+        int lo = 0, hi = p.batch;  // the last entry whose cost0 is not above x: one that has any, as the ones behind it begin above x
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (((volatile PlanSeq*)p.seq)[mid].cost0 <= x)
+            if ((p.batch <= kPlanSeqs ? at[mid] : __ldcg(&p.seq[mid].cost0)) <= st.x)
                 lo = mid;
             else
                 hi = mid - 1;
         }
-        const int n = ((volatile PlanSeq*)p.seq)[lo].n, R = n * p.group, kt = ((volatile PlanSeq*)p.seq)[lo].kt;
-        const long long hc = head_cost(R, kt), local = x - ((volatile PlanSeq*)p.seq)[lo].cost0;
-        PlanStart st = {lo, 0, 0, 0};
-        if (hc > 0) {
-            st.h = (int)(local / hc);
-            long long rem = local % hc;
-            const int u = row_tiles2(R);
-            st.mt = (int)(rem / (2 * (long long)kt));
-            st.mt = st.mt < u - 1 ? st.mt : u - 1;
-            rem -= 2 * (long long)kt * st.mt;
-            const int w = unit_weight(R, st.mt);
-            st.k = (int)((rem + w - 1) / w);  // may be kt: the next unit's first
-        }
+        PlanSeq q;
+        load_seq(q, p.seq + lo);
+        const int R = q.n * p.group, hc = head_cost(R, q.kt), local = st.x - q.cost0;
+        st.s = lo;
+        st.h = local / hc;
+        int rem = local - st.h * hc;
+        const int u = row_tiles2(R);
+        st.mt = min(rem / (2 * q.kt), u - 1);
+        rem -= 2 * q.kt * st.mt;
+        const int w = unit_weight(R, st.mt);
+        st.k = (rem + w - 1) / w;
+        st.x += st.k * w - rem;
         p.start[i] = st;
     }
 }
@@ -216,29 +227,19 @@ struct Piece {
 struct Walk {
     const PlanSeq* seq;
     int last_s, Hk, group;
-    long long x, x1;
+    int x, x1;
     int s, h, mt, k;
     PlanSeq q;
-    __device__ __forceinline__ void load() {
-        const int4* a = (const int4*)(seq + s);
-        ((int4*)&q)[0] = __ldcg(a);
-        ((int4*)&q)[1] = __ldcg(a + 1);
-    }
     __device__ __forceinline__ void begin(const AttnParams& p, int cta) {
         seq = p.seq;
         last_s = p.batch;
         Hk = p.c.kv_heads;
         group = p.group;
-        const long long total = __ldcg(&p.head->total);
-        const int parts = __ldcg(&p.head->parts);
         x = x1 = 0;
-        if (cta >= parts) return;
-        x1 = part_first(total, parts, cta + 1);
-        const int4 st = __ldcg((const int4*)(p.start + cta));
-        s = st.x, h = st.y, mt = st.z, k = st.w;
-        load();
-        const int R = q.n * group;
-        x = q.cost0 + h * head_cost(R, q.kt) + 2LL * q.kt * mt + (long long)k * unit_weight(R, mt);
+        if (cta >= __ldcg(&p.head->parts)) return;
+        const int4 st = __ldcg((const int4*)(p.start + cta)), en = __ldcg((const int4*)(p.start + cta) + 1);
+        s = st.x, h = st.y, mt = st.z, k = st.w, x = en.x, x1 = en.y;
+        load_seq(q, seq + s);
     }
     __device__ __forceinline__ bool next(Piece& pc) {
         if (x >= x1) return false;
@@ -253,19 +254,19 @@ struct Walk {
                     h = 0;
                     s += 1;
                     if (s > last_s) return false;
-                    load();
+                    load_seq(q, seq + s);
                     R = q.n * group;
                 }
             }
         }
         const int w = unit_weight(R, mt);
-        const long long left = (x1 - x + w - 1) / w;
+        const int left = (x1 - x + w - 1) >> (w - 1);
         pc.s = s, pc.h = h, pc.mt = mt, pc.k0 = k;
-        pc.k1 = left < q.kt - k ? k + (int)left : q.kt;
+        pc.k1 = left < q.kt - k ? k + left : q.kt;
         pc.n = q.n, pc.base = q.base, pc.node0 = q.node0, pc.kt = q.kt, pc.R = R;
         pc.unit = q.unit0 + h * row_tiles2(R) + mt;
         pc.rows = min(kUnitRows, R - mt * kUnitRows);
-        x += (long long)(pc.k1 - pc.k0) * w;
+        x += (pc.k1 - pc.k0) * w;
         k = pc.k1;
         return true;
     }
@@ -318,11 +319,15 @@ template <int D, bool Q8>
 struct Shape {
     static constexpr int kHalf = kTile * 128;                 // 128 rows of 128 bytes: 64 numbers of a row, in the 128-byte swizzle
     static constexpr int kTileBytes = kTile * D * 2;          // a tile of Q, K or V in bf16
-    static constexpr int kRawBytes = kTile * D;               // a tile of e4m3 numbers
+    static constexpr int kRawBytes = kTile * D + kTile;       // a tile of e4m3 numbers and its rows' exponents
     static constexpr int kStages = Q8 ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 10);
     static constexpr int kRaw = Q8 ? (D == 128 ? 4 : 8) : 0;
-    static constexpr int kThreads = Q8 ? 448 : 320;
+    static constexpr int kThreads = Q8 ? 512 : 384;
     static constexpr int kConvWarps = Q8 ? 4 : 0;
+    // registers a thread: the softmax's eight warps take over what the others leave (of 64512 or 65536 at the launch)
+    static constexpr int kRegsSoftmax = Q8 ? 168 : 208, kRegsOthers = 88;
+    static constexpr int kCols = Q8 ? 16 : 32;  // scores that a softmax thread holds twice at a time
+    static_assert(256 * kRegsSoftmax + (kThreads - 256) * kRegsOthers <= kThreads * (Q8 ? 128 : 168), "registers of a launch");
     static constexpr size_t kSmem = 1024 + 2 * kTileBytes + (size_t)kStages * kTileBytes + (size_t)kRaw * kRawBytes + 512;
 };
 
@@ -352,11 +357,14 @@ __device__ __forceinline__ void tmem_ld_32x32(uint32_t taddr, uint32_t (&r)[32])
           "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr));
 }
-// the same 32 registers, known to have arrived: nothing that reads them is moved ahead of the wait
-__device__ __forceinline__ void tmem_arrived(uint32_t (&r)[32]) {
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[32]) { tmem_ld_32x32(taddr, r); }
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[16]) { tmem_ld_32x16(taddr, r); }
+// the same registers, known to have arrived: nothing that reads them is moved ahead of the wait
+template <int N>
+__device__ __forceinline__ void tmem_arrived(uint32_t (&r)[N]) {
     tmem_wait_ld();
 #pragma unroll
-    for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
+    for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
@@ -368,6 +376,96 @@ __device__ __forceinline__ bool not_finite2(uint32_t w) { return (w & 0x7F80u) =
 // log(2^m sum); m = -inf: nothing seen, or nothing but what is not a number
 __device__ __forceinline__ float log_sum(float m, float sum) {
     return sum == 0.0f ? -INFINITY : (m > -INFINITY ? m * 0.69314718f : 0.0f) + logf(sum);
+}
+
+struct Yes {
+    static constexpr bool value = true;
+};
+struct No {
+    static constexpr bool value = false;
+};
+// two fp32 numbers in a 64-bit register
+__device__ __forceinline__ uint64_t two(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 apart(uint64_t x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// Largest of the row's 128 scores at tS (of those that `sees` says).
+template <bool kMasked>
+__device__ __forceinline__ float max_of(uint32_t tS, const uint32_t (&sees)[4]) {
+    uint32_t u[32];
+    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        tmem_ld_32x32(tS + 32 * x, u);
+        tmem_arrived(u);
+#pragma unroll
+        for (int y = 0; y < 32; ++y)
+            mx[y & 3] = fmaxf(mx[y & 3], !kMasked || ((sees[x] >> y) & 1) ? __uint_as_float(u[y]) : -INFINITY);
+    }
+    return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+}
+// Weights 2^(c2 s + off) of the row's 128 scores at tS as pairs of bf16, their sum (unrounded), and the largest score: one pass, with the
+// maximum that was known before; the next kCols scores are on their way while kCols are worked on.
+template <bool kMasked, int kCols>
+__device__ __forceinline__ float weigh(uint32_t tS, const uint32_t (&sees)[4], float c2, float off, uint32_t (&w)[64], float& sum) {
+    uint32_t u[2][kCols];
+    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    uint64_t part[2] = {0, 0};
+    const uint64_t cc = two(c2, c2), oo = two(off, off);
+    tmem_ld(tS, u[0]);
+#pragma unroll
+    for (int x = 0; x < kTile / kCols; ++x) {
+        tmem_arrived(u[x & 1]);
+        if (x + 1 < kTile / kCols) tmem_ld(tS + kCols * (x + 1), u[(x + 1) & 1]);
+#pragma unroll
+        for (int y = 0; y < kCols; y += 2) {
+            float s0 = __uint_as_float(u[x & 1][y]), s1 = __uint_as_float(u[x & 1][y + 1]);
+            if (kMasked) {
+                constexpr int kWord = 32 / kCols;  // (words of `sees` are 32 slots)
+                const uint32_t bits = sees[x / kWord] >> (x % kWord * kCols + y);
+                s0 = bits & 1 ? s0 : -INFINITY;
+                s1 = bits & 2 ? s1 : -INFINITY;
+            }
+            mx[(y >> 1) & 3] = fmaxf(mx[(y >> 1) & 3], fmaxf(s0, s1));
+            const float2 t = apart(fma2(two(s0, s1), cc, oo));
+            const float e0 = ex2_approx(t.x), e1 = ex2_approx(t.y);
+            part[(y >> 1) & 1] = add2(part[(y >> 1) & 1], two(e0, e1));
+            w[kCols / 2 * x + (y >> 1)] = pack_bf16(e0, e1);
+        }
+    }
+    const float2 a = apart(add2(part[0], part[1]));
+    sum = a.x + a.y;
+    return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+}
+// O of the row times f
+template <int D>
+__device__ __forceinline__ void rescale(uint32_t tO, float f) {
+    uint32_t u[32];
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x) {
+        tmem_ld_32x32(tO + 32 * x, u);
+        tmem_arrived(u);
+#pragma unroll
+        for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(__uint_as_float(u[y]) * f);
+        tmem_st_32x32(tO + 32 * x, u);
+    }
 }
 
 // Entries of the ring are used in the order K0 V0 K1 V1 ... (two row tiles against every key tile), or K0 K1 V0 K2 V1 K3 ... (one row tile:
@@ -481,143 +579,13 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
     const uint32_t tmem = *tmem_at;
     pdl_wait();
 
-    Walk walk;
-    walk.begin(p, blockIdx.x);
-    Piece pc;
     const CacheView& c = p.c;
 
-    if (warp == 9) {
-        // ---- copies: K and V tiles page by page, into the ring (bf16) or to where the conversion takes them from (e4m3)
-        constexpr int N = Q8 ? NR : NS;
-        constexpr int kParts = Q8 ? 1 : D / 64;  // copies a page and tile
-        uint32_t it = 0;
-        bool ok = true;
-        const int box = p.box_rows, shift = c.page_shift, low = (1 << shift) - 1;
-        while (ok && walk.next(pc)) {
-            const int T = pc.k1 - pc.k0;
-            const bool two = pc.rows > kTile;
-            const int kv0 = pc.s == 0 ? 0 : p.shared, end = pc.s == 0 ? p.shared : pc.base + pc.n;
-            const int32_t* table = c.table + (pc.s == 0 ? 0 : (size_t)(pc.s - 1) * c.width);
-            const auto bring = [&](int t, bool is_v) {
-                const int first = kv0 + (pc.k0 + t) * kTile, upto = min(end, first + kTile);
-                const int copies = (upto - first + box - 1) / box;  // boxes with a slot in use
-                const int i = lane / kParts, part = lane % kParts;
-                int page = 0, at = 0;
-                if (i < copies) {
-                    const int slot = first + i * box;
-                    page = __ldg(table + (slot >> shift));
-                    at = slot & low;
-                }
-                const uint32_t st = it % N, full = Q8 ? raw_full(st) : kv_full(st), empty = Q8 ? raw_empty(st) : kv_empty(st);
-                if (!mbar_wait_bounded(empty, ((it / N) & 1) ^ 1, gave_up)) return false;
-                const uint32_t to = Q8 ? raw_addr + st * S::kRawBytes : kv_addr + st * S::kTileBytes;
-                if (lane == 0) mbar_arrive_expect_tx(full, copies * box * D * (Q8 ? 1 : 2));
-                __syncwarp();
-                if (i < copies)
-                    tma_load_2d(to + (Q8 ? i * box * D : part * S::kHalf + i * box * 128), is_v ? &p.map_v : &p.map_k, Q8 ? 0 : part * 64,
-                                (int)cache_row(c, page, pc.h, at), full);
-                it += 1;
-                return true;
-            };
-            if (two) {
-                for (int t = 0; ok && t < T; ++t) ok = bring(t, false) && bring(t, true);
-            } else {
-                ok = bring(0, false);
-                if (T > 1) ok = ok && bring(1, false);
-                for (int t = 0; ok && t < T; ++t) {
-                    ok = bring(t, true);
-                    if (t + 2 < T) ok = ok && bring(t + 2, false);
-                }
-            }
-        }
-        // (after a wait that ran out: what is on its way arrives before the CTA ends)
-        if (!ok && lane == 0)
-            for (uint32_t i = it > (uint32_t)N ? it - N : 0; i < it; ++i)
-                for (int w = 0; w < (1 << 16) && !mbar_try_wait(Q8 ? raw_full(i % N) : kv_full(i % N), (i / N) & 1); ++w) {
-                }
-        __syncwarp();
-    } else if (warp == 8) {
-        // ---- products
-        constexpr uint32_t id_s = umma_idesc(128, 128, true), id_o = umma_idesc(128, D, true) | (1u << 16);
-        const uint32_t lead = lane == 0;
-        uint32_t it = 0, n_piece = 0, n_p[2] = {0, 0};
-        bool ok = true;
-        const auto qk = [&](int i, bool two, uint32_t entry) {
-            const uint32_t a = q_addr + (two ? i : 0) * S::kTileBytes, b = kv_addr + (entry % NS) * S::kTileBytes;
-#pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks)
-                umma_ss(tmem + i * 128, umma_desc_sw128(a + (ks >> 2) * S::kHalf + (ks & 3) * 32),
-                        umma_desc_sw128(b + (ks >> 2) * S::kHalf + (ks & 3) * 32), id_s, ks > 0, lead);
-        };
-        const auto pv = [&](int i, bool first, uint32_t entry) {
-            const uint32_t b = kv_addr + (entry % NS) * S::kTileBytes;
-#pragma unroll
-            for (int ks = 0; ks < kTile / 16; ++ks)
-                umma_ts(tmem + 256 + i * 128, tmem + i * 128 + ks * 8, desc_v(b + ks * 2048, S::kHalf), id_o, !first || ks > 0, lead);
-        };
-        const auto wait_kv = [&](uint32_t entry) {
-            const bool r = mbar_wait_bounded(kv_full(entry % NS), (entry / NS) & 1, gave_up);
-            tc_fence_after();
-            return r;
-        };
-        const auto wait_p = [&](int i) {
-            const bool r = mbar_wait_bounded(p_full0 + 8 * i, n_p[i] & 1, gave_up);
-            n_p[i] += 1;
-            tc_fence_after();
-            return r;
-        };
-        while (ok && walk.next(pc)) {
-            const int T = pc.k1 - pc.k0;
-            const bool two = pc.rows > kTile;
-            ok = mbar_wait_bounded(q_full, n_piece & 1, gave_up);
-            n_piece += 1;
-            if (!ok) break;
-            if (two) {
-                if (!(ok = wait_kv(it))) break;
-                for (int i = 0; i < 2; ++i) {
-                    qk(i, true, it);
-                    umma_commit_by(s_full0 + 8 * i, lead);
-                }
-                umma_commit_by(kv_empty(it % NS), lead);
-                for (int t = 0; ok && t < T; ++t) {
-                    const uint32_t ev = it + 1 + 2 * t, ek = ev + 1;
-                    for (int i = 0; ok && i < 2; ++i) {
-                        ok = wait_p(i) && (i == 1 || wait_kv(ev));
-                        if (!ok) break;
-                        pv(i, t == 0, ev);
-                        if (i == 1) umma_commit_by(kv_empty(ev % NS), lead);
-                        if (t + 1 < T) {
-                            if (i == 0 && !(ok = wait_kv(ek))) break;
-                            qk(i, true, ek);
-                            if (i == 1) umma_commit_by(kv_empty(ek % NS), lead);
-                        }
-                        umma_commit_by(s_full0 + 8 * i, lead);
-                    }
-                }
-            } else {
-                for (int i = 0; ok && i < min(T, 2); ++i) {
-                    if (!(ok = wait_kv(it + i))) break;
-                    qk(i, false, it + i);
-                    umma_commit_by(kv_empty((it + i) % NS), lead);
-                    umma_commit_by(s_full0 + 8 * i, lead);
-                }
-                for (int t = 0; ok && t < T; ++t) {
-                    const int i = t & 1;
-                    const uint32_t ev = it + v_entry(false, T, t), ek = ev + 1;
-                    if (!(ok = wait_p(i) && wait_kv(ev))) break;
-                    pv(i, t < 2, ev);
-                    umma_commit_by(kv_empty(ev % NS), lead);
-                    if (t + 2 < T) {
-                        if (!(ok = wait_kv(ek))) break;
-                        qk(i, false, ek);
-                        umma_commit_by(kv_empty(ek % NS), lead);
-                    }
-                    umma_commit_by(s_full0 + 8 * i, lead);
-                }
-            }
-            it += 2 * T;
-        }
-    } else if (warp < 8) {
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kRegsSoftmax));
+        Walk walk;
+        Piece pc;
+        walk.begin(p, blockIdx.x);
         // ---- softmax: a thread a row
         const int i = warp >> 2, row_in_tile = tid & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the lanes
@@ -675,68 +643,41 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                 const int first = kv0 + (pc.k0 + t) * kTile;
                 const bool masked = first + kTile > pc.base;  // new slots, or slots that are not there (the shared prefix: base is its end)
                 if (warp_live) {
-                    uint32_t u[32];
-                    uint32_t sees[4] = {0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu};
+                    const auto step = [&](auto is_masked) {
+                        constexpr bool kMasked = decltype(is_masked)::value;
+                        uint32_t sees[4];
+                        if (kMasked)
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+                                sees[x] = live ? seen_word(mask_row, p.words, node, pc.n, pc.base, end, first + 32 * x) : 0;
+                        uint32_t w[64];
+                        float mx;
+                        if (!any) {  // the first tile's maxima are taken before its weights
+                            mx = max_of<kMasked>(tS, sees);
+                            m = mx;
+                        }
+                        for (;;) {
+                            float sum;
+                            mx = weigh<kMasked, S::kCols>(tS, sees, c2, m > -INFINITY ? -m * c2 : 0.0f, w, sum);
+                            // (m = -inf: nothing seen so far, and what O holds is zero)
+                            const bool grown = mx > m && !((mx - m) * c2 <= 8.0f);
+                            if (!__any_sync(0xFFFFFFFFu, grown)) {
+                                l += sum;
+                                break;
+                            }
+                            const float now = fmaxf(mx, m), f = m > -INFINITY ? ex2_approx((m - now) * c2) : 1.0f;
+                            rescale<D>(tO, f);
+                            l *= f;
+                            m = now;
+                        }
+                        tmem_st_32x32(tS, *(uint32_t(*)[32])&w[0]);
+                        tmem_st_32x32(tS + 32, *(uint32_t(*)[32])&w[32]);
+                        tmem_wait_st();
+                    };
                     if (masked)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            sees[x] = live ? seen_word(mask_row, p.words, node, pc.n, pc.base, end, first + 32 * x) : 0;
-                    float mx = -INFINITY;
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        tmem_ld_32x32(tS + 32 * x, u);
-                        tmem_arrived(u);
-                        if (masked) {
-#pragma unroll
-                            for (int y = 0; y < 32; ++y) mx = fmaxf(mx, (sees[x] >> y) & 1 ? __uint_as_float(u[y]) : -INFINITY);
-                        } else {
-#pragma unroll
-                            for (int y = 0; y < 32; ++y) mx = fmaxf(mx, __uint_as_float(u[y]));
-                        }
-                    }
-                    // (m = -inf: nothing seen so far, and what O holds is zero)
-                    const bool grown = mx > m && !((mx - m) * c2 <= 8.0f);
-                    if (__any_sync(0xFFFFFFFFu, grown)) {
-                        const float now = fmaxf(mx, m), f = m > -INFINITY ? ex2_approx((m - now) * c2) : 1.0f;
-                        if (any) {
-#pragma unroll
-                            for (int x = 0; x < D / 32; ++x) {
-                                tmem_ld_32x32(tO + 32 * x, u);
-                                tmem_arrived(u);
-#pragma unroll
-                                for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(__uint_as_float(u[y]) * f);
-                                tmem_st_32x32(tO + 32 * x, u);
-                            }
-                        }
-                        l *= f;
-                        m = now;
-                    }
-                    const float mc = m > -INFINITY ? m * c2 : 0.0f;
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        uint32_t w[32];
-                        float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                        for (int z = 0; z < 2; ++z) {
-                            tmem_ld_32x32(tS + 64 * x + 32 * z, u);
-                            tmem_arrived(u);
-                            if (masked) {
-#pragma unroll
-                                for (int y = 0; y < 32; ++y)
-                                    u[y] = (sees[2 * x + z] >> y) & 1 ? u[y] : 0xFF800000u;
-                            }
-#pragma unroll
-                            for (int y = 0; y < 32; y += 2) {
-                                const float e0 = ex2_approx(fmaf(__uint_as_float(u[y]), c2, -mc));
-                                const float e1 = ex2_approx(fmaf(__uint_as_float(u[y + 1]), c2, -mc));
-                                part[y >> 1 & 3] += e0 + e1;
-                                w[16 * z + (y >> 1)] = pack_bf16(e0, e1);
-                            }
-                        }
-                        tmem_st_32x32(tS + 32 * x, w);
-                        l += (part[0] + part[1]) + (part[2] + part[3]);
-                    }
-                    tmem_wait_st();
+                        step(Yes());
+                    else
+                        step(No());
                 }
                 // Slots that are not there hold anything, and new slots may hold what is not a number and is not for every row: weights of zero do
                 // not keep it out of the sums.  Their rows of V are cleared (a thread a slot); rows that see such a slot get it in the end.
@@ -799,10 +740,11 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                         to[x] = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                 } else {
-                    float4* to = (float4*)(p.part_o + (slot * kUnitRows + r) * D + d0);
+                    // (four columns of all rows side by side: a warp's stores are whole lines)
+                    float4* to = (float4*)p.part_o + (slot * (D / 4) + d0 / 4) * kUnitRows + r;
 #pragma unroll
                     for (int x = 0; x < 8; ++x)
-                        to[x] = make_float4(__uint_as_float(u[4 * x]), __uint_as_float(u[4 * x + 1]), __uint_as_float(u[4 * x + 2]),
+                        to[x * kUnitRows] = make_float4(__uint_as_float(u[4 * x]), __uint_as_float(u[4 * x + 1]), __uint_as_float(u[4 * x + 2]),
                                             __uint_as_float(u[4 * x + 3]));
                 }
             };
@@ -878,70 +820,173 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
             }
             tc_fence_before();  // what follows in TMEM follows these reads
         }
-    } else if (Q8) {
-        // ---- e4m3 tiles to bf16 tiles in the 128-byte swizzle: sixteen numbers a thread and step
-        const int ct = tid - 320;  // 0 .. 127
-        constexpr int kPer = D / 16, kRowsStep = 128 / kPer, kSteps = kTile / kRowsStep;
-        const int col = ct % kPer, row0 = ct / kPer;
-        uint32_t it = 0;
-        bool ok = true;
-        const int shift = c.page_shift, low = (1 << shift) - 1;
-        while (ok && walk.next(pc)) {
-            const int T = pc.k1 - pc.k0;
-            const bool two = pc.rows > kTile;
-            const int kv0 = pc.s == 0 ? 0 : p.shared, end = pc.s == 0 ? p.shared : pc.base + pc.n;
-            const int32_t* table = c.table + (pc.s == 0 ? 0 : (size_t)(pc.s - 1) * c.width);
-            const auto convert = [&](int t, bool is_v) {
-                const int first = kv0 + (pc.k0 + t) * kTile;
-                uint32_t exps[kSteps];
-                const uint8_t* from = is_v ? c.v_exp : c.k_exp;
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kRegsOthers));
+            Walk walk;
+            Piece pc;
+            walk.begin(p, blockIdx.x);
+        if (warp == 9) {
+            // ---- copies: K and V tiles page by page, into the ring (bf16) or to where the conversion takes them from (e4m3)
+            constexpr int N = Q8 ? NR : NS;
+            constexpr int kParts = Q8 ? 2 : D / 64;  // copies a page and tile: halves of its rows, or numbers and exponents
+            uint32_t it = 0;
+            bool ok = true;
+            const int box = p.box_rows, shift = c.page_shift, low = (1 << shift) - 1;
+            while (ok && walk.next(pc)) {
+                const int T = pc.k1 - pc.k0;
+                const bool two = pc.rows > kTile;
+                const int kv0 = pc.s == 0 ? 0 : p.shared, end = pc.s == 0 ? p.shared : pc.base + pc.n;
+                const int32_t* table = c.table + (pc.s == 0 ? 0 : (size_t)(pc.s - 1) * c.width);
+                const auto bring = [&](int t, bool is_v) {
+                    const int first = kv0 + (pc.k0 + t) * kTile, upto = min(end, first + kTile);
+                    const int copies = (upto - first + box - 1) / box;  // boxes with a slot in use
+                    const int i = lane / kParts, part = lane % kParts;
+                    int page = 0, at = 0;
+                    if (i < copies) {
+                        const int slot = first + i * box;
+                        page = __ldg(table + (slot >> shift));
+                        at = slot & low;
+                    }
+                    const uint32_t st = it % N, full = Q8 ? raw_full(st) : kv_full(st), empty = Q8 ? raw_empty(st) : kv_empty(st);
+                    if (!mbar_wait_bounded(empty, ((it / N) & 1) ^ 1, gave_up)) return false;
+                    const uint32_t to = Q8 ? raw_addr + st * S::kRawBytes : kv_addr + st * S::kTileBytes;
+                    if (lane == 0) mbar_arrive_expect_tx(full, copies * box * (Q8 ? D + 1 : 2 * D));
+                    __syncwarp();
+                    if (i < copies) {
+                        const size_t row = cache_row(c, page, pc.h, at);
+                        if (!Q8 || part == 0)
+                            tma_load_2d(to + (Q8 ? i * box * D : part * S::kHalf + i * box * 128), is_v ? &p.map_v : &p.map_k,
+                                        Q8 ? 0 : part * 64, (int)row, full);
+                        else
+                            tma_load_1d(to + kTile * D + i * box, (is_v ? c.v_exp : c.k_exp) + row, box, full);
+                    }
+                    it += 1;
+                    return true;
+                };
+                if (two) {
+                    for (int t = 0; ok && t < T; ++t) ok = bring(t, false) && bring(t, true);
+                } else {
+                    ok = bring(0, false);
+                    if (T > 1) ok = ok && bring(1, false);
+                    for (int t = 0; ok && t < T; ++t) {
+                        ok = bring(t, true);
+                        if (t + 2 < T) ok = ok && bring(t + 2, false);
+                    }
+                }
+            }
+            // (after a wait that ran out: what is on its way arrives before the CTA ends)
+            if (!ok && lane == 0)
+                for (uint32_t i = it > (uint32_t)N ? it - N : 0; i < it; ++i)
+                    for (int w = 0; w < (1 << 16) && !mbar_try_wait(Q8 ? raw_full(i % N) : kv_full(i % N), (i / N) & 1); ++w) {
+                    }
+            __syncwarp();
+        } else if (warp == 8) {
+            // ---- products
+            constexpr uint32_t id_s = umma_idesc(128, 128, true), id_o = umma_idesc(128, D, true) | (1u << 16);
+            const uint32_t lead = lane == 0;
+            uint32_t it = 0, n_piece = 0, turns = 0;  // (turns: bit i, phase of stream i's weights)
+            bool ok = true;
+            const auto qk = [&](int i, bool two, uint32_t entry) {
+                const uint64_t a = umma_desc_sw128(q_addr + (two ? i : 0) * S::kTileBytes), b = umma_desc_sw128(kv_addr + (entry % NS) * S::kTileBytes);
 #pragma unroll
-                for (int x = 0; x < kSteps; ++x) {
-                    const int slot = first + x * kRowsStep + row0;
-                    exps[x] = slot < end ? __ldg(from + cache_row(c, __ldg(table + (slot >> shift)), pc.h, slot & low)) : 127;
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    constexpr int kUnit = 16;  // bytes that the address of a descriptor counts
+                    const uint32_t at = ((ks >> 2) * S::kHalf + (ks & 3) * 32) / kUnit;
+                    umma_ss(tmem + i * 128, a + at, b + at, id_s, ks > 0, lead);
                 }
-                const uint32_t rs = it % NR, ks = it % NS;
-                if (!mbar_wait_bounded(raw_full(rs), (it / NR) & 1, gave_up)) return false;
-                if (!mbar_wait_bounded(kv_empty(ks), ((it / NS) & 1) ^ 1, gave_up)) return false;
-                const uint8_t* raw = raw_ptr + rs * S::kRawBytes;
-                const uint32_t to = kv_addr + ks * S::kTileBytes + (col >> 2) * S::kHalf;
-#pragma unroll
-                for (int x = 0; x < kSteps; ++x) {
-                    const int row = x * kRowsStep + row0;
-                    const uint4 y = *(const uint4*)(raw + row * D + col * 16);
-                    uint32_t f, more;
-                    e4m3_factors(exps[x], f, more);
-                    const uint2 a = e4m3x4_to_bf16(y.x, f, more), d = e4m3x4_to_bf16(y.y, f, more);
-                    const uint2 e = e4m3x4_to_bf16(y.z, f, more), h = e4m3x4_to_bf16(y.w, f, more);
-                    const uint4 lo = make_uint4(a.x, a.y, d.x, d.y), hi = make_uint4(e.x, e.y, h.x, h.y);
-                    // (the second half of a row's threads store their second piece first: eight threads then use all banks)
-                    const uint32_t chunk = (col & 3) * 2, at = to + row * 128, swap = D == 128 ? (uint32_t)col >> 2 : 0u;
-                    const uint4 w0 = swap ? hi : lo, w1 = swap ? lo : hi;
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((chunk + swap) ^ (row & 7)) << 4)), "r"(w0.x),
-                                 "r"(w0.y), "r"(w0.z), "r"(w0.w)
-                                 : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((chunk + 1 - swap) ^ (row & 7)) << 4)), "r"(w1.x),
-                                 "r"(w1.y), "r"(w1.z), "r"(w1.w)
-                                 : "memory");
-                }
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(raw_empty(rs));
-                    mbar_arrive(kv_full(ks));
-                }
-                it += 1;
-                return true;
             };
-            if (two) {
-                for (int t = 0; ok && t < T; ++t) ok = convert(t, false) && convert(t, true);
-            } else {
-                ok = convert(0, false);
-                if (T > 1) ok = ok && convert(1, false);
-                for (int t = 0; ok && t < T; ++t) {
-                    ok = convert(t, true);
-                    if (t + 2 < T) ok = ok && convert(t + 2, false);
+            const auto pv = [&](int i, bool first, uint32_t entry) {
+                const uint64_t b = desc_v(kv_addr + (entry % NS) * S::kTileBytes, S::kHalf);
+#pragma unroll
+                for (int ks = 0; ks < kTile / 16; ++ks)
+                    umma_ts(tmem + 256 + i * 128, tmem + i * 128 + ks * 8, b + ks * (2048 / 16), id_o, !first || ks > 0, lead);
+            };
+            const auto wait_kv = [&](uint32_t entry) {
+                const bool r = mbar_wait_bounded(kv_full(entry % NS), (entry / NS) & 1, gave_up);
+                tc_fence_after();
+                return r;
+            };
+            const auto wait_p = [&](int i) {
+                const bool r = mbar_wait_bounded(p_full0 + 8 * i, (turns >> i) & 1, gave_up);
+                turns ^= 1u << i;
+                tc_fence_after();
+                return r;
+            };
+            while (ok && walk.next(pc)) {
+                const int T = pc.k1 - pc.k0;
+                const bool two = pc.rows > kTile;
+                ok = mbar_wait_bounded(q_full, n_piece & 1, gave_up);
+                n_piece += 1;
+                if (!ok) break;
+                for (int i = 0; i < (two ? 2 : min(T, 2)); ++i) {
+                    const uint32_t ek = it + (two ? 0 : i);
+                    if (!(ok = wait_kv(ek))) break;
+                    qk(i, two, ek);
+                    if (!two || i == 1) umma_commit_by(kv_empty(ek % NS), lead);
+                    umma_commit_by(s_full0 + 8 * i, lead);
                 }
+                // P V of a stream's tile, then Q K of its next
+                const int events = two ? 2 * T : T;
+                for (int e = 0; ok && e < events; ++e) {
+                    const int i = e & 1, t = two ? e >> 1 : e;
+                    const uint32_t ev = it + v_entry(two, T, t), ek = ev + 1;
+                    const bool more = t + (two ? 1 : 2) < T, done = !two || i == 1;  // (done: nobody else reads these entries)
+                    if (!(ok = wait_p(i) && wait_kv(ev))) break;
+                    pv(i, e < 2, ev);
+                    if (done) umma_commit_by(kv_empty(ev % NS), lead);
+                    if (more) {
+                        if (!(ok = wait_kv(ek))) break;
+                        qk(i, two, ek);
+                        if (done) umma_commit_by(kv_empty(ek % NS), lead);
+                    }
+                    umma_commit_by(s_full0 + 8 * i, lead);
+                }
+                it += 2 * T;
+            }
+        } else if (Q8 && warp >= 12) {
+            // ---- e4m3 tiles to bf16 tiles in the 128-byte swizzle: sixteen numbers a thread and step
+            const int ct = tid - 384;  // 0 .. 127
+            constexpr int kPer = D / 16, kRowsStep = 128 / kPer, kSteps = kTile / kRowsStep;
+            const int col = ct % kPer, row0 = ct / kPer;
+            uint32_t it = 0;
+            bool ok = true;
+            while (ok && walk.next(pc)) {
+                const int T = pc.k1 - pc.k0;
+                const auto convert = [&]() {
+                    const uint32_t rs = it % NR, ks = it % NS;
+                    if (!mbar_wait_bounded(raw_full(rs), (it / NR) & 1, gave_up)) return false;
+                    if (!mbar_wait_bounded(kv_empty(ks), ((it / NS) & 1) ^ 1, gave_up)) return false;
+                    const uint8_t* raw = raw_ptr + rs * S::kRawBytes;
+                    const uint32_t to = kv_addr + ks * S::kTileBytes + (col >> 2) * S::kHalf;
+#pragma unroll
+                    for (int x = 0; x < kSteps; ++x) {
+                        const int row = x * kRowsStep + row0;
+                        const uint4 y = *(const uint4*)(raw + row * D + col * 16);
+                        uint32_t f, more;
+                        e4m3_factors(raw[kTile * D + row], f, more);
+                        const uint2 a = e4m3x4_to_bf16(y.x, f, more), d = e4m3x4_to_bf16(y.y, f, more);
+                        const uint2 e = e4m3x4_to_bf16(y.z, f, more), h = e4m3x4_to_bf16(y.w, f, more);
+                        const uint4 lo = make_uint4(a.x, a.y, d.x, d.y), hi = make_uint4(e.x, e.y, h.x, h.y);
+                        // (the second half of a row's threads store their second piece first: eight threads then use all banks)
+                        const uint32_t chunk = (col & 3) * 2, at = to + row * 128, swap = D == 128 ? (uint32_t)col >> 2 : 0u;
+                        const uint4 w0 = swap ? hi : lo, w1 = swap ? lo : hi;
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((chunk + swap) ^ (row & 7)) << 4)), "r"(w0.x),
+                                     "r"(w0.y), "r"(w0.z), "r"(w0.w)
+                                     : "memory");
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((chunk + 1 - swap) ^ (row & 7)) << 4)), "r"(w1.x),
+                                     "r"(w1.y), "r"(w1.z), "r"(w1.w)
+                                     : "memory");
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(raw_empty(rs));
+                        mbar_arrive(kv_full(ks));
+                    }
+                    it += 1;
+                    return true;
+                };
+                for (int e = 0; ok && e < 2 * T; ++e) ok = convert();
             }
         }
     }
@@ -953,134 +998,139 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
 }
 
 // ---- joining the pieces ----------------------------------------------------------------------------------------------
-// pieces of a unit: CTAs that have tiles of it
+// A unit in the line: where its first tile stands, what a tile weighs, how many there are.
 struct UnitAt {
-    long long x0;  // position of its first tile
-    int w, kt;
+    int x0, w, kt;
 };
 __device__ __forceinline__ UnitAt unit_at(const PlanSeq& q, int group, int h, int mt) {
     const int R = q.n * group;
     UnitAt u;
-    u.x0 = q.cost0 + h * head_cost(R, q.kt) + 2LL * q.kt * mt;
+    u.x0 = q.cost0 + h * head_cost(R, q.kt) + 2 * q.kt * mt;
     u.w = unit_weight(R, mt);
     u.kt = q.kt;
     return u;
 }
 // first tile of the unit that is not ahead of CTA c's stretch
-__device__ __forceinline__ int first_tile(const UnitAt& u, long long total, int parts, int c) {
-    const long long d = part_first(total, parts, c) - u.x0;
-    if (d <= 0) return 0;
-    const long long k = (d + u.w - 1) / u.w;
-    return k < u.kt ? (int)k : u.kt;
+__device__ __forceinline__ int first_tile(const UnitAt& u, int total, int parts, int c) {
+    const int d = part_first(total, parts, c) - u.x0;
+    return d <= 0 ? 0 : min((d + u.w - 1) >> (u.w - 1), u.kt);
 }
-__device__ __forceinline__ int cta_of(long long x, long long total, int parts) { return (int)(x * parts / total); }
-
-template <int D>
-struct Joined {
-    static constexpr int kPer = D / 32;
-    float m, l, o[kPer];
-    __device__ __forceinline__ void clear() {
-        m = -INFINITY, l = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) o[i] = 0.0f;
-    }
-    // a piece's row; the whole warp
-    __device__ __forceinline__ void add(const AttnParams& p, size_t slot, int r, int lane) {
-        const float2 ml = __ldcg(p.part_ml + slot * kUnitRows + r);
-        const float* from = p.part_o + (slot * kUnitRows + r) * D + lane * kPer;
-        float x[kPer];
-        if (kPer == 4) {
-            const float4 v = __ldcg((const float4*)from);
-            x[0] = v.x, x[1] = v.y, x[2 % kPer] = v.z, x[3 % kPer] = v.w;
-        } else {
-            const float2 v = __ldcg((const float2*)from);
-            x[0] = v.x, x[1] = v.y;
-        }
-        const float now = fmaxf(m, ml.x);
-        const float f0 = m > -INFINITY ? ex2_approx(m - now) : 0.0f, f1 = ml.x > -INFINITY ? ex2_approx(ml.x - now) : 0.0f;
-        m = now;
-        l = l * f0 + ml.y * f1;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) o[i] = o[i] * f0 + x[i] * f1;
-    }
-    __device__ __forceinline__ void store(const AttnParams& p, size_t out_row, int lane) {
-        const float inv = l != 0.0f ? 1.0f / l : 1.0f;
-        uint32_t* to = (uint32_t*)(p.out + out_row * D) + lane * (kPer / 2);
-        if (kPer == 4)
-            *(uint2*)to = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2 % kPer] * inv, o[3 % kPer] * inv));
-        else
-            *to = pack_bf16(o[0] * inv, o[1] * inv);
-        if (p.lse && lane == 0) p.lse[out_row] = log_sum(m, l);
-    }
-};
+__device__ __forceinline__ int cta_of(int x, int total, int parts) { return (int)((long long)x * parts / total); }
 
 constexpr int kJoinThreads = 256;
+constexpr int kJoinRows = 32;
+constexpr int kJoinMost = 160;  // pieces of a block's rows: no more than CTAs and units (three at most)
 
-// Units that were cut, without a shared prefix: a block row a boundary between CTAs; the first boundary inside a unit joins it.
+struct JoinPiece {
+    int slot, shift, lo, hi;  // rows lo .. hi - 1 of the block are rows lo + shift .. of the piece
+};
+struct JoinList {
+    JoinPiece piece[kJoinMost];
+    float2 ml[kJoinMost][kJoinRows];
+    int n;
+};
+
+// The pieces of a unit that have tiles, to the list (one thread); first_slot + d is the slot of CTA d's piece, but for `ahead` >= 0:
+// that CTA's is the odd one of its two.
+__device__ __forceinline__ void list_unit(JoinList& j, const UnitAt& u, int total, int parts, int unit, int shift, int lo, int hi) {
+    const int f = cta_of(u.x0, total, parts), l = cta_of(u.x0 + (u.kt - 1) * u.w, total, parts);
+    for (int d = f, k = 0; d <= l; ++d) {
+        const int next = first_tile(u, total, parts, d + 1);
+        if (next > k && j.n < kJoinMost) j.piece[j.n++] = {unit >= 0 ? unit + d : d == f ? 2 * d + 1 : 2 * d, shift, lo, hi};
+        k = next;
+    }
+}
+
+// 32 rows of a unit from the pieces on the list: a lane a row, a warp some of the columns.  The weight of a piece's row is 2^(its maximum
+// less the largest), and pieces are added in their order along the line, so that results repeat.
+template <int D>
+__device__ __forceinline__ void join_rows(const AttnParams& p, JoinList& j, bool live, size_t out_row) {
+    constexpr int kWarps = kJoinThreads / 32, kQuads = D / 4 / kWarps;  // groups of four columns a warp
+    const int lane = lane_id(), warp = threadIdx.x >> 5, n = j.n;
+    for (int i = warp; i < n; i += kWarps) {
+        const JoinPiece& a = j.piece[i];
+        j.ml[i][lane] = lane >= a.lo && lane < a.hi ? __ldcg(p.part_ml + (size_t)a.slot * kUnitRows + lane + a.shift) : make_float2(-INFINITY, 0.0f);
+    }
+    __syncthreads();
+    float m = -INFINITY, l = 0.0f;
+    for (int i = 0; i < n; ++i) m = fmaxf(m, j.ml[i][lane].x);
+    const float ref = m > -INFINITY ? m : 0.0f;
+    float o[4 * kQuads] = {};
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+        const JoinPiece& a = j.piece[i];
+        const float2 ml = j.ml[i][lane];
+        if (!(lane >= a.lo && lane < a.hi)) continue;
+        const float f = ex2_approx(ml.x - ref);
+        l += f * ml.y;
+        const float4* from = (const float4*)p.part_o + ((size_t)a.slot * (D / 4) + warp * kQuads) * kUnitRows + lane + a.shift;
+#pragma unroll
+        for (int x = 0; x < kQuads; ++x) {
+            const float4 v = __ldcg(from + x * kUnitRows);
+            o[4 * x] += f * v.x, o[4 * x + 1] += f * v.y, o[4 * x + 2] += f * v.z, o[4 * x + 3] += f * v.w;
+        }
+    }
+    if (!live) return;
+    const float inv = l != 0.0f ? 1.0f / l : 1.0f;
+    uint2* to = (uint2*)(p.out + out_row * D + warp * kQuads * 4);
+#pragma unroll
+    for (int x = 0; x < kQuads; ++x)
+        to[x] = make_uint2(pack_bf16(o[4 * x] * inv, o[4 * x + 1] * inv), pack_bf16(o[4 * x + 2] * inv, o[4 * x + 3] * inv));
+    if (p.lse && warp == 0) p.lse[out_row] = log_sum(m, l);
+}
+
+// Units that were cut, without a shared prefix: blocks for every boundary between CTAs; the first boundary inside a unit joins it.
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_constant__ AttnParams p) {
     pdl_launch_dependents();
     pdl_wait();
-    const int c = blockIdx.y + 1, lane = lane_id();
-    const long long total = __ldcg(&p.head->total);
-    const int parts = __ldcg(&p.head->parts);
+    __shared__ JoinList j;
+    const int c = blockIdx.y + 1, total = __ldcg(&p.head->total), parts = __ldcg(&p.head->parts);
     if (c >= parts) return;
     const int4 st = __ldcg((const int4*)(p.start + c));
     PlanSeq q;
-    ((int4*)&q)[0] = __ldcg((const int4*)(p.seq + st.x));
-    ((int4*)&q)[1] = __ldcg((const int4*)(p.seq + st.x) + 1);
+    load_seq(q, p.seq + st.x);
     if (st.w == 0 || st.w >= q.kt) return;  // the stretch begins with a unit
+    const int R = q.n * p.group, r0 = st.z * kUnitRows + blockIdx.x * kJoinRows;
+    if ((int)blockIdx.x * kJoinRows >= min(kUnitRows, R - st.z * kUnitRows)) return;
     const UnitAt u = unit_at(q, p.group, st.y, st.z);
-    const int f = cta_of(u.x0, total, parts);
-    const int k1f = first_tile(u, total, parts, f + 1);
-    // tiles before this CTA's are those of the unit's first CTA: nobody joins it ahead of this one (CTAs without a tile have none to join)
-    if (k1f != st.w) return;
-    if (first_tile(u, total, parts, c + 1) <= st.w) return;
-    const int l = cta_of(u.x0 + (long long)(u.kt - 1) * u.w, total, parts);
-    const int R = q.n * p.group, rows = min(kUnitRows, R - st.z * kUnitRows);
-    for (int r = blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5); r < rows; r += gridDim.x * (kJoinThreads / 32)) {
-        int b, node, g;
-        row_of(p, st.x, st.z * kUnitRows + r, b, node, g);
-        Joined<D> j;
-        j.clear();
-        j.add(p, 2 * (size_t)f + 1, r, lane);
-        for (int d = f + 1; d <= l; ++d)
-            if (first_tile(u, total, parts, d + 1) > first_tile(u, total, parts, d)) j.add(p, 2 * (size_t)d, r, lane);
-        j.store(p, ((size_t)b * p.rows + node) * p.q_heads + st.y * p.group + g, lane);
+    // the tiles ahead of this CTA's are those of the unit's first CTA, and this one has some
+    if (first_tile(u, total, parts, cta_of(u.x0, total, parts) + 1) != st.w || first_tile(u, total, parts, c + 1) <= st.w) return;
+    if (threadIdx.x == 0) {
+        j.n = 0;
+        list_unit(j, u, total, parts, -1, blockIdx.x * kJoinRows, 0, kJoinRows);
     }
+    __syncthreads();
+    const int r = r0 + lane_id(), node = r / p.group;
+    const bool live = r < R;
+    join_rows<D>(p, j, live, ((size_t)(st.x - 1) * p.rows + node) * p.q_heads + st.y * p.group + (r - node * p.group));
 }
 
-// Behind a shared prefix every row has pieces of two units: a warp a row.
+// Behind a shared prefix every row has pieces of two units; 32 rows of a sequence may lie in two units of the prefix.
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) attn_join_shared_kernel(const __grid_constant__ AttnParams p) {
     pdl_launch_dependents();
     pdl_wait();
-    const int b = blockIdx.y, lane = lane_id();
-    PlanSeq q[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int4* a = (const int4*)(p.seq + (i == 0 ? 0 : b + 1));
-        ((int4*)&q[i])[0] = __ldcg(a);
-        ((int4*)&q[i])[1] = __ldcg(a + 1);
+    __shared__ JoinList j;
+    const int b = blockIdx.z, h = blockIdx.y, r0 = blockIdx.x * kJoinRows;
+    PlanSeq all, q;
+    load_seq(all, p.seq);
+    load_seq(q, p.seq + b + 1);
+    const int total = __ldcg(&p.head->total), parts = __ldcg(&p.head->parts), R = q.n * p.group;
+    if (r0 >= R) return;
+    if (threadIdx.x == 0) {
+        j.n = 0;
+        const int Ra = all.n * p.group, ra = q.node0 * p.group + r0, mt = ra / kUnitRows, upto = (mt + 1) * kUnitRows - ra;
+        const int ua = all.unit0 + h * row_tiles2(Ra);
+        list_unit(j, unit_at(all, p.group, h, mt), total, parts, ua + mt, ra - mt * kUnitRows, 0, min(upto, kJoinRows));
+        if (upto < kJoinRows && (mt + 1) * kUnitRows < Ra)
+            list_unit(j, unit_at(all, p.group, h, mt + 1), total, parts, ua + mt + 1, -upto, upto, kJoinRows);
+        const int mo = r0 / kUnitRows;
+        list_unit(j, unit_at(q, p.group, h, mo), total, parts, q.unit0 + h * row_tiles2(R) + mo, r0 - mo * kUnitRows, 0, kJoinRows);
     }
-    const long long total = __ldcg(&p.head->total);
-    const int parts = __ldcg(&p.head->parts);
-    const int rows = q[1].n * p.q_heads;
-    for (int x = blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5); x < rows; x += gridDim.x * (kJoinThreads / 32)) {
-        const int node = x / p.q_heads, head = x - node * p.q_heads, h = head / p.group, g = head - h * p.group;
-        Joined<D> j;
-        j.clear();
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = ((i == 0 ? q[1].node0 : 0) + node) * p.group + g, mt = r / kUnitRows;
-            const UnitAt u = unit_at(q[i], p.group, h, mt);
-            const int unit = q[i].unit0 + h * row_tiles2(q[i].n * p.group) + mt;
-            const int f = cta_of(u.x0, total, parts), l = cta_of(u.x0 + (long long)(u.kt - 1) * u.w, total, parts);
-            for (int d = f; d <= l; ++d)
-                if (first_tile(u, total, parts, d + 1) > first_tile(u, total, parts, d)) j.add(p, (size_t)unit + d, r - mt * kUnitRows, lane);
-        }
-        j.store(p, ((size_t)b * p.rows + node) * p.q_heads + head, lane);
-    }
+    __syncthreads();
+    const int r = r0 + lane_id(), node = r / p.group;
+    join_rows<D>(p, j, r < R, ((size_t)b * p.rows + node) * p.q_heads + h * p.group + (r - node * p.group));
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -1145,14 +1195,13 @@ cudaError_t launch_attn(graft_ctx* ctx, const AttnParams& p, cudaStream_t st) {
     e = launch_pdl(tree_attn_kernel<D, Q8>, dim3(p.ctas), dim3(S::kThreads), S::kSmem, st, p);
     if (e != cudaSuccess) return e;
     ctx->launches += 1;
-    if (p.shared > 0) {
-        const long long warps = (long long)p.rows * p.q_heads;
-        const int blocks = (int)min((warps + kJoinThreads / 32 - 1) / (kJoinThreads / 32), 1024LL);
-        e = launch_pdl(attn_join_shared_kernel<D>, dim3(blocks, p.batch), dim3(kJoinThreads), 0, st, p);
-    } else if (p.ctas > 1) {
-        const int rows = min((long long)kUnitRows, (long long)p.rows * p.group);
-        e = launch_pdl(attn_join_kernel<D>, dim3((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32), p.ctas - 1), dim3(kJoinThreads), 0, st, p);
-    }
+    const long long most = (long long)p.rows * p.group;  // rows of a sequence and key head
+    if (p.shared > 0)
+        e = launch_pdl(attn_join_shared_kernel<D>, dim3((unsigned)((most + kJoinRows - 1) / kJoinRows), p.c.kv_heads, p.batch),
+                       dim3(kJoinThreads), 0, st, p);
+    else
+        e = launch_pdl(attn_join_kernel<D>, dim3((unsigned)((min(most, (long long)kUnitRows) + kJoinRows - 1) / kJoinRows), max(p.ctas - 1, 1)),
+                       dim3(kJoinThreads), 0, st, p);
     ctx->launches += 1;
     return e;
 }
