@@ -13,8 +13,8 @@
 // exponentials are worked out, the other's products run.  A unit of one row tile gives the streams the even and the odd key tiles
 // instead, joined at the end.  Scores and sums stay in TMEM: S of 128 columns a stream, overwritten in place by the weights p in bf16
 // (which are the second product's first operand from there), and O of head_dim columns.  One thread has one row, so maxima and sums need no
-// exchange.  O is rescaled only when a row's maximum has grown by more than 2^8 since it was last taken: weights are then up to 256,
-// which fp32 sums and bf16 hold as well as those up to 1.
+// exchange.  A row's reference is the maximum of its first tile; maxima are taken again, and O rescaled, only when the weights of a
+// tile add up to more than 2^20 against it: fp32 sums and bf16 weights of that size are as exact as those up to 1.
 #include <cuda.h>
 #include <float.h>
 
@@ -27,6 +27,8 @@ namespace {
 
 constexpr int kTile = 128;      // slots of a key tile, rows of a row tile
 constexpr int kUnitRows = 256;
+constexpr uint32_t kWaitNs = 500;  // that a poll may sleep
+constexpr float kMostSum = 1048576.0f;  // of a tile's weights, which are 1 at the maximum known before: beyond it O is rescaled
 
 // What the plan says of a sequence (entry 0: the shared prefix with the rows of all of them; entry b + 1: sequence b).
 struct __align__(16) PlanSeq {
@@ -219,6 +221,11 @@ __global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const __grid_co
 }
 
 // ---- walking along a CTA's stretch -----------------------------------------------------------------------------------
+// A bounded wait whose polls sleep: the polls of warps that wait would otherwise take the shared-memory pipe from those that work.
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int* gave_up) {
+    return mbar_wait_bounded_hint(bar, parity, gave_up, kWaitNs);
+}
+
 struct Piece {
     int s, h, mt, k0, k1;  // entry of the plan, key head, unit of the head, key tiles
     int n, base, node0, unit, kt, R;
@@ -326,25 +333,41 @@ struct Shape {
     static constexpr int kConvWarps = Q8 ? 4 : 0;
     // registers a thread: the softmax's eight warps take over what the others leave (of 64512 or 65536 at the launch)
     static constexpr int kRegsSoftmax = Q8 ? 168 : 208, kRegsOthers = 88;
-    static constexpr int kCols = Q8 ? 16 : 32;  // scores that a softmax thread holds twice at a time
+    static constexpr int kCols = Q8 ? 64 : 128;  // scores that a softmax thread holds at a time
     static_assert(256 * kRegsSoftmax + (kThreads - 256) * kRegsOthers <= kThreads * (Q8 ? 128 : 168), "registers of a launch");
     static constexpr size_t kSmem = 1024 + 2 * kTileBytes + (size_t)kStages * kTileBytes + (size_t)kRaw * kRawBytes + 512;
 };
 
-// D (+)= A B with both operands in shared memory, a CTA by itself
-__device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate, uint32_t lead) {
+// One thread of the warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+// D (+)= A B with both operands in shared memory, a CTA by itself; one thread issues it.  Descriptors as their low words; the high one is the
+// same for all.
+template <bool kAccumulate>
+__device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc) {
     asm volatile(
-        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t"
-        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u), "r"(lead)
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\tsetp.ne.u32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "n"(kAccumulate ? 1 : 0)
         : "memory");
 }
-// V as the second operand of P V: rows (slots) of 64 numbers of head_dim side by side, so head_dim is the contiguous direction.  In the
-// 128-byte swizzle: blocks of 64 numbers kHalf apart, groups of eight slots 1024 bytes apart.
-__device__ __forceinline__ uint64_t desc_v(uint32_t addr, uint32_t half) {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(half >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
-           ((uint64_t)2 << 61);
+// The same with A in TMEM.
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t hi, uint32_t b_lo, uint32_t idesc, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tmov.b64 b, {%3, %2};\n\tsetp.ne.u32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "r"(hi), "r"(b_lo), "r"(idesc), "r"(accumulate ? 1u : 0u)
+        : "memory");
 }
+// When every matrix instruction that this thread issued so far has completed: one arrival on the barrier.
+__device__ __forceinline__ void umma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// a number that is the same in all lanes, known to be
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
 // 32 columns of the lane's row
 __device__ __forceinline__ void tmem_ld_32x32(uint32_t taddr, uint32_t (&r)[32]) {
     asm volatile(
@@ -368,7 +391,7 @@ __device__ __forceinline__ void tmem_arrived(uint32_t (&r)[N]) {
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    asm volatile("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
 __device__ __forceinline__ bool not_finite2(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
@@ -378,12 +401,12 @@ __device__ __forceinline__ float log_sum(float m, float sum) {
     return sum == 0.0f ? -INFINITY : (m > -INFINITY ? m * 0.69314718f : 0.0f) + logf(sum);
 }
 
-struct Yes {
-    static constexpr bool value = true;
-};
-struct No {
-    static constexpr bool value = false;
-};
+// (the asm statements of a pass over scores are volatile: they stay in the order that hides their latencies)
+__device__ __forceinline__ float ex2_in_order(float x) {
+    float y;
+    asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 // two fp32 numbers in a 64-bit register
 __device__ __forceinline__ uint64_t two(float lo, float hi) {
     uint64_t r;
@@ -397,62 +420,84 @@ __device__ __forceinline__ float2 apart(uint64_t x) {
 }
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    asm volatile("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    asm volatile("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
 
-// Largest of the row's 128 scores at tS (of those that `sees` says).
-template <bool kMasked>
-__device__ __forceinline__ float max_of(uint32_t tS, const uint32_t (&sees)[4]) {
+// kCols scores of the row, all asked for together: while the tensor cores work on the other stream, an answer takes several hundred cycles
+template <int kCols>
+__device__ __forceinline__ void scores(uint32_t tS, uint32_t (&u)[kCols], bool masked, const uint32_t (&sees)[4], int x) {
+#pragma unroll
+    for (int y = 0; y < kCols; y += 32) tmem_ld_32x32(tS + kCols * x + y, *(uint32_t(*)[32]) & u[y]);
+    tmem_arrived(u);
+    if (masked)
+#pragma unroll
+        for (int y = 0; y < kCols; ++y) u[y] = (sees[(kCols * x + y) / 32] >> (y % 32)) & 1 ? u[y] : 0xFF800000u;
+}
+// Largest of the row's 128 scores at tS (masked: of those that `sees` says, -inf in the place of the others).
+__device__ __forceinline__ float max_of(uint32_t tS, bool masked, const uint32_t (&sees)[4]) {
     uint32_t u[32];
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-        tmem_ld_32x32(tS + 32 * x, u);
-        tmem_arrived(u);
+        scores(tS, u, masked, sees, x);
 #pragma unroll
-        for (int y = 0; y < 32; ++y)
-            mx[y & 3] = fmaxf(mx[y & 3], !kMasked || ((sees[x] >> y) & 1) ? __uint_as_float(u[y]) : -INFINITY);
+        for (int y = 0; y < 32; ++y) mx[y & 3] = fmaxf(mx[y & 3], __uint_as_float(u[y]));
     }
     return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
 }
-// Weights 2^(c2 s + off) of the row's 128 scores at tS as pairs of bf16, their sum (unrounded), and the largest score: one pass, with the
-// maximum that was known before; the next kCols scores are on their way while kCols are worked on.
-template <bool kMasked, int kCols>
-__device__ __forceinline__ float weigh(uint32_t tS, const uint32_t (&sees)[4], float c2, float off, uint32_t (&w)[64], float& sum) {
-    uint32_t u[2][kCols];
-    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+// 2^t of two numbers on the FMA pipe: t = n + f, n whole and |f| <= 1/2; 2^f by a polynomial of degree 5 (fitted for the least largest
+// relative error, 1e-7, with 1 at f = 0), n added to its exponent.  t is held to -127 .. 127: at -127, where slots that are not seen
+// come out, the exponent's field is 0 and the result is 0.
+__device__ __forceinline__ float2 exp2_poly(uint64_t t) {
+    float2 x = apart(t);
+    t = two(fminf(fmaxf(x.x, -127.0f), 127.0f), fminf(fmaxf(x.y, -127.0f), 127.0f));
+    const auto both = [](float c) { return two(c, c); };
+    const uint64_t r = add2(t, both(12582912.0f));  // 1.5 2^23: the sum's last bits are n
+    const uint64_t f = fma2(add2(r, both(-12582912.0f)), both(-1.0f), t);
+    uint64_t q = fma2(both(0.0013264727f), f, both(0.0096715127f));
+    q = fma2(q, f, both(0.055507337f));
+    q = fma2(q, f, both(0.24022242f));
+    q = fma2(q, f, both(0.69314698f));
+    q = fma2(q, f, both(1.0f));
+    const float2 a = apart(q), n = apart(r);
+    return make_float2(__int_as_float(__float_as_int(a.x) + (__float_as_int(n.x) << 23)),
+                       __int_as_float(__float_as_int(a.y) + (__float_as_int(n.y) << 23)));
+}
+// Weights 2^(c2 s + off) of the row's 128 scores at tS as pairs of bf16, and their sum (unrounded): one pass.  128 rows' exponentials take the 16-a-clock unit as long as both products take the tensor cores, so one
+// pair of four is worked out on the FMA pipe; sums and conversions follow eight pairs behind.  Cycles for 128 x 128 scores, alone and
+// two warps a scheduler: 1150 and 1910 for two; without polynomials 1350 and 2350, with one in three 1180 and 1960.
+template <int kCols>
+__device__ __forceinline__ float weigh(uint32_t tS, bool masked, const uint32_t (&sees)[4], float c2, float off, uint32_t (&w)[64]) {
+    constexpr int kBehind = 8, kPairs = kCols / 2;
     uint64_t part[2] = {0, 0};
     const uint64_t cc = two(c2, c2), oo = two(off, off);
-    tmem_ld(tS, u[0]);
 #pragma unroll
     for (int x = 0; x < kTile / kCols; ++x) {
-        tmem_arrived(u[x & 1]);
-        if (x + 1 < kTile / kCols) tmem_ld(tS + kCols * (x + 1), u[(x + 1) & 1]);
+        uint32_t v[kCols];
+        scores(tS, v, masked, sees, x);
 #pragma unroll
-        for (int y = 0; y < kCols; y += 2) {
-            float s0 = __uint_as_float(u[x & 1][y]), s1 = __uint_as_float(u[x & 1][y + 1]);
-            if (kMasked) {
-                constexpr int kWord = 32 / kCols;  // (words of `sees` are 32 slots)
-                const uint32_t bits = sees[x / kWord] >> (x % kWord * kCols + y);
-                s0 = bits & 1 ? s0 : -INFINITY;
-                s1 = bits & 2 ? s1 : -INFINITY;
+        for (int y = 0; y < kPairs + kBehind; ++y) {
+            if (y < kPairs) {
+                const uint64_t t = fma2(two(__uint_as_float(v[2 * y]), __uint_as_float(v[2 * y + 1])), cc, oo);
+                const float2 e = y % 4 == 3 ? exp2_poly(t) : make_float2(ex2_in_order(apart(t).x), ex2_in_order(apart(t).y));
+                v[2 * y] = __float_as_uint(e.x), v[2 * y + 1] = __float_as_uint(e.y);
             }
-            mx[(y >> 1) & 3] = fmaxf(mx[(y >> 1) & 3], fmaxf(s0, s1));
-            const float2 t = apart(fma2(two(s0, s1), cc, oo));
-            const float e0 = ex2_approx(t.x), e1 = ex2_approx(t.y);
-            part[(y >> 1) & 1] = add2(part[(y >> 1) & 1], two(e0, e1));
-            w[kCols / 2 * x + (y >> 1)] = pack_bf16(e0, e1);
+            if (y >= kBehind) {
+                const int z = y - kBehind;
+                const float e0 = __uint_as_float(v[2 * z]), e1 = __uint_as_float(v[2 * z + 1]);
+                part[z & 1] = add2(part[z & 1], two(e0, e1));
+                w[kPairs * x + z] = pack_bf16(e0, e1);
+            }
         }
     }
     const float2 a = apart(add2(part[0], part[1]));
-    sum = a.x + a.y;
-    return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+    return a.x + a.y;
 }
 // O of the row times f
 template <int D>
@@ -460,7 +505,7 @@ __device__ __forceinline__ void rescale(uint32_t tO, float f) {
     uint32_t u[32];
 #pragma unroll
     for (int x = 0; x < D / 32; ++x) {
-        tmem_ld_32x32(tO + 32 * x, u);
+        tmem_ld(tO + 32 * x, u);
         tmem_arrived(u);
 #pragma unroll
         for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(__uint_as_float(u[y]) * f);
@@ -478,7 +523,6 @@ template <int D, bool Q8>
 __device__ __noinline__ void add_spoilt(const AttnParams& p, const Piece& pc, uint32_t tO, bool sums, int b, int node, int head, int t0,
                                         int dt, int kv0, int end, float m) {
     const CacheView& c = p.c;
-    const int32_t* table = c.table + (size_t)b * c.width;
     const uint32_t* mask_row = p.mask ? p.mask + ((size_t)b * p.nmax + node) * p.words : nullptr;
     const uint16_t* q = (const uint16_t*)p.q + ((long long)b * p.rows + node) * p.q_stride + (long long)head * D;
     for (int t = t0; t < pc.k1 - pc.k0; t += dt) {
@@ -546,8 +590,8 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
     const auto kv_empty = [&](int i) { return bar0 + 8 * (NS + i); };
     const auto raw_full = [&](int i) { return bar0 + 8 * (2 * NS + i); };
     const auto raw_empty = [&](int i) { return bar0 + 8 * (2 * NS + NR + i); };
-    const uint32_t q_full = bar0 + 8 * (2 * NS + 2 * NR), s_full0 = q_full + 8, p_full0 = q_full + 24, pair = q_full + 40;
-    volatile int* const gave_up = (volatile int*)(bars + 2 * NS + 2 * NR + 6);
+    const uint32_t q_full = bar0 + 8 * (2 * NS + 2 * NR), s_full0 = q_full + 8, p_full0 = q_full + 24, pair = q_full + 40, turn0 = q_full + 48;
+    volatile int* const gave_up = (volatile int*)(bars + 2 * NS + 2 * NR + 8);
     volatile int* const spoilt = gave_up + 1;  // [2] the last piece (counted from 1) with a row of V that was taken out
     uint32_t* const tmem_at = (uint32_t*)(gave_up + 3);
 
@@ -555,17 +599,18 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
     if (tid == 0) {
         for (int i = 0; i < NS; ++i) {
             mbar_init(kv_full(i), Q8 ? S::kConvWarps : 1);
-            mbar_init(kv_empty(i), 1);
+            mbar_init(kv_empty(i), 2);
         }
         for (int i = 0; i < NR; ++i) {
             mbar_init(raw_full(i), 1);
             mbar_init(raw_empty(i), S::kConvWarps > 0 ? S::kConvWarps : 1);
         }
-        mbar_init(q_full, 8);
+        mbar_init(q_full, 10);
         mbar_init(pair, 8);
         for (int i = 0; i < 2; ++i) {
             mbar_init(s_full0 + 8 * i, 1);
             mbar_init(p_full0 + 8 * i, 4);
+            mbar_init(turn0 + 8 * i, 1);
         }
         *gave_up = 0;
         spoilt[0] = spoilt[1] = 0;
@@ -596,12 +641,12 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
         const auto both = [&]() {  // the two streams meet
             __syncwarp();
             if (lane == 0) mbar_arrive(pair);
-            const bool r = mbar_wait_bounded(pair, n_pair & 1, gave_up);
+            const bool r = wait_for(pair, n_pair & 1, gave_up);
             n_pair += 1;
             return r;
         };
         const auto wait_s = [&]() {
-            const bool r = mbar_wait_bounded(s_full0 + 8 * i, n_s & 1, gave_up);
+            const bool r = wait_for(s_full0 + 8 * i, n_s & 1, gave_up);
             n_s += 1;
             tc_fence_after();
             return r;
@@ -638,76 +683,71 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
             const bool warp_live = __any_sync(0xFFFFFFFFu, live);
             float m = -INFINITY, l = 0.0f;  // maximum of the raw scores, sum of 2^(c2 (s - m))
             bool any = false;               // this stream has had a tile
+            // Slots that are not there hold anything, and new slots may hold what is not a number and is not for every row: weights of zero do
+            // not keep it out of the sums.  Their rows of V are cleared (a thread a slot); rows that see such a slot get it in the end.
+            const auto clear_v = [&](int t, int first) {
+                const uint32_t entry = it + v_entry(two, T, t);
+                if (!wait_for(kv_full(entry % NS), (entry / NS) & 1, gave_up)) return false;
+                const int slot = first + row_in_tile;
+                if (slot >= pc.base) {
+                    const uint32_t at = kv_addr + (entry % NS) * S::kTileBytes + row_in_tile * 128;
+                    bool clear = slot >= end;
+                    if (!clear)
+#pragma unroll
+                        for (int x = 0; x < D / 8; ++x) {  // (a row's pieces in an order of its own: eight rows then use all banks)
+                            uint32_t a0, a1, a2, a3;
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                         : "=r"(a0), "=r"(a1), "=r"(a2), "=r"(a3)
+                                         : "r"(at + (x >> 3) * S::kHalf + ((x + row_in_tile) & 7) * 16)
+                                         : "memory");
+                            clear = clear || not_finite2(a0) || not_finite2(a1) || not_finite2(a2) || not_finite2(a3);
+                        }
+                    if (clear) {
+#pragma unroll
+                        for (int x = 0; x < D / 8; ++x)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + (x >> 3) * S::kHalf + ((x + row_in_tile) & 7) * 16),
+                                         "r"(0)
+                                         : "memory");
+                        if (slot < end) spoilt[i] = (int)n_piece;
+                    }
+                }
+                fence_proxy_async();
+                return true;
+            };
             for (int t = two ? 0 : i; t < T; t += two ? 1 : 2) {
-                if (!(ok = wait_s())) break;
                 const int first = kv0 + (pc.k0 + t) * kTile;
                 const bool masked = first + kTile > pc.base;  // new slots, or slots that are not there (the shared prefix: base is its end)
-                if (warp_live) {
-                    const auto step = [&](auto is_masked) {
-                        constexpr bool kMasked = decltype(is_masked)::value;
-                        uint32_t sees[4];
-                        if (kMasked)
+                uint32_t sees[4];
+                if (masked) {
 #pragma unroll
-                            for (int x = 0; x < 4; ++x)
-                                sees[x] = live ? seen_word(mask_row, p.words, node, pc.n, pc.base, end, first + 32 * x) : 0;
-                        uint32_t w[64];
-                        float mx;
-                        if (!any) {  // the first tile's maxima are taken before its weights
-                            mx = max_of<kMasked>(tS, sees);
-                            m = mx;
-                        }
-                        for (;;) {
-                            float sum;
-                            mx = weigh<kMasked, S::kCols>(tS, sees, c2, m > -INFINITY ? -m * c2 : 0.0f, w, sum);
-                            // (m = -inf: nothing seen so far, and what O holds is zero)
-                            const bool grown = mx > m && !((mx - m) * c2 <= 8.0f);
-                            if (!__any_sync(0xFFFFFFFFu, grown)) {
-                                l += sum;
-                                break;
-                            }
-                            const float now = fmaxf(mx, m), f = m > -INFINITY ? ex2_approx((m - now) * c2) : 1.0f;
-                            rescale<D>(tO, f);
+                    for (int x = 0; x < 4; ++x)
+                        sees[x] = live ? seen_word(mask_row, p.words, node, pc.n, pc.base, end, first + 32 * x) : 0;
+                    // (with two row tiles every entry ahead of V's in the ring has been used by this stream, so its phase is certain: see `pass`)
+                    if (two && i == 0 && !(ok = clear_v(t, first))) break;
+                }
+                if (!(ok = wait_s())) break;
+                if (warp_live) {
+                    // The first tile's maxima are taken before its weights.  Then m stays as long as the weights do not grow too large against it
+                    // (or nothing was seen so far): where they do, maxima are taken again and the tile is weighed again.
+                    uint32_t w[64];
+                    float sum;
+                    for (bool again = !any;; again = true) {
+                        if (again) {
+                            const float now = fmaxf(m, max_of(tS, masked, sees)), f = m > -INFINITY ? ex2_approx((m - now) * c2) : 1.0f;
+                            if (any) rescale<D>(tO, f);
                             l *= f;
                             m = now;
                         }
-                        tmem_st_32x32(tS, *(uint32_t(*)[32])&w[0]);
-                        tmem_st_32x32(tS + 32, *(uint32_t(*)[32])&w[32]);
-                        tmem_wait_st();
-                    };
-                    if (masked)
-                        step(Yes());
-                    else
-                        step(No());
-                }
-                // Slots that are not there hold anything, and new slots may hold what is not a number and is not for every row: weights of zero do
-                // not keep it out of the sums.  Their rows of V are cleared (a thread a slot); rows that see such a slot get it in the end.
-                if (masked && (i == 0 || !two)) {
-                    const uint32_t entry = it + v_entry(two, T, t);
-                    if (!(ok = mbar_wait_bounded(kv_full(entry % NS), (entry / NS) & 1, gave_up))) break;
-                    const int slot = first + row_in_tile;
-                    if (slot >= pc.base) {
-                        const uint32_t at = kv_addr + (entry % NS) * S::kTileBytes + row_in_tile * 128;
-                        bool clear = slot >= end;
-                        if (!clear)
-#pragma unroll
-                            for (int x = 0; x < D / 8; ++x) {
-                                uint32_t a0, a1, a2, a3;
-                                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                             : "=r"(a0), "=r"(a1), "=r"(a2), "=r"(a3)
-                                             : "r"(at + (x >> 3) * S::kHalf + (x & 7) * 16)
-                                             : "memory");
-                                clear = clear || not_finite2(a0) || not_finite2(a1) || not_finite2(a2) || not_finite2(a3);
-                            }
-                        if (clear) {
-#pragma unroll
-                            for (int x = 0; x < D / 8; ++x)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + (x >> 3) * S::kHalf + (x & 7) * 16), "r"(0)
-                                             : "memory");
-                            if (slot < end) spoilt[i] = (int)n_piece;
-                        }
+                        sum = weigh<S::kCols>(tS, masked, sees, c2, m > -INFINITY ? -m * c2 : 0.0f, w);
+                        if (again || !__any_sync(0xFFFFFFFFu, sum > kMostSum || (live && m == -INFINITY))) break;
                     }
-                    fence_proxy_async();
+                    l += sum;
+                    tmem_st_32x32(tS, *(uint32_t(*)[32])&w[0]);
+                    tmem_st_32x32(tS + 32, *(uint32_t(*)[32])&w[32]);
+                    tmem_wait_st();
                 }
+                if (masked && !two && !(ok = clear_v(t, first))) break;
+                if (masked && two && !(ok = both())) break;  // (the first stream clears for both)
                 any = true;
                 tc_fence_before();
                 __syncwarp();
@@ -718,7 +758,7 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
             if (any)
                 ok = wait_s();  // the last product is done
             else
-                ok = mbar_wait_bounded(q_full, (n_piece - 1) & 1, gave_up);  // (nor does a stream without a tile run ahead)
+                ok = wait_for(q_full, (n_piece - 1) & 1, gave_up);  // (nor does a stream without a tile run ahead)
             if (!ok) break;
 
             // ---- the end of a piece: O as far as it goes
@@ -848,7 +888,7 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                         at = slot & low;
                     }
                     const uint32_t st = it % N, full = Q8 ? raw_full(st) : kv_full(st), empty = Q8 ? raw_empty(st) : kv_empty(st);
-                    if (!mbar_wait_bounded(empty, ((it / N) & 1) ^ 1, gave_up)) return false;
+                    if (!wait_for(empty, ((it / N) & 1) ^ 1, gave_up)) return false;
                     const uint32_t to = Q8 ? raw_addr + st * S::kRawBytes : kv_addr + st * S::kTileBytes;
                     if (lane == 0) mbar_arrive_expect_tx(full, copies * box * (Q8 ? D + 1 : 2 * D));
                     __syncwarp();
@@ -880,68 +920,96 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                     for (int w = 0; w < (1 << 16) && !mbar_try_wait(Q8 ? raw_full(i % N) : kv_full(i % N), (i / N) & 1); ++w) {
                     }
             __syncwarp();
-        } else if (warp == 8) {
-            // ---- products
-            constexpr uint32_t id_s = umma_idesc(128, 128, true), id_o = umma_idesc(128, D, true) | (1u << 16);
-            const uint32_t lead = lane == 0;
-            uint32_t it = 0, n_piece = 0, turns = 0;  // (turns: bit i, phase of stream i's weights)
+        } else if (warp == 8 || warp == 10) {
+            // ---- products, a warp a stream: while one waits for weights or signals, the other's instructions keep the tensor cores busy
+            constexpr uint32_t id_s = umma_idesc(128, 128, true), id_o = umma_idesc(128, D, true) | (1u << 16);  // (V: head_dim is contiguous)
+            const uint32_t i = warp == 8 ? 0 : 1;
+            uint32_t it = 0, n_piece = 0, n_p = 0, n_turn = 0;
             bool ok = true;
-            const auto qk = [&](int i, bool two, uint32_t entry) {
-                const uint64_t a = umma_desc_sw128(q_addr + (two ? i : 0) * S::kTileBytes), b = umma_desc_sw128(kv_addr + (entry % NS) * S::kTileBytes);
+            // (descriptors differ in their low words alone; the numbers that choose them are loaded, so the compiler is told that they are uniform)
+            constexpr uint32_t kDescHi = (uint32_t)(umma_desc_sw128(0) >> 32);
+            const uint32_t tS = uniform(tmem + i * 128), tO = uniform(tmem + 256 + i * 128);
+            const uint32_t q_lo = uniform((uint32_t)umma_desc_sw128(q_addr)), kv_lo = uniform((uint32_t)umma_desc_sw128(kv_addr));
+            const auto qk = [&](uint32_t a, uint32_t b) {
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
-                    constexpr int kUnit = 16;  // bytes that the address of a descriptor counts
-                    const uint32_t at = ((ks >> 2) * S::kHalf + (ks & 3) * 32) / kUnit;
-                    umma_ss(tmem + i * 128, a + at, b + at, id_s, ks > 0, lead);
+                    const uint32_t at = ((ks >> 2) * S::kHalf + (ks & 3) * 32) / 16;
+                    if (ks == 0)
+                        umma_ss<false>(tS, a + at, b + at, kDescHi, id_s);
+                    else
+                        umma_ss<true>(tS, a + at, b + at, kDescHi, id_s);
                 }
             };
-            const auto pv = [&](int i, bool first, uint32_t entry) {
-                const uint64_t b = desc_v(kv_addr + (entry % NS) * S::kTileBytes, S::kHalf);
+            // V as the second operand of P V: rows (slots) of 64 numbers of head_dim side by side, so head_dim is the contiguous direction.  In
+            // the 128-byte swizzle: blocks of 64 numbers kHalf apart (a field that the other operands leave at 1), groups of eight slots 1024 bytes.
+            constexpr uint32_t kHalfField = (uint32_t)(S::kHalf / 16) << 16, kOneField = 1u << 16;
+            const auto pv = [&](bool first, uint32_t b) {
+                umma_ts(tO, tS, kDescHi, b, id_o, !first);
 #pragma unroll
-                for (int ks = 0; ks < kTile / 16; ++ks)
-                    umma_ts(tmem + 256 + i * 128, tmem + i * 128 + ks * 8, b + ks * (2048 / 16), id_o, !first || ks > 0, lead);
+                for (int ks = 1; ks < kTile / 16; ++ks) umma_ts(tO, tS + ks * 8, kDescHi, b + ks * (2048 / 16), id_o, true);
             };
-            const auto wait_kv = [&](uint32_t entry) {
-                const bool r = mbar_wait_bounded(kv_full(entry % NS), (entry / NS) & 1, gave_up);
-                tc_fence_after();
-                return r;
+            const auto at_entry = [&](uint32_t entry) { return uniform(kv_lo + (entry % NS) * (S::kTileBytes / 16)); };
+            const auto wait_kv = [&](uint32_t entry) { return wait_for(kv_full(entry % NS), (entry / NS) & 1, gave_up); };
+            // Both streams go through all entries in order and an entry is free when both have: one that the other stream alone reads is seen
+            // to be full and let go.  So neither is ever more than one use of a stage away from what it waits for, which is as far as a
+            // barrier's phase tells uses apart (copies may arrive out of order).
+            const auto pass = [&](uint32_t upto) {
+                for (; it != upto; ++it) {
+                    if (!wait_kv(it)) return false;
+                    if (lane == 0) mbar_arrive(kv_empty(it % NS));
+                }
+                return true;
             };
-            const auto wait_p = [&](int i) {
-                const bool r = mbar_wait_bounded(p_full0 + 8 * i, (turns >> i) & 1, gave_up);
-                turns ^= 1u << i;
-                tc_fence_after();
+            // Two row tiles: the streams issue by turns.  Side by side, their instructions would share the tensor cores and both streams'
+            // softmax would then share the rest of the time; by turns, one stream's softmax runs under the other's products.
+            const auto my_turn = [&](bool two) {
+                if (!two) return true;
+                const bool r = wait_for(turn0 + 8 * i, (n_turn & 1) ^ (1 - i), gave_up);
+                n_turn += 1;
                 return r;
             };
             while (ok && walk.next(pc)) {
                 const int T = pc.k1 - pc.k0;
                 const bool two = pc.rows > kTile;
-                ok = mbar_wait_bounded(q_full, n_piece & 1, gave_up);
+                if (lane == 0) mbar_arrive(q_full);  // (with the rows' own arrivals: a piece begins when this warp is there too)
+                if (!(ok = wait_for(q_full, n_piece & 1, gave_up))) break;
                 n_piece += 1;
-                if (!ok) break;
-                for (int i = 0; i < (two ? 2 : min(T, 2)); ++i) {
-                    const uint32_t ek = it + (two ? 0 : i);
-                    if (!(ok = wait_kv(ek))) break;
-                    qk(i, two, ek);
-                    if (!two || i == 1) umma_commit_by(kv_empty(ek % NS), lead);
-                    umma_commit_by(s_full0 + 8 * i, lead);
-                }
-                // P V of a stream's tile, then Q K of its next
-                const int events = two ? 2 * T : T;
-                for (int e = 0; ok && e < events; ++e) {
-                    const int i = e & 1, t = two ? e >> 1 : e;
-                    const uint32_t ev = it + v_entry(two, T, t), ek = ev + 1;
-                    const bool more = t + (two ? 1 : 2) < T, done = !two || i == 1;  // (done: nobody else reads these entries)
-                    if (!(ok = wait_p(i) && wait_kv(ev))) break;
-                    pv(i, e < 2, ev);
-                    if (done) umma_commit_by(kv_empty(ev % NS), lead);
-                    if (more) {
-                        if (!(ok = wait_kv(ek))) break;
-                        qk(i, two, ek);
-                        if (done) umma_commit_by(kv_empty(ek % NS), lead);
+                const uint32_t a = uniform(q_lo + (two ? i : 0) * (S::kTileBytes / 16)), it0 = it;
+                const int t0 = two ? 0 : (int)i, dt = two ? 1 : 2;
+                if (t0 < T) {
+                    if (!(ok = pass(it0 + t0) && wait_kv(it) && my_turn(two))) break;
+                    tc_fence_after();
+                    const uint32_t bk = at_entry(it);
+                    if (elect_one()) {
+                        qk(a, bk);
+                        if (two) mbar_arrive(turn0 + 8 * (1 - i));
+                        umma_commit(kv_empty(it % NS));
+                        umma_commit(s_full0 + 8 * i);
                     }
-                    umma_commit_by(s_full0 + 8 * i, lead);
+                    __syncwarp();
+                    it += 1;
                 }
-                it += 2 * T;
+                // P V of a tile, then Q K of the next, which takes the weights' place
+                for (int t = t0; t < T; t += dt) {
+                    const bool more = t + dt < T;
+                    ok = pass(it0 + v_entry(two, T, t)) && wait_kv(it) && (!more || wait_kv(it + 1)) &&
+                         wait_for(p_full0 + 8 * i, n_p & 1, gave_up) && my_turn(two);
+                    n_p += 1;
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t bv = uniform(at_entry(it) - kOneField + kHalfField), bk = at_entry(it + 1);
+                    if (elect_one()) {
+                        pv(t == t0, bv);
+                        umma_commit(kv_empty(it % NS));
+                        if (more) qk(a, bk);
+                        if (two) mbar_arrive(turn0 + 8 * (1 - i));
+                        umma_commit(s_full0 + 8 * i);
+                        if (more) umma_commit(kv_empty((it + 1) % NS));
+                    }
+                    __syncwarp();
+                    it += more ? 2 : 1;
+                }
+                ok = ok && pass(it0 + 2 * T);
             }
         } else if (Q8 && warp >= 12) {
             // ---- e4m3 tiles to bf16 tiles in the 128-byte swizzle: sixteen numbers a thread and step
@@ -954,8 +1022,8 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                 const int T = pc.k1 - pc.k0;
                 const auto convert = [&]() {
                     const uint32_t rs = it % NR, ks = it % NS;
-                    if (!mbar_wait_bounded(raw_full(rs), (it / NR) & 1, gave_up)) return false;
-                    if (!mbar_wait_bounded(kv_empty(ks), ((it / NS) & 1) ^ 1, gave_up)) return false;
+                    if (!wait_for(raw_full(rs), (it / NR) & 1, gave_up)) return false;
+                    if (!wait_for(kv_empty(ks), ((it / NS) & 1) ^ 1, gave_up)) return false;
                     const uint8_t* raw = raw_ptr + rs * S::kRawBytes;
                     const uint32_t to = kv_addr + ks * S::kTileBytes + (col >> 2) * S::kHalf;
 #pragma unroll
