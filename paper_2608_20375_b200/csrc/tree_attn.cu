@@ -13,8 +13,8 @@
 // exponentials are worked out, the other's products run.  A unit of one row tile gives the streams the even and the odd key tiles
 // instead, joined at the end.  Scores and sums stay in TMEM: S of 128 columns a stream, overwritten in place by the weights p in bf16
 // (which are the second product's first operand from there), and O of head_dim columns.  One thread has one row, so maxima and sums need no
-// exchange.  A row's reference is the maximum of its first tile; maxima are taken again, and O rescaled, only when the weights of a
-// tile add up to more than 2^20 against it: fp32 sums and bf16 weights of that size are as exact as those up to 1.
+// exchange.  O is rescaled only when a row's maximum has grown by more than 2^8 since it was last taken: weights are then up to 256,
+// which fp32 sums and bf16 hold as well as those up to 1.
 #include <cuda.h>
 #include <float.h>
 
@@ -28,7 +28,7 @@ namespace {
 constexpr int kTile = 128;      // slots of a key tile, rows of a row tile
 constexpr int kUnitRows = 256;
 constexpr uint32_t kWaitNs = 500;  // that a poll may sleep
-constexpr float kMostSum = 1048576.0f;  // of a tile's weights, which are 1 at the maximum known before: beyond it O is rescaled
+constexpr float kMostGrowth = 8.0f;  // (powers of two) of a row's maximum, before O is rescaled
 
 // What the plan says of a sequence (entry 0: the shared prefix with the rows of all of them; entry b + 1: sequence b).
 struct __align__(16) PlanSeq {
@@ -226,14 +226,19 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile
     return mbar_wait_bounded_hint(bar, parity, gave_up, kWaitNs);
 }
 
+// What the warps of a CTA are told of a piece.
 struct Piece {
-    int s, h, mt, k0, k1;  // entry of the plan, key head, unit of the head, key tiles
-    int n, base, node0, unit, kt, R;
-    int rows;  // rows of the unit
+    int T;          // key tiles; 0: there are no more pieces
+    int s, h;       // entry of the plan, key head
+    int first, end; // first slot, and how many slots there are
+    int n, base;    // new rows, slots before the first of them
+    int r0, rows;   // first row of the unit among the entry's, rows of the unit
+    int unit;       // number of the unit
+    int head, whole;  // the piece begins with the unit's first tile; is all of it
 };
 struct Walk {
     const PlanSeq* seq;
-    int last_s, Hk, group;
+    int last_s, Hk, group, shared;
     int x, x1;
     int s, h, mt, k;
     PlanSeq q;
@@ -242,6 +247,7 @@ struct Walk {
         last_s = p.batch;
         Hk = p.c.kv_heads;
         group = p.group;
+        shared = p.shared;
         x = x1 = 0;
         if (cta >= __ldcg(&p.head->parts)) return;
         const int4 st = __ldcg((const int4*)(p.start + cta)), en = __ldcg((const int4*)(p.start + cta) + 1);
@@ -266,15 +272,19 @@ struct Walk {
                 }
             }
         }
-        const int w = unit_weight(R, mt);
-        const int left = (x1 - x + w - 1) >> (w - 1);
-        pc.s = s, pc.h = h, pc.mt = mt, pc.k0 = k;
-        pc.k1 = left < q.kt - k ? k + left : q.kt;
-        pc.n = q.n, pc.base = q.base, pc.node0 = q.node0, pc.kt = q.kt, pc.R = R;
+        const int w = unit_weight(R, mt), left = (x1 - x + w - 1) >> (w - 1), kv0 = s == 0 ? 0 : shared;
+        pc.T = min(left, q.kt - k);
+        pc.s = s, pc.h = h;
+        pc.first = kv0 + k * kTile;
+        pc.end = s == 0 ? shared : q.base + q.n;
+        pc.n = q.n, pc.base = q.base;
+        pc.r0 = mt * kUnitRows;
+        pc.rows = min(kUnitRows, R - pc.r0);
         pc.unit = q.unit0 + h * row_tiles2(R) + mt;
-        pc.rows = min(kUnitRows, R - mt * kUnitRows);
-        x += (pc.k1 - pc.k0) * w;
-        k = pc.k1;
+        pc.head = k == 0;
+        pc.whole = k == 0 && pc.T == q.kt && shared == 0;
+        x += pc.T * w;
+        k += pc.T;
         return true;
     }
 };
@@ -322,6 +332,8 @@ __device__ __forceinline__ uint32_t seen_word(const uint32_t* mask_row, int word
 }
 
 // ---- the attention kernel ------------------------------------------------------------------------------------------
+constexpr int kPieces = 4;  // that are told ahead
+
 template <int D, bool Q8>
 struct Shape {
     static constexpr int kHalf = kTile * 128;                 // 128 rows of 128 bytes: 64 numbers of a row, in the 128-byte swizzle
@@ -332,10 +344,9 @@ struct Shape {
     static constexpr int kThreads = Q8 ? 512 : 384;
     static constexpr int kConvWarps = Q8 ? 4 : 0;
     // registers a thread: the softmax's eight warps take over what the others leave (of 64512 or 65536 at the launch)
-    static constexpr int kRegsSoftmax = Q8 ? 168 : 208, kRegsOthers = 88;
-    static constexpr int kCols = Q8 ? 64 : 128;  // scores that a softmax thread holds at a time
+    static constexpr int kRegsSoftmax = Q8 ? 208 : 224, kRegsOthers = Q8 ? 48 : 56;
     static_assert(256 * kRegsSoftmax + (kThreads - 256) * kRegsOthers <= kThreads * (Q8 ? 128 : 168), "registers of a launch");
-    static constexpr size_t kSmem = 1024 + 2 * kTileBytes + (size_t)kStages * kTileBytes + (size_t)kRaw * kRawBytes + 512;
+    static constexpr size_t kSmem = 1024 + 2 * kTileBytes + (size_t)kStages * kTileBytes + (size_t)kRaw * kRawBytes + 1024;
 };
 
 // One thread of the warp.
@@ -380,8 +391,6 @@ __device__ __forceinline__ void tmem_ld_32x32(uint32_t taddr, uint32_t (&r)[32])
           "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr));
 }
-__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[32]) { tmem_ld_32x32(taddr, r); }
-__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[16]) { tmem_ld_32x16(taddr, r); }
 // the same registers, known to have arrived: nothing that reads them is moved ahead of the wait
 template <int N>
 __device__ __forceinline__ void tmem_arrived(uint32_t (&r)[N]) {
@@ -429,26 +438,23 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return r;
 }
 
-// kCols scores of the row, all asked for together: while the tensor cores work on the other stream, an answer takes several hundred cycles
-template <int kCols>
-__device__ __forceinline__ void scores(uint32_t tS, uint32_t (&u)[kCols], bool masked, const uint32_t (&sees)[4], int x) {
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// The row's 128 scores at tS, all asked for together (while the tensor cores work on the other stream, an answer takes several hundred
+// cycles), -inf in the place of those that `sees` leaves out, and their largest.
+__device__ __forceinline__ float scores(uint32_t tS, uint32_t (&u)[kTile], bool masked, const uint32_t (&sees)[4]) {
 #pragma unroll
-    for (int y = 0; y < kCols; y += 32) tmem_ld_32x32(tS + kCols * x + y, *(uint32_t(*)[32]) & u[y]);
+    for (int x = 0; x < kTile; x += 32) tmem_ld_32x32(tS + x, *(uint32_t(*)[32]) & u[x]);
     tmem_arrived(u);
     if (masked)
 #pragma unroll
-        for (int y = 0; y < kCols; ++y) u[y] = (sees[(kCols * x + y) / 32] >> (y % 32)) & 1 ? u[y] : 0xFF800000u;
-}
-// Largest of the row's 128 scores at tS (masked: of those that `sees` says, -inf in the place of the others).
-__device__ __forceinline__ float max_of(uint32_t tS, bool masked, const uint32_t (&sees)[4]) {
-    uint32_t u[32];
+        for (int x = 0; x < kTile; ++x) u[x] = (sees[x / 32] >> (x % 32)) & 1 ? u[x] : 0xFF800000u;
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-        scores(tS, u, masked, sees, x);
-#pragma unroll
-        for (int y = 0; y < 32; ++y) mx[y & 3] = fmaxf(mx[y & 3], __uint_as_float(u[y]));
-    }
+    for (int x = 0; x < kTile; x += 2) mx[x / 2 % 4] = max3(mx[x / 2 % 4], __uint_as_float(u[x]), __uint_as_float(u[x + 1]));
     return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
 }
 // 2^t of two numbers on the FMA pipe: t = n + f, n whole and |f| <= 1/2; 2^f by a polynomial of degree 5 (fitted for the least largest
@@ -469,31 +475,26 @@ __device__ __forceinline__ float2 exp2_poly(uint64_t t) {
     return make_float2(__int_as_float(__float_as_int(a.x) + (__float_as_int(n.x) << 23)),
                        __int_as_float(__float_as_int(a.y) + (__float_as_int(n.y) << 23)));
 }
-// Weights 2^(c2 s + off) of the row's 128 scores at tS as pairs of bf16, and their sum (unrounded): one pass.  128 rows' exponentials take the 16-a-clock unit as long as both products take the tensor cores, so one
-// pair of four is worked out on the FMA pipe; sums and conversions follow eight pairs behind.  Cycles for 128 x 128 scores, alone and
-// two warps a scheduler: 1150 and 1910 for two; without polynomials 1350 and 2350, with one in three 1180 and 1960.
-template <int kCols>
-__device__ __forceinline__ float weigh(uint32_t tS, bool masked, const uint32_t (&sees)[4], float c2, float off, uint32_t (&w)[64]) {
-    constexpr int kBehind = 8, kPairs = kCols / 2;
+// Weights 2^(c2 s + off) of 64 scores as pairs of bf16, and their sum (unrounded).  128 rows' exponentials take the 16-a-clock unit as long
+// as both products take the tensor cores, so one pair of four is worked out on the FMA pipe; sums and conversions follow eight pairs
+// behind.  Cycles for 128 x 128 scores, one and two warps a scheduler: 1150 and 1910 for two; without polynomials 1350 and 2350, with one in
+// three 1180 and 1960.
+__device__ __forceinline__ float weigh(uint32_t* v, float c2, float off, uint32_t (&w)[32]) {
+    constexpr int kBehind = 8, kPairs = 32;
     uint64_t part[2] = {0, 0};
     const uint64_t cc = two(c2, c2), oo = two(off, off);
 #pragma unroll
-    for (int x = 0; x < kTile / kCols; ++x) {
-        uint32_t v[kCols];
-        scores(tS, v, masked, sees, x);
-#pragma unroll
-        for (int y = 0; y < kPairs + kBehind; ++y) {
-            if (y < kPairs) {
-                const uint64_t t = fma2(two(__uint_as_float(v[2 * y]), __uint_as_float(v[2 * y + 1])), cc, oo);
-                const float2 e = y % 4 == 3 ? exp2_poly(t) : make_float2(ex2_in_order(apart(t).x), ex2_in_order(apart(t).y));
-                v[2 * y] = __float_as_uint(e.x), v[2 * y + 1] = __float_as_uint(e.y);
-            }
-            if (y >= kBehind) {
-                const int z = y - kBehind;
-                const float e0 = __uint_as_float(v[2 * z]), e1 = __uint_as_float(v[2 * z + 1]);
-                part[z & 1] = add2(part[z & 1], two(e0, e1));
-                w[kPairs * x + z] = pack_bf16(e0, e1);
-            }
+    for (int y = 0; y < kPairs + kBehind; ++y) {
+        if (y < kPairs) {
+            const uint64_t t = fma2(two(__uint_as_float(v[2 * y]), __uint_as_float(v[2 * y + 1])), cc, oo);
+            const float2 e = y % 4 == 3 ? exp2_poly(t) : make_float2(ex2_in_order(apart(t).x), ex2_in_order(apart(t).y));
+            v[2 * y] = __float_as_uint(e.x), v[2 * y + 1] = __float_as_uint(e.y);
+        }
+        if (y >= kBehind) {
+            const int z = y - kBehind;
+            const float e0 = __uint_as_float(v[2 * z]), e1 = __uint_as_float(v[2 * z + 1]);
+            part[z & 1] = add2(part[z & 1], two(e0, e1));
+            w[z] = pack_bf16(e0, e1);
         }
     }
     const float2 a = apart(add2(part[0], part[1]));
@@ -505,7 +506,7 @@ __device__ __forceinline__ void rescale(uint32_t tO, float f) {
     uint32_t u[32];
 #pragma unroll
     for (int x = 0; x < D / 32; ++x) {
-        tmem_ld(tO + 32 * x, u);
+        tmem_ld_32x32(tO + 32 * x, u);
         tmem_arrived(u);
 #pragma unroll
         for (int y = 0; y < 32; ++y) u[y] = __float_as_uint(__uint_as_float(u[y]) * f);
@@ -521,13 +522,13 @@ __device__ __forceinline__ int v_entry(bool two, int T, int t) { return two ? 1 
 // its own.  Key tiles t0, t0 + dt, .. of the piece; a whole warp calls it, `sums` are the rows that see anything, m their maxima.
 template <int D, bool Q8>
 __device__ __noinline__ void add_spoilt(const AttnParams& p, const Piece& pc, uint32_t tO, bool sums, int b, int node, int head, int t0,
-                                        int dt, int kv0, int end, float m) {
+                                        int dt, float m) {
     const CacheView& c = p.c;
     const uint32_t* mask_row = p.mask ? p.mask + ((size_t)b * p.nmax + node) * p.words : nullptr;
     const uint16_t* q = (const uint16_t*)p.q + ((long long)b * p.rows + node) * p.q_stride + (long long)head * D;
-    for (int t = t0; t < pc.k1 - pc.k0; t += dt) {
-        const int first = kv0 + (pc.k0 + t) * kTile;
-        for (int slot = max(first, pc.base); slot < min(end, first + kTile); ++slot) {
+    for (int t = t0; t < pc.T; t += dt) {
+        const int first = pc.first + t * kTile;
+        for (int slot = max(first, pc.base); slot < min(pc.end, first + kTile); ++slot) {
             const size_t at = cache_row(c, __ldg(c.table + (size_t)(pc.s - 1) * c.width + (slot >> c.page_shift)), pc.h,
                                         slot & ((1 << c.page_shift) - 1));
             const auto entry = [&](const uint8_t* x, const uint8_t* exps, int d) {  // four numbers from d on
@@ -542,7 +543,7 @@ __device__ __noinline__ void add_spoilt(const AttnParams& p, const Piece& pc, ui
                 bad = bad || not_finite2(v.x) || not_finite2(v.y);
             }
             if (!bad) continue;
-            const bool mine = sums && (seen_word(mask_row, p.words, node, pc.n, pc.base, end, slot) & 1);
+            const bool mine = sums && (seen_word(mask_row, p.words, node, pc.n, pc.base, pc.end, slot) & 1);
             float s = 0.0f;
             if (mine)
                 for (int d = 0; d < D; d += 4) {
@@ -591,9 +592,12 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
     const auto raw_full = [&](int i) { return bar0 + 8 * (2 * NS + i); };
     const auto raw_empty = [&](int i) { return bar0 + 8 * (2 * NS + NR + i); };
     const uint32_t q_full = bar0 + 8 * (2 * NS + 2 * NR), s_full0 = q_full + 8, p_full0 = q_full + 24, pair = q_full + 40, turn0 = q_full + 48;
-    volatile int* const gave_up = (volatile int*)(bars + 2 * NS + 2 * NR + 8);
+    const uint32_t piece_full0 = q_full + 64, piece_empty0 = piece_full0 + 8 * kPieces;
+    volatile int* const gave_up = (volatile int*)(bars + 2 * NS + 2 * NR + 8 + 2 * kPieces);
     volatile int* const spoilt = gave_up + 1;  // [2] the last piece (counted from 1) with a row of V that was taken out
     uint32_t* const tmem_at = (uint32_t*)(gave_up + 3);
+    Piece* const pieces = (Piece*)(gave_up + 4);  // [kPieces]
+    static_assert((2 * NS + 2 * NR + 8 + 2 * kPieces) * 8 + 16 + kPieces * sizeof(Piece) <= 1024, "barriers and pieces");
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
@@ -604,6 +608,10 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
         for (int i = 0; i < NR; ++i) {
             mbar_init(raw_full(i), 1);
             mbar_init(raw_empty(i), S::kConvWarps > 0 ? S::kConvWarps : 1);
+        }
+        for (int i = 0; i < kPieces; ++i) {
+            mbar_init(piece_full0 + 8 * i, 1);
+            mbar_init(piece_empty0 + 8 * i, 11 + S::kConvWarps);
         }
         mbar_init(q_full, 10);
         mbar_init(pair, 8);
@@ -625,12 +633,15 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
     pdl_wait();
 
     const CacheView& c = p.c;
+    // Warp 11 walks along the CTA's stretch and tells the others, a few pieces ahead.
+    const auto next_piece = [&](uint32_t n) { return wait_for(piece_full0 + 8 * (n % kPieces), (n / kPieces) & 1, gave_up); };
+    const auto piece_done = [&](uint32_t n) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(piece_empty0 + 8 * (n % kPieces));
+    };
 
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kRegsSoftmax));
-        Walk walk;
-        Piece pc;
-        walk.begin(p, blockIdx.x);
         // ---- softmax: a thread a row
         const int i = warp >> 2, row_in_tile = tid & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the lanes
@@ -651,21 +662,18 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
             tc_fence_after();
             return r;
         };
-        while (ok && walk.next(pc)) {
-            n_piece += 1;
-            const int T = pc.k1 - pc.k0;
+        for (; (ok = next_piece(n_piece)); ++n_piece) {
+            const volatile Piece& pc = pieces[n_piece % kPieces];
+            const int T = pc.T;
+            if (T == 0) break;
             const bool two = pc.rows > kTile;
-            const int kv0 = pc.s == 0 ? 0 : p.shared, end = pc.s == 0 ? p.shared : pc.base + pc.n;
             const int r = (two ? i * kTile : 0) + row_in_tile;  // row of the unit
             const bool live = r < pc.rows;
-            int b = 0, node = 0, g = 0;
-            if (live) row_of(p, pc.s, pc.mt * kUnitRows + r, b, node, g);
-            const int head = pc.h * p.group + g;
-            const size_t q_row = (size_t)b * p.rows + node;
-            const uint32_t* mask_row = p.mask ? p.mask + ((size_t)b * p.nmax + node) * p.words : nullptr;
             if (two || i == 0) {
                 const uint32_t to = q_addr + i * S::kTileBytes + row_in_tile * 128;
-                const uint4* from = (const uint4*)(p.q + 2 * ((long long)q_row * p.q_stride + (long long)head * D));
+                int b = 0, node = 0, g = 0;
+                if (live) row_of(p, pc.s, pc.r0 + r, b, node, g);
+                const uint4* from = (const uint4*)(p.q + 2 * (((long long)b * p.rows + node) * p.q_stride + (long long)(pc.h * p.group + g) * D));
 #pragma unroll
                 for (int x = 0; x < D / 8; ++x) {
                     uint4 u = live ? __ldg(from + x) : make_uint4(0, 0, 0, 0);
@@ -683,12 +691,14 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
             const bool warp_live = __any_sync(0xFFFFFFFFu, live);
             float m = -INFINITY, l = 0.0f;  // maximum of the raw scores, sum of 2^(c2 (s - m))
             bool any = false;               // this stream has had a tile
+            // from this tile on there are new slots, or slots that are not there (the shared prefix: base is its end)
+            const int first0 = pc.first, to_base = pc.base - kTile - first0, t_masked = to_base < 0 ? 0 : to_base / kTile + 1;
             // Slots that are not there hold anything, and new slots may hold what is not a number and is not for every row: weights of zero do
             // not keep it out of the sums.  Their rows of V are cleared (a thread a slot); rows that see such a slot get it in the end.
             const auto clear_v = [&](int t, int first) {
                 const uint32_t entry = it + v_entry(two, T, t);
                 if (!wait_for(kv_full(entry % NS), (entry / NS) & 1, gave_up)) return false;
-                const int slot = first + row_in_tile;
+                const int slot = first + row_in_tile, end = pc.end;
                 if (slot >= pc.base) {
                     const uint32_t at = kv_addr + (entry % NS) * S::kTileBytes + row_in_tile * 128;
                     bool clear = slot >= end;
@@ -708,42 +718,43 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + (x >> 3) * S::kHalf + ((x + row_in_tile) & 7) * 16),
                                          "r"(0)
                                          : "memory");
-                        if (slot < end) spoilt[i] = (int)n_piece;
+                        if (slot < end) spoilt[i] = (int)n_piece + 1;
                     }
                 }
                 fence_proxy_async();
                 return true;
             };
             for (int t = two ? 0 : i; t < T; t += two ? 1 : 2) {
-                const int first = kv0 + (pc.k0 + t) * kTile;
-                const bool masked = first + kTile > pc.base;  // new slots, or slots that are not there (the shared prefix: base is its end)
+                const int first = first0 + t * kTile;
+                const bool masked = t >= t_masked;
                 uint32_t sees[4];
                 if (masked) {
+                    int b = 0, node = 0, g = 0;
+                    if (live) row_of(p, pc.s, pc.r0 + r, b, node, g);
+                    const uint32_t* mask_row = p.mask ? p.mask + ((size_t)b * p.nmax + node) * p.words : nullptr;
+                    const int n = pc.n, base = pc.base, end = pc.end;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        sees[x] = live ? seen_word(mask_row, p.words, node, pc.n, pc.base, end, first + 32 * x) : 0;
+                    for (int x = 0; x < 4; ++x) sees[x] = live ? seen_word(mask_row, p.words, node, n, base, end, first + 32 * x) : 0;
                     // (with two row tiles every entry ahead of V's in the ring has been used by this stream, so its phase is certain: see `pass`)
                     if (two && i == 0 && !(ok = clear_v(t, first))) break;
                 }
                 if (!(ok = wait_s())) break;
                 if (warp_live) {
-                    // The first tile's maxima are taken before its weights.  Then m stays as long as the weights do not grow too large against it
-                    // (or nothing was seen so far): where they do, maxima are taken again and the tile is weighed again.
-                    uint32_t w[64];
-                    float sum;
-                    for (bool again = !any;; again = true) {
-                        if (again) {
-                            const float now = fmaxf(m, max_of(tS, masked, sees)), f = m > -INFINITY ? ex2_approx((m - now) * c2) : 1.0f;
-                            if (any) rescale<D>(tO, f);
-                            l *= f;
-                            m = now;
-                        }
-                        sum = weigh<S::kCols>(tS, masked, sees, c2, m > -INFINITY ? -m * c2 : 0.0f, w);
-                        if (again || !__any_sync(0xFFFFFFFFu, sum > kMostSum || (live && m == -INFINITY))) break;
+                    uint32_t u[kTile], w[32];
+                    const float mx = scores(tS, u, masked, sees);
+                    // (m = -inf: nothing seen so far, and what O holds is zero)
+                    const bool grown = mx > m && !((mx - m) * c2 <= kMostGrowth);
+                    if (__any_sync(0xFFFFFFFFu, grown)) {
+                        const float now = fmaxf(m, mx), f = m > -INFINITY ? ex2_approx((m - now) * c2) : 1.0f;
+                        if (any) rescale<D>(tO, f);
+                        l *= f;
+                        m = now;
                     }
-                    l += sum;
-                    tmem_st_32x32(tS, *(uint32_t(*)[32])&w[0]);
-                    tmem_st_32x32(tS + 32, *(uint32_t(*)[32])&w[32]);
+                    const float off = m > -INFINITY ? -m * c2 : 0.0f;
+                    l += weigh(u, c2, off, w);
+                    tmem_st_32x32(tS, w);
+                    l += weigh(u + 64, c2, off, w);
+                    tmem_st_32x32(tS + 32, w);
                     tmem_wait_st();
                 }
                 if (masked && !two && !(ok = clear_v(t, first))) break;
@@ -758,15 +769,18 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
             if (any)
                 ok = wait_s();  // the last product is done
             else
-                ok = wait_for(q_full, (n_piece - 1) & 1, gave_up);  // (nor does a stream without a tile run ahead)
+                ok = wait_for(q_full, n_piece & 1, gave_up);  // (nor does a stream without a tile run ahead)
             if (!ok) break;
 
             // ---- the end of a piece: O as far as it goes
-            if (spoilt[two ? 0 : i] == (int)n_piece)
-                add_spoilt<D, Q8>(p, pc, tO, live && m > -INFINITY, b, node, head, two ? 0 : i, two ? 1 : 2, kv0, end, m);
-            const bool whole = pc.k0 == 0 && pc.k1 == pc.kt && p.shared == 0;
-            const size_t slot = p.shared > 0 ? (size_t)pc.unit + blockIdx.x : 2 * (size_t)blockIdx.x + (pc.k0 == 0 ? 1 : 0);
-            const size_t out_row = q_row * p.q_heads + head;
+            int b = 0, node = 0, g = 0;
+            if (live) row_of(p, pc.s, pc.r0 + r, b, node, g);
+            const int head = pc.h * p.group + g;
+            if (spoilt[two ? 0 : i] == (int)n_piece + 1)
+                add_spoilt<D, Q8>(p, pieces[n_piece % kPieces], tO, live && m > -INFINITY, b, node, head, two ? 0 : i, two ? 1 : 2, m);
+            const bool whole = pc.whole;
+            const size_t slot = p.shared > 0 ? (size_t)pc.unit + blockIdx.x : 2 * (size_t)blockIdx.x + pc.head;
+            const size_t out_row = ((size_t)b * p.rows + node) * p.q_heads + head;
             const auto put = [&](int d0, const uint32_t (&u)[32], float inv) {
                 if (!live) return;
                 if (whole) {
@@ -859,26 +873,40 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                 if (i == 0 && ok) put_sums(ms, ls);
             }
             tc_fence_before();  // what follows in TMEM follows these reads
+            if (!ok) break;
+            piece_done(n_piece);
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kRegsOthers));
+        uint32_t n_piece = 0;
+        bool ok = true;
+        if (warp == 11) {
             Walk walk;
             Piece pc;
             walk.begin(p, blockIdx.x);
-        if (warp == 9) {
+            for (bool more = true; ok && more; ++n_piece) {
+                more = walk.next(pc);
+                if (!more) pc.T = 0;
+                ok = wait_for(piece_empty0 + 8 * (n_piece % kPieces), ((n_piece / kPieces) & 1) ^ 1, gave_up);
+                if (ok && lane == 0) {
+                    pieces[n_piece % kPieces] = pc;
+                    mbar_arrive(piece_full0 + 8 * (n_piece % kPieces));
+                }
+            }
+        } else if (warp == 9) {
             // ---- copies: K and V tiles page by page, into the ring (bf16) or to where the conversion takes them from (e4m3)
             constexpr int N = Q8 ? NR : NS;
             constexpr int kParts = Q8 ? 2 : D / 64;  // copies a page and tile: halves of its rows, or numbers and exponents
             uint32_t it = 0;
-            bool ok = true;
             const int box = p.box_rows, shift = c.page_shift, low = (1 << shift) - 1;
-            while (ok && walk.next(pc)) {
-                const int T = pc.k1 - pc.k0;
+            for (; (ok = next_piece(n_piece)); ++n_piece) {
+                const volatile Piece& pc = pieces[n_piece % kPieces];
+                const int T = pc.T, h = pc.h, end = pc.end, first0 = pc.first;
+                if (T == 0) break;
                 const bool two = pc.rows > kTile;
-                const int kv0 = pc.s == 0 ? 0 : p.shared, end = pc.s == 0 ? p.shared : pc.base + pc.n;
                 const int32_t* table = c.table + (pc.s == 0 ? 0 : (size_t)(pc.s - 1) * c.width);
                 const auto bring = [&](int t, bool is_v) {
-                    const int first = kv0 + (pc.k0 + t) * kTile, upto = min(end, first + kTile);
+                    const int first = first0 + t * kTile, upto = min(end, first + kTile);
                     const int copies = (upto - first + box - 1) / box;  // boxes with a slot in use
                     const int i = lane / kParts, part = lane % kParts;
                     int page = 0, at = 0;
@@ -893,7 +921,7 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                     if (lane == 0) mbar_arrive_expect_tx(full, copies * box * (Q8 ? D + 1 : 2 * D));
                     __syncwarp();
                     if (i < copies) {
-                        const size_t row = cache_row(c, page, pc.h, at);
+                        const size_t row = cache_row(c, page, h, at);
                         if (!Q8 || part == 0)
                             tma_load_2d(to + (Q8 ? i * box * D : part * S::kHalf + i * box * 128), is_v ? &p.map_v : &p.map_k,
                                         Q8 ? 0 : part * 64, (int)row, full);
@@ -913,6 +941,8 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                         if (t + 2 < T) ok = ok && bring(t + 2, false);
                     }
                 }
+                if (!ok) break;
+                piece_done(n_piece);
             }
             // (after a wait that ran out: what is on its way arrives before the CTA ends)
             if (!ok && lane == 0)
@@ -924,8 +954,7 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
             // ---- products, a warp a stream: while one waits for weights or signals, the other's instructions keep the tensor cores busy
             constexpr uint32_t id_s = umma_idesc(128, 128, true), id_o = umma_idesc(128, D, true) | (1u << 16);  // (V: head_dim is contiguous)
             const uint32_t i = warp == 8 ? 0 : 1;
-            uint32_t it = 0, n_piece = 0, n_p = 0, n_turn = 0;
-            bool ok = true;
+            uint32_t it = 0, n_p = 0, n_turn = 0;
             // (descriptors differ in their low words alone; the numbers that choose them are loaded, so the compiler is told that they are uniform)
             constexpr uint32_t kDescHi = (uint32_t)(umma_desc_sw128(0) >> 32);
             const uint32_t tS = uniform(tmem + i * 128), tO = uniform(tmem + 256 + i * 128);
@@ -944,9 +973,8 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
             // the 128-byte swizzle: blocks of 64 numbers kHalf apart (a field that the other operands leave at 1), groups of eight slots 1024 bytes.
             constexpr uint32_t kHalfField = (uint32_t)(S::kHalf / 16) << 16, kOneField = 1u << 16;
             const auto pv = [&](bool first, uint32_t b) {
-                umma_ts(tO, tS, kDescHi, b, id_o, !first);
 #pragma unroll
-                for (int ks = 1; ks < kTile / 16; ++ks) umma_ts(tO, tS + ks * 8, kDescHi, b + ks * (2048 / 16), id_o, true);
+                for (int ks = 0; ks < kTile / 16; ++ks) umma_ts(tO, tS + ks * 8, kDescHi, b + ks * (2048 / 16), id_o, ks > 0 || !first);
             };
             const auto at_entry = [&](uint32_t entry) { return uniform(kv_lo + (entry % NS) * (S::kTileBytes / 16)); };
             const auto wait_kv = [&](uint32_t entry) { return wait_for(kv_full(entry % NS), (entry / NS) & 1, gave_up); };
@@ -968,12 +996,13 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                 n_turn += 1;
                 return r;
             };
-            while (ok && walk.next(pc)) {
-                const int T = pc.k1 - pc.k0;
+            for (; (ok = next_piece(n_piece)); ++n_piece) {
+                const volatile Piece& pc = pieces[n_piece % kPieces];
+                const int T = pc.T;
+                if (T == 0) break;
                 const bool two = pc.rows > kTile;
                 if (lane == 0) mbar_arrive(q_full);  // (with the rows' own arrivals: a piece begins when this warp is there too)
                 if (!(ok = wait_for(q_full, n_piece & 1, gave_up))) break;
-                n_piece += 1;
                 const uint32_t a = uniform(q_lo + (two ? i : 0) * (S::kTileBytes / 16)), it0 = it;
                 const int t0 = two ? 0 : (int)i, dt = two ? 1 : 2;
                 if (t0 < T) {
@@ -1010,6 +1039,8 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                     it += more ? 2 : 1;
                 }
                 ok = ok && pass(it0 + 2 * T);
+                if (!ok) break;
+                piece_done(n_piece);
             }
         } else if (Q8 && warp >= 12) {
             // ---- e4m3 tiles to bf16 tiles in the 128-byte swizzle: sixteen numbers a thread and step
@@ -1017,9 +1048,9 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
             constexpr int kPer = D / 16, kRowsStep = 128 / kPer, kSteps = kTile / kRowsStep;
             const int col = ct % kPer, row0 = ct / kPer;
             uint32_t it = 0;
-            bool ok = true;
-            while (ok && walk.next(pc)) {
-                const int T = pc.k1 - pc.k0;
+            for (; (ok = next_piece(n_piece)); ++n_piece) {
+                const int T = ((const volatile Piece&)pieces[n_piece % kPieces]).T;
+                if (T == 0) break;
                 const auto convert = [&]() {
                     const uint32_t rs = it % NR, ks = it % NS;
                     if (!wait_for(raw_full(rs), (it / NR) & 1, gave_up)) return false;
@@ -1055,6 +1086,8 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                     return true;
                 };
                 for (int e = 0; ok && e < 2 * T; ++e) ok = convert();
+                if (!ok) break;
+                piece_done(n_piece);
             }
         }
     }
