@@ -68,4 +68,10 @@ __device__ __forceinline__ uint2 e4m3x4_to_bf16(uint32_t w, uint32_t f, uint32_t
     return r;
 }
 
+constexpr uint32_t kOneBf16x2 = 0x3F803F80u;
+// four e4m3 numbers -> the odd two and the even two as pairs of bf16
+__device__ __forceinline__ uint2 e4m3x4_to_bf16_odd_even(uint32_t w, uint32_t f) {
+    return make_uint2(bf16x2_mul(e4m3x2_to_bf16x2_small(w), f), bf16x2_mul(e4m3x2_to_bf16x2_small(w << 8), f));
+}
+
 }  // namespace graft

@@ -334,19 +334,24 @@ __device__ __forceinline__ uint32_t seen_word(const uint32_t* mask_row, int word
 // ---- the attention kernel ------------------------------------------------------------------------------------------
 constexpr int kPieces = 4;  // that are told ahead
 
-template <int D, bool Q8>
+// kOne: no unit has more than one row tile, and there is room for more key tiles.
+template <int D, bool Q8, bool kOne>
 struct Shape {
     static constexpr int kHalf = kTile * 128;                 // 128 rows of 128 bytes: 64 numbers of a row, in the 128-byte swizzle
     static constexpr int kTileBytes = kTile * D * 2;          // a tile of Q, K or V in bf16
     static constexpr int kRawBytes = kTile * D + kTile;       // a tile of e4m3 numbers and its rows' exponents
-    static constexpr int kStages = Q8 ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 10);
-    static constexpr int kRaw = Q8 ? (D == 128 ? 4 : 8) : 0;
-    static constexpr int kThreads = Q8 ? 512 : 384;
-    static constexpr int kConvWarps = Q8 ? 4 : 0;
-    // registers a thread: the softmax's eight warps take over what the others leave (of 64512 or 65536 at the launch)
-    static constexpr int kRegsSoftmax = Q8 ? 208 : 224, kRegsOthers = Q8 ? 48 : 56;
-    static_assert(256 * kRegsSoftmax + (kThreads - 256) * kRegsOthers <= kThreads * (Q8 ? 128 : 168), "registers of a launch");
-    static constexpr size_t kSmem = 1024 + 2 * kTileBytes + (size_t)kStages * kTileBytes + (size_t)kRaw * kRawBytes + 1024;
+    static constexpr int kQTiles = kOne ? 1 : 2;
+    // Tiles in bf16 (and e4m3 tiles on their way).  Two streams on key tiles of their own have four in use.
+    static constexpr int kStages = (Q8 ? kOne ? 5 : 3 : kOne ? 6 : 5) * (128 / D);
+    static constexpr int kRaw = Q8 ? (kOne ? 2 : 4) * (128 / D) : 0;
+    static constexpr int kConvWarps = Q8 ? (kOne ? 8 : 4) : 0;
+    static constexpr int kThreads = 384 + 32 * kConvWarps;
+    // registers a thread: the softmax's eight warps take over what the others leave (of what the launch has)
+    static constexpr int kRegsLaunch = kConvWarps == 8 ? 96 : kConvWarps == 4 ? 128 : 168;
+    static constexpr int kRegsSoftmax = kConvWarps == 8 ? 168 : kConvWarps == 4 ? 208 : 224, kRegsOthers = Q8 ? 48 : 56;
+    static constexpr int kCols = kConvWarps == 8 ? 64 : 128;  // scores that a softmax thread holds at a time
+    static_assert(256 * kRegsSoftmax + (kThreads - 256) * kRegsOthers <= kThreads * kRegsLaunch, "registers of a launch");
+    static constexpr size_t kSmem = 1024 + kQTiles * kTileBytes + (size_t)kStages * kTileBytes + (size_t)kRaw * kRawBytes + 1024;
 };
 
 // One thread of the warp.
@@ -416,6 +421,12 @@ __device__ __forceinline__ float ex2_in_order(float x) {
     asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+struct Yes {
+    static constexpr bool value = true;
+};
+struct No {
+    static constexpr bool value = false;
+};
 // two fp32 numbers in a 64-bit register
 __device__ __forceinline__ uint64_t two(float lo, float hi) {
     uint64_t r;
@@ -443,18 +454,19 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-// The row's 128 scores at tS, all asked for together (while the tensor cores work on the other stream, an answer takes several hundred
-// cycles), -inf in the place of those that `sees` leaves out, and their largest.
-__device__ __forceinline__ float scores(uint32_t tS, uint32_t (&u)[kTile], bool masked, const uint32_t (&sees)[4]) {
+// kCols of the row's scores at tS, from x0 on, all asked for together (while the tensor cores work on the other stream, an answer takes
+// several hundred cycles), -inf in the place of those that `sees` leaves out, and their largest.
+template <int kCols>
+__device__ __forceinline__ float scores(uint32_t tS, int x0, uint32_t (&u)[kCols], bool masked, const uint32_t (&sees)[4]) {
 #pragma unroll
-    for (int x = 0; x < kTile; x += 32) tmem_ld_32x32(tS + x, *(uint32_t(*)[32]) & u[x]);
+    for (int x = 0; x < kCols; x += 32) tmem_ld_32x32(tS + x0 + x, *(uint32_t(*)[32]) & u[x]);
     tmem_arrived(u);
     if (masked)
 #pragma unroll
-        for (int x = 0; x < kTile; ++x) u[x] = (sees[x / 32] >> (x % 32)) & 1 ? u[x] : 0xFF800000u;
+        for (int x = 0; x < kCols; ++x) u[x] = (sees[(x0 + x) / 32] >> (x % 32)) & 1 ? u[x] : 0xFF800000u;
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int x = 0; x < kTile; x += 2) mx[x / 2 % 4] = max3(mx[x / 2 % 4], __uint_as_float(u[x]), __uint_as_float(u[x + 1]));
+    for (int x = 0; x < kCols; x += 2) mx[x / 2 % 4] = max3(mx[x / 2 % 4], __uint_as_float(u[x]), __uint_as_float(u[x + 1]));
     return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
 }
 // 2^t of two numbers on the FMA pipe: t = n + f, n whole and |f| <= 1/2; 2^f by a polynomial of degree 5 (fitted for the least largest
@@ -556,7 +568,8 @@ __device__ __noinline__ void add_spoilt(const AttnParams& p, const Piece& pc, ui
             const float e = mine ? ex2_approx((s - m) * p.c2) : 0.0f;
             for (int d = 0; d < D; d += 4) {
                 const uint2 v = entry(c.v, c.v_exp, d);
-                const uint32_t vw[4] = {v.x << 16, v.x & 0xFFFF0000u, v.y << 16, v.y & 0xFFFF0000u};
+                const uint32_t v0 = v.x << 16, v1 = v.x & 0xFFFF0000u, v2 = v.y << 16, v3 = v.y & 0xFFFF0000u;
+                const uint32_t vw[4] = {Q8 ? v1 : v0, Q8 ? v3 : v1, Q8 ? v0 : v2, Q8 ? v2 : v3};  // (the order of O's columns)
                 uint32_t o[4];
                 asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
                              : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3])
@@ -576,14 +589,14 @@ __device__ __noinline__ void add_spoilt(const AttnParams& p, const Piece& pc, ui
     }
 }
 
-template <int D, bool Q8>
-__global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(const __grid_constant__ AttnParams p) {
-    using S = Shape<D, Q8>;
+template <int D, bool Q8, bool kOne>
+__global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_kernel(const __grid_constant__ AttnParams p) {
+    using S = Shape<D, Q8, kOne>;
     constexpr int NS = S::kStages, NR = S::kRaw > 0 ? S::kRaw : 1;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base_addr = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* const smem = smem_raw + (base_addr - smem_u32(smem_raw));
-    const uint32_t q_addr = base_addr, kv_addr = q_addr + 2 * S::kTileBytes, raw_addr = kv_addr + NS * S::kTileBytes;
+    const uint32_t q_addr = base_addr, kv_addr = q_addr + S::kQTiles * S::kTileBytes, raw_addr = kv_addr + NS * S::kTileBytes;
     uint8_t* const raw_ptr = smem + (raw_addr - base_addr);
     uint64_t* bars = (uint64_t*)(raw_ptr + S::kRaw * S::kRawBytes);
     const uint32_t bar0 = smem_u32(bars);
@@ -666,7 +679,7 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
             const volatile Piece& pc = pieces[n_piece % kPieces];
             const int T = pc.T;
             if (T == 0) break;
-            const bool two = pc.rows > kTile;
+            const bool two = !kOne && pc.rows > kTile;
             const int r = (two ? i * kTile : 0) + row_in_tile;  // row of the unit
             const bool live = r < pc.rows;
             if (two || i == 0) {
@@ -679,6 +692,9 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                     uint4 u = live ? __ldg(from + x) : make_uint4(0, 0, 0, 0);
                     u.x = (u.x ^ p.q_flip) & p.q_keep, u.y = (u.y ^ p.q_flip) & p.q_keep;
                     u.z = (u.z ^ p.q_flip) & p.q_keep, u.w = (u.w ^ p.q_flip) & p.q_keep;
+                    if (Q8)
+                        u = make_uint4(__byte_perm(u.x, u.y, 0x7632), __byte_perm(u.x, u.y, 0x5410), __byte_perm(u.z, u.w, 0x7632),
+                                       __byte_perm(u.z, u.w, 0x5410));
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (x >> 3) * S::kHalf +
                                                                                   ((((uint32_t)x & 7) ^ (row_in_tile & 7)) << 4)),
                                  "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w)
@@ -740,8 +756,11 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                 }
                 if (!(ok = wait_s())) break;
                 if (warp_live) {
-                    uint32_t u[kTile], w[32];
-                    const float mx = scores(tS, u, masked, sees);
+                    // (with fewer registers: the maximum first, then each half again)
+                    constexpr bool kAgain = S::kCols < kTile;
+                    uint32_t u[S::kCols], w[32];
+                    float mx = scores(tS, 0, u, masked, sees);
+                    if (kAgain) mx = fmaxf(mx, scores(tS, 64, u, masked, sees));
                     // (m = -inf: nothing seen so far, and what O holds is zero)
                     const bool grown = mx > m && !((mx - m) * c2 <= kMostGrowth);
                     if (__any_sync(0xFFFFFFFFu, grown)) {
@@ -751,9 +770,11 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                         m = now;
                     }
                     const float off = m > -INFINITY ? -m * c2 : 0.0f;
+                    if (kAgain) scores(tS, 0, u, masked, sees);
                     l += weigh(u, c2, off, w);
                     tmem_st_32x32(tS, w);
-                    l += weigh(u + 64, c2, off, w);
+                    if (kAgain) scores(tS, 64, u, masked, sees);
+                    l += weigh(u + S::kCols - 64, c2, off, w);
                     tmem_st_32x32(tS + 32, w);
                     tmem_wait_st();
                 }
@@ -781,8 +802,14 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
             const bool whole = pc.whole;
             const size_t slot = p.shared > 0 ? (size_t)pc.unit + blockIdx.x : 2 * (size_t)blockIdx.x + pc.head;
             const size_t out_row = ((size_t)b * p.rows + node) * p.q_heads + head;
-            const auto put = [&](int d0, const uint32_t (&u)[32], float inv) {
+            const auto put = [&](int d0, uint32_t (&u)[32], float inv) {
                 if (!live) return;
+                if (Q8)  // (odd two, even two)
+#pragma unroll
+                    for (int x = 0; x < 32; x += 4) {
+                        const uint32_t a = u[x], d = u[x + 1];
+                        u[x] = u[x + 2], u[x + 2] = u[x + 3], u[x + 1] = a, u[x + 3] = d;
+                    }
                 if (whole) {
                     uint4* to = (uint4*)(p.out + out_row * D + d0);
 #pragma unroll
@@ -822,13 +849,14 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                     put_sums(m, l);
                 }
             } else {
-                // the streams' halves are joined: the second one's goes through the shared memory of the row tile that is not there
-                float* const tmp = (float*)(smem + S::kTileBytes);  // [D / 2 columns][128 rows]
+                // the streams' halves are joined: the second one's goes through the shared memory of Q, which nobody reads any more
+                float* const tmp = (float*)smem;  // [D / 2 columns][128 rows]
                 float m1 = 0.0f, l1 = 0.0f, f0 = 1.0f, f1 = 0.0f, ms = 0.0f, ls = 0.0f, inv = 1.0f;
 #pragma unroll
                 for (int half = 0; half < 2 && ok; ++half) {
                     // maximum and sum of the second stream go ahead of its sums
                     if (half == 0) {
+                        if (!(ok = both())) break;  // (both are through with Q)
                         if (i == 1) {
                             tmp[row_in_tile] = m;
                             tmp[128 + row_in_tile] = l;
@@ -903,7 +931,7 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                 const volatile Piece& pc = pieces[n_piece % kPieces];
                 const int T = pc.T, h = pc.h, end = pc.end, first0 = pc.first;
                 if (T == 0) break;
-                const bool two = pc.rows > kTile;
+                const bool two = !kOne && pc.rows > kTile;
                 const int32_t* table = c.table + (pc.s == 0 ? 0 : (size_t)(pc.s - 1) * c.width);
                 const auto bring = [&](int t, bool is_v) {
                     const int first = first0 + t * kTile, upto = min(end, first + kTile);
@@ -1000,7 +1028,7 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                 const volatile Piece& pc = pieces[n_piece % kPieces];
                 const int T = pc.T;
                 if (T == 0) break;
-                const bool two = pc.rows > kTile;
+                const bool two = !kOne && pc.rows > kTile;
                 if (lane == 0) mbar_arrive(q_full);  // (with the rows' own arrivals: a piece begins when this warp is there too)
                 if (!(ok = wait_for(q_full, n_piece & 1, gave_up))) break;
                 const uint32_t a = uniform(q_lo + (two ? i : 0) * (S::kTileBytes / 16)), it0 = it;
@@ -1021,8 +1049,7 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                 // P V of a tile, then Q K of the next, which takes the weights' place
                 for (int t = t0; t < T; t += dt) {
                     const bool more = t + dt < T;
-                    ok = pass(it0 + v_entry(two, T, t)) && wait_kv(it) && (!more || wait_kv(it + 1)) &&
-                         wait_for(p_full0 + 8 * i, n_p & 1, gave_up) && my_turn(two);
+                    ok = pass(it0 + v_entry(two, T, t)) && wait_kv(it) && wait_for(p_full0 + 8 * i, n_p & 1, gave_up) && my_turn(two);
                     n_p += 1;
                     if (!ok) break;
                     tc_fence_after();
@@ -1030,6 +1057,13 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                     if (elect_one()) {
                         pv(t == t0, bv);
                         umma_commit(kv_empty(it % NS));
+                    }
+                    __syncwarp();
+                    if (more) {
+                        if (!(ok = wait_kv(it + 1))) break;
+                        tc_fence_after();
+                    }
+                    if (elect_one()) {
                         if (more) qk(a, bk);
                         if (two) mbar_arrive(turn0 + 8 * (1 - i));
                         umma_commit(s_full0 + 8 * i);
@@ -1043,10 +1077,12 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                 piece_done(n_piece);
             }
         } else if (Q8 && warp >= 12) {
-            // ---- e4m3 tiles to bf16 tiles in the 128-byte swizzle: sixteen numbers a thread and step
-            const int ct = tid - 384;  // 0 .. 127
-            constexpr int kPer = D / 16, kRowsStep = 128 / kPer, kSteps = kTile / kRowsStep;
+            // ---- e4m3 tiles to bf16 tiles in the 128-byte swizzle: sixteen numbers a thread and step.  Four numbers that stand side by side come out
+            // as the odd two and the even two, which takes fewer instructions; the rows of Q and the columns of O have the same order.
+            const int ct = tid - 384;
+            constexpr int kPer = D / 16, kRowsStep = (Q8 ? 32 * S::kConvWarps : 256) / kPer, kSteps = kTile / kRowsStep;
             const int col = ct % kPer, row0 = ct / kPer;
+            constexpr int kBatch = kSteps < 4 ? kSteps : 4;
             uint32_t it = 0;
             for (; (ok = next_piece(n_piece)); ++n_piece) {
                 const int T = ((const volatile Piece&)pieces[n_piece % kPieces]).T;
@@ -1058,23 +1094,49 @@ __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1) tree_attn_kernel(co
                     const uint8_t* raw = raw_ptr + rs * S::kRawBytes;
                     const uint32_t to = kv_addr + ks * S::kTileBytes + (col >> 2) * S::kHalf;
 #pragma unroll
-                    for (int x = 0; x < kSteps; ++x) {
-                        const int row = x * kRowsStep + row0;
-                        const uint4 y = *(const uint4*)(raw + row * D + col * 16);
-                        uint32_t f, more;
-                        e4m3_factors(raw[kTile * D + row], f, more);
-                        const uint2 a = e4m3x4_to_bf16(y.x, f, more), d = e4m3x4_to_bf16(y.y, f, more);
-                        const uint2 e = e4m3x4_to_bf16(y.z, f, more), h = e4m3x4_to_bf16(y.w, f, more);
-                        const uint4 lo = make_uint4(a.x, a.y, d.x, d.y), hi = make_uint4(e.x, e.y, h.x, h.y);
-                        // (the second half of a row's threads store their second piece first: eight threads then use all banks)
-                        const uint32_t chunk = (col & 3) * 2, at = to + row * 128, swap = D == 128 ? (uint32_t)col >> 2 : 0u;
-                        const uint4 w0 = swap ? hi : lo, w1 = swap ? lo : hi;
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((chunk + swap) ^ (row & 7)) << 4)), "r"(w0.x),
-                                     "r"(w0.y), "r"(w0.z), "r"(w0.w)
-                                     : "memory");
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((chunk + 1 - swap) ^ (row & 7)) << 4)), "r"(w1.x),
-                                     "r"(w1.y), "r"(w1.z), "r"(w1.w)
-                                     : "memory");
+                    for (int x0 = 0; x0 < kSteps; x0 += kBatch) {
+                        uint4 y[kBatch];
+                        uint32_t e[kBatch];
+#pragma unroll
+                        for (int x = 0; x < kBatch; ++x) {
+                            const int row = (x0 + x) * kRowsStep + row0;
+                            y[x] = *(const uint4*)(raw + row * D + col * 16);
+                            e[x] = raw[kTile * D + row];
+                        }
+                        // (scales above 2^7 take a second factor: rows of their kind are looked for once a batch)
+                        bool large = false;
+#pragma unroll
+                        for (int x = 0; x < kBatch; ++x) large = large || (e[x] > 134 && e[x] != 255);
+                        const auto put_rows = [&](auto two_factors) {
+#pragma unroll
+                            for (int x = 0; x < kBatch; ++x) {
+                                const int row = (x0 + x) * kRowsStep + row0;
+                                uint32_t f, more;
+                                if (decltype(two_factors)::value)
+                                    e4m3_factors(e[x], f, more);
+                                else
+                                    f = e[x] == 255 ? 0x7FC07FC0u : (e[x] + 120) * 0x00800080u, more = kOneBf16x2;
+                                uint32_t r[8];
+#pragma unroll
+                                for (int y4 = 0; y4 < 4; ++y4) {
+                                    const uint2 a = e4m3x4_to_bf16_odd_even(y4 == 0 ? y[x].x : y4 == 1 ? y[x].y : y4 == 2 ? y[x].z : y[x].w, f);
+                                    r[2 * y4] = decltype(two_factors)::value ? bf16x2_mul(a.x, more) : a.x;
+                                    r[2 * y4 + 1] = decltype(two_factors)::value ? bf16x2_mul(a.y, more) : a.y;
+                                }
+                                // (the second half of a row's threads store their second piece first: eight threads then use all banks)
+                                const uint32_t chunk = (col & 3) * 2, at = to + row * 128, swap = D == 128 ? (uint32_t)col >> 2 : 0u;
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((chunk + swap) ^ (row & 7)) << 4)),
+                                             "r"(swap ? r[4] : r[0]), "r"(swap ? r[5] : r[1]), "r"(swap ? r[6] : r[2]), "r"(swap ? r[7] : r[3])
+                                             : "memory");
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((chunk + 1 - swap) ^ (row & 7)) << 4)),
+                                             "r"(swap ? r[0] : r[4]), "r"(swap ? r[1] : r[5]), "r"(swap ? r[2] : r[6]), "r"(swap ? r[3] : r[7])
+                                             : "memory");
+                            }
+                        };
+                        if (__any_sync(0xFFFFFFFFu, large))
+                            put_rows(Yes());
+                        else
+                            put_rows(No());
                     }
                     fence_proxy_async();
                     __syncwarp();
@@ -1280,20 +1342,20 @@ AttnSizes attn_sizes(const graft_ctx* ctx, int batch, int kv_heads, int head_dim
     return z;
 }
 
-template <int D, bool Q8>
+template <int D, bool Q8, bool kOne>
 cudaError_t launch_attn(graft_ctx* ctx, const AttnParams& p, cudaStream_t st) {
-    using S = Shape<D, Q8>;
-    constexpr int kReady = 1 << ((D == 128) + 2 * Q8);
+    using S = Shape<D, Q8, kOne>;
+    constexpr int kReady = 1 << ((D == 128) + 2 * Q8 + 4 * kOne);
     cudaError_t e;
     if (!(ctx->attn_ready & kReady)) {
-        e = allow_smem((const void*)tree_attn_kernel<D, Q8>, S::kSmem);
+        e = allow_smem((const void*)tree_attn_kernel<D, Q8, kOne>, S::kSmem);
         if (e != cudaSuccess) return e;
         ctx->attn_ready |= kReady;
     }
     e = launch_pdl(attn_plan_kernel, dim3(p.batch), dim3(kPlanThreads), 0, st, p);
     if (e != cudaSuccess) return e;
     ctx->launches += 1;
-    e = launch_pdl(tree_attn_kernel<D, Q8>, dim3(p.ctas), dim3(S::kThreads), S::kSmem, st, p);
+    e = launch_pdl(tree_attn_kernel<D, Q8, kOne>, dim3(p.ctas), dim3(S::kThreads), S::kSmem, st, p);
     if (e != cudaSuccess) return e;
     ctx->launches += 1;
     const long long most = (long long)p.rows * p.group;  // rows of a sequence and key head
@@ -1353,8 +1415,12 @@ cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache
     p.part_ml = (float2*)(base + z.o_ml);
     p.part_o = (float*)(base + z.o_o);
     p.arrivals = ctx->w_attn_n;
-    return cache->head_dim == 128 ? (q8 ? launch_attn<128, true>(ctx, p, st) : launch_attn<128, false>(ctx, p, st))
-                                  : (q8 ? launch_attn<64, true>(ctx, p, st) : launch_attn<64, false>(ctx, p, st));
+    const bool one = shared == 0 && (long long)rows * p.group <= kTile;
+    const auto launch = cache->head_dim == 128 ? (q8 ? (one ? launch_attn<128, true, true> : launch_attn<128, true, false>)
+                                                     : (one ? launch_attn<128, false, true> : launch_attn<128, false, false>))
+                                               : (q8 ? (one ? launch_attn<64, true, true> : launch_attn<64, true, false>)
+                                                     : (one ? launch_attn<64, false, true> : launch_attn<64, false, false>));
+    return launch(ctx, p, st);
 }
 
 }  // namespace graft
