@@ -44,6 +44,15 @@ struct __align__(16) PlanStart {
     int s, h, mt, k;   // where a CTA begins: entry, key head, unit of the head, key tile (may be one behind the unit's last)
     int x, x1, pad[2]; // that tile's position in the line, and where the CTA's stretch ends
 };
+// A unit that is cut at the beginning of CTA c's stretch for the first time: what joining it takes.
+struct __align__(16) PlanJoin {
+    int rows;          // of the unit; 0: nothing to join here
+    int f, l;          // first and last CTA that may have tiles of it
+    int total, parts;  // as in PlanHead
+    int x0, w, kt;     // the unit in the line
+    int s, h, r0;      // entry, key head, first row of the unit among the entry's
+    int pad;
+};
 struct PlanHead {
     int total;  // length of the line
     int parts;  // CTAs that it is cut for
@@ -68,6 +77,7 @@ struct __align__(64) AttnParams {
     PlanHead* head;
     PlanSeq* seq;        // [batch + 1]
     PlanStart* start;    // [gridDim of the attention kernel]
+    PlanJoin* join;      // the same
     int ctas, min_cost;
     int* arrivals;       // zero between calls
     float* part_o;       // [slots][D / 4][256][4]
@@ -92,6 +102,25 @@ __device__ __forceinline__ int part_first(int total, int parts, int c) {
     const int q = total / parts;
     return c * q + (c * (total - q * parts) + parts - 1) / parts;
 }
+
+// A unit in the line: where its first tile stands, what a tile weighs, how many there are.
+struct UnitAt {
+    int x0, w, kt;
+};
+__device__ __forceinline__ UnitAt unit_at(const PlanSeq& q, int group, int h, int mt) {
+    const int R = q.n * group;
+    UnitAt u;
+    u.x0 = q.cost0 + h * head_cost(R, q.kt) + 2 * q.kt * mt;
+    u.w = unit_weight(R, mt);
+    u.kt = q.kt;
+    return u;
+}
+// first tile of the unit that is not ahead of CTA c's stretch
+__device__ __forceinline__ int first_tile(const UnitAt& u, int total, int parts, int c) {
+    const int d = part_first(total, parts, c) - u.x0;
+    return d <= 0 ? 0 : min((d + u.w - 1) >> (u.w - 1), u.kt);
+}
+__device__ __forceinline__ int cta_of(int x, int total, int parts) { return (int)((long long)x * parts / total); }
 
 constexpr int kPlanThreads = 256;
 constexpr int kPlanSeqs = 512;  // sequences whose positions are searched in shared memory; more are in global memory
@@ -191,6 +220,7 @@ __global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const __grid_co
         *p.arrivals = 0;
     }
     __syncthreads();
+    for (int i = parts + tid; i < p.ctas; i += kPlanThreads) p.join[i].rows = 0;
     // where every CTA begins
     for (int i = tid; i < parts; i += kPlanThreads) {
         PlanStart st = {};
@@ -217,6 +247,19 @@ __global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const __grid_co
         st.k = (rem + w - 1) / w;
         st.x += st.k * w - rem;
         p.start[i] = st;
+        PlanJoin j = {};
+        if (p.shared == 0 && st.k > 0 && st.k < q.kt) {  // (else the stretch begins with a unit)
+            const UnitAt un = unit_at(q, p.group, st.h, st.mt);
+            j.f = cta_of(un.x0, total, parts);
+            // the tiles ahead of this CTA's are those of the unit's first CTA, and this one has some
+            if (first_tile(un, total, parts, j.f + 1) == st.k && first_tile(un, total, parts, i + 1) > st.k)
+                j.rows = min(kUnitRows, R - st.mt * kUnitRows);
+            j.l = cta_of(un.x0 + (un.kt - 1) * un.w, total, parts);
+            j.total = total, j.parts = parts;
+            j.x0 = un.x0, j.w = un.w, j.kt = un.kt;
+            j.s = lo, j.h = st.h, j.r0 = st.mt * kUnitRows;
+        }
+        p.join[i] = j;
     }
 }
 
@@ -683,21 +726,30 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
             const int r = (two ? i * kTile : 0) + row_in_tile;  // row of the unit
             const bool live = r < pc.rows;
             if (two || i == 0) {
-                const uint32_t to = q_addr + i * S::kTileBytes + row_in_tile * 128;
+                // a row's pieces side by side in a warp's load; where a row stands is worked out by the lane that has it
                 int b = 0, node = 0, g = 0;
                 if (live) row_of(p, pc.s, pc.r0 + r, b, node, g);
-                const uint4* from = (const uint4*)(p.q + 2 * (((long long)b * p.rows + node) * p.q_stride + (long long)(pc.h * p.group + g) * D));
+                const long long mine = live ? ((long long)b * p.rows + node) * p.q_stride + (long long)(pc.h * p.group + g) * D : -1;
+                constexpr int kPer = D / 8, kRows = 32 / kPer;  // lanes a row, rows a load
+                const int x = lane % kPer;
+                uint4 u[32 / kRows];
 #pragma unroll
-                for (int x = 0; x < D / 8; ++x) {
-                    uint4 u = live ? __ldg(from + x) : make_uint4(0, 0, 0, 0);
-                    u.x = (u.x ^ p.q_flip) & p.q_keep, u.y = (u.y ^ p.q_flip) & p.q_keep;
-                    u.z = (u.z ^ p.q_flip) & p.q_keep, u.w = (u.w ^ p.q_flip) & p.q_keep;
+                for (int y = 0; y < 32 / kRows; ++y) {
+                    const long long at = __shfl_sync(0xFFFFFFFFu, mine, y * kRows + lane / kPer);
+                    u[y] = at >= 0 ? __ldg((const uint4*)(p.q + 2 * at) + x) : make_uint4(0, 0, 0, 0);
+                }
+#pragma unroll
+                for (int y = 0; y < 32 / kRows; ++y) {
+                    uint4 v = u[y];
+                    v.x = (v.x ^ p.q_flip) & p.q_keep, v.y = (v.y ^ p.q_flip) & p.q_keep;
+                    v.z = (v.z ^ p.q_flip) & p.q_keep, v.w = (v.w ^ p.q_flip) & p.q_keep;
                     if (Q8)
-                        u = make_uint4(__byte_perm(u.x, u.y, 0x7632), __byte_perm(u.x, u.y, 0x5410), __byte_perm(u.z, u.w, 0x7632),
-                                       __byte_perm(u.z, u.w, 0x5410));
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (x >> 3) * S::kHalf +
-                                                                                  ((((uint32_t)x & 7) ^ (row_in_tile & 7)) << 4)),
-                                 "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w)
+                        v = make_uint4(__byte_perm(v.x, v.y, 0x7632), __byte_perm(v.x, v.y, 0x5410), __byte_perm(v.z, v.w, 0x7632),
+                                       __byte_perm(v.z, v.w, 0x5410));
+                    const int row = (warp & 3) * 32 + y * kRows + lane / kPer;
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_addr + i * S::kTileBytes + row * 128 + (x >> 3) * S::kHalf +
+                                                                                  ((((uint32_t)x & 7) ^ (row & 7)) << 4)),
+                                 "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
                                  : "memory");
                 }
                 fence_proxy_async();
@@ -1161,25 +1213,6 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
 }
 
 // ---- joining the pieces ----------------------------------------------------------------------------------------------
-// A unit in the line: where its first tile stands, what a tile weighs, how many there are.
-struct UnitAt {
-    int x0, w, kt;
-};
-__device__ __forceinline__ UnitAt unit_at(const PlanSeq& q, int group, int h, int mt) {
-    const int R = q.n * group;
-    UnitAt u;
-    u.x0 = q.cost0 + h * head_cost(R, q.kt) + 2 * q.kt * mt;
-    u.w = unit_weight(R, mt);
-    u.kt = q.kt;
-    return u;
-}
-// first tile of the unit that is not ahead of CTA c's stretch
-__device__ __forceinline__ int first_tile(const UnitAt& u, int total, int parts, int c) {
-    const int d = part_first(total, parts, c) - u.x0;
-    return d <= 0 ? 0 : min((d + u.w - 1) >> (u.w - 1), u.kt);
-}
-__device__ __forceinline__ int cta_of(int x, int total, int parts) { return (int)((long long)x * parts / total); }
-
 constexpr int kJoinThreads = 256;
 constexpr int kJoinRows = 32;
 constexpr int kJoinMost = 160;  // pieces of a block's rows: no more than CTAs and units (three at most)
@@ -1189,48 +1222,61 @@ struct JoinPiece {
 };
 struct JoinList {
     JoinPiece piece[kJoinMost];
-    float2 ml[kJoinMost][kJoinRows];
     int n;
 };
 
-// The pieces of a unit that have tiles, to the list (one thread); first_slot + d is the slot of CTA d's piece, but for `ahead` >= 0:
-// that CTA's is the odd one of its two.
-__device__ __forceinline__ void list_unit(JoinList& j, const UnitAt& u, int total, int parts, int unit, int shift, int lo, int hi) {
-    const int f = cta_of(u.x0, total, parts), l = cta_of(u.x0 + (u.kt - 1) * u.w, total, parts);
-    for (int d = f, k = 0; d <= l; ++d) {
-        const int next = first_tile(u, total, parts, d + 1);
-        if (next > k && j.n < kJoinMost) j.piece[j.n++] = {unit >= 0 ? unit + d : d == f ? 2 * d + 1 : 2 * d, shift, lo, hi};
-        k = next;
+// The pieces of a unit, to the list; a warp calls it, a lane a CTA (of f .. l) that may have tiles of it.  Behind a shared prefix (unit >= 0) a piece's
+// slot is the unit's number and the CTA's added up; else the unit's first CTA has it in the odd one of its two slots.
+__device__ __forceinline__ void list_unit(JoinList& j, const UnitAt& u, int f, int l, int total, int parts, int unit, int shift, int lo, int hi) {
+    const int lane = lane_id();
+    for (int d0 = f; d0 <= l; d0 += 32) {
+        const int d = d0 + lane;
+        const bool has = d <= l && first_tile(u, total, parts, d + 1) > first_tile(u, total, parts, d);
+        const unsigned all = __ballot_sync(0xFFFFFFFFu, has);
+        const int n = j.n, at = n + __popc(all & ((1u << lane) - 1));
+        __syncwarp();
+        if (has && at < kJoinMost) j.piece[at] = {unit >= 0 ? unit + d : d == f ? 2 * d + 1 : 2 * d, shift, lo, hi};
+        if (lane == 0) j.n = min(n + __popc(all), kJoinMost);
+        __syncwarp();
     }
 }
 
-// 32 rows of a unit from the pieces on the list: a lane a row, a warp some of the columns.  The weight of a piece's row is 2^(its maximum
-// less the largest), and pieces are added in their order along the line, so that results repeat.
+// 32 rows of a unit from the pieces on the list: a lane a row, a warp some of the columns.  Pieces are added in their order along the line, results repeat; four are on their way at a time.
 template <int D>
-__device__ __forceinline__ void join_rows(const AttnParams& p, JoinList& j, bool live, size_t out_row) {
+__device__ __forceinline__ void join_rows(const AttnParams& p, const JoinList& j, bool live, size_t out_row) {
     constexpr int kWarps = kJoinThreads / 32, kQuads = D / 4 / kWarps;  // groups of four columns a warp
     const int lane = lane_id(), warp = threadIdx.x >> 5, n = j.n;
-    for (int i = warp; i < n; i += kWarps) {
-        const JoinPiece& a = j.piece[i];
-        j.ml[i][lane] = lane >= a.lo && lane < a.hi ? __ldcg(p.part_ml + (size_t)a.slot * kUnitRows + lane + a.shift) : make_float2(-INFINITY, 0.0f);
-    }
-    __syncthreads();
     float m = -INFINITY, l = 0.0f;
-    for (int i = 0; i < n; ++i) m = fmaxf(m, j.ml[i][lane].x);
-    const float ref = m > -INFINITY ? m : 0.0f;
     float o[4 * kQuads] = {};
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-        const JoinPiece& a = j.piece[i];
-        const float2 ml = j.ml[i][lane];
-        if (!(lane >= a.lo && lane < a.hi)) continue;
-        const float f = ex2_approx(ml.x - ref);
-        l += f * ml.y;
-        const float4* from = (const float4*)p.part_o + ((size_t)a.slot * (D / 4) + warp * kQuads) * kUnitRows + lane + a.shift;
+    constexpr int kAhead = 4;
+    for (int i0 = 0; i0 < n; i0 += kAhead) {
+        float2 ml[kAhead];
+        float4 v[kAhead][kQuads];
 #pragma unroll
-        for (int x = 0; x < kQuads; ++x) {
-            const float4 v = __ldcg(from + x * kUnitRows);
-            o[4 * x] += f * v.x, o[4 * x + 1] += f * v.y, o[4 * x + 2] += f * v.z, o[4 * x + 3] += f * v.w;
+        for (int i = 0; i < kAhead; ++i) {  // (rows that a piece does not have, and pieces behind the last, weigh nothing)
+            const JoinPiece a = j.piece[min(i0 + i, n - 1)];
+            const bool mine = i0 + i < n && lane >= a.lo && lane < a.hi;
+            const int r = mine ? lane + a.shift : 0;
+            const float2 x = __ldcg(p.part_ml + (size_t)a.slot * kUnitRows + r);
+            ml[i] = mine ? x : make_float2(-INFINITY, 0.0f);
+            const float4* from = (const float4*)p.part_o + ((size_t)a.slot * (D / 4) + warp * kQuads) * kUnitRows + r;
+#pragma unroll
+            for (int y = 0; y < kQuads; ++y) {
+                const float4 z = __ldcg(from + y * kUnitRows);
+                v[i][y] = mine ? z : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const float now = fmaxf(m, ml[i].x), f0 = m > -INFINITY ? ex2_approx(m - now) : 0.0f;
+            const float f1 = ml[i].x > -INFINITY ? ex2_approx(ml[i].x - now) : 0.0f;
+            m = now;
+            l = l * f0 + ml[i].y * f1;
+#pragma unroll
+            for (int y = 0; y < kQuads; ++y) {
+                o[4 * y] = o[4 * y] * f0 + f1 * v[i][y].x, o[4 * y + 1] = o[4 * y + 1] * f0 + f1 * v[i][y].y;
+                o[4 * y + 2] = o[4 * y + 2] * f0 + f1 * v[i][y].z, o[4 * y + 3] = o[4 * y + 3] * f0 + f1 * v[i][y].w;
+            }
         }
     }
     if (!live) return;
@@ -1248,25 +1294,21 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_co
     pdl_launch_dependents();
     pdl_wait();
     __shared__ JoinList j;
-    const int c = blockIdx.y + 1, total = __ldcg(&p.head->total), parts = __ldcg(&p.head->parts);
-    if (c >= parts) return;
-    const int4 st = __ldcg((const int4*)(p.start + c));
-    PlanSeq q;
-    load_seq(q, p.seq + st.x);
-    if (st.w == 0 || st.w >= q.kt) return;  // the stretch begins with a unit
-    const int R = q.n * p.group, r0 = st.z * kUnitRows + blockIdx.x * kJoinRows;
-    if ((int)blockIdx.x * kJoinRows >= min(kUnitRows, R - st.z * kUnitRows)) return;
-    const UnitAt u = unit_at(q, p.group, st.y, st.z);
-    // the tiles ahead of this CTA's are those of the unit's first CTA, and this one has some
-    if (first_tile(u, total, parts, cta_of(u.x0, total, parts) + 1) != st.w || first_tile(u, total, parts, c + 1) <= st.w) return;
-    if (threadIdx.x == 0) {
-        j.n = 0;
-        list_unit(j, u, total, parts, -1, blockIdx.x * kJoinRows, 0, kJoinRows);
+    const int4* from = (const int4*)(p.join + blockIdx.y + 1);
+    PlanJoin q;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) ((int4*)&q)[i] = __ldcg(from + i);
+    const int r0 = blockIdx.x * kJoinRows;
+    if (r0 >= q.rows) return;
+    if (threadIdx.x < 32) {
+        if (threadIdx.x == 0) j.n = 0;
+        __syncwarp();
+        list_unit(j, {q.x0, q.w, q.kt}, q.f, q.l, q.total, q.parts, -1, r0, 0, kJoinRows);
     }
     __syncthreads();
-    const int r = r0 + lane_id(), node = r / p.group;
-    const bool live = r < R;
-    join_rows<D>(p, j, live, ((size_t)(st.x - 1) * p.rows + node) * p.q_heads + st.y * p.group + (r - node * p.group));
+    const int r = q.r0 + r0 + lane_id(), node = r / p.group;
+    const bool live = r0 + lane_id() < q.rows;
+    join_rows<D>(p, j, live, ((size_t)(q.s - 1) * p.rows + node) * p.q_heads + q.h * p.group + (r - node * p.group));
 }
 
 // Behind a shared prefix every row has pieces of two units; 32 rows of a sequence may lie in two units of the prefix.
@@ -1281,15 +1323,21 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_shared_kernel(const __
     load_seq(q, p.seq + b + 1);
     const int total = __ldcg(&p.head->total), parts = __ldcg(&p.head->parts), R = q.n * p.group;
     if (r0 >= R) return;
-    if (threadIdx.x == 0) {
-        j.n = 0;
+    if (threadIdx.x < 32) {
+        if (threadIdx.x == 0) j.n = 0;
+        __syncwarp();
         const int Ra = all.n * p.group, ra = q.node0 * p.group + r0, mt = ra / kUnitRows, upto = (mt + 1) * kUnitRows - ra;
         const int ua = all.unit0 + h * row_tiles2(Ra);
-        list_unit(j, unit_at(all, p.group, h, mt), total, parts, ua + mt, ra - mt * kUnitRows, 0, min(upto, kJoinRows));
-        if (upto < kJoinRows && (mt + 1) * kUnitRows < Ra)
-            list_unit(j, unit_at(all, p.group, h, mt + 1), total, parts, ua + mt + 1, -upto, upto, kJoinRows);
+        UnitAt u = unit_at(all, p.group, h, mt);
+        const auto cta = [&](int k) { return cta_of(u.x0 + k * u.w, total, parts); };
+        list_unit(j, u, cta(0), cta(u.kt - 1), total, parts, ua + mt, ra - mt * kUnitRows, 0, min(upto, kJoinRows));
+        if (upto < kJoinRows && (mt + 1) * kUnitRows < Ra) {
+            u = unit_at(all, p.group, h, mt + 1);
+            list_unit(j, u, cta(0), cta(u.kt - 1), total, parts, ua + mt + 1, -upto, upto, kJoinRows);
+        }
         const int mo = r0 / kUnitRows;
-        list_unit(j, unit_at(q, p.group, h, mo), total, parts, q.unit0 + h * row_tiles2(R) + mo, r0 - mo * kUnitRows, 0, kJoinRows);
+        u = unit_at(q, p.group, h, mo);
+        list_unit(j, u, cta(0), cta(u.kt - 1), total, parts, q.unit0 + h * row_tiles2(R) + mo, r0 - mo * kUnitRows, 0, kJoinRows);
     }
     __syncthreads();
     const int r = r0 + lane_id(), node = r / p.group;
@@ -1322,7 +1370,7 @@ bool encode_map(CUtensorMap* map, const void* base, bool q8, int D, uint64_t row
 }
 
 struct AttnSizes {
-    size_t o_seq, o_start, o_ml, o_o, total;
+    size_t o_seq, o_start, o_join, o_ml, o_o, total;
 };
 AttnSizes attn_sizes(const graft_ctx* ctx, int batch, int kv_heads, int head_dim, int group, int rows, int shared) {
     const auto units = [&](long long nodes) { return (size_t)kv_heads * (size_t)((nodes * group + kUnitRows - 1) / kUnitRows); };
@@ -1336,6 +1384,7 @@ AttnSizes attn_sizes(const graft_ctx* ctx, int batch, int kv_heads, int head_dim
     };
     z.o_seq = take((size_t)(batch + 1) * sizeof(PlanSeq));
     z.o_start = take((size_t)ctx->num_sms * sizeof(PlanStart));
+    z.o_join = take((size_t)(ctx->num_sms + 1) * sizeof(PlanJoin));
     z.o_ml = take(slots * kUnitRows * sizeof(float2));
     z.o_o = take(slots * kUnitRows * head_dim * sizeof(float));
     z.total = off;
@@ -1406,12 +1455,13 @@ cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache
     p.words = ctx->mask_words;
     p.batch = batch;
     p.ctas = ctx->num_sms;
-    p.min_cost = 2;
+    p.min_cost = 1;
     const AttnSizes z = attn_sizes(ctx, batch, cache->kv_heads, cache->head_dim, p.group, rows, shared);
     uint8_t* base = (uint8_t*)scratch;
     p.head = (PlanHead*)base;
     p.seq = (PlanSeq*)(base + z.o_seq);
     p.start = (PlanStart*)(base + z.o_start);
+    p.join = (PlanJoin*)(base + z.o_join);
     p.part_ml = (float2*)(base + z.o_ml);
     p.part_o = (float*)(base + z.o_o);
     p.arrivals = ctx->w_attn_n;
