@@ -36,13 +36,14 @@ struct __align__(16) PlanSeq {
     int base;    // slots before the first row's (shared prefix: its length)
     int node0;   // nodes of the sequences before
     int unit0;   // units before
-    int cost0;   // key tiles before, each times its row tiles
+    int cost0;   // position in the line: key tiles before, each times its row tiles
     int kt;      // key tiles
     int pad[2];
 };
 struct __align__(16) PlanStart {
-    int s, h, mt, k;   // where a CTA begins: entry, key head, unit of the head, key tile (may be one behind the unit's last)
-    int x, x1, pad[2]; // that tile's position in the line, and where the CTA's stretch ends
+    int s, h, mt, k;         // where a CTA begins: entry, key head, unit of the head, key tile (may be one behind the unit's last)
+    int x, x1, chunk, pad;   // that tile's position in the line, and where the CTA's stretch ends
+    PlanSeq q;               // the entry
 };
 // A unit that is cut at the beginning of CTA c's stretch for the first time: what joining it takes.
 struct __align__(16) PlanJoin {
@@ -56,6 +57,7 @@ struct __align__(16) PlanJoin {
 struct PlanHead {
     int total;  // length of the line
     int parts;  // CTAs that it is cut for
+    int chunk;  // units begin at multiples of it
 };
 
 struct __align__(64) AttnParams {
@@ -78,10 +80,11 @@ struct __align__(64) AttnParams {
     PlanSeq* seq;        // [batch + 1]
     PlanStart* start;    // [gridDim of the attention kernel]
     PlanJoin* join;      // the same
-    int ctas, min_cost;
+    int ctas;
+    int part_rows;       // rows that a piece has room for
     int* arrivals;       // zero between calls
-    float* part_o;       // [slots][D / 4][256][4]
-    float2* part_ml;     // [slots][256]: maximum (log2 domain), sum
+    float* part_o;       // [slots][D / 4][part_rows][4]
+    float2* part_ml;     // [slots][part_rows]: maximum (log2 domain), sum
 };
 
 __device__ __forceinline__ void load_seq(PlanSeq& q, const PlanSeq* from) {
@@ -92,9 +95,11 @@ __device__ __forceinline__ void load_seq(PlanSeq& q, const PlanSeq* from) {
 // ---- the plan ------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ int row_tiles2(int R) { return (R + kUnitRows - 1) / kUnitRows; }  // units of R rows
 __device__ __forceinline__ int unit_weight(int R, int mt) { return R - mt * kUnitRows > kTile ? 2 : 1; }
-__device__ __forceinline__ int head_cost(int R, int kt) {
+// a unit's length in the line
+__device__ __forceinline__ int padded(int cost, int chunk) { return chunk == 1 ? cost : (cost + chunk - 1) / chunk * chunk; }
+__device__ __forceinline__ int head_cost(int R, int kt, int chunk) {
     const int u = row_tiles2(R);
-    return u == 0 ? 0 : kt * (2 * (u - 1) + unit_weight(R, u - 1));
+    return u == 0 ? 0 : (u - 1) * padded(2 * kt, chunk) + padded(kt * unit_weight(R, u - 1), chunk);
 }
 
 // first position of CTA c's stretch: ceil(c total / parts)
@@ -107,10 +112,10 @@ __device__ __forceinline__ int part_first(int total, int parts, int c) {
 struct UnitAt {
     int x0, w, kt;
 };
-__device__ __forceinline__ UnitAt unit_at(const PlanSeq& q, int group, int h, int mt) {
+__device__ __forceinline__ UnitAt unit_at(const PlanSeq& q, int group, int h, int mt, int chunk) {
     const int R = q.n * group;
     UnitAt u;
-    u.x0 = q.cost0 + h * head_cost(R, q.kt) + 2 * q.kt * mt;
+    u.x0 = q.cost0 + h * head_cost(R, q.kt, chunk) + padded(2 * q.kt, chunk) * mt;
     u.w = unit_weight(R, mt);
     u.kt = q.kt;
     return u;
@@ -123,14 +128,48 @@ __device__ __forceinline__ int first_tile(const UnitAt& u, int total, int parts,
 __device__ __forceinline__ int cta_of(int x, int total, int parts) { return (int)((long long)x * parts / total); }
 
 constexpr int kPlanThreads = 256;
-constexpr int kPlanSeqs = 512;  // sequences whose positions are searched in shared memory; more are in global memory
+constexpr int kPlanSeqs = 512;  // sequences whose entries are held in shared memory; more are read from global memory
+
+// Sums of three numbers over the block, and over the threads before this one; by_warp: every warp by itself.
+struct Sums {
+    int before[3], all[3];
+};
+__device__ __forceinline__ Sums block_sums(int (*scratch)[kPlanThreads / 32], bool by_warp, int a, int b, int c) {
+    constexpr int kWarps = kPlanThreads / 32;
+    const int lane = lane_id(), warp = threadIdx.x >> 5, mine[3] = {a, b, c};
+    Sums s;
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+        int x = mine[q];
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+            if (lane >= o) x += y;
+        }
+        s.before[q] = x - mine[q];
+        s.all[q] = __shfl_sync(0xFFFFFFFFu, x, 31);
+        if (!by_warp && lane == 31) scratch[q][warp] = x;
+    }
+    if (by_warp) return s;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+        s.all[q] = 0;
+        for (int w = 0; w < kWarps; ++w) {
+            if (w == warp) s.before[q] += s.all[q];
+            s.all[q] += scratch[q][w];
+        }
+    }
+    __syncthreads();
+    return s;
+}
 __global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const __grid_constant__ AttnParams p) {
     pdl_launch_dependents();
     pdl_wait();
     constexpr int kWarps = kPlanThreads / 32;
     const CacheView& c = p.c;
     __shared__ int fine[kWarps], last;
-    __shared__ int sums[3][kWarps], at[kPlanSeqs + 1];
+    __shared__ int scratch[3][kWarps];
+    __shared__ PlanSeq entries[kPlanSeqs + 1];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int n0 = p.count[b], base0 = p.prefix_len[b] - 1;
     {
@@ -156,109 +195,117 @@ __global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const __grid_co
         __syncthreads();
         if (!last) return;
     }
-    // the last block adds up: nodes, units, cost
+    // the last block: what sequence i has
     const int Hk = c.kv_heads;
-    int run[3] = {0, 0, 0};
-    for (int b0 = 0; b0 < p.batch; b0 += kPlanThreads) {
-        const int i = b0 + tid;
-        int n = 0, base = 0;
+    const bool held = p.batch <= kPlanSeqs, small = p.batch <= 32;  // (few sequences: every warp goes through them by itself)
+    const int me = small ? lane : tid;
+    const auto of = [&](int i, int& n, int& base, int& kt, int& R) {
+        n = base = 0;
         if (gridDim.x == 1) {
             if (i == 0) n = n0, base = base0;
         } else if (i < p.batch) {
             const int2 v = __ldcg((const int2*)&p.seq[i + 1]);
             n = v.x, base = v.y;
         }
-        const int kt = n > 0 ? (base + n - p.shared + kTile - 1) / kTile : 0;
-        const int R = n * p.group;
-        const int mine[3] = {n, Hk * row_tiles2(R), Hk * head_cost(R, kt)};
-        int upto[3];
-#pragma unroll
-        for (int q = 0; q < 3; ++q) {
-            int x = mine[q];
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xFFFFFFFFu, x, o);
-                if (lane >= o) x += y;
-            }
-            upto[q] = x;
-            if (lane == 31) sums[q][warp] = x;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int q = 0; q < 3; ++q) {
-            int before = run[q];
-            for (int w = 0; w < kWarps; ++w) {
-                if (w < warp) before += sums[q][w];
-                run[q] += sums[q][w];
-            }
-            upto[q] += before - mine[q];
-        }
-        if (i < p.batch) {
-            PlanSeq s = {n, base, upto[0], upto[1], upto[2], kt, {0, 0}};
-            p.seq[i + 1] = s;
-            if (i < kPlanSeqs) at[i + 1] = upto[2];
-        }
-        __syncthreads();
+        kt = n > 0 ? (base + n - p.shared + kTile - 1) / kTile : 0;
+        R = n * p.group;
+    };
+    int nodes = 0, total = 0, chunk = 1;
+    for (int b0 = 0; b0 < p.batch; b0 += kPlanThreads) {
+        int n, base, kt, R;
+        of(b0 + me, n, base, kt, R);
+        const Sums s = block_sums(scratch, small, n, Hk * head_cost(R, kt, 1), 0);
+        nodes += s.all[0], total += s.all[1];
     }
-    // the shared prefix goes first
-    const int nodes = run[0], Rs = p.shared > 0 ? nodes * p.group : 0, kts = (p.shared + kTile - 1) / kTile;
-    const int us = Hk * row_tiles2(Rs), cs = Hk * head_cost(Rs, kts);
-    if (us > 0)
-        for (int i = tid; i < p.batch; i += kPlanThreads) {
-            p.seq[i + 1].unit0 += us;
-            p.seq[i + 1].cost0 += cs;
-            if (i < kPlanSeqs) at[i + 1] += cs;
+    const int Rs = p.shared > 0 ? nodes * p.group : 0, kts = (p.shared + kTile - 1) / kTile;
+    total += Hk * head_cost(Rs, kts, 1);
+    // A CTA's share of the line may begin and end inside of units; every piece of one costs some microseconds beside its tiles.  Where shares
+    // are short, units are given lengths of whole shares instead, so that a CTA has one piece, if shares two double tiles longer than equal ones
+    // are enough for it.
+    const int share = (total + p.ctas - 1) / p.ctas;
+    if (share > 1 && share <= 64 && p.batch <= kPlanThreads) {
+        int n, base, kt, R;
+        of(me, n, base, kt, R);
+        for (int c2 = (share + 1) & ~1; c2 <= share + 4; c2 += 2) {
+            const Sums s = block_sums(scratch, small, Hk * (head_cost(R, kt, c2) / c2), 0, 0);
+            if (s.all[0] + Hk * (head_cost(Rs, kts, c2) / c2) <= p.ctas) {
+                chunk = c2;
+                break;
+            }
         }
-    const int total = run[2] + cs, parts = min(p.ctas, (total + p.min_cost - 1) / p.min_cost);
+    }
+    // (the shared prefix goes first)
+    int units = Hk * row_tiles2(Rs), cost = Hk * head_cost(Rs, kts, chunk), seen = 0;
     if (tid == 0) {
-        PlanSeq s = {};
-        s.n = Rs > 0 ? nodes : 0;
-        s.base = p.shared;
-        s.kt = kts;
+        PlanSeq s = {Rs > 0 ? nodes : 0, p.shared, 0, 0, 0, kts, {0, 0}};
         p.seq[0] = s;
+        entries[0] = s;
+    }
+    for (int b0 = 0; b0 < p.batch; b0 += kPlanThreads) {
+        const int i = b0 + me;
+        int n, base, kt, R;
+        of(i, n, base, kt, R);
+        const Sums s = block_sums(scratch, small, n, Hk * row_tiles2(R), Hk * head_cost(R, kt, chunk));
+        if (i < p.batch && (!small || warp == 0)) {
+            PlanSeq q = {n, base, seen + s.before[0], units + s.before[1], cost + s.before[2], kt, {0, 0}};
+            p.seq[i + 1] = q;
+            if (held) entries[i + 1] = q;
+        }
+        seen += s.all[0], units += s.all[1], cost += s.all[2];
+    }
+    total = cost;
+    const int parts = chunk > 1 ? total / chunk : min(p.ctas, total);
+    if (tid == 0) {
         p.head->total = total;
         p.head->parts = parts;
+        p.head->chunk = chunk;
         *p.arrivals = 0;
     }
     __syncthreads();
-    for (int i = parts + tid; i < p.ctas; i += kPlanThreads) p.join[i].rows = 0;
     // where every CTA begins
-    for (int i = tid; i < parts; i += kPlanThreads) {
+    for (int i = tid; i < p.ctas; i += kPlanThreads) {
         PlanStart st = {};
-        st.x = part_first(total, parts, i);
-        st.x1 = part_first(total, parts, i + 1);
-        int lo = 0, hi = p.batch;  // the last entry whose cost0 is not above x: one that has any, as the ones behind it begin above x
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if ((p.batch <= kPlanSeqs ? at[mid] : __ldcg(&p.seq[mid].cost0)) <= st.x)
-                lo = mid;
-            else
-                hi = mid - 1;
-        }
-        PlanSeq q;
-        load_seq(q, p.seq + lo);
-        const int R = q.n * p.group, hc = head_cost(R, q.kt), local = st.x - q.cost0;
-        st.s = lo;
-        st.h = local / hc;
-        int rem = local - st.h * hc;
-        const int u = row_tiles2(R);
-        st.mt = min(rem / (2 * q.kt), u - 1);
-        rem -= 2 * q.kt * st.mt;
-        const int w = unit_weight(R, st.mt);
-        st.k = (rem + w - 1) / w;
-        st.x += st.k * w - rem;
-        p.start[i] = st;
         PlanJoin j = {};
-        if (p.shared == 0 && st.k > 0 && st.k < q.kt) {  // (else the stretch begins with a unit)
-            const UnitAt un = unit_at(q, p.group, st.h, st.mt);
-            j.f = cta_of(un.x0, total, parts);
-            // the tiles ahead of this CTA's are those of the unit's first CTA, and this one has some
-            if (first_tile(un, total, parts, j.f + 1) == st.k && first_tile(un, total, parts, i + 1) > st.k)
-                j.rows = min(kUnitRows, R - st.mt * kUnitRows);
-            j.l = cta_of(un.x0 + (un.kt - 1) * un.w, total, parts);
-            j.total = total, j.parts = parts;
-            j.x0 = un.x0, j.w = un.w, j.kt = un.kt;
-            j.s = lo, j.h = st.h, j.r0 = st.mt * kUnitRows;
+        if (i < parts) {
+            st.x = part_first(total, parts, i);
+            st.x1 = part_first(total, parts, i + 1);
+            st.chunk = chunk;
+            int lo = 0, hi = p.batch;  // the last entry whose position is not above x: one that has any, as the ones behind it begin above x
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if ((held ? entries[mid].cost0 : __ldcg(&p.seq[mid].cost0)) <= st.x)
+                    lo = mid;
+                else
+                    hi = mid - 1;
+            }
+            PlanSeq q;
+            if (held)
+                q = entries[lo];
+            else
+                load_seq(q, p.seq + lo);
+            const int R = q.n * p.group, hc = head_cost(R, q.kt, chunk), local = st.x - q.cost0, full = padded(2 * q.kt, chunk);
+            st.s = lo;
+            st.h = local / hc;
+            int rem = local - st.h * hc;
+            st.mt = min(rem / full, row_tiles2(R) - 1);
+            rem -= full * st.mt;
+            const int w = unit_weight(R, st.mt);
+            st.k = (rem + w - 1) / w;
+            st.x += st.k * w - rem;
+            st.q = q;
+            if (p.shared == 0 && st.k > 0 && st.k < q.kt) {  // (else the stretch begins with a unit)
+                const UnitAt un = unit_at(q, p.group, st.h, st.mt, chunk);
+                j.f = cta_of(un.x0, total, parts);
+                // the tiles ahead of this CTA's are those of the unit's first CTA, and this one has some
+                if (first_tile(un, total, parts, j.f + 1) == st.k && first_tile(un, total, parts, i + 1) > st.k)
+                    j.rows = min(kUnitRows, R - st.mt * kUnitRows);
+                j.l = cta_of(un.x0 + (un.kt - 1) * un.w, total, parts);
+                j.total = total, j.parts = parts;
+                j.x0 = un.x0, j.w = un.w, j.kt = un.kt;
+                j.s = lo, j.h = st.h, j.r0 = st.mt * kUnitRows;
+            }
         }
+        p.start[i] = st;
         p.join[i] = j;
     }
 }
@@ -282,7 +329,7 @@ struct Piece {
 struct Walk {
     const PlanSeq* seq;
     int last_s, Hk, group, shared;
-    int x, x1;
+    int x, x1, chunk;
     int s, h, mt, k;
     PlanSeq q;
     __device__ __forceinline__ void begin(const AttnParams& p, int cta) {
@@ -291,15 +338,18 @@ struct Walk {
         Hk = p.c.kv_heads;
         group = p.group;
         shared = p.shared;
-        x = x1 = 0;
-        if (cta >= __ldcg(&p.head->parts)) return;
-        const int4 st = __ldcg((const int4*)(p.start + cta)), en = __ldcg((const int4*)(p.start + cta) + 1);
-        s = st.x, h = st.y, mt = st.z, k = st.w, x = en.x, x1 = en.y;
-        load_seq(q, seq + s);
+        const PlanStart* from = p.start + cta;
+        const int4 st = __ldcg((const int4*)from), en = __ldcg((const int4*)from + 1);
+        load_seq(q, &from->q);
+        s = st.x, h = st.y, mt = st.z, k = st.w, x = en.x, x1 = en.y, chunk = en.z;
     }
     __device__ __forceinline__ bool next(Piece& pc) {
         if (x >= x1) return false;
         int R = q.n * group;
+        if (k >= q.kt) {
+            x = padded(x, chunk);
+            if (x >= x1) return false;
+        }
         while (q.n == 0 || k >= q.kt) {  // the next unit
             k = 0;
             mt += 1;
@@ -352,26 +402,23 @@ __device__ __forceinline__ void row_of(const AttnParams& p, int s, int r, int& b
     }
 }
 
-// which of the 32 slots from `slot` on row `node` sees; end: slots there are
-__device__ __forceinline__ uint32_t seen_word(const uint32_t* mask_row, int words, int node, int n, int base, int end, int slot) {
-    const int left = end - slot;
-    if (left <= 0) return 0;
-    const uint32_t in = left >= 32 ? 0xFFFFFFFFu : (1u << left) - 1;
-    const int j0 = slot - base;  // new row of the first slot
-    if (j0 <= -32) return in;
-    const uint32_t prefix = j0 < 0 ? (1u << -j0) - 1 : 0;
-    uint32_t tree;
-    if (mask_row == nullptr) {
-        const int upto = node - j0;  // slots up to this one
-        tree = upto < 0 ? 0 : upto >= 31 ? 0xFFFFFFFFu : (2u << upto) - 1;
-    } else if (j0 < 0) {
-        tree = mask_row[0] << -j0;
-    } else {
-        const int w = j0 >> 5, sh = j0 & 31;
-        const uint32_t lo = w < words ? mask_row[w] : 0, hi = sh && w + 1 < words ? mask_row[w + 1] : 0;
-        tree = __funnelshift_r(lo, hi, sh);
+// which of the 128 slots from `first` on row `node` sees; end: slots there are.  (Words of the mask are loaded without branches, all together.)
+__device__ __forceinline__ void seen_words(const uint32_t* mask_row, int words, int node, int base, int end, int first, uint32_t (&sees)[4]) {
+    const int j0 = first - base, w0 = j0 >> 5;  // new row of the first slot (below 0: slots of the prefix) and its word
+    uint32_t m[5] = {0, 0, 0, 0, 0};
+    if (mask_row != nullptr)
+#pragma unroll
+        for (int x = 0; x < 5; ++x) {
+            const uint32_t v = __ldg(mask_row + min(max(w0 + x, 0), words - 1));
+            m[x] = w0 + x >= 0 && w0 + x < words ? v : 0;
+        }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        const auto low = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1; };  // the n lowest bits
+        const int j = j0 + 32 * x;
+        const uint32_t tree = mask_row != nullptr ? __funnelshift_r(m[x], m[x + 1], j0 & 31) : low(node - j + 1);
+        sees[x] = (tree | low(-j)) & low(end - first - 32 * x);
     }
-    return in & (prefix | (tree & ~prefix));
 }
 
 // ---- the attention kernel ------------------------------------------------------------------------------------------
@@ -598,7 +645,8 @@ __device__ __noinline__ void add_spoilt(const AttnParams& p, const Piece& pc, ui
                 bad = bad || not_finite2(v.x) || not_finite2(v.y);
             }
             if (!bad) continue;
-            const bool mine = sums && (seen_word(mask_row, p.words, node, pc.n, pc.base, pc.end, slot) & 1);
+            const int j = slot - pc.base;
+            const bool mine = sums && (mask_row == nullptr ? j <= node : j < 32 * p.words && ((mask_row[j >> 5] >> (j & 31)) & 1));
             float s = 0.0f;
             if (mine)
                 for (int d = 0; d < D; d += 4) {
@@ -681,6 +729,7 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
         mbar_fence_init();
     }
     if (warp == 8) tmem_alloc<false>(smem_u32(tmem_at), 512);
+    if (warp == 9 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &p.map_k : &p.map_v) : "memory");
     pdl_launch_dependents();
     tc_fence_before();
     __syncthreads();
@@ -736,13 +785,14 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
 #pragma unroll
                 for (int y = 0; y < 32 / kRows; ++y) {
                     const long long at = __shfl_sync(0xFFFFFFFFu, mine, y * kRows + lane / kPer);
-                    u[y] = at >= 0 ? __ldg((const uint4*)(p.q + 2 * at) + x) : make_uint4(0, 0, 0, 0);
+                    u[y] = __ldg((const uint4*)(p.q + 2 * max(at, 0LL)) + x);  // (no branches between the loads: rows that are not there read row 0)
                 }
 #pragma unroll
                 for (int y = 0; y < 32 / kRows; ++y) {
                     uint4 v = u[y];
-                    v.x = (v.x ^ p.q_flip) & p.q_keep, v.y = (v.y ^ p.q_flip) & p.q_keep;
-                    v.z = (v.z ^ p.q_flip) & p.q_keep, v.w = (v.w ^ p.q_flip) & p.q_keep;
+                    const uint32_t keep = __shfl_sync(0xFFFFFFFFu, live, y * kRows + lane / kPer) ? p.q_keep : 0u;
+                    v.x = (v.x ^ p.q_flip) & keep, v.y = (v.y ^ p.q_flip) & keep;
+                    v.z = (v.z ^ p.q_flip) & keep, v.w = (v.w ^ p.q_flip) & keep;
                     if (Q8)
                         v = make_uint4(__byte_perm(v.x, v.y, 0x7632), __byte_perm(v.x, v.y, 0x5410), __byte_perm(v.z, v.w, 0x7632),
                                        __byte_perm(v.z, v.w, 0x5410));
@@ -800,9 +850,7 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                     int b = 0, node = 0, g = 0;
                     if (live) row_of(p, pc.s, pc.r0 + r, b, node, g);
                     const uint32_t* mask_row = p.mask ? p.mask + ((size_t)b * p.nmax + node) * p.words : nullptr;
-                    const int n = pc.n, base = pc.base, end = pc.end;
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) sees[x] = live ? seen_word(mask_row, p.words, node, n, base, end, first + 32 * x) : 0;
+                    seen_words(mask_row, p.words, node, pc.base, live ? pc.end : 0, first, sees);
                     // (with two row tiles every entry ahead of V's in the ring has been used by this stream, so its phase is certain: see `pass`)
                     if (two && i == 0 && !(ok = clear_v(t, first))) break;
                 }
@@ -874,17 +922,17 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                     }
                 } else {
                     // (four columns of all rows side by side: a warp's stores are whole lines)
-                    float4* to = (float4*)p.part_o + (slot * (D / 4) + d0 / 4) * kUnitRows + r;
+                    float4* to = (float4*)p.part_o + (slot * (D / 4) + d0 / 4) * p.part_rows + r;
 #pragma unroll
                     for (int x = 0; x < 8; ++x)
-                        to[x * kUnitRows] = make_float4(__uint_as_float(u[4 * x]), __uint_as_float(u[4 * x + 1]), __uint_as_float(u[4 * x + 2]),
+                        to[x * p.part_rows] = make_float4(__uint_as_float(u[4 * x]), __uint_as_float(u[4 * x + 1]), __uint_as_float(u[4 * x + 2]),
                                             __uint_as_float(u[4 * x + 3]));
                 }
             };
             const auto put_sums = [&](float mm, float ll) {
                 if (!live) return;
                 if (!whole)
-                    p.part_ml[slot * kUnitRows + r] = make_float2(mm > -INFINITY ? mm * c2 : -INFINITY, ll);
+                    p.part_ml[slot * p.part_rows + r] = make_float2(mm > -INFINITY ? mm * c2 : -INFINITY, ll);
                 else if (p.lse)
                     p.lse[out_row] = log_sum(mm > -INFINITY ? mm * c2 : -INFINITY, ll);
             };
@@ -1257,12 +1305,12 @@ __device__ __forceinline__ void join_rows(const AttnParams& p, const JoinList& j
             const JoinPiece a = j.piece[min(i0 + i, n - 1)];
             const bool mine = i0 + i < n && lane >= a.lo && lane < a.hi;
             const int r = mine ? lane + a.shift : 0;
-            const float2 x = __ldcg(p.part_ml + (size_t)a.slot * kUnitRows + r);
+            const float2 x = __ldcg(p.part_ml + (size_t)a.slot * p.part_rows + r);
             ml[i] = mine ? x : make_float2(-INFINITY, 0.0f);
-            const float4* from = (const float4*)p.part_o + ((size_t)a.slot * (D / 4) + warp * kQuads) * kUnitRows + r;
+            const float4* from = (const float4*)p.part_o + ((size_t)a.slot * (D / 4) + warp * kQuads) * p.part_rows + r;
 #pragma unroll
             for (int y = 0; y < kQuads; ++y) {
-                const float4 z = __ldcg(from + y * kUnitRows);
+                const float4 z = __ldcg(from + y * p.part_rows);
                 v[i][y] = mine ? z : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
         }
@@ -1321,22 +1369,22 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_shared_kernel(const __
     PlanSeq all, q;
     load_seq(all, p.seq);
     load_seq(q, p.seq + b + 1);
-    const int total = __ldcg(&p.head->total), parts = __ldcg(&p.head->parts), R = q.n * p.group;
+    const int total = __ldcg(&p.head->total), parts = __ldcg(&p.head->parts), chunk = __ldcg(&p.head->chunk), R = q.n * p.group;
     if (r0 >= R) return;
     if (threadIdx.x < 32) {
         if (threadIdx.x == 0) j.n = 0;
         __syncwarp();
         const int Ra = all.n * p.group, ra = q.node0 * p.group + r0, mt = ra / kUnitRows, upto = (mt + 1) * kUnitRows - ra;
         const int ua = all.unit0 + h * row_tiles2(Ra);
-        UnitAt u = unit_at(all, p.group, h, mt);
+        UnitAt u = unit_at(all, p.group, h, mt, chunk);
         const auto cta = [&](int k) { return cta_of(u.x0 + k * u.w, total, parts); };
         list_unit(j, u, cta(0), cta(u.kt - 1), total, parts, ua + mt, ra - mt * kUnitRows, 0, min(upto, kJoinRows));
         if (upto < kJoinRows && (mt + 1) * kUnitRows < Ra) {
-            u = unit_at(all, p.group, h, mt + 1);
+            u = unit_at(all, p.group, h, mt + 1, chunk);
             list_unit(j, u, cta(0), cta(u.kt - 1), total, parts, ua + mt + 1, -upto, upto, kJoinRows);
         }
         const int mo = r0 / kUnitRows;
-        u = unit_at(q, p.group, h, mo);
+        u = unit_at(q, p.group, h, mo, chunk);
         list_unit(j, u, cta(0), cta(u.kt - 1), total, parts, q.unit0 + h * row_tiles2(R) + mo, r0 - mo * kUnitRows, 0, kJoinRows);
     }
     __syncthreads();
@@ -1370,12 +1418,14 @@ bool encode_map(CUtensorMap* map, const void* base, bool q8, int D, uint64_t row
 }
 
 struct AttnSizes {
+    int part_rows;
     size_t o_seq, o_start, o_join, o_ml, o_o, total;
 };
 AttnSizes attn_sizes(const graft_ctx* ctx, int batch, int kv_heads, int head_dim, int group, int rows, int shared) {
     const auto units = [&](long long nodes) { return (size_t)kv_heads * (size_t)((nodes * group + kUnitRows - 1) / kUnitRows); };
     const size_t slots = shared > 0 ? units((long long)batch * rows) + (size_t)batch * units(rows) + ctx->num_sms : 2 * (size_t)ctx->num_sms;
     AttnSizes z;
+    z.part_rows = shared > 0 ? kUnitRows : (int)min((long long)kUnitRows, ((long long)rows * group + 31) / 32 * 32);
     size_t off = 256;
     const auto take = [&](size_t bytes) {
         const size_t o = off;
@@ -1385,8 +1435,8 @@ AttnSizes attn_sizes(const graft_ctx* ctx, int batch, int kv_heads, int head_dim
     z.o_seq = take((size_t)(batch + 1) * sizeof(PlanSeq));
     z.o_start = take((size_t)ctx->num_sms * sizeof(PlanStart));
     z.o_join = take((size_t)(ctx->num_sms + 1) * sizeof(PlanJoin));
-    z.o_ml = take(slots * kUnitRows * sizeof(float2));
-    z.o_o = take(slots * kUnitRows * head_dim * sizeof(float));
+    z.o_ml = take(slots * z.part_rows * sizeof(float2));
+    z.o_o = take(slots * z.part_rows * head_dim * sizeof(float));
     z.total = off;
     return z;
 }
@@ -1455,7 +1505,6 @@ cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache
     p.words = ctx->mask_words;
     p.batch = batch;
     p.ctas = ctx->num_sms;
-    p.min_cost = 1;
     const AttnSizes z = attn_sizes(ctx, batch, cache->kv_heads, cache->head_dim, p.group, rows, shared);
     uint8_t* base = (uint8_t*)scratch;
     p.head = (PlanHead*)base;
@@ -1465,6 +1514,7 @@ cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache
     p.part_ml = (float2*)(base + z.o_ml);
     p.part_o = (float*)(base + z.o_o);
     p.arrivals = ctx->w_attn_n;
+    p.part_rows = z.part_rows;
     const bool one = shared == 0 && (long long)rows * p.group <= kTile;
     const auto launch = cache->head_dim == 128 ? (q8 ? (one ? launch_attn<128, true, true> : launch_attn<128, true, false>)
                                                      : (one ? launch_attn<128, false, true> : launch_attn<128, false, false>))
