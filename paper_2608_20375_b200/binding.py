@@ -162,27 +162,35 @@ def _stream():
     return torch.cuda.current_stream().cuda_stream
 
 
-def _shaped(name, t, dtype, shape):
-    """The pointer of a dense tensor of this type and shape on the current device (None: NULL)."""
+def _shaped(name, t, dtype, shape, dev):
+    """The pointer of a dense tensor of this type and shape on device number `dev` (None: NULL).  One test when all is well, as _ptr."""
     if t is None:
         return None
+    if t.shape == shape and t.get_device() == dev and t.dtype is dtype and t.is_contiguous():
+        return t.data_ptr()
     if t.shape != shape:
         raise GraftError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
+    if t.is_cuda and t.get_device() != dev:
         raise GraftError(f"{name} is on another device than the current one")
     return _ptr(t, dtype)
 
 
-def _token_rows(name, t, heads, head_dim):
+def _device():
+    """Number of the current device (without one: none that a tensor could be on)."""
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+
+
+def _token_rows(name, t, heads, head_dim, dev):
     """[batch, rows, heads, head_dim] bf16, whose tokens may stand further apart than dense (slices of a fused projection): pointer,
     rows, numbers from one token to the next."""
-    if t.dim() != 4 or t.shape[2] != heads or t.shape[3] != head_dim:
-        raise GraftError(f"{name} must be [batch, rows, {heads}, {head_dim}], got {tuple(t.shape)}")
-    if t.dtype is not torch.bfloat16 or not t.is_cuda:
+    shape = t.shape
+    if len(shape) != 4 or shape[2] != heads or shape[3] != head_dim:
+        raise GraftError(f"{name} must be [batch, rows, {heads}, {head_dim}], got {tuple(shape)}")
+    if t.get_device() != dev or t.dtype is not torch.bfloat16:
+        if t.is_cuda and t.dtype is torch.bfloat16:
+            raise GraftError(f"{name} is on another device than the current one")
         raise GraftError(f"{name} must be a bfloat16 CUDA tensor")
-    if t.get_device() != torch._C._cuda_getDevice():
-        raise GraftError(f"{name} is on another device than the current one")
-    batch, rows = t.shape[:2]
+    batch, rows = shape[0], shape[1]
     if t.is_contiguous():
         return t.data_ptr(), rows, heads * head_dim
     sb, st, sh, sd = t.stride()
@@ -208,20 +216,24 @@ class KVCache:
         e = lambda: torch.zeros(shape[:-1], dtype=torch.uint8, device="cuda") if dtype == E4M3 else None  # noqa: E731
         return cls(torch.zeros(shape, dtype=dt, device="cuda"), torch.zeros(shape, dtype=dt, device="cuda"), e(), e())
 
-    def _c(self, table, batch):
-        if self.k.dim() != 5 or self.k.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+    def _c(self, table, batch, dev):
+        k = self.k
+        shape, dt = k.shape, k.dtype
+        q8 = dt is torch.float8_e4m3fn
+        if len(shape) != 5 or not (q8 or dt is torch.bfloat16):
             raise GraftError("a cache is [layers, n_pages, kv_heads, page_size, head_dim], bfloat16 or float8_e4m3fn")
         if table.dim() != 2:
             raise GraftError(f"table must be [batch, pages], got {tuple(table.shape)}")
-        shape, q8 = self.k.shape, self.k.dtype is torch.float8_e4m3fn
         if q8 != (self.k_exp is not None) or q8 != (self.v_exp is not None):
             raise GraftError("an e4m3 cache has exponents, a bfloat16 one has none")
         layers, n_pages, heads, page, dim = shape
-        u8 = torch.uint8
-        return _Cache(layers, n_pages, heads, page, dim, E4M3 if q8 else BF16, _shaped("k", self.k, self.k.dtype, shape),
-                      _shaped("v", self.v, self.k.dtype, shape), _shaped("k_exp", self.k_exp, u8, shape[:-1]),
-                      _shaped("v_exp", self.v_exp, u8, shape[:-1]), _shaped("table", table, torch.int32, (batch, table.shape[1])),
-                      table.shape[1])
+        width = table.shape[1]
+        ke = ve = None
+        if q8:
+            ke = _shaped("k_exp", self.k_exp, torch.uint8, shape[:-1], dev)
+            ve = _shaped("v_exp", self.v_exp, torch.uint8, shape[:-1], dev)
+        return _Cache(layers, n_pages, heads, page, dim, E4M3 if q8 else BF16, _shaped("k", k, dt, shape, dev),
+                      _shaped("v", self.v, dt, shape, dev), ke, ve, _shaped("table", table, torch.int32, (batch, width), dev), width)
 
 
 def vocab_pass_static(logits, K, topk_id, topk_lp, lse, row_status):
@@ -425,61 +437,61 @@ class Graft:
     # ---- verification of the trees
     def cache_write(self, cache: KVCache, layer, table, prefix_len, count, key, value, status=None):
         """Row i < count[b] of key and value [batch, rows, kv_heads, head_dim] into slot prefix_len[b] - 1 + i of the layer."""
-        batch, i32 = key.shape[0], torch.int32
-        cc = cache._c(table, batch)
-        kp, rows, stride = _token_rows("key", key, cc.kv_heads, cc.head_dim)
-        vp, v_rows, v_stride = _token_rows("value", value, cc.kv_heads, cc.head_dim)
+        batch, i32, dev = key.shape[0], torch.int32, _device()
+        cc = cache._c(table, batch, dev)
+        kp, rows, stride = _token_rows("key", key, cc.kv_heads, cc.head_dim, dev)
+        vp, v_rows, v_stride = _token_rows("value", value, cc.kv_heads, cc.head_dim, dev)
         if value.shape[0] != batch or v_rows != rows or v_stride != stride:
             raise GraftError("key and value must be laid out alike")
         _check(self.lib, self.lib.graft_cache_write(
-            self._ctx, batch, C.byref(cc), int(layer), _shaped("prefix_len", prefix_len, i32, (batch,)),
-            _shaped("count", count, i32, (batch,)), rows, stride, kp, vp, _shaped("status", status, i32, (batch,)), _stream()),
+            self._ctx, batch, C.byref(cc), int(layer), _shaped("prefix_len", prefix_len, i32, (batch,), dev),
+            _shaped("count", count, i32, (batch,), dev), rows, stride, kp, vp, _shaped("status", status, i32, (batch,), dev), _stream()),
             "graft_cache_write")
 
     def cache_read(self, cache: KVCache, layer, table, prefix_len, count, key, value, status=None):
         """The entries of the same slots back into dense key and value; rows behind the count are left as they were."""
-        batch, i32 = key.shape[0], torch.int32
-        cc = cache._c(table, batch)
+        batch, i32, dev = key.shape[0], torch.int32, _device()
+        cc = cache._c(table, batch, dev)
         if key.dim() != 4:
             raise GraftError(f"key must be [batch, rows, {cc.kv_heads}, {cc.head_dim}], got {tuple(key.shape)}")
         shape = (batch, key.shape[1], cc.kv_heads, cc.head_dim)
         _check(self.lib, self.lib.graft_cache_read(
-            self._ctx, batch, C.byref(cc), int(layer), _shaped("prefix_len", prefix_len, i32, (batch,)),
-            _shaped("count", count, i32, (batch,)), key.shape[1], _shaped("key", key, torch.bfloat16, shape),
-            _shaped("value", value, torch.bfloat16, shape), _shaped("status", status, i32, (batch,)), _stream()), "graft_cache_read")
+            self._ctx, batch, C.byref(cc), int(layer), _shaped("prefix_len", prefix_len, i32, (batch,), dev),
+            _shaped("count", count, i32, (batch,), dev), key.shape[1], _shaped("key", key, torch.bfloat16, shape, dev),
+            _shaped("value", value, torch.bfloat16, shape, dev), _shaped("status", status, i32, (batch,), dev), _stream()), "graft_cache_read")
 
     def cache_keep(self, cache: KVCache, table, prefix_len, accept_len, accept_path, next_prefix=None, status=None):
         """The accepted nodes' entries move up behind the prefix, in all layers; next_prefix (may be prefix_len): the new lengths."""
-        batch, i32 = accept_len.shape[0], torch.int32
-        cc = cache._c(table, batch)
+        batch, i32, dev = accept_len.shape[0], torch.int32, _device()
+        cc = cache._c(table, batch, dev)
         one = (batch,)
         _check(self.lib, self.lib.graft_cache_keep(
-            self._ctx, batch, C.byref(cc), _shaped("prefix_len", prefix_len, i32, one), _shaped("accept_len", accept_len, i32, one),
-            _shaped("accept_path", accept_path, i32, (batch, self.cfg.L)), _shaped("next_prefix", next_prefix, i32, one),
-            _shaped("status", status, i32, one), _stream()), "graft_cache_keep")
+            self._ctx, batch, C.byref(cc), _shaped("prefix_len", prefix_len, i32, one, dev), _shaped("accept_len", accept_len, i32, one, dev),
+            _shaped("accept_path", accept_path, i32, (batch, self.cfg.L), dev), _shaped("next_prefix", next_prefix, i32, one, dev),
+            _shaped("status", status, i32, one, dev), _stream()), "graft_cache_keep")
 
     def tree_attention(self, cache: KVCache, layer, table, q, prefix_len, count, mask, out, lse=None, scale=None, shared=0, status=None):
         """Attention of q [batch, rows, q_heads, head_dim] over one layer of the cache: the prefix, and of the rows' own entries those
         that mask [batch, nmax, mask_words] (None: a chain) lets a row see.  scale: head_dim ** -0.5 unless given.  shared: the first
         slots that are the same pages for all sequences."""
-        batch, i32 = q.shape[0], torch.int32
-        cc = cache._c(table, batch)
+        batch, i32, dev = q.shape[0], torch.int32, _device()
+        cc = cache._c(table, batch, dev)
         if q.dim() != 4:
             raise GraftError(f"q must be [batch, rows, heads, {cc.head_dim}], got {tuple(q.shape)}")
         heads = q.shape[2]
-        qp, rows, stride = _token_rows("q", q, heads, cc.head_dim)
+        qp, rows, stride = _token_rows("q", q, heads, cc.head_dim, dev)
         _check(self.lib, self.lib.graft_tree_attention(
             self._ctx, batch, C.byref(cc), int(layer), heads, rows, stride, qp, cc.head_dim ** -0.5 if scale is None else scale,
-            _shaped("prefix_len", prefix_len, i32, (batch,)), _shaped("count", count, i32, (batch,)),
-            _shaped("mask", mask, i32, (batch, self.nmax, self.mask_words)), int(shared),
-            _shaped("out", out, torch.bfloat16, (batch, rows, heads, cc.head_dim)),
-            _shaped("lse", lse, torch.float32, (batch, rows, heads)), _shaped("status", status, i32, (batch,)), _stream()),
+            _shaped("prefix_len", prefix_len, i32, (batch,), dev), _shaped("count", count, i32, (batch,), dev),
+            _shaped("mask", mask, i32, (batch, self.nmax, self.mask_words), dev), int(shared),
+            _shaped("out", out, torch.bfloat16, (batch, rows, heads, cc.head_dim), dev),
+            _shaped("lse", lse, torch.float32, (batch, rows, heads), dev), _shaped("status", status, i32, (batch,), dev), _stream()),
             "graft_tree_attention")
 
     def verify(self, trees: TreeOut, target_logits, temperature, uniform, accept_len, accept_path, bonus_token, status=None):
         """The acceptance walk for a target that samples: target_logits [batch, rows, V] bfloat16 or float32, temperature [batch] or
         None (1), uniform [batch, nmax] in [0, 1); outputs as accept()."""
-        i32, f32 = torch.int32, torch.float32
+        i32, f32, dev = torch.int32, torch.float32, _device()
         if target_logits.dim() != 3 or target_logits.shape[2] != self.cfg.V:
             raise GraftError(f"target_logits must be [batch, rows, {self.cfg.V}], got {tuple(target_logits.shape)}")
         if target_logits.dtype not in (torch.bfloat16, f32):
@@ -487,15 +499,15 @@ class Graft:
         batch, rows = target_logits.shape[:2]
         one, nodes = (batch,), (batch, self.nmax)
         oc = _TreeOut()
-        oc.d_n_nodes = _shaped("n_nodes", trees.n_nodes, i32, one)
-        oc.d_token = _shaped("token", trees.token, i32, nodes)
-        oc.d_parent = _shaped("parent", trees.parent, i32, nodes)
+        oc.d_n_nodes = _shaped("n_nodes", trees.n_nodes, i32, one, dev)
+        oc.d_token = _shaped("token", trees.token, i32, nodes, dev)
+        oc.d_parent = _shaped("parent", trees.parent, i32, nodes, dev)
         _check(self.lib, self.lib.graft_verify(
             self._ctx, batch, C.byref(oc), rows, F32 if target_logits.dtype is f32 else BF16,
-            _shaped("target_logits", target_logits, None, target_logits.shape), _shaped("temperature", temperature, f32, one),
-            _shaped("uniform", uniform, f32, nodes), _shaped("accept_len", accept_len, i32, one),
-            _shaped("accept_path", accept_path, i32, (batch, self.cfg.L)), _shaped("bonus_token", bonus_token, i32, one),
-            _shaped("status", status, i32, one), _stream()), "graft_verify")
+            _shaped("target_logits", target_logits, target_logits.dtype, target_logits.shape, dev), _shaped("temperature", temperature, f32, one, dev),
+            _shaped("uniform", uniform, f32, nodes, dev), _shaped("accept_len", accept_len, i32, one, dev),
+            _shaped("accept_path", accept_path, i32, (batch, self.cfg.L), dev), _shaped("bonus_token", bonus_token, i32, one, dev),
+            _shaped("status", status, i32, one, dev), _stream()), "graft_verify")
 
     def tdes_loss(self, groups, pairs, edges, gamma, w1, lambda_kl, lambda_pair, lambda_bce, loss, skipped=None,
                   gP=None, gC=None, gu=None, gs=None):

@@ -112,6 +112,7 @@ struct graft_ctx {
     graft::Grown tables_scratch, attn_scratch;
     int attn_ready;  // variants of the attention kernel that may use their shared memory
     int* w_attn_n;   // graft_tree_attention: arrivals, zero between calls
+    int verify_ready;  // variants of graft_verify's kernel that may be launched in clusters of 16
     // host-buffer staging (allocated on first use of graft_build_trees_host)
     void* stage;
     size_t stage_bytes;

@@ -13,10 +13,11 @@ namespace graft {
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;  // four CTAs an SM: a sequence's cluster then spreads over as many SMs as can be
 constexpr int kWarps = kThreads / 32;
-constexpr int kMaxCluster = 8;
-constexpr int kVec = 8;              // tokens a step and thread
+constexpr int kMaxCluster = 16;
+constexpr int kRoots = 256;          // entries of the table of 2^(j / 256)
+constexpr int kGroups = 64;          // sums that a warp keeps of its stretch of the last row
 constexpr float kNear = 1e-5f;       // sums of fp32 exponentials are nearer than that (of the whole) to the exact ones
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
@@ -32,18 +33,11 @@ struct VerifyParams {
     int32_t* bonus;
     int32_t* status;
     int rows, V, nmax, L;
+    int bring_ahead;  // the likeliest next rows are brought to L2
     int hist_w;
     int32_t* hist_window;
     int32_t* hist_count;
     float* hist_out;
-};
-
-// what one CTA tells the others about its share of a row
-struct Share {
-    float m, s;        // largest logit, sum of exp((z - m) / T)
-    double sum;        // fp64 sum of exp((z - row's largest) / T)
-    uint64_t key;      // T = 0: (order of the largest logit << 32) | ~its id
-    int bad;
 };
 
 template <bool BF16>
@@ -51,26 +45,56 @@ __device__ __forceinline__ float logit(const uint8_t* row, int v) {
     return BF16 ? __uint_as_float((uint32_t)((const uint16_t*)row)[v] << 16) : ((const float*)row)[v];
 }
 
-// eight tokens from v on (those at `end` and behind it: -inf); `al`: rows start on 16-byte boundaries
+// A row as 16-byte pieces on 16-byte boundaries, whatever it begins on: piece s holds tokens s kE - skip .. + kE - 1, at least one of them of
+// the row.
 template <bool BF16>
-__device__ __forceinline__ void load8(const uint8_t* row, int v, int end, bool al, float (&x)[kVec]) {
-    if (al && v + kVec <= end) {
-        if (BF16) {
-            const uint4 u = __ldg((const uint4*)((const uint16_t*)row + v));
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[2 * i] = __uint_as_float(w[i] << 16);
-                x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-            }
-        } else {
-            const float4 a = __ldg((const float4*)((const float*)row + v)), d = __ldg((const float4*)((const float*)row + v) + 1);
-            x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = d.x, x[5] = d.y, x[6] = d.z, x[7] = d.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) x[i] = v + i < end ? logit<BF16>(row, v + i) : -INFINITY;
+struct Row {
+    static constexpr int kE = BF16 ? 8 : 4;
+    const uint4* at;
+    int skip, pieces, V;
+    __device__ __forceinline__ Row(const uint8_t* row, int V_) {
+        const int low = (int)((uintptr_t)row & 15);
+        at = (const uint4*)(row - low);
+        skip = low / (BF16 ? 2 : 4);
+        V = V_;
+        pieces = (V + skip + kE - 1) / kE;
     }
+    __device__ __forceinline__ int first(int s) const { return s * kE - skip; }
+    // -inf in the place of what is not the row's
+    __device__ __forceinline__ void unpack(const uint4& u, int s, bool there, float (&x)[kE]) const {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        const int v = first(s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (BF16) {
+                x[(2 * i) % kE] = __uint_as_float(w[i] << 16);
+                x[(2 * i + 1) % kE] = __uint_as_float(w[i] & 0xFFFF0000u);
+            } else
+                x[i % kE] = __uint_as_float(w[i]);
+        }
+        if (!there || v < 0 || v + kE > V)
+#pragma unroll
+            for (int i = 0; i < kE; ++i) x[i] = there && v + i >= 0 && v + i < V ? x[i] : -INFINITY;
+    }
+};
+
+// x as a double by integer operations (conversions run at a quarter of the rate of the arithmetic): zero comes out as 2^-127, which is
+// nothing beside what it is added to, and -inf as -2^128.
+__device__ __forceinline__ double widen(float x) {
+    const uint32_t u = __float_as_uint(x);
+    return __hiloint2double((int)((u & 0x80000000u) | (((u & 0x7FFFFFFFu) >> 3) + 0x38000000u)), (int)(u << 29));
+}
+// 2^t in fp64 for t <= 0 or so (below -1000: 0): t = n + j / 256 + r, |r| <= 1/512, a table of 2^(j / 256) and the exponential series to the
+// third power, whose rest is below 2e-13.  The sum with 1.5 2^44 leaves 256 (n + j / 256) in its last bits.
+__device__ __forceinline__ double exp2_fine(double t, const double* roots) {
+    const double kMagic = 26388279066624.0;
+    const double m = t + kMagic, r = t - (m - kMagic);
+    const int k = __double2loint(m);
+    double q = fma(r, 0.05550410866482158, 0.24022650695910072);  // ln 2 cubed over 6, squared over 2
+    q = fma(q, r, 0.69314718055994531);
+    q = fma(q, r, 1.0);
+    q *= roots[k & (kRoots - 1)];
+    return t > -1000.0 ? __hiloint2double(__double2hiint(q) + ((k >> 8) << 20), __double2loint(q)) : 0.0;
 }
 
 __device__ __forceinline__ float warp_max(float x) {
@@ -91,26 +115,27 @@ __device__ __forceinline__ uint64_t warp_max_key(uint64_t k) {
 }
 
 template <bool BF16>
-__global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyParams p) {
+__global__ void __launch_bounds__(kThreads, 4) verify_kernel(const VerifyParams p) {
+    using R = Row<BF16>;
+    constexpr int kE = R::kE, kAhead = 8;  // pieces that a thread has on their way
     pdl_launch_dependents();
-    pdl_wait();
     extern __shared__ __align__(16) int32_t vsm[];
     int32_t* first_child = vsm;          // [nmax], 0: none (the root is nobody's child)
     int32_t* par = vsm + p.nmax;         // [nmax]
     int32_t* tok = par + p.nmax;         // [nmax]
-    __shared__ Share mine, heard[2][kMaxCluster];
-    __shared__ float w_m[kWarps], w_s[kWarps];
-    __shared__ double w_d[kWarps];
-    __shared__ uint64_t w_k[kWarps];
-    __shared__ uint32_t filter[32];      // of the children's tokens
-    __shared__ int step_next, step_again, step_first, step_n, found;
+    float* uni = (float*)(tok + p.nmax);  // [nmax]
+    __shared__ uint64_t heard[2][kMaxCluster * kWarps];
+    __shared__ double roots[kRoots], group[kWarps][kGroups];
+    __shared__ uint32_t filter[32];  // of the children's tokens
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint32_t n_cta;
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_cta));
-    const int rank = (int)cluster_ctarank(), ctas = (int)n_cta;
+    const int rank = (int)cluster_ctarank(), ctas = (int)n_cta, ctas_log = 31 - __clz(ctas);  // (a power of two)
     const int b = blockIdx.y;
     const size_t ob = (size_t)b * p.nmax;
     const int esz = BF16 ? 2 : 4, V = p.V;
+    for (int i = tid; i < kRoots; i += kThreads) roots[i] = exp2((double)i / kRoots);
+    pdl_wait();
 
     const int n = p.n_nodes[b];
     const float T = p.temperature ? p.temperature[b] : 1.0f;
@@ -120,6 +145,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyParams p) 
         first_child[i] = 0;
         par[i] = p.parent[ob + i];
         tok[i] = p.token[ob + i];
+        uni[i] = p.uniform[ob + i];
     }
     __syncthreads();
     if (tree_ok)
@@ -128,185 +154,201 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyParams p) 
             if (q >= 0 && q < i && (i == 1 || par[i - 1] != q)) first_child[q] = i;
         }
     __syncthreads();
-    // every CTA's share of a row: whole steps of kVec tokens
-    const int steps = (V + kVec - 1) / kVec;
-    const int s0 = (int)((long long)steps * rank / ctas), s1 = (int)((long long)steps * (rank + 1) / ctas);
-    const double inv_T = greedy ? 1.0 : 1.0 / (double)T;
-    const float cf = (float)((double)kLog2e * inv_T);
+    const double inv_T = greedy ? 1.0 : 1.0 / (double)T, c64 = 1.4426950408889634 * inv_T;
+    const float cf = (float)c64;
 
     int cur = 0, a = 0, status = !tree_ok ? GRAFT_ST_BAD_TREE : !t_ok ? GRAFT_ST_BAD_LOGITS : 0, bonus = -1;
     int path = -1;  // lane l of warp 0 keeps step l
-    // Tell the others, hear the others: `heard` by turns, so that one barrier an exchange is enough (who writes to a half again has
-    // passed the barrier that all arrive at after they read it).
+    // Every warp tells every warp of the cluster eight bytes (the same in all its lanes); `heard` by turns, so that one barrier an exchange is
+    // enough (who writes to a half again has passed the barrier that all arrive at after they read it).  Then all warps work out the same.
     int turn = 0;
-    const Share* all = nullptr;
-    auto exchange = [&]() {
-        __syncthreads();  // `mine` is written
-        if (tid < ctas) {
-            const uint32_t to = mapa_u32(smem_u32(&heard[turn][rank]), tid);
-            const uint32_t* w = (const uint32_t*)&mine;
-#pragma unroll
-            for (int i = 0; i < (int)(sizeof(Share) / 4); ++i)
-                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to + 4 * i), "r"(w[i]) : "memory");
-        }
+    const uint64_t* all = nullptr;
+    const int voices = ctas * kWarps, voice = rank * kWarps + warp;
+    const auto exchange = [&](uint64_t mine) {
+        __syncwarp();
+        if (lane < ctas) asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(mapa_u32(smem_u32(&heard[turn][voice]), lane)), "l"(mine) : "memory");
         cluster_sync();
         all = heard[turn];
         turn ^= 1;
     };
+    // the sum of all warps' numbers, and of those ahead of voice v: every warp gets the same for the same v
+    const auto sum_all = [&]() {
+        double t = 0.0;
+        for (int i = lane; i < voices; i += 32) t += __longlong_as_double((long long)all[i]);
+        return warp_sum(t);
+    };
+    const auto sum_ahead = [&](int v) {
+        double t = 0.0;
+        for (int i = lane; i < v; i += 32) t += __longlong_as_double((long long)all[i]);
+        return warp_sum(t);
+    };
+    // this CTA's share of n things begins at
+    const auto share = [&](int n, int r) { return (int)(((long long)n * r) >> ctas_log); };
     while (status == 0) {
-        const uint8_t* row = p.logits + ((size_t)b * p.rows + cur) * V * esz;
-        const bool al = ((uintptr_t)row & 15) == 0;
+        const uint8_t* base = p.logits + ((size_t)b * p.rows + cur) * V * esz;
+        const R row(base, V);
+        const int s0 = share(row.pieces, rank), s1 = share(row.pieces, rank + 1);
+        // f(numbers, piece) for this thread's pieces of [from, to), `step` apart; loads of kAhead pieces go ahead of the work on them
+        const auto each = [&](int from, int to, int step, auto f) {
+            for (int st = from; st < to; st += step * kAhead) {
+                uint4 u[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) u[i] = __ldg(row.at + min(st + i * step, to - 1));
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    if (st + i * step >= to) break;
+                    float x[kE];
+                    row.unpack(u[i], st + i * step, true, x);
+                    f(x, st + i * step);
+                }
+            }
+        };
+        // the first children's logits are asked for ahead of the row, and the row of the first of them, the likeliest next, is brought to L2
+        const int fc = a < p.L ? first_child[cur] : 0;
+        int v_c = -1;
+        float z_c = 0.0f;
+        if (fc > 0) {
+            if (fc + lane < n && par[fc + lane] == cur) {
+                v_c = tok[fc + lane];
+                if (v_c >= 0 && v_c < V) z_c = logit<BF16>(base, v_c);
+            }
+            if (fc < p.rows && p.bring_ahead) {
+                const uint8_t* ahead = base + (size_t)(fc - cur) * V * esz;
+                for (int i = s0 + 8 * tid; i < s1; i += 8 * kThreads) asm volatile("prefetch.global.L2 [%0];" ::"l"(ahead + (size_t)i * 16));
+            }
+        }
+        // the same a piece at a time, the next one on its way: passes that are made once are short code, as most of their time would go to
+        // fetching it
+        const auto each_short = [&](int from, int to, int step, auto f) {
+            uint4 u = __ldg(row.at + max(min(from, to - 1), 0));
+#pragma unroll 1
+            for (int st = from; st < to; st += step) {
+                const uint4 next = __ldg(row.at + min(st + step, to - 1));
+                float x[kE];
+                row.unpack(u, st, true, x);
+                f(x, st);
+                u = next;
+            }
+        };
         // ---- largest logit and the sum of exponentials of this CTA's share
         float m = -FLT_MAX, s = 0.0f;
         bool bad = false;
         uint64_t key = 0;
-        for (int st = s0 + tid; st < s1; st += kThreads) {
-            float x[kVec];
-            load8<BF16>(row, st * kVec, V, al, x);
-            float vm = x[0];
+        if (greedy)
+            each(s0 + tid, s1, kThreads, [&](const float (&x)[kE], int st) {
+                float vm = x[0];
 #pragma unroll
-            for (int i = 1; i < kVec; ++i) vm = fmaxf(vm, x[i]);
+                for (int i = 1; i < kE; ++i) vm = fmaxf(vm, x[i]);
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) bad = bad || !(x[i] <= FLT_MAX);
-            if (greedy) {
+                for (int i = 0; i < kE; ++i) bad = bad || !(x[i] <= FLT_MAX);
                 if (key == 0 || vm > m) {
                     m = vm;
                     int at = 0;
 #pragma unroll
-                    for (int i = kVec - 1; i >= 0; --i)
-                        if (x[i] == vm) at = i;
-                    key = make_key(__float_as_uint(vm), (uint32_t)(st * kVec + at));
+                    for (int i = kE - 1; i >= 0; --i)
+                        if (x[i] == vm && row.first(st) + i >= 0 && row.first(st) + i < V) at = i;
+                    key = make_key(__float_as_uint(vm), (uint32_t)(row.first(st) + at));
                 }
-            } else {
+            });
+        else
+            each(s0 + tid, s1, kThreads, [&](const float (&x)[kE], int st) {
+                float vm = x[0];
+#pragma unroll
+                for (int i = 1; i < kE; ++i) vm = fmaxf(vm, x[i]);
                 if (vm > m) {
                     s *= ex2_approx((m - vm) * cf);
                     m = vm;
                 }
-                float t[kVec];
+                float t = 0.0f;
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) t[i] = ex2_approx((x[i] - m) * cf);
-                s += ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
-            }
-        }
-        const float wm = warp_max(m);
-        const float ws = warp_sum(s * ex2_approx((m - wm) * cf));
-        const uint64_t wk = warp_max_key(key);
-        const bool wb = __any_sync(kAll, bad);
-        if (lane == 0) {
-            w_m[warp] = wm;
-            w_s[warp] = ws;
-            w_k[warp] = wk;
-            w_d[warp] = wb ? 1.0 : 0.0;
-        }
-        __syncthreads();
-        if (warp == 0) {
-            const float xm = lane < kWarps ? w_m[lane] : -FLT_MAX, xs = lane < kWarps ? w_s[lane] : 0.0f;
-            const float am = warp_max(xm), as = warp_sum(xs * ex2_approx((xm - am) * cf));
-            const uint64_t ak = warp_max_key(lane < kWarps ? w_k[lane] : 0);
-            const bool ab = __any_sync(kAll, lane < kWarps && w_d[lane] != 0.0);
-            if (lane == 0) {
-                mine.m = am;
-                mine.s = as;
-                mine.key = ak;
-                mine.bad = ab;
-            }
-        }
-        exchange();
-        float top = -FLT_MAX, Zf = 0.0f;
+                for (int i = 0; i < kE; ++i) t += ex2_approx((x[i] - m) * cf);  // (NaN and +inf: NaN)
+                s += t;
+            });
+        float top, Zf;
         uint64_t best = 0;
         bool row_bad = false;
-        for (int r = 0; r < ctas; ++r) {
-            top = fmaxf(top, all[r].m);
-            best = all[r].key > best ? all[r].key : best;
-            row_bad = row_bad || all[r].bad;
+        if (greedy) {
+            best = warp_max_key(key);
+            exchange(__any_sync(kAll, bad) ? ~0ull : best);
+            best = 0;
+            for (int i = lane; i < voices; i += 32) best = all[i] > best ? all[i] : best;
+            best = warp_max_key(best);
+            row_bad = best == ~0ull;
+            top = 0.0f, Zf = 1.0f;
+        } else {
+            const float wm = warp_max(m), ws = warp_sum(s * ex2_approx((m - wm) * cf));
+            exchange((uint64_t)__float_as_uint(ws) << 32 | __float_as_uint(wm));
+            float xm = -FLT_MAX;
+            for (int i = lane; i < voices; i += 32) xm = fmaxf(xm, __uint_as_float((uint32_t)all[i]));
+            top = warp_max(xm);
+            float xs = 0.0f;
+            for (int i = lane; i < voices; i += 32)
+                xs += __uint_as_float((uint32_t)(all[i] >> 32)) * ex2_approx((__uint_as_float((uint32_t)all[i]) - top) * cf);
+            Zf = warp_sum(xs);
         }
-        for (int r = 0; r < ctas; ++r) Zf += all[r].s * ex2_approx((all[r].m - top) * cf);
         // (a row without a finite entry: no exponential above zero, or as key the one of -inf)
         row_bad = row_bad || (greedy ? (uint32_t)(best >> 32) <= ord_from_float(-INFINITY) : !(Zf > 0.0f));
         if (row_bad) {
             status = GRAFT_ST_BAD_LOGITS;
             break;
         }
-        const double dtop = (double)top;
-        // ---- the children, in turn: every CTA finds the same
+        const double off = -(double)top * c64;
+        const auto weight = [&](float x) { return exp2_fine(fma(widen(x), c64, off), roots); };
+        // ---- the children, in turn: every warp finds the same
         double Z = (double)Zf;
         bool exact = greedy;
         int next = 0, n_child = 0;
-        const int fc = a < p.L ? first_child[cur] : 0;
         for (;;) {
-            if (warp == 0) {
-                double ahead = 0.0;
-                int nx = 0, again = 0, c0 = fc;
-                if (fc > 0)
-                    for (;; c0 += 32) {
-                        const int c = c0 + lane;
-                        const bool is = c < n && par[c] == cur;
-                        const unsigned kids = __ballot_sync(kAll, is);
-                        if (kids == 0) break;
-                        const int v = is ? tok[c] : -1;
-                        double w = 0.0;
-                        if (is && v >= 0 && v < V) {
-                            if (greedy)
-                                w = (uint32_t)v == key_id(best) ? 1.0 : 0.0;
-                            else
-                                w = exp(((double)logit<BF16>(row, v) - dtop) * inv_T);
-                            for (int e = fc; e < c; ++e)
-                                if (tok[e] == v) w = 0.0;  // an earlier sibling's token is taken already
-                        }
-                        double sum = w;
-                        for (int o = 1; o < 32; o <<= 1) {
-                            const double y = __shfl_up_sync(kAll, sum, o);
-                            if (lane >= o) sum += y;
-                        }
-                        const double left = (greedy ? 1.0 : Z) - (ahead + (sum - w));
-                        const double u = is ? (double)p.uniform[ob + c] : 2.0;
-                        const bool ok = is && u * left < w;
-                        const bool near = is && !exact && w > 0.0 && fabs(u * left - w) <= (double)kNear * Z;
-                        const unsigned oks = __ballot_sync(kAll, ok), nears = __ballot_sync(kAll, near);
-                        const int f = oks ? __ffs(oks) - 1 : 32;
-                        if (nears & (f >= 31 ? kAll : ((2u << f) - 1))) {
-                            again = 1;
-                            break;
-                        }
-                        if (oks) {
-                            nx = c0 + f;
-                            break;
-                        }
-                        ahead += __shfl_sync(kAll, sum, 31);
-                        n_child = c0 + __popc(kids) - fc;
-                        if (kids != kAll) break;
+            double ahead = 0.0;
+            bool again = false;
+            if (fc > 0)
+                for (int c0 = fc;; c0 += 32) {
+                    const int c = c0 + lane;
+                    const bool is = c < n && par[c] == cur;
+                    const unsigned kids = __ballot_sync(kAll, is);
+                    if (kids == 0) break;
+                    const int v = is ? tok[c] : -1;
+                    const double u = is ? (double)uni[c] : 2.0;
+                    double w = 0.0;
+                    if (is && v >= 0 && v < V) {
+                        if (greedy)
+                            w = (uint32_t)v == key_id(best) ? 1.0 : 0.0;
+                        else
+                            w = weight(c0 == fc ? z_c : logit<BF16>(base, v));
+                        for (int e = fc; e < c; ++e)
+                            if (tok[e] == v) w = 0.0;  // an earlier sibling's token is taken already
                     }
-                if (lane == 0) {
-                    step_next = nx;
-                    step_again = again;
-                    step_n = n_child;
+                    double sum = w;
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const double y = __shfl_up_sync(kAll, sum, o);
+                        if (lane >= o) sum += y;
+                    }
+                    const double left = (greedy ? 1.0 : Z) - (ahead + (sum - w));
+                    const bool ok = is && u * left < w;
+                    const bool near = is && !exact && w > 0.0 && fabs(u * left - w) <= (double)kNear * Z;
+                    const unsigned oks = __ballot_sync(kAll, ok), nears = __ballot_sync(kAll, near);
+                    const int f = oks ? __ffs(oks) - 1 : 32;
+                    if (nears & (f >= 31 ? kAll : ((2u << f) - 1))) {
+                        again = true;
+                        break;
+                    }
+                    if (oks) {
+                        next = c0 + f;
+                        break;
+                    }
+                    ahead += __shfl_sync(kAll, sum, 31);
+                    n_child = c0 + __popc(kids) - fc;
+                    if (kids != kAll) break;
                 }
-            }
-            __syncthreads();
-            next = step_next;
-            n_child = step_n;
-            const int again = step_again;
-            __syncthreads();
             if (!again) break;
             // too close for sums of fp32 exponentials: the row's sum again in fp64
             double d = 0.0;
-            for (int st = s0 + tid; st < s1; st += kThreads) {
-                float x[kVec];
-                load8<BF16>(row, st * kVec, V, al, x);
+            each_short(s0 + tid, s1, kThreads, [&](const float (&x)[kE], int) {
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) d += exp(((double)x[i] - dtop) * inv_T);
-            }
-            d = warp_sum(d);
-            if (lane == 0) w_d[warp] = d;
-            __syncthreads();
-            if (tid == 0) {
-                double t = 0.0;
-                for (int i = 0; i < kWarps; ++i) t += w_d[i];
-                mine.sum = t;
-            }
-            exchange();
-            Z = 0.0;
-            for (int r = 0; r < ctas; ++r) Z += all[r].sum;
+                for (int i = 0; i < kE; ++i) d += weight(x[i]);
+            });
+            exchange((uint64_t)__double_as_longlong(warp_sum(d)));
+            Z = sum_all();
             exact = true;
         }
         if (next > 0) {
@@ -320,114 +362,125 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyParams p) 
             bonus = (int)key_id(best);
             break;
         }
-        // (a step's tokens share a bit of the filter; a step whose bit is set looks through the children)
+        // (a piece's tokens share a bit of the filter; a piece whose bit is set looks through the children)
+        __syncthreads();
         if (tid < 32) filter[tid] = 0;
         __syncthreads();
         for (int e = tid; e < n_child; e += kThreads) {
             const int v = tok[fc + e];
-            if (v >= 0 && v < V) atomicOr(&filter[(v >> 8) & 31], 1u << ((v >> 3) & 31));
+            if (v >= 0 && v < V) {
+                const int st = (v + row.skip) / kE;
+                atomicOr(&filter[(st >> 5) & 31], 1u << (st & 31));
+            }
         }
         __syncthreads();
-        auto weights = [&](int st, double (&w)[kVec]) {
-            float x[kVec];
-            load8<BF16>(row, st * kVec, V, al, x);
+        const auto weights = [&](const float (&x)[kE], int st, double (&w)[kE]) {
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) w[i] = exp(((double)x[i] - dtop) * inv_T);
+            for (int i = 0; i < kE; ++i) w[i] = weight(x[i]);
             if ((filter[(st >> 5) & 31] >> (st & 31)) & 1)
                 for (int e = 0; e < n_child; ++e) {
-                    const int v = tok[fc + e];
-                    if (v >> 3 == st) {
+                    const int i0 = tok[fc + e] - row.first(st);
 #pragma unroll
-                        for (int i = 0; i < kVec; ++i)
-                            if (i == (v & 7)) w[i] = 0.0;
-                    }
+                    for (int i = 0; i < kE; ++i)
+                        if (i == i0) w[i] = 0.0;
                 }
         };
-        // a warp's steps follow one another, so that its sum is one stretch of the distribution
-        const int own = s1 - s0, v0 = s0 + (int)((long long)own * warp / kWarps), v1 = s0 + (int)((long long)own * (warp + 1) / kWarps);
-        double d = 0.0;
-        for (int st = v0 + lane; st < v1; st += 32) {
-            double w[kVec];
-            weights(st, w);
-            d += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        const auto add_up = [](const double (&w)[kE]) {
+            double t = (w[0] + w[1]) + (w[2] + w[3]);
+            if (kE == 8) t += (w[4 % kE] + w[5 % kE]) + (w[6 % kE] + w[7 % kE]);
+            return t;
+        };
+        // a warp's pieces follow one another, so that its sum is one stretch of the distribution
+        const int own = s1 - s0, v0 = s0 + own * warp / kWarps, v1 = s0 + own * (warp + 1) / kWarps;
+        // (sums of groups of it are kept, so that the place of the goal is found without going through all of it again)
+        const int steps = (v1 - v0 + 31) / 32, per = (steps + kGroups - 1) / kGroups;
+        if (lane + 32 < kGroups) group[warp][lane + 32] = 0.0;
+        group[warp][lane] = 0.0;
+        __syncwarp();
+#pragma unroll 1
+        for (int k = 0; k * per < steps; ++k) {
+            double d = 0.0;
+            each_short(v0 + 32 * per * k + lane, min(v1, v0 + 32 * per * (k + 1)), 32, [&](const float (&x)[kE], int st) {
+                double w[kE];
+                weights(x, st, w);
+                d += add_up(w);
+            });
+            d = warp_sum(d);
+            if (lane == 0) group[warp][k] = d;
         }
-        d = warp_sum(d);
-        if (lane == 0) w_d[warp] = d;
-        if (tid == 0) found = -1;
-        __syncthreads();
-        if (tid == 0) {
-            double t = 0.0;
-            for (int i = 0; i < kWarps; ++i) t += w_d[i];
-            mine.sum = t;
+        __syncwarp();
+        static_assert(kGroups == 64, "two groups a lane");
+        const double g0 = group[warp][2 * lane], g1 = group[warp][2 * lane + 1];
+        double upto = g0 + g1;
+        for (int o = 1; o < 32; o <<= 1) {
+            const double y = __shfl_up_sync(kAll, upto, o);
+            if (lane >= o) upto += y;
         }
-        exchange();
-        double total = 0.0, before = 0.0;
-        for (int r = 0; r < ctas; ++r) {
-            if (r == rank) before = total;
-            total += all[r].sum;
-        }
-        const double goal = (double)p.uniform[ob] * total;
-        double upto = before;
-        for (int i = 0; i < warp; ++i) upto += w_d[i];
-        // the warp whose stretch holds the goal goes through it once more
-        if (upto <= goal && goal < upto + w_d[warp]) {
-            double at = upto;
-            int hit = -1;
-            for (int st = v0; st < v1 && hit < 0; st += 32) {
-                double w[kVec] = {0, 0, 0, 0, 0, 0, 0, 0};
-                if (st + lane < v1) weights(st + lane, w);
-                const double sum = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        exchange((uint64_t)__double_as_longlong(__shfl_sync(kAll, upto, 31)));
+        const double goal = (double)uni[0] * sum_all(), mine_from = sum_ahead(voice), mine_to = voice + 1 < voices ? sum_ahead(voice + 1) : 1e300;
+        // The warp whose stretch holds the goal finds the group and goes through it once more.  (No two warps do, and one does if anything
+        // is left, as all have the same sums.)
+        int hit = -1;
+        if (mine_from <= goal && goal < mine_to) {
+            const double before = upto - (g0 + g1);
+            const unsigned some = __ballot_sync(kAll, g0 + g1 > 0.0), over = __ballot_sync(kAll, mine_from + upto > goal) & some;
+            const int l = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : 0;  // (the last with any, should rounding have it so)
+            const bool second = !(g0 > 0.0) || (g1 > 0.0 && !(mine_from + before + g0 > goal));
+            const int k = __shfl_sync(kAll, 2 * lane + (second ? 1 : 0), l);
+            double at = __shfl_sync(kAll, mine_from + before + (second ? g0 : 0.0), l);
+            int last = -1;  // token with the last weight above zero so far: the one, should rounding leave the goal behind the end
+            const int from = v0 + 32 * per * k, to = min(v1, from + 32 * per);
+#pragma unroll 1
+            for (int st = from; st < to && hit < 0; st += 32) {
+                float x[kE];
+                double w[kE];
+                row.unpack(__ldg(row.at + min(st + lane, to - 1)), st + lane, st + lane < to, x);
+                weights(x, st + lane, w);
+                const double sum = add_up(w);
                 double incl = sum;
+#pragma unroll 1
                 for (int o = 1; o < 32; o <<= 1) {
                     const double y = __shfl_up_sync(kAll, incl, o);
                     if (lane >= o) incl += y;
                 }
-                const unsigned over = __ballot_sync(kAll, at + incl > goal);
-                if (over) {
-                    const int l = __ffs(over) - 1;
+                const unsigned some = __ballot_sync(kAll, sum > 0.0), over = __ballot_sync(kAll, at + incl > goal) & some;
+                if (some) {
+                    const int l = over ? __ffs(over) - 1 : 31 - __clz(some);
+                    double q = at + (incl - sum);
+                    bool over_it = false;
                     int h = -1;
-                    if (lane == l) {
-                        double q = at + (incl - sum);
-                        bool over_it = false;
 #pragma unroll
-                        for (int i = 0; i < kVec; ++i) {
-                            q += w[i];
-                            if (w[i] > 0.0 && !over_it) h = (st + lane) * kVec + i;  // (the last, should rounding have it so)
-                            over_it = over_it || q > goal;
-                        }
+                    for (int e = 0; e < kE; ++e) {
+                        q += w[e];
+                        if (w[e] > 0.0 && !over_it) h = row.first(st + lane) + e;
+                        over_it = over_it || q > goal;
                     }
-                    hit = __shfl_sync(kAll, h, l);
+                    h = __shfl_sync(kAll, h, l);
+                    if (over)
+                        hit = h;
+                    else
+                        last = h;
                 }
                 at += __shfl_sync(kAll, incl, 31);
             }
-            if (lane == 0 && hit >= 0) found = hit;
+            if (hit < 0) hit = last;
         }
-        __syncthreads();
-        if (tid == 0) mine.key = (uint64_t)(uint32_t)found;
-        exchange();
-        for (int r = 0; r < ctas; ++r)
-            if ((int)(uint32_t)all[r].key >= 0) bonus = (int)(uint32_t)all[r].key;
+        exchange((uint64_t)(uint32_t)(hit + 1));
+        int got = 0;
+        for (int i = lane; i < voices; i += 32) got = max(got, (int)all[i]);
+        bonus = __reduce_max_sync(kAll, got) - 1;
         if (bonus >= 0) break;
         // nothing is left (the children held all of it, and rounding kept each from being accepted): the row's likeliest token
         int id = 0x7FFFFFFF;
-        for (int st = s0 + tid; st < s1; st += kThreads) {
-            float x[kVec];
-            load8<BF16>(row, st * kVec, V, al, x);
+        each_short(s0 + tid, s1, kThreads, [&](const float (&x)[kE], int st) {
 #pragma unroll
-            for (int i = 0; i < kVec; ++i)
-                if (x[i] == top) id = min(id, st * kVec + i);
-        }
-        id = __reduce_min_sync(kAll, id);
-        if (lane == 0) w_k[warp] = (uint64_t)(uint32_t)id;
-        __syncthreads();
-        if (tid == 0) {
-            uint64_t k = w_k[0];
-            for (int i = 1; i < kWarps; ++i) k = w_k[i] < k ? w_k[i] : k;
-            mine.key = k;
-        }
-        exchange();
+            for (int i = 0; i < kE; ++i)
+                if (x[i] == top) id = min(id, row.first(st) + i);
+        });
+        exchange((uint64_t)(uint32_t)__reduce_min_sync(kAll, id));
         bonus = 0x7FFFFFFF;
-        for (int r = 0; r < ctas; ++r) bonus = min(bonus, (int)(uint32_t)all[r].key);
+        for (int i = lane; i < voices; i += 32) bonus = min(bonus, (int)all[i]);
+        bonus = __reduce_min_sync(kAll, bonus);
         break;
     }
     cluster_sync();  // nobody leaves while others write to it
@@ -473,17 +526,27 @@ cudaError_t verify_launch(graft_ctx* ctx, int batch, const graft_tree_out* trees
     p.rows = rows;
     p.V = ctx->cfg.V;
     p.nmax = ctx->nmax;
+    // (a step of the whole batch in a few microseconds' reading: there is room for rows that may not be needed)
+    p.bring_ahead = (double)batch * ctx->cfg.V * (dt == GRAFT_BF16 ? 2 : 4) <= 8e6;
     p.L = ctx->cfg.L;
     p.hist_w = ctx->hist_w;
     p.hist_window = ctx->hist_window;
     p.hist_count = ctx->hist_count;
     p.hist_out = ctx->hist_out;
+    // A cluster takes a step of one sequence in a few microseconds, however short its CTAs' shares are: as many CTAs as keep a piece for every
+    // thread, and as are on the GPU together (four an SM)
     int ctas = kMaxCluster;
-    while (ctas > 1 && ctas * batch > 2 * ctx->num_sms) ctas >>= 1;
+    while (ctas > 1 && ((long long)ctas * batch > 4 * ctx->num_sms || (long long)ctas * kThreads * (dt == GRAFT_BF16 ? 8 : 4) > p.V)) ctas >>= 1;
+    const void* kernel = dt == GRAFT_BF16 ? (const void*)verify_kernel<true> : (const void*)verify_kernel<false>;
+    if (!(ctx->verify_ready & (1 << dt))) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+        ctx->verify_ready |= 1 << dt;
+    }
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3(ctas, batch);
     lc.blockDim = dim3(kThreads);
-    lc.dynamicSmemBytes = (size_t)3 * ctx->nmax * sizeof(int32_t);
+    lc.dynamicSmemBytes = (size_t)4 * ctx->nmax * sizeof(int32_t);
     lc.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -81,17 +81,17 @@ def test_binding_refuses_what_it_can_see():
     c = KVCache(torch.zeros((1, 2, 2, 16, 64), dtype=torch.bfloat16), torch.zeros((1, 2, 2, 16, 64), dtype=torch.bfloat16))
     t = torch.zeros((1, 2), dtype=torch.int32)
     with pytest.raises(GraftError, match="CUDA"):
-        c._c(t, 1)
+        c._c(t, 1, 0)
     with pytest.raises(GraftError, match="pages"):
-        c._c(t[0], 1)
+        c._c(t[0], 1, 0)
     with pytest.raises(GraftError, match="exponents"):
-        KVCache(c.k, c.v, torch.zeros((1, 2, 2, 16), dtype=torch.uint8))._c(t, 1)
+        KVCache(c.k, c.v, torch.zeros((1, 2, 2, 16), dtype=torch.uint8))._c(t, 1, 0)
     with pytest.raises(GraftError, match="bfloat16 or float8"):
-        KVCache(c.k.float(), c.v.float())._c(t, 1)
+        KVCache(c.k.float(), c.v.float())._c(t, 1, 0)
     with pytest.raises(GraftError, match="shape"):
-        binding._shaped("x", torch.zeros(3), torch.float32, (4,))
+        binding._shaped("x", torch.zeros(3), torch.float32, (4,), 0)
     with pytest.raises(GraftError, match=r"\[batch, rows, 2, 64\]"):
-        binding._token_rows("key", torch.zeros((1, 3, 2, 32), dtype=torch.bfloat16), 2, 64)
+        binding._token_rows("key", torch.zeros((1, 3, 2, 32), dtype=torch.bfloat16), 2, 64, 0)
     with pytest.raises(GraftError, match="CUDA"):
-        binding._token_rows("key", torch.zeros((1, 3, 2, 64), dtype=torch.bfloat16), 2, 64)
+        binding._token_rows("key", torch.zeros((1, 3, 2, 64), dtype=torch.bfloat16), 2, 64, 0)
     assert (BF16, E4M3) == (1, 2)
