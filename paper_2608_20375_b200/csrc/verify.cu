@@ -17,6 +17,7 @@ constexpr int kThreads = 256;  // four CTAs an SM: a sequence's cluster then spr
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;
 constexpr int kRoots = 256;          // entries of the table of 2^(j / 256)
+constexpr int kHeldWords = 2048;     // (shares of more than 65,536 pieces: bits are used again)
 constexpr int kGroups = 64;          // sums that a warp keeps of its stretch of the last row
 constexpr float kNear = 1e-5f;       // sums of fp32 exponentials are nearer than that (of the whole) to the exact ones
 constexpr uint32_t kAll = 0xFFFFFFFFu;
@@ -86,12 +87,12 @@ __device__ __forceinline__ double widen(float x) {
 }
 // 2^t in fp64 for t <= 0 or so (below -1000: 0): t = n + j / 256 + r, |r| <= 1/512, a table of 2^(j / 256) and the exponential series to the
 // third power, whose rest is below 2e-13.  The sum with 1.5 2^44 leaves 256 (n + j / 256) in its last bits.
+constexpr double kFineMagic = 26388279066624.0, kFine1 = 0.69314718055994531, kFine2 = 0.24022650695910072, kFine3 = 0.05550410866482158;  // (ln 2, its square over 2, its cube over 6)
 __device__ __forceinline__ double exp2_fine(double t, const double* roots) {
-    const double kMagic = 26388279066624.0;
-    const double m = t + kMagic, r = t - (m - kMagic);
+    const double m = t + kFineMagic, r = t - (m - kFineMagic);
     const int k = __double2loint(m);
-    double q = fma(r, 0.05550410866482158, 0.24022650695910072);  // ln 2 cubed over 6, squared over 2
-    q = fma(q, r, 0.69314718055994531);
+    double q = fma(r, kFine3, kFine2);
+    q = fma(q, r, kFine1);
     q = fma(q, r, 1.0);
     q *= roots[k & (kRoots - 1)];
     return t > -1000.0 ? __hiloint2double(__double2hiint(q) + ((k >> 8) << 20), __double2loint(q)) : 0.0;
@@ -126,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const VerifyParams 
     float* uni = (float*)(tok + p.nmax);  // [nmax]
     __shared__ uint64_t heard[2][kMaxCluster * kWarps];
     __shared__ double roots[kRoots], group[kWarps][kGroups];
-    __shared__ uint32_t filter[32];  // of the children's tokens
+    __shared__ uint32_t held[kHeldWords];  // pieces of this CTA's share that hold a token of the children
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint32_t n_cta;
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_cta));
@@ -362,22 +363,45 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const VerifyParams 
             bonus = (int)key_id(best);
             break;
         }
-        // (a piece's tokens share a bit of the filter; a piece whose bit is set looks through the children)
+        // (a piece that holds a token of the children is marked, and looks through them)
+        const auto word = [&](int st) -> uint32_t& { return held[((st - s0) >> 5) & (kHeldWords - 1)]; };
         __syncthreads();
-        if (tid < 32) filter[tid] = 0;
+        for (int i = tid; i < min(kHeldWords, (s1 - s0 + 31) / 32); i += kThreads) held[i] = 0;
         __syncthreads();
         for (int e = tid; e < n_child; e += kThreads) {
-            const int v = tok[fc + e];
-            if (v >= 0 && v < V) {
-                const int st = (v + row.skip) / kE;
-                atomicOr(&filter[(st >> 5) & 31], 1u << (st & 31));
-            }
+            const int v = tok[fc + e], st = (v + row.skip) / kE;
+            if (v >= 0 && v < V && st >= s0 && st < s1) atomicOr(&word(st), 1u << ((st - s0) & 31));
         }
         __syncthreads();
         const auto weights = [&](const float (&x)[kE], int st, double (&w)[kE]) {
+            // (four at a time, step by step: an fp64 result takes some thirty cycles, and registers are for four)
 #pragma unroll
-            for (int i = 0; i < kE; ++i) w[i] = weight(x[i]);
-            if ((filter[(st >> 5) & 31] >> (st & 31)) & 1)
+            for (int i0 = 0; i0 < kE; i0 += 4) {
+                double r[4], q[4];
+                int k[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r[i] = fma(widen(x[i0 + i]), c64, off);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i0 + i] = r[i];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q[i] = r[i] + kFineMagic, k[i] = __double2loint(q[i]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q[i] -= kFineMagic;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r[i] -= q[i];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q[i] = fma(r[i], kFine3, kFine2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q[i] = fma(q[i], r[i], kFine1);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q[i] = fma(q[i], r[i], 1.0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q[i] *= roots[k[i] & (kRoots - 1)];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    w[i0 + i] = w[i0 + i] > -1000.0 ? __hiloint2double(__double2hiint(q[i]) + ((k[i] >> 8) << 20), __double2loint(q[i])) : 0.0;
+            }
+            if (st < s1 && (word(st) >> ((st - s0) & 31)) & 1)
                 for (int e = 0; e < n_child; ++e) {
                     const int i0 = tok[fc + e] - row.first(st);
 #pragma unroll
