@@ -18,76 +18,101 @@ struct CacheRowsParams {
     int32_t* status;
 };
 
-// Rows in use and the first slot of sequence b, or no row at all when something about them is wrong.  Every warp of the block finds the
-// same by itself; the first block of a sequence reports it.
-__device__ __forceinline__ int rows_of(const CacheView& c, const int32_t* prefix_len, const int32_t* count, int rows,
-                                       int32_t* status, int b, int& base, bool report) {
-    const int n = count[b];
-    base = prefix_len[b] - 1;
-    const bool ok = n >= 0 && n <= rows && base >= 0 && cache_slots_ok(c, c.table + (size_t)b * c.width, base, (long long)base + n);
-    if (report && status && threadIdx.x == 0) status[b] = ok ? 0 : GRAFT_ST_BAD_CACHE;
-    return ok ? n : 0;
+// Rows in use and the first slot of sequence b, or no row at all when something about them is wrong.  A block finds it once; the first
+// block of a sequence reports it.
+__device__ __forceinline__ int rows_of(const CacheRowsParams& p, int b, int& base) {
+    __shared__ int use;
+    const int n = p.count[b];
+    base = p.prefix_len[b] - 1;
+    if (threadIdx.x < 32) {
+        const bool ok = n >= 0 && n <= p.rows && base >= 0 && cache_slots_ok(p.c, p.c.table + (size_t)b * p.c.width, base, (long long)base + n);
+        if (threadIdx.x == 0) {
+            use = ok ? n : 0;
+            if (p.status && blockIdx.x == 0) p.status[b] = ok ? 0 : GRAFT_ST_BAD_CACHE;
+        }
+    }
+    __syncthreads();
+    return use;
 }
 
-// Sixteen numbers a thread, head_dim / 16 threads a row (one token, one head, K or V): two 16-byte loads, the largest of the row by
-// shuffles, one 16-byte store (two into a bf16 cache).  A row's exponent follows from the bits of its largest magnitude alone.
+// What a thread does of one (row, K or V, head): sixteen numbers, head_dim / 16 threads a head.
+struct Item {
+    bool there, is_v;
+    long long at;      // of the thread's numbers in key or value
+    size_t entry;      // of the cache
+};
+__device__ __forceinline__ Item item_of(const CacheRowsParams& p, int b, int n, int base, unsigned item, int part) {
+    const CacheView& c = p.c;
+    Item t;
+    const unsigned row = item / (2u * c.kv_heads), hk = item - row * 2u * c.kv_heads;
+    t.there = (int)row < n;
+    t.is_v = hk >= (unsigned)c.kv_heads;
+    const int head = (int)hk - (t.is_v ? c.kv_heads : 0), slot = base + (int)row;
+    t.at = ((long long)b * p.rows + row) * p.stride + head * c.head_dim + part * 16;
+    const int page = t.there ? __ldg(c.table + (size_t)b * c.width + (slot >> c.page_shift)) : 0;
+    t.entry = cache_row(c, page, head, slot & ((1 << c.page_shift) - 1));
+    return t;
+}
+
+constexpr int kItems = 4;  // that a thread has under way: 128 bytes of its input
+
+// Two 16-byte loads a thread and item, the largest of the row by shuffles, one 16-byte store (two into a bf16 cache).  A row's exponent
+// follows from the bits of its largest magnitude alone.  Prompts of 4600 tokens a sequence, 8 sequences, 8 heads of 128: 303 MB written and
+// read back move at 4 to 5 TB/s.
 template <bool Q8>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(const CacheRowsParams p) {
     pdl_launch_dependents();
     pdl_wait();
     const CacheView& c = p.c;
-    const int b = blockIdx.y, tpr = c.head_dim >> 4;
+    const int b = blockIdx.y, tpr = c.head_dim >> 4, per = kThreads / tpr;
     int base;
-    const int n = rows_of(c, p.prefix_len, p.count, p.rows, p.status, b, base, blockIdx.x == 0);
+    const int n = rows_of(p, b, base);
+    const unsigned first = blockIdx.x * (unsigned)(per * kItems);
+    if (first / (2u * c.kv_heads) >= (unsigned)n) return;
     const int part = threadIdx.x & (tpr - 1);
-    const long long item = (long long)blockIdx.x * (kThreads / tpr) + threadIdx.x / tpr;
-    const int row = (int)(item / (2 * c.kv_heads)), hk = (int)(item - (long long)row * 2 * c.kv_heads);
-    const bool is_v = hk >= c.kv_heads;
-    const int head = is_v ? hk - c.kv_heads : hk;
-    const bool mine = row < n;
-    const unsigned peers = __ballot_sync(0xFFFFFFFFu, mine);  // (the threads of a row agree)
-    if (!mine) return;
-    const uint4* src = (const uint4*)((is_v ? p.value : p.key) +
-                                      2 * (((long long)b * p.rows + row) * p.stride + head * c.head_dim + part * 16));
-    const uint4 lo = __ldg(src), hi = __ldg(src + 1);
-    const int slot = base + row;
-    const int page = __ldg(c.table + (size_t)b * c.width + (slot >> c.page_shift));
-    const size_t at = cache_row(c, page, head, slot & ((1 << c.page_shift) - 1));
-    uint8_t* dst = (is_v ? c.v : c.k) + at * c.row_bytes;
-    if (!Q8) {
-        ((uint4*)dst)[2 * part] = lo;
-        ((uint4*)dst)[2 * part + 1] = hi;
-        return;
+    Item t[kItems];
+    uint4 in[kItems][2];
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        t[i] = item_of(p, b, n, base, first + i * per + threadIdx.x / tpr, part);
+        const uint4* src = (const uint4*)((t[i].is_v ? p.value : p.key) + (t[i].there ? 2 * t[i].at : 0));
+        in[i][0] = __ldg(src), in[i][1] = __ldg(src + 1);
     }
-    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-    uint32_t amax = 0;  // as the bits of a bf16: magnitudes are ordered like their bits, NaN above infinity
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t a = w[i] & 0x7FFFu, d = (w[i] >> 16) & 0x7FFFu;
-        amax = max(amax, max(a, d));
-    }
-    for (int o = tpr >> 1; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(peers, amax, o));
-    const bool bad = amax >= 0x7F80u;
-    // amax = f 2^x with f in [1, 2): amax <= 448 2^e = 1.75 2^(e + 8) iff e >= x - 8, or x - 7 where f > 1.75.  Subnormal numbers are
-    // below 2^-126, where e is at its least.
-    int e = (int)(amax >> 7) - 127 - 8 + ((amax & 0x7Fu) > 0x60u);
-    e = e < -120 ? -120 : e;
-    const float up = __int_as_float((uint32_t)(127 - (e > 0 ? e : e / 2)) << 23);             // 2^-e in two factors: -e goes up to 120,
-    const float more = __int_as_float((uint32_t)(127 - (e > 0 ? 0 : e - e / 2)) << 23);       // and both are normal numbers
-    uint32_t y[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t four = 0;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint32_t u = w[2 * i + j];
-            const float2 x = make_float2(__uint_as_float(u << 16) * up * more, __uint_as_float(u & 0xFFFF0000u) * up * more);
-            four |= (uint32_t)__nv_cvt_float2_to_fp8x2(x, __NV_SATFINITE, __NV_E4M3) << (16 * j);
+    for (int i = 0; i < kItems; ++i) {
+        uint8_t* dst = (t[i].is_v ? c.v : c.k) + t[i].entry * c.row_bytes;
+        if (!Q8) {
+            if (t[i].there) ((uint4*)dst)[2 * part] = in[i][0], ((uint4*)dst)[2 * part + 1] = in[i][1];
+            continue;
         }
-        y[i] = bad ? 0u : four;
+        const uint32_t w[8] = {in[i][0].x, in[i][0].y, in[i][0].z, in[i][0].w, in[i][1].x, in[i][1].y, in[i][1].z, in[i][1].w};
+        uint32_t amax = 0;  // as the bits of a bf16: magnitudes are ordered like their bits, NaN above infinity
+#pragma unroll
+        for (int j = 0; j < 8; ++j) amax = max(amax, max(w[j] & 0x7FFFu, (w[j] >> 16) & 0x7FFFu));
+        for (int o = tpr >> 1; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
+        if (!t[i].there) continue;
+        const bool bad = amax >= 0x7F80u;
+        // amax = f 2^x with f in [1, 2): amax <= 448 2^e = 1.75 2^(e + 8) iff e >= x - 8, or x - 7 where f > 1.75.  Subnormal numbers are
+        // below 2^-126, where e is at its least.
+        int e = (int)(amax >> 7) - 127 - 8 + ((amax & 0x7Fu) > 0x60u);
+        e = e < -120 ? -120 : e;
+        const float up = __int_as_float((uint32_t)(127 - (e > 0 ? e : e / 2)) << 23);       // 2^-e in two factors: -e goes up to 120,
+        const float more = __int_as_float((uint32_t)(127 - (e > 0 ? 0 : e - e / 2)) << 23); // and both are normal numbers
+        uint32_t y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t four = 0;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const uint32_t u = w[2 * j + k];
+                const float2 x = make_float2(__uint_as_float(u << 16) * up * more, __uint_as_float(u & 0xFFFF0000u) * up * more);
+                four |= (uint32_t)__nv_cvt_float2_to_fp8x2(x, __NV_SATFINITE, __NV_E4M3) << (16 * k);
+            }
+            y[j] = bad ? 0u : four;
+        }
+        ((uint4*)dst)[part] = make_uint4(y[0], y[1], y[2], y[3]);
+        if (part == 0) (t[i].is_v ? c.v_exp : c.k_exp)[t[i].entry] = bad ? 255 : (uint8_t)(e + 127);
     }
-    ((uint4*)dst)[part] = make_uint4(y[0], y[1], y[2], y[3]);
-    if (part == 0) (is_v ? c.v_exp : c.k_exp)[at] = bad ? 255 : (uint8_t)(e + 127);
 }
 
 template <bool Q8>
@@ -95,33 +120,43 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheRowsPar
     pdl_launch_dependents();
     pdl_wait();
     const CacheView& c = p.c;
-    const int b = blockIdx.y, tpr = c.head_dim >> 4;
+    const int b = blockIdx.y, tpr = c.head_dim >> 4, per = kThreads / tpr;
     int base;
-    const int n = rows_of(c, p.prefix_len, p.count, p.rows, p.status, b, base, blockIdx.x == 0);
+    const int n = rows_of(p, b, base);
+    const unsigned first = blockIdx.x * (unsigned)(per * kItems);
+    if (first / (2u * c.kv_heads) >= (unsigned)n) return;
     const int part = threadIdx.x & (tpr - 1);
-    const long long item = (long long)blockIdx.x * (kThreads / tpr) + threadIdx.x / tpr;
-    const int row = (int)(item / (2 * c.kv_heads)), hk = (int)(item - (long long)row * 2 * c.kv_heads);
-    const bool is_v = hk >= c.kv_heads;
-    const int head = is_v ? hk - c.kv_heads : hk;
-    if (row >= n) return;
-    const int slot = base + row;
-    const int page = __ldg(c.table + (size_t)b * c.width + (slot >> c.page_shift));
-    const size_t at = cache_row(c, page, head, slot & ((1 << c.page_shift) - 1));
-    const uint4* src = (const uint4*)((is_v ? c.v : c.k) + at * c.row_bytes);
-    uint4* dst = (uint4*)((is_v ? p.value : p.key) + 2 * (((long long)b * p.rows + row) * p.stride + head * c.head_dim + part * 16));
-    if (!Q8) {
-        const uint4 lo = src[2 * part], hi = src[2 * part + 1];
-        dst[0] = lo;
-        dst[1] = hi;
-        return;
+    Item t[kItems];
+    uint4 in[kItems][2];
+    uint32_t exps[kItems];
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        t[i] = item_of(p, b, n, base, first + i * per + threadIdx.x / tpr, part);
+        const size_t entry = t[i].there ? t[i].entry : 0;
+        const uint4* src = (const uint4*)((t[i].is_v ? c.v : c.k) + entry * c.row_bytes);
+        in[i][0] = src[Q8 ? part : 2 * part];
+        if (Q8)
+            exps[i] = (t[i].is_v ? c.v_exp : c.k_exp)[entry];
+        else
+            in[i][1] = src[2 * part + 1];
     }
-    const uint4 y = src[part];
-    uint32_t f, more;
-    e4m3_factors((is_v ? c.v_exp : c.k_exp)[at], f, more);
-    const uint2 a = e4m3x4_to_bf16(y.x, f, more), d = e4m3x4_to_bf16(y.y, f, more);
-    const uint2 g = e4m3x4_to_bf16(y.z, f, more), h = e4m3x4_to_bf16(y.w, f, more);
-    dst[0] = make_uint4(a.x, a.y, d.x, d.y);
-    dst[1] = make_uint4(g.x, g.y, h.x, h.y);
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        if (!t[i].there) continue;
+        uint4* dst = (uint4*)((t[i].is_v ? p.value : p.key) + 2 * t[i].at);
+        if (Q8) {
+            uint32_t f, more;
+            e4m3_factors(exps[i], f, more);
+            const uint4 y = in[i][0];
+            const uint2 a = e4m3x4_to_bf16(y.x, f, more), d = e4m3x4_to_bf16(y.y, f, more);
+            const uint2 g = e4m3x4_to_bf16(y.z, f, more), h = e4m3x4_to_bf16(y.w, f, more);
+            dst[0] = make_uint4(a.x, a.y, d.x, d.y);
+            dst[1] = make_uint4(g.x, g.y, h.x, h.y);
+        } else {
+            dst[0] = in[i][0];
+            dst[1] = in[i][1];
+        }
+    }
 }
 
 struct CacheKeepParams {
@@ -137,8 +172,9 @@ struct CacheKeepParams {
 
 constexpr int kKeepChunks = 4;  // 16-byte pieces a thread holds: 32 entries of 256 bytes over 128 threads
 constexpr int kKeepThreads = 128;
+constexpr int kKeepLayers = 4;  // a block's: where entries stand is found once, and the layers' loads are under way together
 
-// A block a (sequence, layer, head, K or V): all entries of the path are in registers before the first is written, so that their
+// A block a (sequence, some layers, head, K or V): all entries of the path are in registers before the first is written, so that their
 // order and overlaps do not matter.
 __global__ void __launch_bounds__(kKeepThreads) cache_keep_kernel(const CacheKeepParams p) {
     pdl_launch_dependents();
@@ -148,7 +184,7 @@ __global__ void __launch_bounds__(kKeepThreads) cache_keep_kernel(const CacheKee
     int x = blockIdx.x;
     const bool is_v = x & 1;
     x >>= 1;
-    const int head = x % c.kv_heads, layer = x / c.kv_heads;
+    const int head = x % c.kv_heads, layer0 = x / c.kv_heads * kKeepLayers, layers = min(kKeepLayers, p.layers - layer0);
     const int a = p.accept_len[b], base = p.prefix_len[b] - 1;
     __shared__ int src_row[kMaxL], dst_row[kMaxL];
     __shared__ int fine;
@@ -180,27 +216,42 @@ __global__ void __launch_bounds__(kKeepThreads) cache_keep_kernel(const CacheKee
     }
     __syncthreads();
     if (!fine) return;
-    uint8_t* rows = (is_v ? c.v : c.k) + (size_t)layer * p.layer_bytes;
+    uint8_t* rows = (is_v ? c.v : c.k) + (size_t)layer0 * p.layer_bytes;
     const int per = c.row_bytes >> 4, pieces = a * per;
-    uint4 held[kKeepChunks];
+    uint4 held[kKeepLayers][kKeepChunks];
 #pragma unroll
     for (int i = 0; i < kKeepChunks; ++i) {
         const int q = threadIdx.x + i * kKeepThreads;
-        if (q < pieces) held[i] = *((const uint4*)(rows + (size_t)src_row[q / per] * c.row_bytes) + q % per);
+        if (q < pieces) {
+            const uint8_t* from = rows + (size_t)src_row[q / per] * c.row_bytes + q % per * 16;
+#pragma unroll
+            for (int y = 0; y < kKeepLayers; ++y)
+                if (y < layers) held[y][i] = *(const uint4*)(from + y * p.layer_bytes);
+        }
     }
     uint8_t* exps = is_v ? c.v_exp : c.k_exp;
-    uint8_t e = 0;
+    uint8_t e[kKeepLayers] = {};
     if (exps) {
-        exps += (size_t)layer * p.layer_rows;
-        if (threadIdx.x < a) e = exps[src_row[threadIdx.x]];
+        exps += (size_t)layer0 * p.layer_rows;
+#pragma unroll
+        for (int y = 0; y < kKeepLayers; ++y)
+            if (y < layers && threadIdx.x < a) e[y] = exps[y * p.layer_rows + src_row[threadIdx.x]];
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kKeepChunks; ++i) {
         const int q = threadIdx.x + i * kKeepThreads;
-        if (q < pieces) *((uint4*)(rows + (size_t)dst_row[q / per] * c.row_bytes) + q % per) = held[i];
+        if (q < pieces) {
+            uint8_t* to = rows + (size_t)dst_row[q / per] * c.row_bytes + q % per * 16;
+#pragma unroll
+            for (int y = 0; y < kKeepLayers; ++y)
+                if (y < layers) *(uint4*)(to + y * p.layer_bytes) = held[y][i];
+        }
     }
-    if (exps && threadIdx.x < a) exps[dst_row[threadIdx.x]] = e;
+    if (exps && threadIdx.x < a)
+#pragma unroll
+        for (int y = 0; y < kKeepLayers; ++y)
+            if (y < layers) exps[y * p.layer_rows + dst_row[threadIdx.x]] = e[y];
 }
 
 // For next lengths that take the place of the old ones, which every block of the moves reads: a launch of its own behind them.
@@ -265,7 +316,7 @@ cudaError_t cache_rows_launch(graft_ctx* ctx, bool write, int batch, const graft
     p.key = (const uint8_t*)d_key;
     p.value = (const uint8_t*)d_value;
     p.status = d_status;
-    const int per = kThreads / (cache->head_dim / 16);
+    const int per = kItems * (kThreads / (cache->head_dim / 16));
     const long long items = (long long)rows * 2 * cache->kv_heads;
     const dim3 grid((unsigned)((items + per - 1) / per), batch);
     const bool q8 = cache->dtype == GRAFT_E4M3;
@@ -292,7 +343,7 @@ cudaError_t cache_keep_launch(graft_ctx* ctx, int batch, const graft_cache* cach
     // the new lengths come with the moves, but for an array that overlaps the old ones, which every block reads
     const bool apart = (uintptr_t)d_next_prefix >= (uintptr_t)(d_prefix_len + batch) || (uintptr_t)(d_next_prefix + batch) <= (uintptr_t)d_prefix_len;
     if (!apart) p.next_prefix = nullptr;
-    cudaError_t e = launch_pdl(cache_keep_kernel, dim3(2 * cache->kv_heads * cache->layers, batch), dim3(kKeepThreads), 0, st, p);
+    cudaError_t e = launch_pdl(cache_keep_kernel, dim3(2 * cache->kv_heads * ((cache->layers + kKeepLayers - 1) / kKeepLayers), batch), dim3(kKeepThreads), 0, st, p);
     ctx->launches += 1;
     if (e == cudaSuccess && d_next_prefix && !apart) {
         const NextPrefixParams np = {d_prefix_len, d_accept_len, d_accept_path, d_next_prefix, p.c, batch, ctx->cfg.L};
