@@ -15,6 +15,8 @@
 // (which are the second product's first operand from there), and O of head_dim columns.  One thread has one row, so maxima and sums need no
 // exchange.  O is rescaled only when a row's maximum has grown by more than 2^8 since it was last taken: weights are then up to 256,
 // which fp32 sums and bf16 hold as well as those up to 1.
+//
+// Sequences of up to eight rows a key head (single tokens) have a kernel of their own, on the same plan: see "few rows".
 #include <cuda.h>
 #include <float.h>
 
@@ -81,6 +83,7 @@ struct __align__(64) AttnParams {
     PlanStart* start;    // [gridDim of the attention kernel]
     PlanJoin* join;      // the same
     int ctas;
+    int most_share;      // shares up to this length may be made whole
     int part_rows;       // rows that a piece has room for
     int* arrivals;       // zero between calls
     float* part_o;       // [slots][D / 4][part_rows][4]
@@ -223,7 +226,7 @@ __global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const __grid_co
     // are short, units are given lengths of whole shares instead, so that a CTA has one piece, if shares two double tiles longer than equal ones
     // are enough for it.
     const int share = (total + p.ctas - 1) / p.ctas;
-    if (share > 1 && share <= 64 && p.batch <= kPlanThreads) {
+    if (share > 1 && share <= p.most_share && p.batch <= kPlanThreads) {
         int n, base, kt, R;
         of(me, n, base, kt, R);
         for (int c2 = (share + 1) & ~1; c2 <= share + 4; c2 += 2) {
@@ -1260,10 +1263,363 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
     if (warp == 8) tmem_free<false>(tmem, 512);
 }
 
+// ---- few rows ----------------------------------------------------------------------------------------------------------
+// Single tokens (up to eight rows a sequence and key head) are bound by the bytes of K and V, and a tile of 128 rows would be nearly empty.
+// Here a warp takes 16 slots at a time into the fragments of m16n8k16 products, S^T = K Q^T and O^T = V^T P^T, with slots and head_dim in
+// the long directions and the rows in the short one; e4m3 entries become bf16 in registers.  The order of head_dim inside a product is free,
+// so a lane loads pieces of 16 bytes straight into what it multiplies: of K, a quarter of those of two slots; of V, an eighth of four.  The next
+// step's K is asked for when this one's scores are done, and V when its products are: the warps of an SM then have 50 to 60 KB under way.
+// 64 sequences of 2000 to 16000 slots, 8 key heads of 128: bf16 371 us (6.36 TB/s; through the tiles of 128 rows 417), e4m3 288 us (4.1
+// TB/s; 553), which conversions bound: 500 instructions for 16 slots, three warps a scheduler to hide their latencies.  Through a ring of
+// cp.async in shared memory 543 and 295; with 8 warps of two steps 297, with 16 warps 294 (registers spill).
+constexpr int kFewRows = 8;
+
+template <int D, bool Q8>
+struct FewShape {
+    static constexpr int kBytes = Q8 ? 1 : 2;
+    static constexpr int kK = D / 4 * kBytes / 16;                                     // pieces of a slot's K that a lane has
+    static constexpr int kPiece = D / 8 * kBytes < 16 ? D / 8 * kBytes : 16;           // bytes of a piece of V (D = 64, e4m3: 8)
+    static constexpr int kV = D / 8 * kBytes / kPiece;                                 // pieces of a slot's V
+    // as many warps an SM as have room in registers for a step's K and V (16 to 64 of them) beside Q and O
+    static constexpr int kWarps = Q8 && D == 128 ? 12 : 8, kThreads = 32 * kWarps;
+    static constexpr int kCtas = D == 128 ? 1 : 2;
+    static constexpr size_t kSmem = (size_t)kWarps * kFewRows * (D + 2) * sizeof(float);
+};
+
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+// bytes ia and ib (0 .. 3 of a, 4 .. 7 of b) as e4m3 -> bf16 times 2^-120.  A byte with its sign eight times above it, four places up, has
+// sign, exponent and mantissa where bf16 has them, and signs in the exponent's upper bits, which go.
+__device__ __forceinline__ uint32_t e4m3_pair_small(uint32_t a, uint32_t b, int ia, int ib) {
+    uint32_t x;  // (__byte_perm has no signs)
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(x) : "r"(a), "r"(b), "r"(ia | (ia | 8) << 4 | ib << 8 | (ib | 8) << 12));
+    return (x << 4) & 0x87F087F0u;
+}
+__device__ __forceinline__ uint4 load_once(const uint8_t* p) {
+    uint4 r;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
+}
+template <int D, bool Q8>
+__global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kCtas) few_attn_kernel(const __grid_constant__ AttnParams p) {
+    using S = FewShape<D, Q8>;
+    constexpr int kBytes = S::kBytes, kK = S::kK, kV = S::kV, kPiece = S::kPiece, kWarps = S::kWarps;
+    constexpr int kCk = 16 / kBytes, kCv = kPiece / kBytes;  // numbers of a piece
+    extern __shared__ __align__(16) float few_sm[];  // [warps][rows][D], then [warps][rows][2]
+    float* const sm_ml = few_sm + kWarps * kFewRows * D;
+    __shared__ Piece pc;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q4 = lane & 3;
+    const CacheView& c = p.c;
+    const int shift = c.page_shift, low = (1 << shift) - 1;
+    const float c2 = p.c2, most = kMostGrowth / c2;
+    pdl_launch_dependents();
+    pdl_wait();
+    Walk walk;
+    if (tid == 0) walk.begin(p, blockIdx.x);
+    for (;;) {
+        if (tid == 0) {
+            Piece x;
+            if (!walk.next(x)) x.T = 0;
+            pc = x;
+        }
+        __syncthreads();
+        const int T = pc.T;
+        if (T == 0) break;
+        const int h = pc.h, b = pc.s - 1, base = pc.base, end = pc.end, R = pc.rows, first0 = pc.first;
+        const int32_t* table = c.table + (size_t)b * c.width;
+        // A step's 16 slots lie in one page; the warps take steps by turns.
+        const int all = min(8 * T, (end - first0 + 15) / 16), steps = warp < all ? (all - warp + kWarps - 1) / kWarps : 0;
+        const auto slot_of = [&](int step) { return first0 + (warp + step * kWarps) * 16; };
+        const auto page_of = [&](int step) { return __ldg(table + (slot_of(min(step, steps - 1)) >> shift)); };
+        const auto row_at = [&](int step, int page) { return cache_row(c, page, h, slot_of(step) & low); };
+        uint4 kr[2][kK], k_exps = {}, v_exps = {};  // (exponents of all 16 slots)
+        uint32_t vr[4][4 * kV];
+        const auto bring_k = [&](size_t row0) {
+            const uint8_t* const k = c.k + (row0 + g) * (D * kBytes) + q4 * 16;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int y = 0; y < kK; ++y) kr[i][y] = load_once(k + i * 8 * (D * kBytes) + y * 64);
+            }
+            if (Q8) k_exps = __ldg((const uint4*)(c.k_exp + row0));
+        };
+        const auto bring_v = [&](size_t row0) {
+            const uint8_t* const v = c.v + (row0 + 2 * q4) * (D * kBytes) + g * kPiece;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int y = 0; y < kV; ++y) {
+                    const uint8_t* const from = v + ((i & 1) + 8 * (i >> 1)) * (D * kBytes) + y * 8 * kPiece;
+                    if (kPiece == 16) {
+                        const uint4 u = load_once(from);
+                        vr[i][4 * y] = u.x, vr[i][4 * y + 1] = u.y, vr[i][4 * y + 2] = u.z, vr[i][4 * y + 3] = u.w;
+                    } else {
+                        const uint2 u = __ldg((const uint2*)from);
+                        vr[i][0] = u.x, vr[i][1] = u.y, vr[i][2] = vr[i][3] = 0;
+                    }
+                }
+            if (Q8) v_exps = __ldg((const uint4*)(c.v_exp + row0));
+        };
+        size_t row0 = 0;
+        int page = 0;
+        if (steps > 0) {
+            row0 = row_at(0, page_of(0));
+            page = page_of(1);
+            bring_k(row0);
+            bring_v(row0);
+        }
+        // rows of Q: lane (g, q4) has row g of the second operand, in the order of K's pieces
+        uint32_t qf[D / 8];
+        {
+            const bool live = g < R;
+            const int node = live ? g / p.group : 0, hg = live ? g - node * p.group : 0;
+            const uint8_t* from = p.q + 2 * (((long long)b * p.rows + node) * p.q_stride + (long long)(h * p.group + hg) * D);
+            const uint32_t keep = live ? p.q_keep : 0u;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                const int d = 8 * i / kCk * (4 * kCk) + q4 * kCk + 8 * i % kCk;
+                uint4 u = __ldg((const uint4*)(from + 2 * d));
+                u.x = (u.x ^ p.q_flip) & keep, u.y = (u.y ^ p.q_flip) & keep, u.z = (u.z ^ p.q_flip) & keep, u.w = (u.w ^ p.q_flip) & keep;
+                qf[4 * i] = u.x, qf[4 * i + 1] = u.y, qf[4 * i + 2] = u.z, qf[4 * i + 3] = u.w;
+            }
+        }
+        float o[D / 16][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, upto[2] = {-INFINITY, -INFINITY}, off[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
+        for (int step = 0; step < steps; ++step) {
+            const int s0 = slot_of(step);
+            const bool more_steps = step + 1 < steps;
+            const size_t row1 = row_at(step + 1, page);
+            page = page_of(step + 2);
+            // factors of K's slots g, g + 8: 2^(e + 120), a second one where that is above bf16's largest (rare, and not numbers)
+            uint32_t f[2] = {0, 0}, ke[2] = {0, 0};
+            float more[2] = {1.0f, 1.0f};
+            bool large = false;
+            if (Q8) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    ke[i] = __byte_perm(i ? k_exps.z : k_exps.x, i ? k_exps.w : k_exps.y, g) & 255;
+                    f[i] = (ke[i] + 120) * 0x00800080u;
+                }
+                large = __any_sync(0xFFFFFFFFu, max(ke[0], ke[1]) > 134);
+                if (large)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t x;
+                        e4m3_factors(ke[i], f[i], x);
+                        more[i] = __uint_as_float(x << 16);
+                    }
+            }
+            // ---- scores: rows 2 q4, 2 q4 + 1 at slots g, g + 8
+            float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s2[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int y = 0; y < kK; ++y) {
+                uint2 a[4 / kBytes][2];
+#pragma unroll
+                for (int x = 0; x < 4 / kBytes; ++x)  // four numbers of the lane's a product
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t w[4] = {kr[i][y].x, kr[i][y].y, kr[i][y].z, kr[i][y].w};
+                        a[x][i] = Q8 ? make_uint2(bf16x2_mul(e4m3_pair_small(w[x], 0, 0, 1), f[i]), bf16x2_mul(e4m3_pair_small(w[x], 0, 2, 3), f[i]))
+                                     : make_uint2(w[2 * x & 3], w[(2 * x + 1) & 3]);
+                    }
+#pragma unroll
+                for (int x = 0; x < 4 / kBytes; ++x) {
+                    const int ks = y * (4 / kBytes) + x;
+                    mma_16816(x & 1 ? s2 : s, a[x][0].x, a[x][1].x, a[x][0].y, a[x][1].y, qf[2 * ks], qf[2 * ks + 1]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] += s2[i];
+            if (Q8 && large)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] *= more[i >> 1];
+            if (more_steps) bring_k(row1);
+            // the same for V's pairs of slots; second factors go to the weights (slots g, g + 8)
+            uint32_t f2[2] = {0, 0}, x[2] = {0, 0};  // (x: the exponents of two slots)
+            float big[2] = {1.0f, 1.0f};
+            bool large_v = false;
+            if (Q8) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    x[i] = __byte_perm(i ? v_exps.z : v_exps.x, i ? v_exps.w : v_exps.y, 2 * q4 | (2 * q4 + 1) << 8) & 0x00FF00FFu;
+                    f2[i] = (x[i] + 0x00780078u) << 7;
+                }
+                large_v = __any_sync(0xFFFFFFFFu, ((x[0] + 0x00790079u) | (x[1] + 0x00790079u)) & 0x01000100u);  // (one above 134)
+                if (large_v)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t fa, fb, y;
+                        e4m3_factors(x[i] & 255, fa, y), e4m3_factors(x[i] >> 16, fb, y);
+                        f2[i] = __byte_perm(fa, fb, 0x5410);
+                        const uint32_t pair = __shfl_sync(0xFFFFFFFFu, x[i], g >> 1);
+                        e4m3_factors(g & 1 ? pair >> 16 : pair & 255, fa, y);
+                        big[i] = __uint_as_float(y << 16);
+                    }
+            }
+            const bool masked = s0 + 16 > base;
+            bool spoilt[4] = {false, false, false, false};
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int slot = s0 + g + 8 * (i >> 1), r = 2 * q4 + (i & 1), j = slot - base, node = r / p.group;
+                    bool seen = slot < end && r < R;
+                    if (seen && j >= 0)
+                        seen = p.mask == nullptr ? j <= node
+                                                 : j < 32 * p.words && ((p.mask[((size_t)b * p.nmax + node) * p.words + (j >> 5)] >> (j & 31)) & 1);
+                    s[i] = seen ? s[i] : -INFINITY;
+                }
+                // V of slots that are not there is taken out, and of new slots that are not numbers: what of those is seen is added in the end
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int slot = s0 + 2 * q4 + (i & 1) + 8 * (i >> 1);
+                    bool bad = Q8 && (x[i >> 1] >> (16 * (i & 1)) & 255) > 246;  // (up to 480 2^119 is below 2^128)
+                    if (!Q8)
+#pragma unroll
+                        for (int x = 0; x < 4 * kV; ++x) bad = bad || not_finite2(vr[i][x]);
+                    // (a slot's lanes differ in g: any of them)
+                    const unsigned who = __ballot_sync(0xFFFFFFFFu, bad && slot >= base && slot < end);
+                    spoilt[i] = (who & (0x11111111u << q4)) != 0;
+                    if (slot >= end || spoilt[i]) {
+#pragma unroll
+                        for (int x = 0; x < 4 * kV; ++x) vr[i][x] = 0;
+                        f2[i >> 1] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+                    }
+                }
+            }
+            // ---- weights, against the maximum known before as long as it has not grown by more than 2^8
+            if (__any_sync(0xFFFFFFFFu, fmaxf(s[0], s[2]) > upto[0] || fmaxf(s[1], s[3]) > upto[1])) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float x = fmaxf(s[i], s[i + 2]);
+                    for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, d));
+                    const float now = fmaxf(m[i], x), k = m[i] > -INFINITY ? ex2_approx((m[i] - now) * c2) : 1.0f;
+                    m[i] = now;
+                    upto[i] = now + most;
+                    off[i] = now > -INFINITY ? -now * c2 : 0.0f;
+                    l[i] *= k;
+#pragma unroll
+                    for (int y = 0; y < D / 16; ++y) o[y][i] *= k, o[y][i + 2] *= k;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[i] = ex2_approx(fmaf(s[i], c2, off[i & 1]));
+                l[i & 1] += s[i];
+            }
+            // P^T as the second operand: rows where the slots were
+            float e[4] = {s[0], s[1], s[2], s[3]};
+            if (Q8 && large_v)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] *= big[i >> 1];
+            const uint32_t pb0 = transpose_8x8(pack_bf16(e[0], e[1])), pb1 = transpose_8x8(pack_bf16(e[2], e[3]));
+            // ---- O^T += V^T P^T: rows of the first operand are head_dim, two numbers of the lane's D / 8 a product
+#pragma unroll
+            for (int y0 = 0; y0 < D / 16; y0 += 4) {
+                uint32_t a[4][2][2];  // [product][slot pair][number]
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            const int y = y0 + x, byte = (2 * y + z) & 3;
+                            if (Q8) {
+                                a[x][i][z] = bf16x2_mul(e4m3_pair_small(vr[2 * i][y / 2], vr[2 * i + 1][y / 2], byte, 4 + byte), f2[i]);
+                            } else
+                                a[x][i][z] = __byte_perm(vr[2 * i][y], vr[2 * i + 1][y], z ? 0x7632 : 0x5410);
+                        }
+#pragma unroll
+                for (int x = 0; x < 4; ++x) mma_16816(o[y0 + x], a[x][0][0], a[x][0][1], a[x][1][0], a[x][1][1], pb0, pb1);
+            }
+            if (more_steps) bring_v(row1);
+            // number y of the lane's of V: o[y / 2][..], [rows + 2 (y & 1)]
+            const auto dim = [&](int y) { return y / kCv * (8 * kCv) + g * kCv + y % kCv; };
+            // ---- new slots whose V is not a number: to the rows that see them
+            if (masked && __any_sync(0xFFFFFFFFu, spoilt[0] || spoilt[1] || spoilt[2] || spoilt[3])) {
+#pragma unroll 1
+                for (int i = 0; i < 16; ++i) {
+                    const int owner = (i & 7) >> 1, which = (i & 1) + 2 * (i >> 3);
+                    const bool bad = __shfl_sync(0xFFFFFFFFu, which == 0 ? spoilt[0] : which == 1 ? spoilt[1] : which == 2 ? spoilt[2] : spoilt[3], owner);
+                    if (!bad) continue;
+                    const size_t r = row0 + i;
+                    uint32_t fv = 0, mv = kOneBf16x2;
+                    if (Q8) e4m3_factors(__ldg(c.v_exp + r), fv, mv);
+                    const float w0 = __shfl_sync(0xFFFFFFFFu, i < 8 ? s[0] : s[2], (i & 7) * 4 + q4);
+                    const float w1 = __shfl_sync(0xFFFFFFFFu, i < 8 ? s[1] : s[3], (i & 7) * 4 + q4);
+#pragma unroll
+                    for (int y = 0; y < D / 8; ++y) {
+                        const uint8_t* from = c.v + (r * D + dim(y)) * kBytes;
+                        float v;
+                        if (Q8)
+                            v = __uint_as_float(e4m3x4_to_bf16(*from, fv, mv).x << 16);
+                        else
+                            v = __uint_as_float((uint32_t) * (const uint16_t*)from << 16);
+                        if (w0 > 0.0f) o[y / 2][2 * (y & 1)] += w0 * v;
+                        if (w1 > 0.0f) o[y / 2][2 * (y & 1) + 1] += w1 * v;
+                    }
+                }
+            }
+            row0 = row1;
+        }
+        // ---- the warps' sums are joined
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float x = l[i];
+            for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
+            const int r = 2 * q4 + i;
+            if (g == 0) {
+                sm_ml[(warp * kFewRows + r) * 2] = m[i] > -INFINITY ? m[i] * c2 : -INFINITY;
+                sm_ml[(warp * kFewRows + r) * 2 + 1] = x;
+            }
+#pragma unroll
+            for (int y = 0; y < D / 16; ++y)
+                *(float2*)&few_sm[(warp * kFewRows + r) * D + 2 * y / kCv * (8 * kCv) + g * kCv + 2 * y % kCv] = make_float2(o[y][i], o[y][i + 2]);
+        }
+        __syncthreads();
+        const bool whole = pc.whole;
+        const size_t slot = 2 * (size_t)blockIdx.x + pc.head;
+        for (int x = tid; x < R * (D / 4); x += S::kThreads) {
+            const int r = x / (D / 4), d = x % (D / 4) * 4;
+            float mm = -INFINITY, ll = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) mm = fmaxf(mm, sm_ml[(w * kFewRows + r) * 2]);
+            float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float mw = sm_ml[(w * kFewRows + r) * 2], lw = sm_ml[(w * kFewRows + r) * 2 + 1];
+                const float k = mw > -INFINITY ? ex2_approx(mw - mm) : 0.0f;
+                ll += k * lw;
+                const float4 v = *(const float4*)&few_sm[(w * kFewRows + r) * D + d];
+                sum.x += k * v.x, sum.y += k * v.y, sum.z += k * v.z, sum.w += k * v.w;
+            }
+            const int node = r / p.group;
+            const size_t out_row = ((size_t)b * p.rows + node) * p.q_heads + h * p.group + (r - node * p.group);
+            if (whole) {
+                const float inv = ll != 0.0f ? 1.0f / ll : 1.0f;
+                *(uint2*)(p.out + out_row * D + d) = make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
+                if (p.lse && d == 0) p.lse[out_row] = log_sum(mm, ll);
+            } else {
+                ((float4*)p.part_o)[(slot * (D / 4) + d / 4) * p.part_rows + r] = sum;
+                if (d == 0) p.part_ml[slot * p.part_rows + r] = make_float2(mm, ll);
+            }
+        }
+        __syncthreads();  // (the sums and the piece are read)
+    }
+}
+
 // ---- joining the pieces ----------------------------------------------------------------------------------------------
 constexpr int kJoinThreads = 256;
 constexpr int kJoinRows = 32;
-constexpr int kJoinMost = 160;  // pieces of a block's rows: no more than CTAs and units (three at most)
+constexpr int kJoinMost = 320;  // pieces of a block's rows: no more than CTAs and units (three at most)
 
 struct JoinPiece {
     int slot, shift, lo, hi;  // rows lo .. hi - 1 of the block are rows lo + shift .. of the piece
@@ -1417,13 +1773,20 @@ bool encode_map(CUtensorMap* map, const void* base, bool q8, int D, uint64_t row
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool few_rows(int group, int rows, int shared) { return shared == 0 && (long long)rows * group <= kFewRows; }
+int attn_ctas(const graft_ctx* ctx, bool q8, int head_dim, int group, int rows, int shared) {
+    const int ctas = head_dim == 128 ? (q8 ? FewShape<128, true>::kCtas : FewShape<128, false>::kCtas)
+                                     : (q8 ? FewShape<64, true>::kCtas : FewShape<64, false>::kCtas);
+    return ctx->num_sms * (few_rows(group, rows, shared) ? ctas : 1);
+}
+
 struct AttnSizes {
     int part_rows;
     size_t o_seq, o_start, o_join, o_ml, o_o, total;
 };
-AttnSizes attn_sizes(const graft_ctx* ctx, int batch, int kv_heads, int head_dim, int group, int rows, int shared) {
+AttnSizes attn_sizes(const graft_ctx* ctx, int ctas, int batch, int kv_heads, int head_dim, int group, int rows, int shared) {
     const auto units = [&](long long nodes) { return (size_t)kv_heads * (size_t)((nodes * group + kUnitRows - 1) / kUnitRows); };
-    const size_t slots = shared > 0 ? units((long long)batch * rows) + (size_t)batch * units(rows) + ctx->num_sms : 2 * (size_t)ctx->num_sms;
+    const size_t slots = shared > 0 ? units((long long)batch * rows) + (size_t)batch * units(rows) + ctas : 2 * (size_t)ctas;
     AttnSizes z;
     z.part_rows = shared > 0 ? kUnitRows : (int)min((long long)kUnitRows, ((long long)rows * group + 31) / 32 * 32);
     size_t off = 256;
@@ -1433,28 +1796,27 @@ AttnSizes attn_sizes(const graft_ctx* ctx, int batch, int kv_heads, int head_dim
         return o;
     };
     z.o_seq = take((size_t)(batch + 1) * sizeof(PlanSeq));
-    z.o_start = take((size_t)ctx->num_sms * sizeof(PlanStart));
-    z.o_join = take((size_t)(ctx->num_sms + 1) * sizeof(PlanJoin));
+    z.o_start = take((size_t)ctas * sizeof(PlanStart));
+    z.o_join = take((size_t)(ctas + 1) * sizeof(PlanJoin));
     z.o_ml = take(slots * z.part_rows * sizeof(float2));
     z.o_o = take(slots * z.part_rows * head_dim * sizeof(float));
     z.total = off;
     return z;
 }
 
-template <int D, bool Q8, bool kOne>
-cudaError_t launch_attn(graft_ctx* ctx, const AttnParams& p, cudaStream_t st) {
-    using S = Shape<D, Q8, kOne>;
-    constexpr int kReady = 1 << ((D == 128) + 2 * Q8 + 4 * kOne);
+// The plan, the attention kernel, the joining of what it cut.
+template <int D, typename Kernel>
+cudaError_t launch_three(graft_ctx* ctx, const AttnParams& p, Kernel kernel, int threads, size_t smem, uint32_t ready, cudaStream_t st) {
     cudaError_t e;
-    if (!(ctx->attn_ready & kReady)) {
-        e = allow_smem((const void*)tree_attn_kernel<D, Q8, kOne>, S::kSmem);
+    if (!(ctx->attn_ready & ready)) {
+        e = allow_smem((const void*)kernel, smem);
         if (e != cudaSuccess) return e;
-        ctx->attn_ready |= kReady;
+        ctx->attn_ready |= ready;
     }
     e = launch_pdl(attn_plan_kernel, dim3(p.batch), dim3(kPlanThreads), 0, st, p);
     if (e != cudaSuccess) return e;
     ctx->launches += 1;
-    e = launch_pdl(tree_attn_kernel<D, Q8, kOne>, dim3(p.ctas), dim3(S::kThreads), S::kSmem, st, p);
+    e = launch_pdl(kernel, dim3(p.ctas), dim3(threads), smem, st, p);
     if (e != cudaSuccess) return e;
     ctx->launches += 1;
     const long long most = (long long)p.rows * p.group;  // rows of a sequence and key head
@@ -1467,11 +1829,24 @@ cudaError_t launch_attn(graft_ctx* ctx, const AttnParams& p, cudaStream_t st) {
     ctx->launches += 1;
     return e;
 }
+template <int D, bool Q8, bool kOne>
+cudaError_t launch_attn(graft_ctx* ctx, const AttnParams& p, cudaStream_t st) {
+    using S = Shape<D, Q8, kOne>;
+    return launch_three<D>(ctx, p, tree_attn_kernel<D, Q8, kOne>, S::kThreads, S::kSmem, 1u << ((D == 128) + 2 * Q8 + 4 * kOne), st);
+}
+template <int D, bool Q8>
+cudaError_t launch_any(graft_ctx* ctx, const AttnParams& p, cudaStream_t st) {
+    const long long rows = (long long)p.rows * p.group;
+    if (few_rows(p.group, p.rows, p.shared))
+        return launch_three<D>(ctx, p, few_attn_kernel<D, Q8>, FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kSmem, 256u << ((D == 128) + 2 * Q8), st);
+    return p.shared == 0 && rows <= kTile ? launch_attn<D, Q8, true>(ctx, p, st) : launch_attn<D, Q8, false>(ctx, p, st);
+}
 
 }  // namespace
 
 size_t tree_attn_scratch_bytes(const graft_ctx* ctx, int batch, const graft_cache* cache, int q_heads, int rows, int shared) {
-    return attn_sizes(ctx, batch, cache->kv_heads, cache->head_dim, q_heads / cache->kv_heads, rows, shared).total;
+    const int group = q_heads / cache->kv_heads, ctas = attn_ctas(ctx, cache->dtype == GRAFT_E4M3, cache->head_dim, group, rows, shared);
+    return attn_sizes(ctx, ctas, batch, cache->kv_heads, cache->head_dim, group, rows, shared).total;
 }
 
 cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache, int layer, int q_heads, int rows, long long q_stride,
@@ -1504,8 +1879,8 @@ cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache
     p.nmax = ctx->nmax;
     p.words = ctx->mask_words;
     p.batch = batch;
-    p.ctas = ctx->num_sms;
-    const AttnSizes z = attn_sizes(ctx, batch, cache->kv_heads, cache->head_dim, p.group, rows, shared);
+    p.ctas = attn_ctas(ctx, q8, cache->head_dim, p.group, rows, shared);
+    const AttnSizes z = attn_sizes(ctx, p.ctas, batch, cache->kv_heads, cache->head_dim, p.group, rows, shared);
     uint8_t* base = (uint8_t*)scratch;
     p.head = (PlanHead*)base;
     p.seq = (PlanSeq*)(base + z.o_seq);
@@ -1515,11 +1890,9 @@ cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache
     p.part_o = (float*)(base + z.o_o);
     p.arrivals = ctx->w_attn_n;
     p.part_rows = z.part_rows;
-    const bool one = shared == 0 && (long long)rows * p.group <= kTile;
-    const auto launch = cache->head_dim == 128 ? (q8 ? (one ? launch_attn<128, true, true> : launch_attn<128, true, false>)
-                                                     : (one ? launch_attn<128, false, true> : launch_attn<128, false, false>))
-                                               : (q8 ? (one ? launch_attn<64, true, true> : launch_attn<64, true, false>)
-                                                     : (one ? launch_attn<64, false, true> : launch_attn<64, false, false>));
+    p.most_share = few_rows(p.group, rows, shared) ? 0 : 64;
+    const auto launch = cache->head_dim == 128 ? (q8 ? launch_any<128, true> : launch_any<128, false>)
+                                               : (q8 ? launch_any<64, true> : launch_any<64, false>);
     return launch(ctx, p, st);
 }
 
