@@ -7,6 +7,10 @@ its own library context (scratch memory) and CUDA stream: while the target model
 builder of another runs, and the tree kernel, which keeps fewer CTAs than the GPU has SMs, shares the GPU with the
 verifier's kernels.  This module only orders the calls; every step still runs in the library's kernels (the
 verifier is the caller's).
+
+A verifier may answer with the target's likeliest tokens (the greedy walk) or with its logits and random numbers (`Sampled`: the walk that
+keeps the target's distribution).  A micro-batch that holds the target's key/value cache gives the verifier its attention (`attend`), and
+after the walk the accepted nodes' entries are moved up behind the prefix.
 """
 from __future__ import annotations
 
@@ -15,7 +19,7 @@ from typing import Callable, Sequence
 
 import torch
 
-from .binding import Graft, TreeOut
+from .binding import Graft, GraftError, KVCache, TreeOut
 
 
 @dataclass
@@ -30,6 +34,12 @@ class MicroBatch:
     accept_path: torch.Tensor = None
     bonus_token: torch.Tensor = None
     rounds_done: int = field(default=0)
+    # the target's cache and its page table [batch, pages] (None: the verifier keeps its own); after every walk prefix_len [batch] is
+    # moved on by the committed tokens, status [batch] is the last call's
+    cache: KVCache = None
+    table: torch.Tensor = None
+    prefix_len: torch.Tensor = None
+    status: torch.Tensor = None
 
     def __post_init__(self):
         dev = torch.device("cuda", torch.cuda.current_device())
@@ -44,12 +54,35 @@ class MicroBatch:
             self.accept_path = torch.empty((self.batch, self.L), dtype=i32, device=dev)
         if self.bonus_token is None:
             self.bonus_token = torch.empty(self.batch, dtype=i32, device=dev)
+        if self.cache is not None:
+            if self.table is None or self.prefix_len is None:
+                raise GraftError("a micro-batch with a cache has a table and prefix lengths")
+            if self.status is None:
+                self.status = torch.zeros(self.batch, dtype=i32, device=dev)
+
+    def attend(self, layer, q, key, value, out, lse=None, scale=None, shared=0):
+        """One layer of the target over this round's trees: the nodes' new entries go into the cache, q [batch, rows, q_heads, head_dim]
+        sees the prefix and the nodes above its own."""
+        if self.cache is None:
+            raise GraftError("the micro-batch has no cache")
+        self.graft.cache_write(self.cache, layer, self.table, self.prefix_len, self.out.n_nodes, key, value, self.status)
+        self.graft.tree_attention(self.cache, layer, self.table, q, self.prefix_len, self.out.n_nodes, self.out.mask, out, lse, scale, shared,
+                                  self.status)
+
+
+@dataclass
+class Sampled:
+    """What a verifier that samples answers: the target's logits behind every node [batch, rows, V], numbers in [0, 1)
+    [batch, n_max], temperatures [batch] (None: 1)."""
+    logits: torch.Tensor
+    uniform: torch.Tensor
+    temperature: torch.Tensor = None
 
 
 # draft(mb_index, round) -> dict(logits, hidden, root_token, hist, prefix_len, fixed_budget) of device tensors
 DraftFn = Callable[[int, int], dict]
-# verify(mb_index, round, tree_out) -> target_next [batch, n_max] int32 device tensor, enqueued on the current stream
-VerifyFn = Callable[[int, int, TreeOut], torch.Tensor]
+# verify(mb_index, round, tree_out) -> target_next [batch, n_max] int32 device tensor, or Sampled; enqueued on the current stream
+VerifyFn = Callable[[int, int, TreeOut], "torch.Tensor | Sampled"]
 
 
 def run_rounds(micro: Sequence[MicroBatch], n_rounds: int, draft: DraftFn, verify: VerifyFn, overlap: bool = True,
@@ -72,9 +105,15 @@ def run_rounds(micro: Sequence[MicroBatch], n_rounds: int, draft: DraftFn, verif
             with torch.cuda.stream(mb.stream if overlap else cur):
                 x = draft(i, r)
                 mb.graft.build_trees(x["logits"], x.get("hidden"), x["root_token"], x.get("hist"),
-                                     x.get("prefix_len"), x.get("fixed_budget"), mb.out)
-                tn = verify(i, r, mb.out)
-                mb.graft.accept(mb.out, tn, mb.accept_len, mb.accept_path, mb.bonus_token)
+                                     x.get("prefix_len", mb.prefix_len), x.get("fixed_budget"), mb.out)
+                answer = verify(i, r, mb.out)
+                if isinstance(answer, Sampled):
+                    mb.graft.verify(mb.out, answer.logits, answer.temperature, answer.uniform, mb.accept_len, mb.accept_path,
+                                    mb.bonus_token)
+                else:
+                    mb.graft.accept(mb.out, answer, mb.accept_len, mb.accept_path, mb.bonus_token)
+                if mb.cache is not None:
+                    mb.graft.cache_keep(mb.cache, mb.table, mb.prefix_len, mb.accept_len, mb.accept_path, mb.prefix_len, mb.status)
                 mb.rounds_done += 1
                 if after_round is not None:
                     after_round(i, r, mb)

@@ -97,3 +97,81 @@ def test_rows_of_q_with_a_stride(dtype, rows):
         g.tree_attention(c, 0, _i32(table), qq, _i32([151] * B), _i32([rows] * B), None, out)
         outs.append(out)
     assert torch.equal(*outs) and outs[0].abs().sum() > 0
+
+
+@pytest.mark.parametrize("dtype", [BF, Q8])
+def test_micro_batches_with_caches(dtype):
+    """Two micro-batches around a target of one attention layer, each with its cache: on streams of their own the rounds' results are the
+    sequential schedule's, and those of the calls made one by one; the cache holds the committed tokens."""
+    from paper_2608_20375_b200 import BF16, E4M3, Graft, KVCache, MicroBatch, Sampled, join, run_rounds
+    B, L, V, K, Hq, Hk, D, page, rounds = 3, 6, 300, 5, 4, 2, 64, 16, 4
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    r = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    E = Hq * D
+    emb, head = r(V, E), 0.5 * r(E, V)
+    w = [(r(E, h * D) / E ** 0.5) for h in (Hq, Hk, Hk)]
+    table = torch.arange(B * 8, dtype=torch.int32, device="cuda").view(B, 8)
+    drafts = [[3.0 * r(B, L, V) for _ in range(rounds)] for _ in range(2)]
+    uniform = [[torch.rand((B, 64), generator=gen, device="cuda") for _ in range(rounds)] for _ in range(2)]
+
+    def run(how):
+        log, micro, roots = [], [], []
+        for i in range(2):
+            g = Graft(V, L, K, 16, 8, B, 4, 24, 4, 0.0)
+            c = KVCache.alloc(1, B * 8, Hk, page, D, E4M3 if dtype is Q8 else BF16)
+            micro.append(MicroBatch(g, B, L, cache=c, table=table, prefix_len=_i32([1, 1, 1])))
+            roots.append(_i32([3, 5 + i, 7]))
+
+        def draft(i, k):
+            mb = micro[i]
+            root = roots[i] if k == 0 else mb.bonus_token.clone()
+            return dict(logits=drafts[i][k].to(BF), root_token=root, fixed_budget=_i32([20, 4, 24]))
+
+        def verify(i, k, out):
+            mb = micro[i]
+            x = emb[out.token.long().clamp(0)]
+            q, key, value = ((x @ m).to(BF).view(B, mb.graft.nmax, -1, D) for m in w)
+            o = torch.zeros((B, mb.graft.nmax, Hq, D), dtype=BF, device="cuda")
+            if how == "by hand":
+                mb.graft.cache_write(mb.cache, 0, table, mb.prefix_len, out.n_nodes, key, value)
+                mb.graft.tree_attention(mb.cache, 0, table, q, mb.prefix_len, out.n_nodes, out.mask, o)
+            else:
+                mb.attend(0, q, key, value, o)
+            z = (x + o.float().view(B, mb.graft.nmax, E)) @ head
+            z.view(B, -1).scatter_add_(1, out.parent.long().clamp(0) * V + out.token.long().clamp(0), torch.where(out.parent >= 0, 9.0, 0.0))
+            return Sampled(z, uniform[i][k][:, :mb.graft.nmax].contiguous())
+
+        def after(i, k, mb):
+            log.append([t.clone() for t in (mb.accept_len, mb.accept_path, mb.bonus_token, mb.prefix_len, mb.status)])
+
+        if how == "by hand":
+            for k in range(rounds):
+                for i, mb in enumerate(micro):
+                    x = draft(i, k)
+                    mb.graft.build_trees(x["logits"], None, x["root_token"], None, mb.prefix_len, x["fixed_budget"], mb.out)
+                    a = verify(i, k, mb.out)
+                    mb.graft.verify(mb.out, a.logits, a.temperature, a.uniform, mb.accept_len, mb.accept_path, mb.bonus_token)
+                    mb.graft.cache_keep(mb.cache, table, mb.prefix_len, mb.accept_len, mb.accept_path, mb.prefix_len, mb.status)
+                    after(i, k, mb)
+        else:
+            run_rounds(micro, rounds, draft, verify, overlap=how == "overlapped", after_round=after)
+            join(micro)
+        torch.cuda.synchronize()
+        return [[t.cpu() for t in x] for x in log], micro
+
+    want, micro = run("by hand")
+    for how in ("sequential", "overlapped"):
+        got, other = run(how)
+        for a, b in zip(want, got):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+        for a, b in zip(micro, other):
+            n = int(a.prefix_len.min()) - 1
+            kb = [torch.empty((B, n, Hk, D), dtype=BF, device="cuda") for _ in range(4)]
+            for mb, x in ((a, kb[:2]), (b, kb[2:])):
+                mb.graft.cache_read(mb.cache, 0, table, _i32([1] * B), _i32([n] * B), *x)
+            torch.cuda.synchronize()
+            assert torch.equal(kb[0], kb[2]) and torch.equal(kb[1], kb[3])
+    for i, mb in enumerate(micro):
+        lens = sum(x[0] for x in want[i::2]) + rounds + 1
+        assert torch.equal(lens.int(), mb.prefix_len.cpu()) and not mb.status.any()
+    assert sum(int(x[0].sum()) for x in want) > 0
