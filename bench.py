@@ -545,6 +545,76 @@ def run_overlap(args):
     }))
 
 
+def run_verifier(args):
+    """--verifier: rounds that build the workload's trees, write the nodes' entries into the target's cache, attend over it in every layer, walk
+    the trees by sampling and move the accepted entries; each part and the round timed on the device.  Prints its own JSON line (not the
+    benchmark's metric)."""
+    from paper_2608_20375_b200 import BF16, E4M3, Graft, KVCache, MicroBatch, Sampled, join, run_rounds
+
+    w = gi.WORKLOADS[args.workload]
+    dev = torch.device("cuda", 0)
+    torch.cuda.set_device(dev)
+    layers, q_heads, kv_heads, dim, page, prefix = 4, 32, 8, 128, 64, 2000
+    dt = {"f32": 0, "bf16": 1}
+    tb = gi.tdes_tables(w)
+    g = Graft(w.V, w.L, w.K, w.m, w.hidden_dim, w.batch, w.budget_min, w.budget_max, w.budget_step, w.beta, 1, dt[w.logits_dtype],
+              dt[w.hidden_dtype])
+    g.set_tdes_tables(tb["P"].to(dev), tb["C"].to(dev), tb["u"].to(dev), tb["s"])
+    g.set_saba(**gi.saba_defaults(w))
+    x = {k: (v.to(dev) if torch.is_tensor(v) else v) for k, v in _host_inputs(w, 0, w.batch, 1)[0].items()}
+    rows, pages = g.nmax, -(-(prefix + g.nmax) // page)
+    table = torch.randperm(w.batch * pages, device=dev).view(w.batch, pages).int()
+    cache = KVCache.alloc(layers, w.batch * pages, kv_heads, page, dim, E4M3 if args.verifier == "e4m3" else BF16)
+    start = torch.full((w.batch,), prefix, dtype=torch.int32, device=dev)
+    mb = MicroBatch(g, w.batch, w.L, cache=cache, table=table, prefix_len=start.clone())
+    rand = lambda *shape: torch.randn(shape, device=dev).to(torch.bfloat16)  # noqa: E731
+    # the prefix: random entries, written as a prompt
+    for layer in range(layers):
+        key, value = rand(w.batch, prefix - 1, kv_heads, dim), rand(w.batch, prefix - 1, kv_heads, dim)
+        g.cache_write(cache, layer, table, torch.ones_like(start), start - 1, key, value)
+    del key, value
+    q, key, value = rand(w.batch, rows, q_heads, dim), rand(w.batch, rows, kv_heads, dim), rand(w.batch, rows, kv_heads, dim)
+    out = torch.empty_like(q)
+    logits = torch.empty((w.batch, rows, w.V), dtype=torch.bfloat16, device=dev)
+    for b in range(w.batch):
+        logits[b].normal_()
+    uniform = torch.rand((w.batch, rows), device=dev)
+    marks = [[torch.cuda.Event(enable_timing=True) for _ in range(4)] for _ in range(args.steps)]
+    step = [0]
+
+    def draft(i, r):
+        mb.prefix_len.copy_(start)
+        marks[step[0]][0].record()
+        return x
+
+    def verify(i, r, trees):
+        marks[step[0]][1].record()
+        for layer in range(layers):
+            mb.attend(layer, q, key, value, out)
+        marks[step[0]][2].record()
+        return Sampled(logits, uniform)
+
+    def after(i, r, _):
+        marks[step[0]][3].record()
+
+    def rounds(n):
+        for k in range(n):
+            step[0] = k
+            run_rounds([mb], 1, draft, verify, overlap=False, after_round=after)
+
+    rounds(min(args.steps, 5))
+    rounds(args.steps)
+    torch.cuda.synchronize()
+    part = lambda a, b: round(sorted(m[a].elapsed_time(m[b]) for m in marks)[args.steps // 2] * 1e3, 2)  # noqa: E731
+    nodes = mb.out.n_nodes.float()
+    print(json.dumps({
+        "kind": "rounds with the target's cache (median microseconds on the device)", "workload": args.workload, "batch": w.batch, "rounds": args.steps,
+        "layers": layers, "q_heads": q_heads, "kv_heads": kv_heads, "head_dim": dim, "prefix": prefix, "cache": args.verifier,
+        "nodes_mean": round(float(nodes.mean()), 1), "nodes_max": int(nodes.max()), "build_us": part(0, 1),
+        "write_and_attend_us_per_layer": round(part(1, 2) / layers, 2), "walk_and_move_us": part(2, 3), "round_us": part(0, 3),
+    }))
+
+
 def run_tdes_loss(args):
     """--tdes-loss: the TDES training objective forward + backward (graft_tdes_loss) on one synthetic batch of traces
     at the paper's shapes; prints its own JSON line (not the benchmark's metric)."""
@@ -859,6 +929,8 @@ def main():
     ap.add_argument("--overlap-verifier-ms", type=float, default=None,
                     help="instead of the benchmark: two micro-batches on two streams around a stub verifier of this "
                          "duration, sequential against overlapped schedule")
+    ap.add_argument("--verifier", choices=["bf16", "e4m3"], default=None,
+                    help="instead of the benchmark: rounds with the target's cache of this type, attention, sampled walk (own JSON line)")
     ap.add_argument("--tdes-loss", action="store_true",
                     help="instead of the benchmark: time the TDES training objective (forward + backward)")
     ap.add_argument("--saba-fit", action="store_true",
@@ -896,6 +968,10 @@ def main():
     if args.overlap_verifier_ms is not None and args.impl == "graft":
         args.steps = 200 if args.steps is None else args.steps
         run_overlap(args)
+        return
+    if args.verifier is not None and args.impl == "graft":
+        args.steps = 50 if args.steps is None else args.steps
+        run_verifier(args)
         return
     if args.impl == "reference":
         args.steps = 10 if args.steps is None else args.steps
