@@ -36,16 +36,20 @@ __device__ __forceinline__ bool cache_slots_ok(const CacheView& c, const int32_t
     return __all_sync(0xFFFFFFFFu, ok);
 }
 
-// two e4m3 numbers (the low 16 bits) -> bf16 times 2^-120: their exponent and mantissa bits in the places of bf16's; exact
-__device__ __forceinline__ uint32_t e4m3x2_to_bf16x2_small(uint32_t two_in_bytes_1_and_3) {
-    return ((two_in_bytes_1_and_3 >> 4) & 0x07F007F0u) | (two_in_bytes_1_and_3 & 0x80008000u);
+// Bytes ia and ib (0 .. 3 of a, 4 .. 7 of b), e4m3 numbers -> bf16 times 2^-120; exact.  A byte with its sign eight times above it, moved up
+// four places, has sign, exponent and mantissa where bf16 has them, and signs in the exponent's upper bits, which go.  (prmt replicates signs,
+// __byte_perm does not.)
+__device__ __forceinline__ uint32_t e4m3_pair_small(uint32_t a, uint32_t b, int ia, int ib) {
+    uint32_t x;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(x) : "r"(a), "r"(b), "r"(ia | (ia | 8) << 4 | ib << 8 | (ib | 8) << 12));
+    return (x << 4) & 0x87F087F0u;
 }
 __device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-// Factors that take what e4m3x2_to_bf16x2_small gives to the numbers that it stands for, as pairs of bf16: 2^(e + 120) with
+// Factors that take what e4m3_pair_small gives to the numbers that it stands for, as pairs of bf16: 2^(e + 120) with
 // e = byte - 127.  Up to 2^127 one factor holds it and the second is 1; byte 255 is NaN.
 __device__ __forceinline__ void e4m3_factors(uint32_t byte, uint32_t& f, uint32_t& more) {
     int x = (int)byte - 7;  // e + 120
@@ -59,8 +63,8 @@ __device__ __forceinline__ void e4m3_factors(uint32_t byte, uint32_t& f, uint32_
 // four e4m3 numbers -> two pairs of bf16
 __device__ __forceinline__ uint2 e4m3x4_to_bf16(uint32_t w, uint32_t f, uint32_t more) {
     uint2 r;
-    r.x = bf16x2_mul(e4m3x2_to_bf16x2_small(__byte_perm(w, 0, 0x1404)), f);
-    r.y = bf16x2_mul(e4m3x2_to_bf16x2_small(__byte_perm(w, 0, 0x3424)), f);
+    r.x = bf16x2_mul(e4m3_pair_small(w, 0, 0, 1), f);
+    r.y = bf16x2_mul(e4m3_pair_small(w, 0, 2, 3), f);
     if (more != 0x3F803F80u) {
         r.x = bf16x2_mul(r.x, more);
         r.y = bf16x2_mul(r.y, more);
@@ -69,9 +73,5 @@ __device__ __forceinline__ uint2 e4m3x4_to_bf16(uint32_t w, uint32_t f, uint32_t
 }
 
 constexpr uint32_t kOneBf16x2 = 0x3F803F80u;
-// four e4m3 numbers -> the odd two and the even two as pairs of bf16
-__device__ __forceinline__ uint2 e4m3x4_to_bf16_odd_even(uint32_t w, uint32_t f) {
-    return make_uint2(bf16x2_mul(e4m3x2_to_bf16x2_small(w), f), bf16x2_mul(e4m3x2_to_bf16x2_small(w << 8), f));
-}
 
 }  // namespace graft

@@ -663,7 +663,7 @@ __device__ __noinline__ void add_spoilt(const AttnParams& p, const Piece& pc, ui
             for (int d = 0; d < D; d += 4) {
                 const uint2 v = entry(c.v, c.v_exp, d);
                 const uint32_t v0 = v.x << 16, v1 = v.x & 0xFFFF0000u, v2 = v.y << 16, v3 = v.y & 0xFFFF0000u;
-                const uint32_t vw[4] = {Q8 ? v1 : v0, Q8 ? v3 : v1, Q8 ? v0 : v2, Q8 ? v2 : v3};  // (the order of O's columns)
+                const uint32_t vw[4] = {v0, v1, v2, v3};
                 uint32_t o[4];
                 asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
                              : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3])
@@ -796,9 +796,6 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                     const uint32_t keep = __shfl_sync(0xFFFFFFFFu, live, y * kRows + lane / kPer) ? p.q_keep : 0u;
                     v.x = (v.x ^ p.q_flip) & keep, v.y = (v.y ^ p.q_flip) & keep;
                     v.z = (v.z ^ p.q_flip) & keep, v.w = (v.w ^ p.q_flip) & keep;
-                    if (Q8)
-                        v = make_uint4(__byte_perm(v.x, v.y, 0x7632), __byte_perm(v.x, v.y, 0x5410), __byte_perm(v.z, v.w, 0x7632),
-                                       __byte_perm(v.z, v.w, 0x5410));
                     const int row = (warp & 3) * 32 + y * kRows + lane / kPer;
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_addr + i * S::kTileBytes + row * 128 + (x >> 3) * S::kHalf +
                                                                                   ((((uint32_t)x & 7) ^ (row & 7)) << 4)),
@@ -907,12 +904,6 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
             const size_t out_row = ((size_t)b * p.rows + node) * p.q_heads + head;
             const auto put = [&](int d0, uint32_t (&u)[32], float inv) {
                 if (!live) return;
-                if (Q8)  // (odd two, even two)
-#pragma unroll
-                    for (int x = 0; x < 32; x += 4) {
-                        const uint32_t a = u[x], d = u[x + 1];
-                        u[x] = u[x + 2], u[x + 2] = u[x + 3], u[x + 1] = a, u[x + 3] = d;
-                    }
                 if (whole) {
                     uint4* to = (uint4*)(p.out + out_row * D + d0);
 #pragma unroll
@@ -1180,8 +1171,7 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                 piece_done(n_piece);
             }
         } else if (Q8 && warp >= 12) {
-            // ---- e4m3 tiles to bf16 tiles in the 128-byte swizzle: sixteen numbers a thread and step.  Four numbers that stand side by side come out
-            // as the odd two and the even two, which takes fewer instructions; the rows of Q and the columns of O have the same order.
+            // ---- e4m3 tiles to bf16 tiles in the 128-byte swizzle: sixteen numbers a thread and step
             const int ct = tid - 384;
             constexpr int kPer = D / 16, kRowsStep = (Q8 ? 32 * S::kConvWarps : 256) / kPer, kSteps = kTile / kRowsStep;
             const int col = ct % kPer, row0 = ct / kPer;
@@ -1222,7 +1212,8 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                                 uint32_t r[8];
 #pragma unroll
                                 for (int y4 = 0; y4 < 4; ++y4) {
-                                    const uint2 a = e4m3x4_to_bf16_odd_even(y4 == 0 ? y[x].x : y4 == 1 ? y[x].y : y4 == 2 ? y[x].z : y[x].w, f);
+                                    const uint32_t v4 = y4 == 0 ? y[x].x : y4 == 1 ? y[x].y : y4 == 2 ? y[x].z : y[x].w;
+                                    const uint2 a = make_uint2(bf16x2_mul(e4m3_pair_small(v4, 0, 0, 1), f), bf16x2_mul(e4m3_pair_small(v4, 0, 2, 3), f));
                                     r[2 * y4] = decltype(two_factors)::value ? bf16x2_mul(a.x, more) : a.x;
                                     r[2 * y4 + 1] = decltype(two_factors)::value ? bf16x2_mul(a.y, more) : a.y;
                                 }
@@ -1295,13 +1286,6 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
     uint32_t r;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
     return r;
-}
-// bytes ia and ib (0 .. 3 of a, 4 .. 7 of b) as e4m3 -> bf16 times 2^-120.  A byte with its sign eight times above it, four places up, has
-// sign, exponent and mantissa where bf16 has them, and signs in the exponent's upper bits, which go.
-__device__ __forceinline__ uint32_t e4m3_pair_small(uint32_t a, uint32_t b, int ia, int ib) {
-    uint32_t x;  // (__byte_perm has no signs)
-    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(x) : "r"(a), "r"(b), "r"(ia | (ia | 8) << 4 | ib << 8 | (ib | 8) << 12));
-    return (x << 4) & 0x87F087F0u;
 }
 __device__ __forceinline__ uint4 load_once(const uint8_t* p) {
     uint4 r;
