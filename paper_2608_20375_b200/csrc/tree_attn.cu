@@ -97,12 +97,15 @@ __device__ __forceinline__ void load_seq(PlanSeq& q, const PlanSeq* from) {
 
 // ---- the plan ------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ int row_tiles2(int R) { return (R + kUnitRows - 1) / kUnitRows; }  // units of R rows
-__device__ __forceinline__ int unit_weight(int R, int mt) { return R - mt * kUnitRows > kTile ? 2 : 1; }
+// What a key tile weighs: one row tile keeps the streams half as busy as two, but copies and conversions are the same (256 rows take 1.5 times as
+// long as 68, in bf16 and e4m3).
+constexpr int kOneTile = 2, kTwoTiles = 3;
+__device__ __forceinline__ int unit_weight(int R, int mt) { return R - mt * kUnitRows > kTile ? kTwoTiles : kOneTile; }
 // a unit's length in the line
 __device__ __forceinline__ int padded(int cost, int chunk) { return chunk == 1 ? cost : (cost + chunk - 1) / chunk * chunk; }
 __device__ __forceinline__ int head_cost(int R, int kt, int chunk) {
     const int u = row_tiles2(R);
-    return u == 0 ? 0 : (u - 1) * padded(2 * kt, chunk) + padded(kt * unit_weight(R, u - 1), chunk);
+    return u == 0 ? 0 : (u - 1) * padded(kTwoTiles * kt, chunk) + padded(kt * unit_weight(R, u - 1), chunk);
 }
 
 // first position of CTA c's stretch: ceil(c total / parts)
@@ -118,7 +121,7 @@ struct UnitAt {
 __device__ __forceinline__ UnitAt unit_at(const PlanSeq& q, int group, int h, int mt, int chunk) {
     const int R = q.n * group;
     UnitAt u;
-    u.x0 = q.cost0 + h * head_cost(R, q.kt, chunk) + padded(2 * q.kt, chunk) * mt;
+    u.x0 = q.cost0 + h * head_cost(R, q.kt, chunk) + padded(kTwoTiles * q.kt, chunk) * mt;
     u.w = unit_weight(R, mt);
     u.kt = q.kt;
     return u;
@@ -126,7 +129,7 @@ __device__ __forceinline__ UnitAt unit_at(const PlanSeq& q, int group, int h, in
 // first tile of the unit that is not ahead of CTA c's stretch
 __device__ __forceinline__ int first_tile(const UnitAt& u, int total, int parts, int c) {
     const int d = part_first(total, parts, c) - u.x0;
-    return d <= 0 ? 0 : min((d + u.w - 1) >> (u.w - 1), u.kt);
+    return d <= 0 ? 0 : min((d + u.w - 1) / u.w, u.kt);
 }
 __device__ __forceinline__ int cta_of(int x, int total, int parts) { return (int)((long long)x * parts / total); }
 
@@ -223,13 +226,13 @@ __global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const __grid_co
     const int Rs = p.shared > 0 ? nodes * p.group : 0, kts = (p.shared + kTile - 1) / kTile;
     total += Hk * head_cost(Rs, kts, 1);
     // A CTA's share of the line may begin and end inside of units; every piece of one costs some microseconds beside its tiles.  Where shares
-    // are short, units are given lengths of whole shares instead, so that a CTA has one piece, if shares two double tiles longer than equal ones
+    // are short, units are given lengths of whole shares instead, so that a CTA has one piece, if shares a few tiles longer than equal ones
     // are enough for it.
     const int share = (total + p.ctas - 1) / p.ctas;
     if (share > 1 && share <= p.most_share && p.batch <= kPlanThreads) {
         int n, base, kt, R;
         of(me, n, base, kt, R);
-        for (int c2 = (share + 1) & ~1; c2 <= share + 4; c2 += 2) {
+        for (int c2 = (share + 5) / 6 * 6; c2 <= share + 11; c2 += 6) {  // (whole tiles of either weight)
             const Sums s = block_sums(scratch, small, Hk * (head_cost(R, kt, c2) / c2), 0, 0);
             if (s.all[0] + Hk * (head_cost(Rs, kts, c2) / c2) <= p.ctas) {
                 chunk = c2;
@@ -286,7 +289,7 @@ __global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const __grid_co
                 q = entries[lo];
             else
                 load_seq(q, p.seq + lo);
-            const int R = q.n * p.group, hc = head_cost(R, q.kt, chunk), local = st.x - q.cost0, full = padded(2 * q.kt, chunk);
+            const int R = q.n * p.group, hc = head_cost(R, q.kt, chunk), local = st.x - q.cost0, full = padded(kTwoTiles * q.kt, chunk);
             st.s = lo;
             st.h = local / hc;
             int rem = local - st.h * hc;
@@ -368,7 +371,7 @@ struct Walk {
                 }
             }
         }
-        const int w = unit_weight(R, mt), left = (x1 - x + w - 1) >> (w - 1), kv0 = s == 0 ? 0 : shared;
+        const int w = unit_weight(R, mt), left = (x1 - x + w - 1) / w, kv0 = s == 0 ? 0 : shared;
         pc.T = min(left, q.kt - k);
         pc.s = s, pc.h = h;
         pc.first = kv0 + k * kTile;
@@ -435,14 +438,14 @@ struct Shape {
     static constexpr int kRawBytes = kTile * D + kTile;       // a tile of e4m3 numbers and its rows' exponents
     static constexpr int kQTiles = kOne ? 1 : 2;
     // Tiles in bf16 (and e4m3 tiles on their way).  Two streams on key tiles of their own have four in use.
-    static constexpr int kStages = (Q8 ? kOne ? 5 : 3 : kOne ? 6 : 5) * (128 / D);
-    static constexpr int kRaw = Q8 ? (kOne ? 2 : 4) * (128 / D) : 0;
-    static constexpr int kConvWarps = Q8 ? (kOne ? 8 : 4) : 0;
+    static constexpr int kStages = (Q8 ? kOne ? 5 : 4 : kOne ? 6 : 5) * (128 / D);
+    static constexpr int kRaw = Q8 ? 2 * (128 / D) : 0;
+    static constexpr int kConvWarps = Q8 ? 8 : 0;
     static constexpr int kThreads = 384 + 32 * kConvWarps;
     // registers a thread: the softmax's eight warps take over what the others leave (of what the launch has)
-    static constexpr int kRegsLaunch = kConvWarps == 8 ? 96 : kConvWarps == 4 ? 128 : 168;
-    static constexpr int kRegsSoftmax = kConvWarps == 8 ? 168 : kConvWarps == 4 ? 208 : 224, kRegsOthers = Q8 ? 48 : 56;
-    static constexpr int kCols = kConvWarps == 8 ? 64 : 128;  // scores that a softmax thread holds at a time
+    static constexpr int kRegsLaunch = Q8 ? 96 : 168;
+    static constexpr int kRegsSoftmax = Q8 ? 168 : 224, kRegsOthers = Q8 ? 48 : 56;
+    static constexpr int kCols = Q8 ? 64 : 128;  // scores that a softmax thread holds at a time
     static_assert(256 * kRegsSoftmax + (kThreads - 256) * kRegsOthers <= kThreads * kRegsLaunch, "registers of a launch");
     static constexpr size_t kSmem = 1024 + kQTiles * kTileBytes + (size_t)kStages * kTileBytes + (size_t)kRaw * kRawBytes + 1024;
 };
@@ -1874,7 +1877,7 @@ cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache
     p.part_o = (float*)(base + z.o_o);
     p.arrivals = ctx->w_attn_n;
     p.part_rows = z.part_rows;
-    p.most_share = few_rows(p.group, rows, shared) ? 0 : 64;
+    p.most_share = few_rows(p.group, rows, shared) ? 0 : 128;
     const auto launch = cache->head_dim == 128 ? (q8 ? launch_any<128, true> : launch_any<128, false>)
                                                : (q8 ? launch_any<64, true> : launch_any<64, false>);
     return launch(ctx, p, st);
