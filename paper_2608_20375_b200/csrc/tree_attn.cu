@@ -101,8 +101,10 @@ __device__ __forceinline__ int row_tiles2(int R) { return (R + kUnitRows - 1) / 
 // long as 68, in bf16 and e4m3).
 constexpr int kOneTile = 2, kTwoTiles = 3;
 __device__ __forceinline__ int unit_weight(int R, int mt) { return R - mt * kUnitRows > kTile ? kTwoTiles : kOneTile; }
-// a unit's length in the line
-__device__ __forceinline__ int padded(int cost, int chunk) { return chunk == 1 ? cost : (cost + chunk - 1) / chunk * chunk; }
+// A unit's length in the line: its tiles' and, for what a piece costs beside them (Q's rows, the first products, O: 4 to 5 us), kPieceCost; or
+// what fills the last share.
+constexpr int kPieceCost = 4;
+__device__ __forceinline__ int padded(int cost, int chunk) { return chunk == 1 ? cost + kPieceCost : (cost + chunk - 1) / chunk * chunk; }
 __device__ __forceinline__ int head_cost(int R, int kt, int chunk) {
     const int u = row_tiles2(R);
     return u == 0 ? 0 : (u - 1) * padded(kTwoTiles * kt, chunk) + padded(kt * unit_weight(R, u - 1), chunk);
@@ -296,7 +298,7 @@ __global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const __grid_co
             st.mt = min(rem / full, row_tiles2(R) - 1);
             rem -= full * st.mt;
             const int w = unit_weight(R, st.mt);
-            st.k = (rem + w - 1) / w;
+            st.k = min((rem + w - 1) / w, q.kt);  // (behind the tiles: kt, as if at their end)
             st.x += st.k * w - rem;
             st.q = q;
             if (p.shared == 0 && st.k > 0 && st.k < q.kt) {  // (else the stretch begins with a unit)
