@@ -536,7 +536,8 @@ graft_status graft_tree_attention(graft_ctx* ctx, int32_t batch, const graft_cac
     if ((gs = check_rows(cache, rows, q_heads, q_stride)) != GRAFT_OK) return gs;
     if (d_mask && rows > ctx->nmax) return GRAFT_ERR_INVALID_ARG;
     if (shared < 0 || shared % cache->page_size || shared > cache->table_width * cache->page_size) return GRAFT_ERR_INVALID_ARG;
-    // positions in the line of key tiles are 32-bit numbers (a tile of 128 rows against 128 slots is one)
+    // positions in the line of key tiles are 32-bit numbers (up to 256 rows against 128 slots count as at most three, and
+    // eight for every 256 rows)
     const double row_tiles = (double)batch * ((double)rows * (q_heads / cache->kv_heads) / 128 + 2);
     if (2 * row_tiles * cache->kv_heads * ((double)cache->table_width * cache->page_size / 128 + 2) >= 2147483648.0) return GRAFT_ERR_UNSUPPORTED;
     if (cache->kv_heads > 65535 || batch > 65535) return GRAFT_ERR_UNSUPPORTED;

@@ -5,7 +5,7 @@
 // whole tree; with a shared prefix, once for the nodes of all sequences.
 //
 // Units and pieces.  A unit is a sequence (or, for the shared prefix, all of them), a key head and up to 256 rows (two row tiles
-// of 128), against all key tiles of 128 slots.  The units' key tiles stand in one line, weighted by the row tiles that they feed, and every
+// of 128), against all key tiles of 128 slots.  The units' key tiles stand in one line, weighted by what they cost, and every
 // CTA takes an equal stretch of it: lengths and trees may be as unlike as they want, and one sequence's prefix spreads over all SMs.  A
 // unit that is cut leaves unnormalised sums with their maximum and denominator behind, which a second kernel joins.
 //
@@ -38,7 +38,7 @@ struct __align__(16) PlanSeq {
     int base;    // slots before the first row's (shared prefix: its length)
     int node0;   // nodes of the sequences before
     int unit0;   // units before
-    int cost0;   // position in the line: key tiles before, each times its row tiles
+    int cost0;   // position in the line: lengths of the units before
     int kt;      // key tiles
     int pad[2];
 };
@@ -101,9 +101,10 @@ __device__ __forceinline__ int row_tiles2(int R) { return (R + kUnitRows - 1) / 
 // long as 68, in bf16 and e4m3).
 constexpr int kOneTile = 2, kTwoTiles = 3;
 __device__ __forceinline__ int unit_weight(int R, int mt) { return R - mt * kUnitRows > kTile ? kTwoTiles : kOneTile; }
-// A unit's length in the line: its tiles' and, for what a piece costs beside them (Q's rows, the first products, O: 4 to 5 us), kPieceCost; or
-// what fills the last share.
-constexpr int kPieceCost = 4;
+// A unit's length in the line: its tiles' and kPieceCost for what a piece costs beside them (Q's rows, the first products, O), or what fills
+// the last share.  64 x 17 nodes behind 8192 shared slots, where 256 short pieces follow the long ones: 317 us with 0, 243 with 4, 214 with 7,
+// 215 with 10, 218 with 14; 32 sequences of up to 65 nodes over e4m3: 234, 196, 186, 175, 176.
+constexpr int kPieceCost = 8;
 __device__ __forceinline__ int padded(int cost, int chunk) { return chunk == 1 ? cost + kPieceCost : (cost + chunk - 1) / chunk * chunk; }
 __device__ __forceinline__ int head_cost(int R, int kt, int chunk) {
     const int u = row_tiles2(R);
@@ -1265,9 +1266,9 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
 // the long directions and the rows in the short one; e4m3 entries become bf16 in registers.  The order of head_dim inside a product is free,
 // so a lane loads pieces of 16 bytes straight into what it multiplies: of K, a quarter of those of two slots; of V, an eighth of four.  The next
 // step's K is asked for when this one's scores are done, and V when its products are: the warps of an SM then have 50 to 60 KB under way.
-// 64 sequences of 2000 to 16000 slots, 8 key heads of 128: bf16 371 us (6.36 TB/s; through the tiles of 128 rows 417), e4m3 288 us (4.1
-// TB/s; 553), which conversions bound: 500 instructions for 16 slots, three warps a scheduler to hide their latencies.  Through a ring of
-// cp.async in shared memory 543 and 295; with 8 warps of two steps 297, with 16 warps 294 (registers spill).
+// 64 sequences of 2000 to 16000 slots, 8 key heads of 128: bf16 357 us (6.6 TB/s; through the tiles of 128 rows 417), e4m3 269 us (4.4
+// TB/s; 553), which conversions bound: 500 instructions for 16 slots, three warps a scheduler to hide their latencies.  Before pieces' own cost
+// was counted (371 and 288): through a ring of cp.async in shared memory 543 and 295; with 8 warps of two steps 297, with 16 warps 294 (registers spill).
 constexpr int kFewRows = 8;
 
 template <int D, bool Q8>

@@ -80,6 +80,54 @@ def test_few_rows_that_do_not_see_what_is_not_a_number(rows, Hq, Hk, dtype, D):
 
 
 @pytest.mark.parametrize("dtype", [BF, Q8])
+@pytest.mark.parametrize("rows,shared", [(1, 0), (30, 0), (30, 32), (100, 0)])
+def test_no_sequence_has_rows(dtype, rows, shared):
+    _attend(3, 3, rows, 4, 2, 64, 16, [33, 40, 90], [0, 0, 0], dtype, "tree", shared=shared)
+    _attend(3, 3, rows, 4, 2, 64, 16, [33, 40, 90], [0, 1, 0], dtype, "tree", shared=shared)
+
+
+@pytest.mark.parametrize("dtype", [BF, Q8])
+def test_short_units_among_long_ones(dtype):
+    """What a unit costs beside its tiles is in the line too: stretches may begin behind a unit's tiles, or have none of any."""
+    rng = np.random.default_rng(4)
+    for rows, lens in ((1, [1] * 70 + [1800]), (40, [1] * 40 + [3000]), (70, rng.integers(1, 140, 37).tolist())):
+        _attend(rows, len(lens), rows, 4, 2, 64, 16, lens, [rows] * len(lens), dtype, None)
+    _attend(9, 30, 9, 32, 2, 64, 16, [129 + i for i in range(30)], [9] * 30, dtype, "tree", shared=128)
+
+
+@pytest.mark.parametrize("dtype", [BF, Q8])
+def test_calls_in_two_graphs_and_of_two_shapes_follow_one_another(dtype):
+    """Captured calls of several shapes share their context's workspace: replayed one behind another on one stream, results stay."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    B, Hq, Hk, D, page = 4, 8, 2, 128, 16
+    g = _graft(64, B)
+    table, n_pages = ref.page_table(np.random.default_rng(2), B, 60)
+    c = _cache(gen, (1, n_pages, Hk, page, D), dtype, garbage=False)
+    key, value = (torch.randn((B, 900, Hk, D), generator=gen, device="cuda").to(BF) for _ in range(2))
+    tb = _i32(table)
+    g.cache_write(c, 0, tb, _i32([1] * B), _i32([900] * B), key, value)
+    calls = []
+    for rows in (1, 20, 64):
+        q = torch.randn((B, rows, Hq, D), generator=gen, device="cuda").to(BF)
+        o = torch.zeros_like(q)
+        args = (c, 0, tb, q, _i32([900 - rows - 7 * b for b in range(B)]), _i32([rows] * B), None, o)
+        g.tree_attention(*args)
+        calls.append((args, o, o.clone()))
+    torch.cuda.synchronize()
+    graphs = []
+    for args, o, _ in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            g.tree_attention(*args)
+    for _ in range(3):
+        for graph, (_, o, _) in zip(graphs, calls):
+            o.zero_()
+            graph.replay()
+        for _, o, want in calls:
+            assert torch.equal(o, want)
+
+
+@pytest.mark.parametrize("dtype", [BF, Q8])
 @pytest.mark.parametrize("rows", [2, 20])
 def test_rows_of_q_with_a_stride(dtype, rows):
     """Q taken where it stands in a fused projection: the same bits as from a copy."""
