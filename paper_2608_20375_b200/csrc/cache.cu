@@ -57,8 +57,8 @@ __device__ __forceinline__ Item item_of(const CacheRowsParams& p, int b, int n, 
 constexpr int kItems = 4;  // that a thread has under way: 128 bytes of its input
 
 // Two 16-byte loads a thread and item, the largest of the row by shuffles, one 16-byte store (two into a bf16 cache).  A row's exponent
-// follows from the bits of its largest magnitude alone.  Prompts of 4600 tokens a sequence, 8 sequences, 8 heads of 128: 303 MB written and
-// read back move at 4 to 5 TB/s.
+// follows from the bits of its largest magnitude alone.  Prompts of 1000 to 8192 tokens, 8 sequences, 8 heads of 128, written and
+// read back: 453 MB in 107 us, 4.2 TB/s (165 us with one item a thread).
 template <bool Q8>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(const CacheRowsParams p) {
     pdl_launch_dependents();
@@ -173,6 +173,7 @@ struct CacheKeepParams {
 constexpr int kKeepChunks = 4;  // 16-byte pieces a thread holds: 32 entries of 256 bytes over 128 threads
 constexpr int kKeepThreads = 128;
 constexpr int kKeepLayers = 4;  // a block's: where entries stand is found once, and the layers' loads are under way together
+// (24 layers, 64 sequences, 101 MB: 20 us, 28 with a layer a block; 36 layers of one sequence: 2.4 us)
 
 // A block a (sequence, some layers, head, K or V): all entries of the path are in registers before the first is written, so that their
 // order and overlaps do not matter.
