@@ -223,3 +223,89 @@ def test_micro_batches_with_caches(dtype):
         lens = sum(x[0] for x in want[i::2]) + rounds + 1
         assert torch.equal(lens.int(), mb.prefix_len.cpu()) and not mb.status.any()
     assert sum(int(x[0].sum()) for x in want) > 0
+
+
+@pytest.mark.parametrize("dtype", [BF, torch.float32])
+@pytest.mark.parametrize("V,offset", [(4001, 0), (4001, 1), (150001, 1), (150001, 3), (13, 1)])
+def test_walk_of_wide_trees_and_rows_on_any_address(dtype, V, offset):
+    """Hundreds of children of one node (tokens twice among them), logits that begin on any element."""
+    from test_gpu_verifier import _verify
+    from paper_2608_20375_b200 import Graft
+    B, nmax, L, n = 6, 401, 4, 401
+    rng, gen = np.random.default_rng(V), torch.Generator(device="cuda").manual_seed(V)
+    g = Graft(V, L, 4, 16, 8, B, 1, nmax - 1, 1, 0.0)
+    rows = 5
+    parent, token = np.full((B, nmax), -1, np.int32), np.full((B, nmax), -1, np.int32)
+    counts = np.full(B, rows)
+    flat = torch.zeros(offset + B * nmax * V if V < 50000 else offset + B * rows * V, dtype=dtype, device="cuda")
+    wide = V < 50000
+    rows = nmax if wide else rows
+    counts[:] = rows
+    for b in range(B):
+        parent[b, 1:rows] = 0
+        parent[b, rows - 2:rows] = 1  # two grandchildren
+        token[b, 1:rows] = rng.integers(0, V, rows - 1)
+    z = flat[offset:].view(B, rows, V)
+    z.copy_(torch.randn((B, rows, V), generator=gen, device="cuda"))
+    for b in range(B):
+        z[b, 0, torch.from_numpy(token[b, 1:rows].astype(np.int64)).cuda()] += 5.0 if b % 2 else 1.0
+    u = torch.rand((B, nmax), generator=gen, device="cuda")
+    u[1, 1:] = 0.999
+    alen, path, bonus, st = _verify(g, B, rows, nmax, counts, parent, token, z, None, u, L)
+    again = _verify(g, B, rows, nmax, counts, parent, token, z, None, u, L)
+    assert not st.any() and all(np.array_equal(x, y) for x, y in zip((alen, path, bonus), again))
+    uc = u.cpu().double().numpy()
+    for b in range(B):
+        a, pa, bo = ref.walk(rows, parent[b], token[b], lambda i: z[b, i].cpu().double().numpy(), 1.0, uc[b], L)
+        assert (alen[b], bonus[b]) == (a, bo) and np.array_equal(path[b], pa), (b, alen[b], a, bonus[b], bo)
+
+
+def test_walk_and_move_captured():
+    """A round's walk and move in a graph, replayed with other numbers: the results of the calls."""
+    from paper_2608_20375_b200 import Graft, TreeOut
+    B, nmax, L, V, Hk, D, page, layers = 4, 33, 8, 5003, 2, 64, 16, 5
+    rng, gen = np.random.default_rng(1), torch.Generator(device="cuda").manual_seed(1)
+    from test_gpu_verifier import _trees
+    g = Graft(V, L, 4, 16, 8, B, 1, nmax - 1, 1, 0.0)
+    counts = np.array([33, 20, 1, 30])
+    parent, _, _, token = _trees(rng, B, nmax, counts, V, L)
+    tr = TreeOut(_i32(counts), None, _i32(token), _i32(parent), None, None, None, None, None)
+    table, n_pages = ref.page_table(rng, B, 10)
+    c = _cache(gen, (layers, n_pages, Hk, page, D), BF, garbage=False)
+    tb, z, u = _i32(table), torch.zeros((B, nmax, V), device="cuda"), torch.zeros((B, nmax), device="cuda")
+    pl, nxt = _i32([1, 30, 77, 100]), _i32([0] * B)
+    outs = [torch.full(s, -9, dtype=torch.int32, device="cuda") for s in ((B,), (B, L), (B,))]
+
+    def fill(seed):
+        gen.manual_seed(seed)
+        z.copy_(torch.randn(z.shape, generator=gen, device="cuda"))
+        for b in range(B):
+            for i in range(1, counts[b]):
+                z[b, parent[b, i], token[b, i]] += 9.0
+        u.copy_(torch.rand(u.shape, generator=gen, device="cuda"))
+        c.k.copy_(torch.randn(c.k.shape, generator=gen, device="cuda"))
+        c.v.copy_(torch.randn(c.v.shape, generator=gen, device="cuda"))
+
+    def call():
+        g.verify(tr, z, None, u, *outs)
+        g.cache_keep(c, tb, pl, outs[0], outs[1], nxt)
+
+    fill(1)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    seen = 0
+    for seed in (2, 3):
+        fill(seed)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (*outs, nxt, c.k, c.v)]
+        fill(seed)
+        call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, (*outs, nxt, c.k, c.v)))
+        assert torch.equal(nxt, pl + outs[0] + 1)
+        seen += int(outs[0].sum())
+    assert seen > 0
