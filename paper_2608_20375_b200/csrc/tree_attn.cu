@@ -26,6 +26,7 @@
 // which plan 4, attention 10 to 15, joining 8, and the hand-overs of three kernels.
 #include <cuda.h>
 #include <float.h>
+#include <string.h>
 
 #include "cache.cuh"
 #include "umma.cuh"
@@ -93,6 +94,7 @@ struct __align__(64) AttnParams {
     int most_share;      // shares up to this length may be made whole
     int part_rows;       // rows that a piece has room for
     int* arrivals;       // zero between calls
+    int* ready;          // [ctas] few rows: pieces that are there of the unit that is cut behind its beginning in a CTA
     float* part_o;       // [slots][D / 4][part_rows][4]
     float2* part_ml;     // [slots][part_rows]: maximum (log2 domain), sum
 };
@@ -323,6 +325,7 @@ __global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const __grid_co
         }
         p.start[i] = st;
         p.join[i] = j;
+        p.ready[i] = 0;
     }
 }
 
@@ -1267,13 +1270,89 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
     if (warp == 8) tmem_free<false>(tmem, 512);
 }
 
+// ---- joining the pieces ----------------------------------------------------------------------------------------------
+constexpr int kJoinThreads = 256;
+constexpr int kJoinRows = 32;
+constexpr int kJoinMost = 320;  // pieces of a block's rows: no more than CTAs and units (three at most)
+
+struct JoinPiece {
+    int slot, shift, lo, hi;  // rows lo .. hi - 1 of the block are rows lo + shift .. of the piece
+};
+struct JoinList {
+    JoinPiece piece[kJoinMost];
+    int n;
+};
+
+// The pieces of a unit, to the list; a warp calls it, a lane a CTA (of f .. l) that may have tiles of it.  Behind a shared prefix (unit >= 0) a piece's
+// slot is the unit's number and the CTA's added up; else the unit's first CTA has it in the odd one of its two slots.
+__device__ __forceinline__ void list_unit(JoinList& j, const UnitAt& u, int f, int l, int total, int parts, int unit, int shift, int lo, int hi) {
+    const int lane = lane_id();
+    for (int d0 = f; d0 <= l; d0 += 32) {
+        const int d = d0 + lane;
+        const bool has = d <= l && first_tile(u, total, parts, d + 1) > first_tile(u, total, parts, d);
+        const unsigned all = __ballot_sync(0xFFFFFFFFu, has);
+        const int n = j.n, at = n + __popc(all & ((1u << lane) - 1));
+        __syncwarp();
+        if (has && at < kJoinMost) j.piece[at] = {unit >= 0 ? unit + d : d == f ? 2 * d + 1 : 2 * d, shift, lo, hi};
+        if (lane == 0) j.n = min(n + __popc(all), kJoinMost);
+        __syncwarp();
+    }
+}
+
+// 32 rows of a unit from the pieces on the list: a lane a row, a warp some of the columns.  Pieces are added in their order along the line, results repeat; four are on their way at a time.
+template <int D>
+__device__ __forceinline__ void join_rows(const AttnParams& p, const JoinList& j, bool live, size_t out_row) {
+    constexpr int kWarps = kJoinThreads / 32, kQuads = D / 4 / kWarps;  // groups of four columns a warp
+    const int lane = lane_id(), warp = threadIdx.x >> 5, n = j.n;
+    float m = -INFINITY, l = 0.0f;
+    float o[4 * kQuads] = {};
+    constexpr int kAhead = 4;
+    for (int i0 = 0; i0 < n; i0 += kAhead) {
+        float2 ml[kAhead];
+        float4 v[kAhead][kQuads];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {  // (rows that a piece does not have, and pieces behind the last, weigh nothing)
+            const JoinPiece a = j.piece[min(i0 + i, n - 1)];
+            const bool mine = i0 + i < n && lane >= a.lo && lane < a.hi;
+            const int r = mine ? lane + a.shift : 0;
+            const float2 x = __ldcg(p.part_ml + (size_t)a.slot * p.part_rows + r);
+            ml[i] = mine ? x : make_float2(-INFINITY, 0.0f);
+            const float4* from = (const float4*)p.part_o + ((size_t)a.slot * (D / 4) + warp * kQuads) * p.part_rows + r;
+#pragma unroll
+            for (int y = 0; y < kQuads; ++y) {
+                const float4 z = __ldcg(from + y * p.part_rows);
+                v[i][y] = mine ? z : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const float now = fmaxf(m, ml[i].x), f0 = m > -INFINITY ? ex2_approx(m - now) : 0.0f;
+            const float f1 = ml[i].x > -INFINITY ? ex2_approx(ml[i].x - now) : 0.0f;
+            m = now;
+            l = l * f0 + ml[i].y * f1;
+#pragma unroll
+            for (int y = 0; y < kQuads; ++y) {
+                o[4 * y] = o[4 * y] * f0 + f1 * v[i][y].x, o[4 * y + 1] = o[4 * y + 1] * f0 + f1 * v[i][y].y;
+                o[4 * y + 2] = o[4 * y + 2] * f0 + f1 * v[i][y].z, o[4 * y + 3] = o[4 * y + 3] * f0 + f1 * v[i][y].w;
+            }
+        }
+    }
+    if (!live) return;
+    const float inv = l != 0.0f ? 1.0f / l : 1.0f;
+    uint2* to = (uint2*)(p.out + out_row * D + warp * kQuads * 4);
+#pragma unroll
+    for (int x = 0; x < kQuads; ++x)
+        to[x] = make_uint2(pack_bf16(o[4 * x] * inv, o[4 * x + 1] * inv), pack_bf16(o[4 * x + 2] * inv, o[4 * x + 3] * inv));
+    if (p.lse && warp == 0) p.lse[out_row] = log_sum(m, l);
+}
+
 // ---- few rows ----------------------------------------------------------------------------------------------------------
 // Single tokens (up to eight rows a sequence and key head) are bound by the bytes of K and V, and a tile of 128 rows would be nearly empty.
 // Here a warp takes 16 slots at a time into the fragments of m16n8k16 products, S^T = K Q^T and O^T = V^T P^T, with slots and head_dim in
 // the long directions and the rows in the short one; e4m3 entries become bf16 in registers.  The order of head_dim inside a product is free,
 // so a lane loads pieces of 16 bytes straight into what it multiplies: of K, a quarter of those of two slots; of V, an eighth of four.  The next
 // step's K is asked for when this one's scores are done, and V when its products are: the warps of an SM then have 50 to 60 KB under way.
-// 64 sequences of 2000 to 16000 slots, 8 key heads of 128: bf16 357 us (6.6 TB/s; through the tiles of 128 rows 417), e4m3 269 us (4.4
+// 64 sequences of 2000 to 16000 slots, 8 key heads of 128: bf16 354 us (6.6 TB/s; through the tiles of 128 rows 417), e4m3 274 us (4.3
 // TB/s; 553), which conversions bound: 500 instructions for 16 slots, three warps a scheduler to hide their latencies.  Before pieces' own cost
 // was counted (371 and 288): through a ring of cp.async in shared memory 543 and 295; with 8 warps of two steps 297, with 16 warps 294 (registers spill).
 constexpr int kFewRows = 8;
@@ -1313,6 +1392,8 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
     extern __shared__ __align__(16) float few_sm[];  // [warps][rows][D], then [warps][rows][2]
     float* const sm_ml = few_sm + kWarps * kFewRows * D;
     __shared__ Piece pc;
+    __shared__ JoinList list;
+    __shared__ int cut_f, cut_x0, cut_kt, last;  // of the unit that the piece is of
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q4 = lane & 3;
     const CacheView& c = p.c;
     const int shift = c.page_shift, low = (1 << shift) - 1;
@@ -1320,12 +1401,19 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
     pdl_launch_dependents();
     pdl_wait();
     Walk walk;
+    const int total = __ldcg(&p.head->total), parts = __ldcg(&p.head->parts);
     if (tid == 0) walk.begin(p, blockIdx.x);
     for (;;) {
         if (tid == 0) {
             Piece x;
             if (!walk.next(x)) x.T = 0;
             pc = x;
+            if (x.T > 0 && !x.whole) {
+                cut_x0 = unit_at(walk.q, p.group, walk.h, 0, 1).x0;
+                cut_kt = walk.q.kt;
+                cut_f = cta_of(cut_x0, total, parts);
+                list.n = 0;
+            }
         }
         __syncthreads();
         const int T = pc.T;
@@ -1609,84 +1697,26 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
                 if (d == 0) p.part_ml[slot * p.part_rows + r] = make_float2(mm, ll);
             }
         }
+        if (!whole) __threadfence();
         __syncthreads();  // (the sums and the piece are read)
-    }
-}
-
-// ---- joining the pieces ----------------------------------------------------------------------------------------------
-constexpr int kJoinThreads = 256;
-constexpr int kJoinRows = 32;
-constexpr int kJoinMost = 320;  // pieces of a block's rows: no more than CTAs and units (three at most)
-
-struct JoinPiece {
-    int slot, shift, lo, hi;  // rows lo .. hi - 1 of the block are rows lo + shift .. of the piece
-};
-struct JoinList {
-    JoinPiece piece[kJoinMost];
-    int n;
-};
-
-// The pieces of a unit, to the list; a warp calls it, a lane a CTA (of f .. l) that may have tiles of it.  Behind a shared prefix (unit >= 0) a piece's
-// slot is the unit's number and the CTA's added up; else the unit's first CTA has it in the odd one of its two slots.
-__device__ __forceinline__ void list_unit(JoinList& j, const UnitAt& u, int f, int l, int total, int parts, int unit, int shift, int lo, int hi) {
-    const int lane = lane_id();
-    for (int d0 = f; d0 <= l; d0 += 32) {
-        const int d = d0 + lane;
-        const bool has = d <= l && first_tile(u, total, parts, d + 1) > first_tile(u, total, parts, d);
-        const unsigned all = __ballot_sync(0xFFFFFFFFu, has);
-        const int n = j.n, at = n + __popc(all & ((1u << lane) - 1));
-        __syncwarp();
-        if (has && at < kJoinMost) j.piece[at] = {unit >= 0 ? unit + d : d == f ? 2 * d + 1 : 2 * d, shift, lo, hi};
-        if (lane == 0) j.n = min(n + __popc(all), kJoinMost);
-        __syncwarp();
-    }
-}
-
-// 32 rows of a unit from the pieces on the list: a lane a row, a warp some of the columns.  Pieces are added in their order along the line, results repeat; four are on their way at a time.
-template <int D>
-__device__ __forceinline__ void join_rows(const AttnParams& p, const JoinList& j, bool live, size_t out_row) {
-    constexpr int kWarps = kJoinThreads / 32, kQuads = D / 4 / kWarps;  // groups of four columns a warp
-    const int lane = lane_id(), warp = threadIdx.x >> 5, n = j.n;
-    float m = -INFINITY, l = 0.0f;
-    float o[4 * kQuads] = {};
-    constexpr int kAhead = 4;
-    for (int i0 = 0; i0 < n; i0 += kAhead) {
-        float2 ml[kAhead];
-        float4 v[kAhead][kQuads];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {  // (rows that a piece does not have, and pieces behind the last, weigh nothing)
-            const JoinPiece a = j.piece[min(i0 + i, n - 1)];
-            const bool mine = i0 + i < n && lane >= a.lo && lane < a.hi;
-            const int r = mine ? lane + a.shift : 0;
-            const float2 x = __ldcg(p.part_ml + (size_t)a.slot * p.part_rows + r);
-            ml[i] = mine ? x : make_float2(-INFINITY, 0.0f);
-            const float4* from = (const float4*)p.part_o + ((size_t)a.slot * (D / 4) + warp * kQuads) * p.part_rows + r;
-#pragma unroll
-            for (int y = 0; y < kQuads; ++y) {
-                const float4 z = __ldcg(from + y * p.part_rows);
-                v[i][y] = mine ? z : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (!whole) {
+            // The last of a unit's pieces to be there joins them, in the pieces' order: eight rows are little work, and a kernel behind this one
+            // takes longer to begin.  One token behind 1000 and 32000 slots: 17.0 -> 14.2 and 34.3 -> 28.3 us (e4m3), 64 tokens 269 -> 274.
+            if (warp == 0) {
+                list_unit(list, {cut_x0, kOneTile, cut_kt}, cut_f, cta_of(cut_x0 + (cut_kt - 1) * kOneTile, total, parts), total, parts, -1, 0, 0,
+                          kJoinRows);
+                if (lane == 0) last = atomicAdd(p.ready + cut_f, 1) == list.n - 1;
             }
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const float now = fmaxf(m, ml[i].x), f0 = m > -INFINITY ? ex2_approx(m - now) : 0.0f;
-            const float f1 = ml[i].x > -INFINITY ? ex2_approx(ml[i].x - now) : 0.0f;
-            m = now;
-            l = l * f0 + ml[i].y * f1;
-#pragma unroll
-            for (int y = 0; y < kQuads; ++y) {
-                o[4 * y] = o[4 * y] * f0 + f1 * v[i][y].x, o[4 * y + 1] = o[4 * y + 1] * f0 + f1 * v[i][y].y;
-                o[4 * y + 2] = o[4 * y + 2] * f0 + f1 * v[i][y].z, o[4 * y + 3] = o[4 * y + 3] * f0 + f1 * v[i][y].w;
+            __syncthreads();
+            if (last) {
+                __threadfence();
+                const int node = lane / p.group;
+                if (tid < kJoinThreads)
+                    join_rows<D>(p, list, lane < R, ((size_t)b * p.rows + node) * p.q_heads + h * p.group + (lane - node * p.group));
             }
+            __syncthreads();
         }
     }
-    if (!live) return;
-    const float inv = l != 0.0f ? 1.0f / l : 1.0f;
-    uint2* to = (uint2*)(p.out + out_row * D + warp * kQuads * 4);
-#pragma unroll
-    for (int x = 0; x < kQuads; ++x)
-        to[x] = make_uint2(pack_bf16(o[4 * x] * inv, o[4 * x + 1] * inv), pack_bf16(o[4 * x + 2] * inv, o[4 * x + 3] * inv));
-    if (p.lse && warp == 0) p.lse[out_row] = log_sum(m, l);
 }
 
 // Units that were cut, without a shared prefix: blocks for every boundary between CTAs; the first boundary inside a unit joins it.
@@ -1779,7 +1809,7 @@ int attn_ctas(const graft_ctx* ctx, bool q8, int head_dim, int group, int rows, 
 
 struct AttnSizes {
     int part_rows;
-    size_t o_seq, o_start, o_join, o_ml, o_o, total;
+    size_t o_seq, o_start, o_join, o_ready, o_ml, o_o, total;
 };
 AttnSizes attn_sizes(const graft_ctx* ctx, int ctas, int batch, int kv_heads, int head_dim, int group, int rows, int shared) {
     const auto units = [&](long long nodes) { return (size_t)kv_heads * (size_t)((nodes * group + kUnitRows - 1) / kUnitRows); };
@@ -1795,15 +1825,16 @@ AttnSizes attn_sizes(const graft_ctx* ctx, int ctas, int batch, int kv_heads, in
     z.o_seq = take((size_t)(batch + 1) * sizeof(PlanSeq));
     z.o_start = take((size_t)ctas * sizeof(PlanStart));
     z.o_join = take((size_t)(ctas + 1) * sizeof(PlanJoin));
+    z.o_ready = take((size_t)ctas * sizeof(int));
     z.o_ml = take(slots * z.part_rows * sizeof(float2));
     z.o_o = take(slots * z.part_rows * head_dim * sizeof(float));
     z.total = off;
     return z;
 }
 
-// The plan, the attention kernel, the joining of what it cut.
+// The plan, the attention kernel, the joining of what it cut (unless the kernel joins it itself).
 template <int D, typename Kernel>
-cudaError_t launch_three(graft_ctx* ctx, const AttnParams& p, Kernel kernel, int threads, size_t smem, uint32_t ready, cudaStream_t st) {
+cudaError_t launch_kernels(graft_ctx* ctx, const AttnParams& p, Kernel kernel, int threads, size_t smem, uint32_t ready, bool join, cudaStream_t st) {
     cudaError_t e;
     if (!(ctx->attn_ready & ready)) {
         e = allow_smem((const void*)kernel, smem);
@@ -1816,6 +1847,7 @@ cudaError_t launch_three(graft_ctx* ctx, const AttnParams& p, Kernel kernel, int
     e = launch_pdl(kernel, dim3(p.ctas), dim3(threads), smem, st, p);
     if (e != cudaSuccess) return e;
     ctx->launches += 1;
+    if (!join) return e;
     const long long most = (long long)p.rows * p.group;  // rows of a sequence and key head
     if (p.shared > 0)
         e = launch_pdl(attn_join_shared_kernel<D>, dim3((unsigned)((most + kJoinRows - 1) / kJoinRows), p.c.kv_heads, p.batch),
@@ -1829,13 +1861,14 @@ cudaError_t launch_three(graft_ctx* ctx, const AttnParams& p, Kernel kernel, int
 template <int D, bool Q8, bool kOne>
 cudaError_t launch_attn(graft_ctx* ctx, const AttnParams& p, cudaStream_t st) {
     using S = Shape<D, Q8, kOne>;
-    return launch_three<D>(ctx, p, tree_attn_kernel<D, Q8, kOne>, S::kThreads, S::kSmem, 1u << ((D == 128) + 2 * Q8 + 4 * kOne), st);
+    return launch_kernels<D>(ctx, p, tree_attn_kernel<D, Q8, kOne>, S::kThreads, S::kSmem, 1u << ((D == 128) + 2 * Q8 + 4 * kOne), true, st);
 }
 template <int D, bool Q8>
 cudaError_t launch_any(graft_ctx* ctx, const AttnParams& p, cudaStream_t st) {
     const long long rows = (long long)p.rows * p.group;
     if (few_rows(p.group, p.rows, p.shared))
-        return launch_three<D>(ctx, p, few_attn_kernel<D, Q8>, FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kSmem, 256u << ((D == 128) + 2 * Q8), st);
+        return launch_kernels<D>(ctx, p, few_attn_kernel<D, Q8>, FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kSmem,
+                                 256u << ((D == 128) + 2 * Q8), false, st);
     return p.shared == 0 && rows <= kTile ? launch_attn<D, Q8, true>(ctx, p, st) : launch_attn<D, Q8, false>(ctx, p, st);
 }
 
@@ -1849,14 +1882,17 @@ size_t tree_attn_scratch_bytes(const graft_ctx* ctx, int batch, const graft_cach
 cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache, int layer, int q_heads, int rows, long long q_stride,
                              const void* d_q, float scale, const int32_t* d_prefix_len, const int32_t* d_count, const uint32_t* d_mask,
                              int shared, void* d_out, float* d_lse, int32_t* d_status, void* scratch, cudaStream_t st) {
-    if (encode_tiled() == nullptr) return cudaErrorNotSupported;
     AttnParams p;
     p.c = cache_view(cache, layer);
     const bool q8 = cache->dtype == GRAFT_E4M3;
     p.box_rows = cache->page_size < kTile ? cache->page_size : kTile;
     const uint64_t cache_rows = (uint64_t)cache->n_pages * cache->kv_heads * cache->page_size;
-    if (!encode_map(&p.map_k, p.c.k, q8, cache->head_dim, cache_rows, p.box_rows) ||
-        !encode_map(&p.map_v, p.c.v, q8, cache->head_dim, cache_rows, p.box_rows))
+    const bool few = few_rows(q_heads / cache->kv_heads, rows, shared);
+    if (!few && encode_tiled() == nullptr) return cudaErrorNotSupported;
+    if (few)  // (no copies by TMA)
+        memset(&p.map_k, 0, sizeof p.map_k), memset(&p.map_v, 0, sizeof p.map_v);
+    else if (!encode_map(&p.map_k, p.c.k, q8, cache->head_dim, cache_rows, p.box_rows) ||
+             !encode_map(&p.map_v, p.c.v, q8, cache->head_dim, cache_rows, p.box_rows))
         return cudaErrorInvalidValue;
     p.q = (const uint8_t*)d_q;
     p.q_stride = q_stride;
@@ -1883,11 +1919,12 @@ cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache
     p.seq = (PlanSeq*)(base + z.o_seq);
     p.start = (PlanStart*)(base + z.o_start);
     p.join = (PlanJoin*)(base + z.o_join);
+    p.ready = (int*)(base + z.o_ready);
     p.part_ml = (float2*)(base + z.o_ml);
     p.part_o = (float*)(base + z.o_o);
     p.arrivals = ctx->w_attn_n;
     p.part_rows = z.part_rows;
-    p.most_share = few_rows(p.group, rows, shared) ? 0 : 128;
+    p.most_share = few ? 0 : 128;
     const auto launch = cache->head_dim == 128 ? (q8 ? launch_any<128, true> : launch_any<128, false>)
                                                : (q8 ? launch_any<64, true> : launch_any<64, false>);
     return launch(ctx, p, st);
