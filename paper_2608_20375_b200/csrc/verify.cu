@@ -125,6 +125,8 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const VerifyParams 
     using R = Row<BF16>;
     constexpr int kE = R::kE, kAhead = 8;  // pieces that a thread has on their way
     pdl_launch_dependents();
+    // (this CTA is there: others write to its shared memory once all have arrived, see the wait below)
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     extern __shared__ __align__(16) int32_t vsm[];
     int32_t* first_child = vsm;          // [nmax], 0: none (the root is nobody's child)
     int32_t* par = vsm + p.nmax;         // [nmax]
@@ -188,6 +190,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const VerifyParams 
         for (int i = lane; i < v; i += 32) t += __longlong_as_double((long long)all[i]);
         return warp_sum(t);
     };
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // all CTAs of the cluster have begun
     // this CTA's share of n things begins at
     const auto share = [&](int n, int r) { return (int)(((long long)n * r) >> ctas_log); };
     while (status == 0) {
