@@ -442,6 +442,10 @@ __device__ __forceinline__ void seen_words(const uint32_t* mask_row, int words, 
 
 // ---- the attention kernel ------------------------------------------------------------------------------------------
 constexpr int kPieces = 4;  // that are told ahead
+// Pieces that the flags of rows of V that were taken out are held for.  A warp of the first stream may set the next piece's flag while others
+// have yet to test this one's (it clears V ahead of its first scores); none is two pieces ahead, as a piece's first scores wait for all eight
+// warps' arrivals on q_full, which follow their test.
+constexpr int kSpoiltPieces = 2;
 
 // kOne: no unit has more than one row tile, and there is room for more key tiles.
 template <int D, bool Q8, bool kOne>
@@ -717,10 +721,11 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
     const uint32_t q_full = bar0 + 8 * (2 * NS + 2 * NR), s_full0 = q_full + 8, p_full0 = q_full + 24, pair = q_full + 40, turn0 = q_full + 48;
     const uint32_t piece_full0 = q_full + 64, piece_empty0 = piece_full0 + 8 * kPieces;
     volatile int* const gave_up = (volatile int*)(bars + 2 * NS + 2 * NR + 8 + 2 * kPieces);
-    volatile int* const spoilt = gave_up + 1;  // [2] the last piece (counted from 1) with a row of V that was taken out
-    uint32_t* const tmem_at = (uint32_t*)(gave_up + 3);
-    Piece* const pieces = (Piece*)(gave_up + 4);  // [kPieces]
-    static_assert((2 * NS + 2 * NR + 8 + 2 * kPieces) * 8 + 16 + kPieces * sizeof(Piece) <= 1024, "barriers and pieces");
+    volatile int* const spoilt = gave_up + 1;  // [kSpoiltPieces][2 streams] the last piece (counted from 1) with a row of V that was taken out
+    uint32_t* const tmem_at = (uint32_t*)(gave_up + 1 + 2 * kSpoiltPieces);
+    Piece* const pieces = (Piece*)(gave_up + 2 + 2 * kSpoiltPieces);  // [kPieces]
+    static_assert((2 * NS + 2 * NR + 8 + 2 * kPieces) * 8 + (2 + 2 * kSpoiltPieces) * 4 + kPieces * sizeof(Piece) <= 1024, "barriers and pieces");
+    static_assert((2 + 2 * kSpoiltPieces) * 4 % 8 == 0, "pieces begin where they may be copied eight bytes at a time");
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
@@ -744,7 +749,7 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
             mbar_init(turn0 + 8 * i, 1);
         }
         *gave_up = 0;
-        spoilt[0] = spoilt[1] = 0;
+        for (int i = 0; i < 2 * kSpoiltPieces; ++i) spoilt[i] = 0;
         mbar_fence_init();
     }
     if (warp == 8) tmem_alloc<false>(smem_u32(tmem_at), 512);
@@ -852,7 +857,7 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + (x >> 3) * S::kHalf + ((x + row_in_tile) & 7) * 16),
                                          "r"(0)
                                          : "memory");
-                        if (slot < end) spoilt[i] = (int)n_piece + 1;
+                        if (slot < end) spoilt[2 * (n_piece % kSpoiltPieces) + i] = (int)n_piece + 1;
                     }
                 }
                 fence_proxy_async();
@@ -913,7 +918,7 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
             int b = 0, node = 0, g = 0;
             if (live) row_of(p, pc.s, pc.r0 + r, b, node, g);
             const int head = pc.h * p.group + g;
-            if (spoilt[two ? 0 : i] == (int)n_piece + 1)
+            if (spoilt[2 * (n_piece % kSpoiltPieces) + (two ? 0 : i)] == (int)n_piece + 1)
                 add_spoilt<D, Q8>(p, pieces[n_piece % kPieces], tO, live && m > -INFINITY, b, node, head, two ? 0 : i, two ? 1 : 2, m);
             const bool whole = pc.whole;
             const size_t slot = p.shared > 0 ? (size_t)pc.unit + blockIdx.x : 2 * (size_t)blockIdx.x + pc.head;
