@@ -306,7 +306,8 @@ graft_status graft_cache_keep(graft_ctx* ctx, int32_t batch, const graft_cache* 
  *   bit j of d_mask[b, i] set (d_mask [batch, Nmax, W] as graft_build_trees emits it; then rows <= Nmax), or those with j <= i where
  *   d_mask is NULL (single tokens, chains, chunks of a prompt).
  *   d_out [batch, rows, q_heads, head_dim] bf16 dense: sum_j p_j v_j, p = softmax(scale q . k_j); d_lse [batch, rows, q_heads] fp32 or
- *   NULL: log sum_j exp(scale q . k_j).  A row that sees nothing: 0 and -inf.  Rows behind the count are left as they were.
+ *   NULL: log sum_j exp(scale q . k_j).  A row that sees nothing: 0 and -inf.  A row that sees a score of
+ *   NaN or +inf (an entry that is not a number): NaN in both; a score of -inf weighs nothing.  Rows behind the count are left as they were.
  *   shared: the first `shared` slots (a multiple of page_size; 0: none) are the same pages in every sequence's table (sequence 0's
  *   are read) and are gone through once for the rows of all sequences; every prefix_len is above `shared` (else GRAFT_ST_BAD_CACHE).
  * Scores, statistics and sums are fp32; the weights p enter the second product as bf16, as a bf16 cache's values do. */

@@ -562,13 +562,19 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return r;
 }
 
+// the largest; NaN if one of them is
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float max2(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
 // kCols of the row's scores at tS, from x0 on, all asked for together (while the tensor cores work on the other stream, an answer takes
-// several hundred cycles), -inf in the place of those that `sees` leaves out, and their largest.
+// several hundred cycles), -inf in the place of those that `sees` leaves out, and their largest (NaN if one of them is).
 template <int kCols>
 __device__ __forceinline__ float scores(uint32_t tS, int x0, uint32_t (&u)[kCols], bool masked, const uint32_t (&sees)[4]) {
 #pragma unroll
@@ -580,11 +586,11 @@ __device__ __forceinline__ float scores(uint32_t tS, int x0, uint32_t (&u)[kCols
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
     for (int x = 0; x < kCols; x += 2) mx[x / 2 % 4] = max3(mx[x / 2 % 4], __uint_as_float(u[x]), __uint_as_float(u[x + 1]));
-    return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+    return max2(max3(mx[0], mx[1], mx[2]), mx[3]);
 }
 // 2^t of two numbers on the FMA pipe: t = n + f, n whole and |f| <= 1/2; 2^f by a polynomial of degree 5 (fitted for the least largest
 // relative error, 1e-7, with 1 at f = 0), n added to its exponent.  t is held to -127 .. 127: at -127, where slots that are not seen
-// come out, the exponent's field is 0 and the result is 0.
+// come out, the exponent's field is 0 and the result is 0.  (So it is for NaN, which the kernel knows of from the tile's maximum.)
 __device__ __forceinline__ float2 exp2_poly(uint64_t t) {
     float2 x = apart(t);
     t = two(fminf(fmaxf(x.x, -127.0f), 127.0f), fminf(fmaxf(x.y, -127.0f), 127.0f));
@@ -881,7 +887,7 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                     constexpr bool kAgain = S::kCols < kTile;
                     uint32_t u[S::kCols], w[32];
                     float mx = scores(tS, 0, u, masked, sees);
-                    if (kAgain) mx = fmaxf(mx, scores(tS, 64, u, masked, sees));
+                    if (kAgain) mx = max2(mx, scores(tS, 64, u, masked, sees));
                     // (m = -inf: nothing seen so far, and what O holds is zero)
                     const bool grown = mx > m && !((mx - m) * c2 <= kMostGrowth);
                     if (__any_sync(0xFFFFFFFFu, grown)) {
@@ -890,6 +896,9 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                         l *= f;
                         m = now;
                     }
+                    // (a score of NaN or +inf, which some of the exponentials below would lose: the row's sum is NaN from here on, and so is all that
+                    // is divided by it)
+                    if (!(mx < INFINITY)) l = __int_as_float(0x7FFFFFFF);
                     const float off = m > -INFINITY ? -m * c2 : 0.0f;
                     if (kAgain) scores(tS, 0, u, masked, sees);
                     l += weigh(u, c2, off, w);
