@@ -320,7 +320,8 @@ graft_status graft_tree_attention(graft_ctx* ctx, int32_t batch, const graft_cac
  * tokens are the drafter's best, not draws, so a child is kept with the target's own probability and what is left of the target's
  * distribution is sampled when none is: the committed tokens are distributed as the target's, whatever the tree.
  *   d_target_logits [batch, rows, V] (V of the context, rows <= Nmax, dtype given): the target's logits behind every node; n_nodes <= rows.
- *   d_temperature [batch] fp32 or NULL (1 everywhere); 0: the likeliest token (lowest id among equals), as graft_accept.
+ *   d_temperature [batch] fp32 or NULL (1 everywhere); 0: the likeliest token (lowest id among equals), as graft_accept; between 0 and
+ *   2^-64: as 2^-64 (where logits that differ at all are told apart, but for those of less than 2^-33).
  *   d_uniform [batch, Nmax] fp32 in [0, 1): entry i > 0 decides on node i, entry 0 draws the bonus token.
  * At a node, with w_v = exp((z_v - max z) / T): its children c in index order are taken in turn; c is accepted iff
  * u_c (sum of w without the tokens of earlier children) < w(token of c).  The first accepted child is the next node; without one the

@@ -24,6 +24,7 @@ constexpr int kMaxCluster = 16;
 constexpr int kRoots = 256;          // entries of the table of 2^(j / 256)
 constexpr int kHeldWords = 2048;     // (shares of more than 65,536 pieces: bits are used again)
 constexpr int kGroups = 64;          // sums that a warp keeps of its stretch of the last row
+constexpr float kLeastT = 0x1p-64f;  // temperatures between 0 and this one count as it: exponents then stay in fp32's range
 constexpr float kNear = 1e-5f;       // sums of fp32 exponentials are nearer than that (of the whole) to the exact ones
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
@@ -84,23 +85,23 @@ struct Row {
     }
 };
 
-// x as a double by integer operations (conversions run at a quarter of the rate of the arithmetic): zero comes out as 2^-127, which is
-// nothing beside what it is added to, and -inf as -2^128.
+// x as a double by integer operations (conversions run at a quarter of the rate of the arithmetic): zero and what is below 2^-126 come out up
+// to 2^-126 off, which is 2^-61 in an exponent at the least temperature, and -inf as -2^128.
 __device__ __forceinline__ double widen(float x) {
     const uint32_t u = __float_as_uint(x);
     return __hiloint2double((int)((u & 0x80000000u) | (((u & 0x7FFFFFFFu) >> 3) + 0x38000000u)), (int)(u << 29));
 }
-// 2^t in fp64 for t <= 0 or so (below -1000: 0): t = n + j / 256 + r, |r| <= 1/512, a table of 2^(j / 256) and the exponential series to the
+// 2^t in fp64 for t <= 0 or so (up to `none`, -1000 or above it: 0): t = n + j / 256 + r, |r| <= 1/512, a table of 2^(j / 256) and the exponential series to the
 // third power, whose rest is below 2e-13.  The sum with 1.5 2^44 leaves 256 (n + j / 256) in its last bits.
 constexpr double kFineMagic = 26388279066624.0, kFine1 = 0.69314718055994531, kFine2 = 0.24022650695910072, kFine3 = 0.05550410866482158;  // (ln 2, its square over 2, its cube over 6)
-__device__ __forceinline__ double exp2_fine(double t, const double* roots) {
+__device__ __forceinline__ double exp2_fine(double t, double none, const double* roots) {
     const double m = t + kFineMagic, r = t - (m - kFineMagic);
     const int k = __double2loint(m);
     double q = fma(r, kFine3, kFine2);
     q = fma(q, r, kFine1);
     q = fma(q, r, 1.0);
     q *= roots[k & (kRoots - 1)];
-    return t > -1000.0 ? __hiloint2double(__double2hiint(q) + ((k >> 8) << 20), __double2loint(q)) : 0.0;
+    return t > none ? __hiloint2double(__double2hiint(q) + ((k >> 8) << 20), __double2loint(q)) : 0.0;
 }
 
 __device__ __forceinline__ float warp_max(float x) {
@@ -162,8 +163,10 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const VerifyParams 
             if (q >= 0 && q < i && (i == 1 || par[i - 1] != q)) first_child[q] = i;
         }
     __syncthreads();
-    const double inv_T = greedy ? 1.0 : 1.0 / (double)T, c64 = 1.4426950408889634 * inv_T;
+    const double inv_T = greedy ? 1.0 : 1.0 / (double)fmaxf(T, kLeastT), c64 = 1.4426950408889634 * inv_T;
     const float cf = (float)c64;
+    // (at temperatures near fp32's largest, differences that fp32 does not hold weigh something: all comparisons take the exact sum)
+    const double near_by = T > 0x1p100f ? 1e300 : (double)kNear;
 
     int cur = 0, a = 0, status = !tree_ok ? GRAFT_ST_BAD_TREE : !t_ok ? GRAFT_ST_BAD_LOGITS : 0, bonus = -1;
     int path = -1;  // lane l of warp 0 keeps step l
@@ -301,8 +304,10 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const VerifyParams 
             status = GRAFT_ST_BAD_LOGITS;
             break;
         }
-        const double off = -(double)top * c64;
-        const auto weight = [&](float x) { return exp2_fine(fma(widen(x), c64, off), roots); };
+        // (the difference first: it is exact or nearly so, and 0 for the largest, whatever the temperature; -inf is told from the lowest
+        // finite numbers at the highest ones too)
+        const double zero = widen(top), none = fmax(-1000.0, (widen(-INFINITY) - zero) * c64);
+        const auto weight = [&](float x) { return exp2_fine((widen(x) - zero) * c64, none, roots); };
         // ---- the children, in turn: every warp finds the same
         double Z = (double)Zf;
         bool exact = greedy;
@@ -334,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const VerifyParams 
                     }
                     const double left = (greedy ? 1.0 : Z) - (ahead + (sum - w));
                     const bool ok = is && u * left < w;
-                    const bool near = is && !exact && w > 0.0 && fabs(u * left - w) <= (double)kNear * Z;
+                    const bool near = is && !exact && w > 0.0 && fabs(u * left - w) <= near_by * Z;
                     const unsigned oks = __ballot_sync(kAll, ok), nears = __ballot_sync(kAll, near);
                     const int f = oks ? __ffs(oks) - 1 : 32;
                     if (nears & (f >= 31 ? kAll : ((2u << f) - 1))) {
@@ -388,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const VerifyParams 
                 double r[4], q[4];
                 int k[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) r[i] = fma(widen(x[i0 + i]), c64, off);
+                for (int i = 0; i < 4; ++i) r[i] = (widen(x[i0 + i]) - zero) * c64;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w[i0 + i] = r[i];
 #pragma unroll
@@ -407,7 +412,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const VerifyParams 
                 for (int i = 0; i < 4; ++i) q[i] *= roots[k[i] & (kRoots - 1)];
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    w[i0 + i] = w[i0 + i] > -1000.0 ? __hiloint2double(__double2hiint(q[i]) + ((k[i] >> 8) << 20), __double2loint(q[i])) : 0.0;
+                    w[i0 + i] = w[i0 + i] > none ? __hiloint2double(__double2hiint(q[i]) + ((k[i] >> 8) << 20), __double2loint(q[i])) : 0.0;
             }
             if (st < s1 && (word(st) >> ((st - s0) & 31)) & 1)
                 for (int e = 0; e < n_child; ++e) {
