@@ -10,7 +10,8 @@ verifier is the caller's).
 
 A verifier may answer with the target's likeliest tokens (the greedy walk) or with its logits and random numbers (`Sampled`: the walk that
 keeps the target's distribution).  A micro-batch that holds the target's key/value cache gives the verifier its attention (`attend`), and
-after the walk the accepted nodes' entries are moved up behind the prefix.
+after the walk the accepted nodes' entries are moved up behind the prefix.  What goes wrong with a sequence in any call of its round is in
+the micro-batch's `status`, and such a sequence is not moved on: its prefix and entries stay as they were before the round's nodes.
 """
 from __future__ import annotations
 
@@ -35,7 +36,8 @@ class MicroBatch:
     bonus_token: torch.Tensor = None
     rounds_done: int = field(default=0)
     # the target's cache and its page table [batch, pages] (None: the verifier keeps its own); after every walk prefix_len [batch] is
-    # moved on by the committed tokens, status [batch] is the last call's
+    # moved on by the committed tokens.  status [batch]: the bits of all calls of the round, 0 when all is well (greedy walks without a
+    # cache report nothing); a sequence with any is not moved on, and what the round says it accepted is not to be used
     cache: KVCache = None
     table: torch.Tensor = None
     prefix_len: torch.Tensor = None
@@ -57,17 +59,48 @@ class MicroBatch:
         if self.cache is not None:
             if self.table is None or self.prefix_len is None:
                 raise GraftError("a micro-batch with a cache has a table and prefix lengths")
-            if self.status is None:
-                self.status = torch.zeros(self.batch, dtype=i32, device=dev)
+            # a row of statuses a call: two a layer (write, attention), earlier calls of layers that were attended to again, walk, move
+            self._calls = torch.zeros((2 * self.cache.k.shape[0] + 3, self.batch), dtype=i32, device=dev)
+            self._bits = (1 << torch.arange(6, dtype=i32, device=dev)).view(-1, 1, 1)  # (ST_BAD_LOGITS .. ST_BAD_TREE)
+            self._attended = set()
+        if self.status is None:
+            self.status = torch.zeros(self.batch, dtype=i32, device=dev)
+
+    def begin_round(self):
+        """Forget the statuses of the round before."""
+        if self.cache is not None:
+            self._calls.zero_()
+            self._attended.clear()
 
     def attend(self, layer, q, key, value, out, lse=None, scale=None, shared=0):
         """One layer of the target over this round's trees: the nodes' new entries go into the cache, q [batch, rows, q_heads, head_dim]
         sees the prefix and the nodes above its own."""
         if self.cache is None:
             raise GraftError("the micro-batch has no cache")
-        self.graft.cache_write(self.cache, layer, self.table, self.prefix_len, self.out.n_nodes, key, value, self.status)
+        if not 0 <= layer < self.cache.k.shape[0]:
+            raise GraftError(f"layer must be below {self.cache.k.shape[0]}, got {layer}")
+        written, attended = self._calls[2 * layer], self._calls[2 * layer + 1]
+        if layer in self._attended:
+            self._calls[-3].bitwise_or_(written | attended)
+        self._attended.add(layer)
+        self.graft.cache_write(self.cache, layer, self.table, self.prefix_len, self.out.n_nodes, key, value, written)
         self.graft.tree_attention(self.cache, layer, self.table, q, self.prefix_len, self.out.n_nodes, self.out.mask, out, lse, scale, shared,
-                                  self.status)
+                                  attended)
+
+    def walk(self, answer):
+        """The walk along this round's trees by what the verifier answered, and with a cache the move of what was accepted."""
+        at = self._calls[-2] if self.cache is not None else self.status
+        if isinstance(answer, Sampled):
+            self.graft.verify(self.out, answer.logits, answer.temperature, answer.uniform, self.accept_len, self.accept_path, self.bonus_token, at)
+        else:
+            self.graft.accept(self.out, answer, self.accept_len, self.accept_path, self.bonus_token)
+        if self.cache is None:
+            return
+        torch.sum((self._calls[:-1] & self._bits).amax(1), 0, dtype=torch.int32, out=self.status)
+        # (an accepted length below 0 leaves a sequence where it is; lengths are below 64)
+        moved = torch.sub(self.accept_len, self.status, alpha=64)
+        self.graft.cache_keep(self.cache, self.table, self.prefix_len, moved, self.accept_path, self.prefix_len, self._calls[-1])
+        torch.where(self.status == 0, self._calls[-1], self.status, out=self.status)
 
 
 @dataclass
@@ -103,17 +136,11 @@ def run_rounds(micro: Sequence[MicroBatch], n_rounds: int, draft: DraftFn, verif
     for r in range(n_rounds):
         for i, mb in enumerate(micro):
             with torch.cuda.stream(mb.stream if overlap else cur):
+                mb.begin_round()
                 x = draft(i, r)
                 mb.graft.build_trees(x["logits"], x.get("hidden"), x["root_token"], x.get("hist"),
                                      x.get("prefix_len", mb.prefix_len), x.get("fixed_budget"), mb.out)
-                answer = verify(i, r, mb.out)
-                if isinstance(answer, Sampled):
-                    mb.graft.verify(mb.out, answer.logits, answer.temperature, answer.uniform, mb.accept_len, mb.accept_path,
-                                    mb.bonus_token)
-                else:
-                    mb.graft.accept(mb.out, answer, mb.accept_len, mb.accept_path, mb.bonus_token)
-                if mb.cache is not None:
-                    mb.graft.cache_keep(mb.cache, mb.table, mb.prefix_len, mb.accept_len, mb.accept_path, mb.prefix_len, mb.status)
+                mb.walk(verify(i, r, mb.out))
                 mb.rounds_done += 1
                 if after_round is not None:
                     after_round(i, r, mb)
