@@ -268,8 +268,8 @@ graft_status graft_set_hist_window(graft_ctx* ctx, int32_t w, int32_t* d_window,
  * NULL; overwritten, 0 when all is well) is GRAFT_ST_BAD_CACHE.  Entries of the table behind the slots in use are not read.
  * Pages may be shared between sequences as long as no call writes to them.
  * Limits: head_dim 64 or 128, page_size a power of two from 16 to 1024, kv_heads * n_pages * page_size < 2^31, d_k, d_v, the exponents
- * and rows of q, key, value and out 16-byte aligned, batch <= cfg.max_batch; in graft_tree_attention kv_heads and batch <= 65535.  Beyond
- * the last slot in use a page's rest is read and not used: n_pages whole pages have to be there. */
+ * and rows of q, key, value and out 16-byte aligned, batch <= cfg.max_batch and 65535 (graft_verify too); in graft_tree_attention kv_heads
+ * <= 65535.  Beyond the last slot in use a page's rest is read and not used: n_pages whole pages have to be there. */
 typedef struct graft_cache {
     int32_t layers, n_pages, kv_heads, page_size, head_dim;
     graft_dtype dtype;        /* GRAFT_BF16 or GRAFT_E4M3 */

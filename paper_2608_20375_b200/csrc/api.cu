@@ -465,6 +465,8 @@ graft_status graft_accept(graft_ctx* ctx, int32_t batch, const graft_tree_out* t
     return GRAFT_OK;
 }
 
+constexpr int32_t kMostSequences = 65535;  // of a call on a cache or a sampled walk: a grid's second dimension
+
 // Arguments that the calls on a cache have in common.
 static graft_status check_cache(const graft_ctx* ctx, int32_t batch, const graft_cache* c, int32_t layer) {
     if (!ctx || !c || !c->d_k || !c->d_v || !c->d_table) return GRAFT_ERR_INVALID_ARG;
@@ -474,6 +476,7 @@ static graft_status check_cache(const graft_ctx* ctx, int32_t batch, const graft
         return GRAFT_ERR_INVALID_ARG;
     if (c->layers < 1 || c->n_pages < 1 || c->kv_heads < 1 || c->table_width < 1) return GRAFT_ERR_INVALID_ARG;
     if (layer < 0 || layer >= c->layers) return GRAFT_ERR_INVALID_ARG;
+    if (batch > kMostSequences) return GRAFT_ERR_UNSUPPORTED;
     if (((uintptr_t)c->d_k | (uintptr_t)c->d_v | (uintptr_t)c->d_k_exp | (uintptr_t)c->d_v_exp) & 15) return GRAFT_ERR_INVALID_ARG;
     if (c->head_dim != 64 && c->head_dim != 128) return GRAFT_ERR_UNSUPPORTED;
     if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return GRAFT_ERR_UNSUPPORTED;
@@ -540,7 +543,7 @@ graft_status graft_tree_attention(graft_ctx* ctx, int32_t batch, const graft_cac
     // eight for every 256 rows)
     const double row_tiles = (double)batch * ((double)rows * (q_heads / cache->kv_heads) / 128 + 2);
     if (2 * row_tiles * cache->kv_heads * ((double)cache->table_width * cache->page_size / 128 + 2) >= 2147483648.0) return GRAFT_ERR_UNSUPPORTED;
-    if (cache->kv_heads > 65535 || batch > 65535) return GRAFT_ERR_UNSUPPORTED;
+    if (cache->kv_heads > 65535) return GRAFT_ERR_UNSUPPORTED;
     void* scratch = grown(ctx->attn_scratch, tree_attn_scratch_bytes(ctx, batch, cache, q_heads, rows, shared));
     if (scratch == nullptr) return GRAFT_ERR_WORKSPACE;
     if (tree_attn_launch(ctx, batch, cache, layer, q_heads, rows, q_stride, d_q, scale, d_prefix_len, d_count, d_mask, shared, d_out,
@@ -560,6 +563,7 @@ graft_status graft_verify(graft_ctx* ctx, int32_t batch, const graft_tree_out* t
     if (batch < 1 || batch > ctx->cfg.max_batch || rows < 1 || rows > ctx->nmax) return GRAFT_ERR_INVALID_ARG;
     if (logits_dtype != GRAFT_F32 && logits_dtype != GRAFT_BF16) return GRAFT_ERR_INVALID_ARG;
     if ((uintptr_t)d_target_logits % (logits_dtype == GRAFT_BF16 ? 2 : 4)) return GRAFT_ERR_INVALID_ARG;
+    if (batch > kMostSequences) return GRAFT_ERR_UNSUPPORTED;
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess) {
         cudaGetLastError();
