@@ -489,6 +489,12 @@ static graft_status check_cache(const graft_ctx* ctx, int32_t batch, const graft
     }
     return dev == ctx->device ? GRAFT_OK : GRAFT_ERR_INVALID_ARG;
 }
+// What a call says of its launches.  One that failed is not left behind as CUDA's last error, where the next call would take it for its own.
+static graft_status launched(cudaError_t e) {
+    if (e == cudaSuccess) return GRAFT_OK;
+    cudaGetLastError();
+    return GRAFT_ERR_CUDA;
+}
 // rows a call brings or takes: `heads` of them a token, `stride` numbers from one token's to the next's
 static graft_status check_rows(const graft_cache* c, int32_t rows, int32_t heads, int64_t stride) {
     if (rows < 1 || stride < (int64_t)heads * c->head_dim || stride % 8) return GRAFT_ERR_INVALID_ARG;
@@ -503,8 +509,8 @@ graft_status graft_cache_write(graft_ctx* ctx, int32_t batch, const graft_cache*
     if (gs != GRAFT_OK) return gs;
     if (!d_prefix_len || !d_count || !d_key || !d_value || (((uintptr_t)d_key | (uintptr_t)d_value) & 15)) return GRAFT_ERR_INVALID_ARG;
     if ((gs = check_rows(cache, rows, cache->kv_heads, stride)) != GRAFT_OK) return gs;
-    return cache_rows_launch(ctx, true, batch, cache, layer, d_prefix_len, d_count, rows, stride, d_key, d_value, d_status,
-                             (cudaStream_t)stream) == cudaSuccess ? GRAFT_OK : GRAFT_ERR_CUDA;
+    return launched(cache_rows_launch(ctx, true, batch, cache, layer, d_prefix_len, d_count, rows, stride, d_key, d_value, d_status,
+                                      (cudaStream_t)stream));
 }
 
 graft_status graft_cache_read(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer, const int32_t* d_prefix_len,
@@ -514,8 +520,8 @@ graft_status graft_cache_read(graft_ctx* ctx, int32_t batch, const graft_cache* 
     if (!d_prefix_len || !d_count || !d_key || !d_value || (((uintptr_t)d_key | (uintptr_t)d_value) & 15)) return GRAFT_ERR_INVALID_ARG;
     const int64_t stride = (int64_t)cache->kv_heads * cache->head_dim;
     if ((gs = check_rows(cache, rows, cache->kv_heads, stride)) != GRAFT_OK) return gs;
-    return cache_rows_launch(ctx, false, batch, cache, layer, d_prefix_len, d_count, rows, stride, d_key, d_value, d_status,
-                             (cudaStream_t)stream) == cudaSuccess ? GRAFT_OK : GRAFT_ERR_CUDA;
+    return launched(cache_rows_launch(ctx, false, batch, cache, layer, d_prefix_len, d_count, rows, stride, d_key, d_value, d_status,
+                                      (cudaStream_t)stream));
 }
 
 graft_status graft_cache_keep(graft_ctx* ctx, int32_t batch, const graft_cache* cache, const int32_t* d_prefix_len,
@@ -525,8 +531,8 @@ graft_status graft_cache_keep(graft_ctx* ctx, int32_t batch, const graft_cache* 
     if (gs != GRAFT_OK) return gs;
     if (!d_prefix_len || !d_accept_len || !d_accept_path) return GRAFT_ERR_INVALID_ARG;
     if ((double)2 * cache->kv_heads * cache->layers >= 2147483648.0) return GRAFT_ERR_UNSUPPORTED;
-    return cache_keep_launch(ctx, batch, cache, d_prefix_len, d_accept_len, d_accept_path, d_next_prefix, d_status,
-                             (cudaStream_t)stream) == cudaSuccess ? GRAFT_OK : GRAFT_ERR_CUDA;
+    return launched(cache_keep_launch(ctx, batch, cache, d_prefix_len, d_accept_len, d_accept_path, d_next_prefix, d_status,
+                                      (cudaStream_t)stream));
 }
 
 graft_status graft_tree_attention(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer, int32_t q_heads, int32_t rows,
@@ -546,12 +552,8 @@ graft_status graft_tree_attention(graft_ctx* ctx, int32_t batch, const graft_cac
     if (cache->kv_heads > 65535) return GRAFT_ERR_UNSUPPORTED;
     void* scratch = grown(ctx->attn_scratch, tree_attn_scratch_bytes(ctx, batch, cache, q_heads, rows, shared));
     if (scratch == nullptr) return GRAFT_ERR_WORKSPACE;
-    if (tree_attn_launch(ctx, batch, cache, layer, q_heads, rows, q_stride, d_q, scale, d_prefix_len, d_count, d_mask, shared, d_out,
-                         d_lse, d_status, scratch, (cudaStream_t)stream) != cudaSuccess) {
-        cudaGetLastError();
-        return GRAFT_ERR_CUDA;
-    }
-    return GRAFT_OK;
+    return launched(tree_attn_launch(ctx, batch, cache, layer, q_heads, rows, q_stride, d_q, scale, d_prefix_len, d_count, d_mask, shared,
+                                     d_out, d_lse, d_status, scratch, (cudaStream_t)stream));
 }
 
 graft_status graft_verify(graft_ctx* ctx, int32_t batch, const graft_tree_out* trees, int32_t rows, graft_dtype logits_dtype,
@@ -570,10 +572,8 @@ graft_status graft_verify(graft_ctx* ctx, int32_t batch, const graft_tree_out* t
         return GRAFT_ERR_CUDA;
     }
     if (dev != ctx->device) return GRAFT_ERR_INVALID_ARG;
-    if (verify_launch(ctx, batch, trees, rows, logits_dtype, d_target_logits, d_temperature, d_uniform, d_accept_len, d_accept_path,
-                      d_bonus_token, d_status, (cudaStream_t)stream) != cudaSuccess)
-        return GRAFT_ERR_CUDA;
-    return GRAFT_OK;
+    return launched(verify_launch(ctx, batch, trees, rows, logits_dtype, d_target_logits, d_temperature, d_uniform, d_accept_len,
+                                  d_accept_path, d_bonus_token, d_status, (cudaStream_t)stream));
 }
 
 static_assert(sizeof(graft_vocab_partial) == 280, "the Python binding gathers partials as 280-byte records");
