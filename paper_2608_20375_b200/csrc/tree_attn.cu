@@ -1566,6 +1566,7 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
             }
             const bool masked = s0 + 16 > base;
             bool spoilt[4] = {false, false, false, false};
+            uint32_t sees = 0;  // bit i: score i is of a slot that its row sees
             if (masked) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -1575,6 +1576,7 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
                         seen = p.mask == nullptr ? j <= node
                                                  : j < 32 * p.words && ((p.mask[((size_t)b * p.nmax + node) * p.words + (j >> 5)] >> (j & 31)) & 1);
                     s[i] = seen ? s[i] : -INFINITY;
+                    sees |= (seen ? 1u : 0u) << i;
                 }
                 // V of slots that are not there is taken out, and of new slots that are not numbers: what of those is seen is added in the end
 #pragma unroll
@@ -1654,6 +1656,8 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
                     if (Q8) e4m3_factors(__ldg(c.v_exp + r), fv, mv);
                     const float w0 = __shfl_sync(0xFFFFFFFFu, i < 8 ? s[0] : s[2], (i & 7) * 4 + q4);
                     const float w1 = __shfl_sync(0xFFFFFFFFu, i < 8 ? s[1] : s[3], (i & 7) * 4 + q4);
+                    // (a weight of a slot that is seen may be too small for fp32 and 0: what it stands before is not a number all the same)
+                    const uint32_t see = __shfl_sync(0xFFFFFFFFu, sees >> (i < 8 ? 0 : 2), (i & 7) * 4 + q4);
 #pragma unroll
                     for (int y = 0; y < D / 8; ++y) {
                         const uint8_t* from = c.v + (r * D + dim(y)) * kBytes;
@@ -1662,8 +1666,8 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
                             v = __uint_as_float(e4m3x4_to_bf16(*from, fv, mv).x << 16);
                         else
                             v = __uint_as_float((uint32_t) * (const uint16_t*)from << 16);
-                        if (w0 > 0.0f) o[y / 2][2 * (y & 1)] += w0 * v;
-                        if (w1 > 0.0f) o[y / 2][2 * (y & 1) + 1] += w1 * v;
+                        if (see & 1) o[y / 2][2 * (y & 1)] += w0 * v;
+                        if (see & 2) o[y / 2][2 * (y & 1) + 1] += w1 * v;
                     }
                 }
             }

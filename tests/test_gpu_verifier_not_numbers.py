@@ -117,3 +117,26 @@ def test_a_key_of_a_shared_prefix_that_is_not_a_number_reaches_all_sequences(pla
         key[:, 24 + place, 1, 7] = math.nan
 
     assert _keys(dtype, 20, 8, 2, 128, [81, 90, 200, 400], spoil, shared=64) == 4
+
+
+@pytest.mark.parametrize("dtype", [BF, Q8])
+@pytest.mark.parametrize("rows,Hq,Hk,D", [(8, 1, 1, 64), (4, 4, 2, 128), (20, 4, 2, 64), (40, 8, 2, 128)])
+@pytest.mark.parametrize("where", [-50, 1])  # in the prefix, the second new row
+def test_a_value_that_is_not_a_number_behind_the_smallest_weight(where, rows, Hq, Hk, D, dtype):
+    """A weight below fp32's smallest number is 0 there, not in the definition: infinity in its slot's value reaches the rows that see it."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    base, page = 90, 16
+    g = _graft(max(2, rows), 1)
+    table, n_pages = ref.page_table(np.random.default_rng(1), 1, 10)
+    c = _cache(gen, (1, n_pages, Hk, page, D), dtype)
+    key, value = (torch.randn((1, base + rows, Hk, D), generator=gen, device="cuda").to(BF) for _ in range(2))
+    key[:, base + where], value[:, base + where, :, 3] = -60.0, math.inf  # (scores of -200 and less)
+    q = torch.randn((1, rows, Hq, D), generator=gen, device="cuda").abs().to(BF)
+    tb, out = _i32(table), torch.zeros((1, rows, Hq, D), dtype=BF, device="cuda")
+    g.cache_write(c, 0, tb, _i32([1]), _i32([base + rows]), key, value)
+    g.tree_attention(c, 0, tb, q, _i32([base + 1]), _i32([rows]), None, out)
+    assert ((q.float().sum(3) * -60.0 * D ** -0.5) < -200).all()
+    first = max(where, 0)
+    assert not torch.isfinite(out[0, first:, :, 3]).any() and torch.isfinite(out[0, :first]).all()
+    if dtype is BF:  # (a row of e4m3 numbers is NaN as a whole)
+        assert torch.isfinite(out[..., 4:]).all()
