@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const VerifyParams 
                         if (lane >= o) sum += y;
                     }
                     const double left = (greedy ? 1.0 : Z) - (ahead + (sum - w));
-                    const bool ok = is && u * left < w;
+                    const bool ok = is && w > 0.0 && u * left < w;  // (rounding may leave less than nothing behind the siblings)
                     const bool near = is && !exact && w > 0.0 && fabs(u * left - w) <= near_by * Z;
                     const unsigned oks = __ballot_sync(kAll, ok), nears = __ballot_sync(kAll, near);
                     const int f = oks ? __ffs(oks) - 1 : 32;
