@@ -262,6 +262,7 @@ graft_status graft_set_hist_window(graft_ctx* ctx, int32_t w, int32_t* d_window,
  * GRAFT_BF16: entries as they come.  GRAFT_E4M3: a row x (one token, one head, K or V) is held as e4m3 numbers y = x 2^-e, rounded
  * to nearest even, and e + 127 in a byte, e the smallest whole number with max |x| <= 448 2^e, at least -120.  A power of two costs
  * no precision (what is not below 2^-13 of its row's largest keeps its four bits) and makes reading back exact in bf16.  A row with a NaN or an infinity: byte 255, reads back as NaN.
+ * A number of 1.9375 2^127 or more is rounded to 2^128, which is infinity in bf16.
  *
  * A sequence that would touch a slot beyond its table or a page outside [0, n_pages), or whose prefix length is below 1 or whose
  * count is negative or above `rows`, is left out of the call as a whole: nothing of it is read or written, and d_status[b] (may be
@@ -310,7 +311,8 @@ graft_status graft_cache_keep(graft_ctx* ctx, int32_t batch, const graft_cache* 
  *   NaN or +inf (an entry that is not a number): NaN in both; a score of -inf weighs nothing.  Rows behind the count are left as they were.
  *   shared: the first `shared` slots (a multiple of page_size; 0: none) are the same pages in every sequence's table (sequence 0's
  *   are read) and are gone through once for the rows of all sequences; every prefix_len is above `shared` (else GRAFT_ST_BAD_CACHE).
- * Scores, statistics and sums are fp32; the weights p enter the second product as bf16, as a bf16 cache's values do. */
+ *   |scale| <= 2.2e38.
+ * Scores (log2(e) times as large), statistics and sums are fp32; the weights p enter the second product as bf16, as a bf16 cache's values do. */
 graft_status graft_tree_attention(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer, int32_t q_heads,
                                   int32_t rows, int64_t q_stride, const void* d_q, float scale, const int32_t* d_prefix_len,
                                   const int32_t* d_count, const uint32_t* d_mask, int32_t shared, void* d_out, float* d_lse,

@@ -1,4 +1,5 @@
 // C ABI of libgraft: context, argument validation, kernel sequencing.  See include/graft.h.
+#include <float.h>
 #include <math.h>
 #include <stdlib.h>
 #include <string.h>
@@ -541,7 +542,8 @@ graft_status graft_tree_attention(graft_ctx* ctx, int32_t batch, const graft_cac
     graft_status gs = check_cache(ctx, batch, cache, layer);
     if (gs != GRAFT_OK) return gs;
     if (!d_q || !d_prefix_len || !d_count || !d_out || (((uintptr_t)d_q | (uintptr_t)d_out) & 15)) return GRAFT_ERR_INVALID_ARG;
-    if (q_heads < 1 || q_heads % cache->kv_heads || !(scale == scale) || scale - scale != 0.0f) return GRAFT_ERR_INVALID_ARG;
+    // (the kernels work with scale log2(e) in fp32)
+    if (q_heads < 1 || q_heads % cache->kv_heads || !(fabs((double)scale) <= FLT_MAX / 1.5)) return GRAFT_ERR_INVALID_ARG;
     if ((gs = check_rows(cache, rows, q_heads, q_stride)) != GRAFT_OK) return gs;
     if (d_mask && rows > ctx->nmax) return GRAFT_ERR_INVALID_ARG;
     if (shared < 0 || shared % cache->page_size || shared > cache->table_width * cache->page_size) return GRAFT_ERR_INVALID_ARG;

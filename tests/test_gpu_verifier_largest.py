@@ -66,3 +66,35 @@ def test_one_sequence_more_is_refused():
             call()
         torch.cuda.synchronize()
         assert int(one.sum()) == MOST + 1  # (nothing of a refusal is left for the next launch)
+
+
+@pytest.mark.parametrize("dtype", [BF, torch.float8_e4m3fn])
+@pytest.mark.parametrize("rows", [1, 20])
+def test_the_largest_scale(rows, dtype):
+    """Scores of the usual size from tiny products; a scale beyond fp32's range once it stands in powers of two is refused."""
+    import verifier_ref as ref
+    from paper_2608_20375_b200 import GraftError
+    from test_gpu_verifier import _cache, _graft
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    g, n = _graft(max(2, rows), 1), 300 + rows
+    table, n_pages = ref.page_table(np.random.default_rng(1), 1, 30)
+    c = _cache(gen, (1, n_pages, 1, page, D), dtype)
+    r = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    key, value, q = (2.0 ** -60 * r(1, n, 1, D)).to(BF), r(1, n, 1, D).to(BF), (2.0 ** -60 * r(1, rows, 2, D)).to(BF)
+    out, lse, one = torch.zeros_like(q), torch.zeros((1, rows, 2), device="cuda"), _i32([1])
+    g.cache_write(c, 0, _i32(table), one, _i32([n]), key, value)
+    call = lambda scale: g.tree_attention(c, 0, _i32(table), q, _i32([301]), _i32([rows]), None, out, lse, scale=scale)  # noqa: E731
+    call(2.0 ** 118)
+    torch.cuda.synchronize()
+    slots = np.arange(n)
+    exps = (None, None) if dtype is BF else (c.k_exp[0].cpu(), c.v_exp[0].cpu())
+    k, v = (ref.entries(t[0].cpu(), e, table[0], slots) for t, e in zip((c.k, c.v), exps))
+    seen = slots[None, :] <= 300 + np.arange(rows)[:, None]
+    wo, wl, tol, ltol = ref.attention(q[0].cpu().double().numpy(), k, v, seen, 2.0 ** 118)
+    assert (np.abs(out[0].cpu().double().numpy() - wo) <= tol).all() and (np.abs(lse[0].cpu().double().numpy() - wl) <= ltol).all()
+    for scale in (2.2e38, -2.2e38):
+        call(scale)
+    for scale in (2.4e38, -2.4e38, 3.4e38):
+        with pytest.raises(GraftError, match="invalid"):
+            call(scale)
+    torch.cuda.synchronize()
