@@ -10,7 +10,8 @@
  * Conventions
  *   - Pointers named d_* are DEVICE pointers; all others are HOST pointers.  The caller owns
  *     every buffer it passes in; the library never frees or reallocates them.  A context owns
- *     only its own scratch (sized from max_batch at creation) and copies of the parameters.
+ *     only its own scratch (sized from max_batch at creation; that of graft_tdes_precompute and graft_tree_attention comes
+ *     with the calls, see there) and copies of the parameters.
  *   - All tensors are dense, row-major, contiguous.  Logits rows may start at any address that
  *     is a multiple of the element size (rows need not be 16-byte aligned).
  *   - `stream` is a cudaStream_t passed as void* (NULL = the legacy default stream).  Calls only
@@ -312,6 +313,10 @@ graft_status graft_cache_keep(graft_ctx* ctx, int32_t batch, const graft_cache* 
  *   shared: the first `shared` slots (a multiple of page_size; 0: none) are the same pages in every sequence's table (sequence 0's
  *   are read) and are gone through once for the rows of all sequences; every prefix_len is above `shared` (else GRAFT_ST_BAD_CACHE).
  *   |scale| <= 2.2e38.
+ * A call uses scratch of the context: up to 42 MB; behind a shared prefix 256 (head_dim + 2) fp32 numbers for each of kv_heads
+ * (ceil(batch R / 256) + batch ceil(R / 256)) units and of the SMs, R = rows q_heads / kv_heads (64 trees of 513 nodes, 32 query heads on 8 of 128:
+ * 1.2 GB).  The first call allocates it and one that needs more replaces it (by at least twice as much, if there is memory for that), under
+ * stream capture too; a captured call keeps the scratch that it was captured with until the context is destroyed.
  * Scores (log2(e) times as large), statistics and sums are fp32; the weights p enter the second product as bf16, as a bf16 cache's values do. */
 graft_status graft_tree_attention(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer, int32_t q_heads,
                                   int32_t rows, int64_t q_stride, const void* d_q, float scale, const int32_t* d_prefix_len,

@@ -58,7 +58,7 @@ CtxExtra* extra_of(graft_ctx* ctx) { return (CtxExtra*)ctx->stage; }
 // Scratch of a call, `need` bytes at least, or NULL if there is no memory for it.  It comes with the first call that needs
 // it, be it under stream capture: the allocation is made outside of any capture.  A captured call keeps the address, so
 // scratch that has become too small lives on until the context goes; a new piece is at least twice the size of the last, so
-// that all the old ones together are smaller than the one in use.
+// that all the old ones together are smaller than the one in use, unless there is memory for no more than the call needs.
 void* grown(Grown& g, size_t need) {
     if (g.bytes >= need) return g.p;
     if (g.p && g.n_old == kMaxOld) return nullptr;
@@ -67,11 +67,14 @@ void* grown(Grown& g, size_t need) {
         cudaGetLastError();
         return nullptr;
     }
-    const size_t bytes = need > 2 * g.bytes ? need : 2 * g.bytes;
+    size_t bytes = need > 2 * g.bytes ? need : 2 * g.bytes;
     void* buf = nullptr;
-    if (cudaMalloc(&buf, bytes) != cudaSuccess) {
+    for (;;) {
+        if (cudaMalloc(&buf, bytes) == cudaSuccess) break;
         cudaGetLastError();
         buf = nullptr;
+        if (bytes == need) break;
+        bytes = need;
     }
     cudaThreadExchangeStreamCaptureMode(&mode);
     if (buf == nullptr) return nullptr;
