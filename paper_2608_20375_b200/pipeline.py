@@ -62,7 +62,7 @@ class MicroBatch:
             # a row of statuses a call: two a layer (write, attention), earlier calls of layers that were attended to again, walk, move
             self._calls = torch.zeros((2 * self.cache.k.shape[0] + 3, self.batch), dtype=i32, device=dev)
             self._bits = (1 << torch.arange(6, dtype=i32, device=dev)).view(-1, 1, 1)  # (ST_BAD_LOGITS .. ST_BAD_TREE)
-            self._attended = set()
+            self._attended = None  # layers of the round under way (None: there is none, calls are made by hand)
         if self.status is None:
             self.status = torch.zeros(self.batch, dtype=i32, device=dev)
 
@@ -70,22 +70,25 @@ class MicroBatch:
         """Forget the statuses of the round before."""
         if self.cache is not None:
             self._calls.zero_()
-            self._attended.clear()
+            self._attended = set()
 
     def attend(self, layer, q, key, value, out, lse=None, scale=None, shared=0):
         """One layer of the target over this round's trees: the nodes' new entries go into the cache, q [batch, rows, q_heads, head_dim]
-        sees the prefix and the nodes above its own."""
+        sees the prefix and the nodes above its own.  Called by hand, between no begin_round and walk, it leaves its own status."""
         if self.cache is None:
             raise GraftError("the micro-batch has no cache")
         if not 0 <= layer < self.cache.k.shape[0]:
             raise GraftError(f"layer must be below {self.cache.k.shape[0]}, got {layer}")
         written, attended = self._calls[2 * layer], self._calls[2 * layer + 1]
-        if layer in self._attended:
-            self._calls[-3].bitwise_or_(written | attended)
-        self._attended.add(layer)
+        if self._attended is not None:
+            if layer in self._attended:
+                self._calls[-3].bitwise_or_(written | attended)
+            self._attended.add(layer)
         self.graft.cache_write(self.cache, layer, self.table, self.prefix_len, self.out.n_nodes, key, value, written)
         self.graft.tree_attention(self.cache, layer, self.table, q, self.prefix_len, self.out.n_nodes, self.out.mask, out, lse, scale, shared,
                                   attended)
+        if self._attended is None:
+            torch.bitwise_or(written, attended, out=self.status)
 
     def walk(self, answer):
         """The walk along this round's trees by what the verifier answered, and with a cache the move of what was accepted."""
@@ -96,6 +99,7 @@ class MicroBatch:
             self.graft.accept(self.out, answer, self.accept_len, self.accept_path, self.bonus_token)
         if self.cache is None:
             return
+        self._attended = None
         torch.sum((self._calls[:-1] & self._bits).amax(1), 0, dtype=torch.int32, out=self.status)
         # (an accepted length below 0 leaves a sequence where it is; lengths are below 64)
         moved = torch.sub(self.accept_len, self.status, alpha=64)

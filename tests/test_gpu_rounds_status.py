@@ -194,3 +194,22 @@ def test_rounds_captured_in_a_graph_report_too():
 
     before = t.round(fine)
     t.check(before, [0] * B)
+
+
+def test_attention_by_hand_leaves_its_status():
+    """Outside of a round a layer's call reports what it found, as the library's calls do."""
+    t = _Target()
+    x = t.draft(0, 0)
+    t.mb.graft.build_trees(x["logits"], None, x["root_token"], None, t.mb.prefix_len, x["fixed_budget"], t.mb.out)
+    good = t.mb.table.clone()
+    for layer in (0, 1, 1):
+        t.mb.table[3, 1] = -1
+        t.attend(layer)
+        assert t.mb.status.tolist() == [0, 0, 0, BAD_CACHE]
+        t.mb.table.copy_(good)
+        t.attend(layer)
+        assert not t.mb.status.any()
+    t.well()
+    t.mb.table[3, 1] = -1
+    t.attend(0)
+    assert t.mb.status.tolist() == [0, 0, 0, BAD_CACHE]
