@@ -19,8 +19,8 @@
 // Sequences of up to eight rows a key head (single tokens) have a kernel of their own, on the same plan: see "few rows".
 //
 // What bounds it.  Large trees (16 of up to 513 nodes behind 6000 to 8192 slots, bf16, 717 GFLOP): 840 to 875 us, the tensor cores busy for 47 % of
-// the time, the exponentials' unit for 36 %: a stream's next product waits for the weights of the one before, and two streams (TMEM holds
-// no more) do not fill the gaps; the clock falls to 1.3 GHz under that load in a long run (980 to 1040 us).  A tile of e4m3 slots is converted
+// the time, the exponentials' unit for 36 %: a stream's next product waits for all of a tile's weights, and two streams (TMEM holds
+// no more) do not fill the gaps; the clock falls to 1.3 GHz under that load in a long run (980 to 1060 us).  A tile of e4m3 slots is converted
 // once a unit, 0.5 to 0.6 us, and is as long on its way as the products: 823 us against 621 for 8 sequences of 512 nodes.  17 nodes (68 rows)
 // behind 4000 slots, bf16: 213 us, 0.78 of the copy's rate.  Small calls are latencies: one tree of 65 nodes behind 1500 slots 31 us, of
 // which plan 4, attention 10 to 15, joining 8, and the hand-overs of three kernels.

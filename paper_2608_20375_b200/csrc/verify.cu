@@ -4,10 +4,10 @@
 // One cluster of CTAs a sequence; each CTA goes through its share of the visited node's row.  Visited rows only are read, one after
 // another: which row comes next is known when the one before is summed up.
 //
-// What bounds it: a chain of dependent steps, one a visited node.  64 sequences, 65 nodes, V = 151,936 bf16, 13 steps in the longest walk: 84 to
-// 89 us, of which 5 a step (a row of 304 KB by 16 CTAs, their sums exchanged through the cluster's shared memory) and 14 for the bonus token, whose
-// row is summed in fp64 (64 operations a clock and SM) and gone through twice more.  One sequence, V = 32,000 fp32: 13 to 16 us.  Rows read: 58 MB,
-// 9 us at the copy's rate.
+// What bounds it: a chain of dependent steps, one a visited node.  64 sequences, 65 nodes, V = 151,936 bf16, 13 steps in the longest walk: 78 to
+// 89 us, of which 5 a step (a row of 304 KB by 8 CTAs, their sums exchanged through the cluster's shared memory) and 14 for the bonus token, whose
+// row is summed in fp64 (64 operations a clock and SM) and gone through twice more.  One sequence, V = 32,000 fp32, 16 CTAs: 12 to 19 us, by the
+// walk's length.  Rows read: 58 MB, 9 us at the copy's rate.
 #include <float.h>
 
 #include "common.cuh"
