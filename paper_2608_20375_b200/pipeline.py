@@ -59,30 +59,40 @@ class MicroBatch:
         if self.cache is not None:
             if self.table is None or self.prefix_len is None:
                 raise GraftError("a micro-batch with a cache has a table and prefix lengths")
-            # a row of statuses a call: two a layer (write, attention), earlier calls of layers that were attended to again, walk, move
-            self._calls = torch.zeros((2 * self.cache.k.shape[0] + 3, self.batch), dtype=i32, device=dev)
-            self._bits = (1 << torch.arange(6, dtype=i32, device=dev)).view(-1, 1, 1)  # (ST_BAD_LOGITS .. ST_BAD_TREE)
-            self._attended = None  # layers of the round under way (None: there is none, calls are made by hand)
         if self.status is None:
             self.status = torch.zeros(self.batch, dtype=i32, device=dev)
+        self._attended = None  # layers of the round under way (None: there is none, calls are made by hand)
+        self._calls = None
+        if self.cache is not None:
+            self._rows()
+
+    def _rows(self):
+        """A row of statuses a call: two a layer (write, attention), earlier calls of layers that were attended to again, walk, move."""
+        n = 2 * self.cache.k.shape[0] + 3
+        if self._calls is None or self._calls.shape[0] != n:  # (a micro-batch may be given its cache later)
+            self._calls = torch.zeros((n, self.batch), dtype=torch.int32, device=self.status.device)
+            self._bits = (1 << torch.arange(6, dtype=torch.int32, device=self.status.device)).view(-1, 1, 1)  # (ST_BAD_LOGITS .. ST_BAD_TREE)
+        return self._calls
 
     def begin_round(self):
-        """Forget the statuses of the round before."""
+        """Forget the statuses of the round before.  run_rounds calls it, then draft and verify, then walk."""
         if self.cache is not None:
-            self._calls.zero_()
+            self._rows().zero_()
             self._attended = set()
 
     def attend(self, layer, q, key, value, out, lse=None, scale=None, shared=0):
         """One layer of the target over this round's trees: the nodes' new entries go into the cache, q [batch, rows, q_heads, head_dim]
-        sees the prefix and the nodes above its own.  Called by hand, between no begin_round and walk, it leaves its own status."""
+        sees the prefix and the nodes above its own.  Outside of a round (by hand, without begin_round) status
+        is this call's."""
         if self.cache is None:
             raise GraftError("the micro-batch has no cache")
         if not 0 <= layer < self.cache.k.shape[0]:
             raise GraftError(f"layer must be below {self.cache.k.shape[0]}, got {layer}")
-        written, attended = self._calls[2 * layer], self._calls[2 * layer + 1]
+        calls = self._rows()
+        written, attended = calls[2 * layer], calls[2 * layer + 1]
         if self._attended is not None:
             if layer in self._attended:
-                self._calls[-3].bitwise_or_(written | attended)
+                calls[-3].bitwise_or_(written | attended)
             self._attended.add(layer)
         self.graft.cache_write(self.cache, layer, self.table, self.prefix_len, self.out.n_nodes, key, value, written)
         self.graft.tree_attention(self.cache, layer, self.table, q, self.prefix_len, self.out.n_nodes, self.out.mask, out, lse, scale, shared,
@@ -92,19 +102,20 @@ class MicroBatch:
 
     def walk(self, answer):
         """The walk along this round's trees by what the verifier answered, and with a cache the move of what was accepted."""
-        at = self._calls[-2] if self.cache is not None else self.status
+        calls = self._rows() if self.cache is not None else None
+        at = self.status if calls is None else calls[-2]
         if isinstance(answer, Sampled):
             self.graft.verify(self.out, answer.logits, answer.temperature, answer.uniform, self.accept_len, self.accept_path, self.bonus_token, at)
         else:
             self.graft.accept(self.out, answer, self.accept_len, self.accept_path, self.bonus_token)
-        if self.cache is None:
+        if calls is None:
             return
         self._attended = None
-        torch.sum((self._calls[:-1] & self._bits).amax(1), 0, dtype=torch.int32, out=self.status)
+        torch.sum((calls[:-1] & self._bits).amax(1), 0, dtype=torch.int32, out=self.status)
         # (an accepted length below 0 leaves a sequence where it is; lengths are below 64)
         moved = torch.sub(self.accept_len, self.status, alpha=64)
-        self.graft.cache_keep(self.cache, self.table, self.prefix_len, moved, self.accept_path, self.prefix_len, self._calls[-1])
-        torch.where(self.status == 0, self._calls[-1], self.status, out=self.status)
+        self.graft.cache_keep(self.cache, self.table, self.prefix_len, moved, self.accept_path, self.prefix_len, calls[-1])
+        torch.where(self.status == 0, calls[-1], self.status, out=self.status)
 
 
 @dataclass

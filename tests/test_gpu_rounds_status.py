@@ -213,3 +213,27 @@ def test_attention_by_hand_leaves_its_status():
     t.mb.table[3, 1] = -1
     t.attend(0)
     assert t.mb.status.tolist() == [0, 0, 0, BAD_CACHE]
+
+
+def test_a_cache_that_comes_after_the_micro_batch():
+    """A micro-batch that was made without a cache is given one, and another of more layers: rounds report as if it had had it."""
+    from paper_2608_20375_b200 import KVCache
+    t = _Target()
+    for more in (layers, layers + 3):
+        mb = _Target(cache=False).mb
+        c = KVCache.alloc(more, B * pages, Hk, page, D)
+        mb.cache, mb.table, mb.prefix_len = c, t.mb.table, _i32([20, 33, 1, 47])
+        t.mb, t.cache = mb, True
+        t.well()
+
+        def verify(i, r, out):
+            good = t.mb.table.clone()
+            t.mb.table[1, 2] = B * pages
+            t.attend(more - 1)
+            t.mb.table.copy_(good)
+            t.attend(0)
+            return t.answer(out)
+
+        t.check(t.round(verify), [0, BAD_CACHE, 0, 0])
+    t.mb.cache = KVCache.alloc(1, B * pages, Hk, page, D)
+    t.check(t.round(lambda i, r, out: (t.attend(0), t.answer(out))[1]), [0] * B)
