@@ -323,6 +323,44 @@ graft_status graft_tree_attention(graft_ctx* ctx, int32_t batch, const graft_cac
                                   const int32_t* d_count, const uint32_t* d_mask, int32_t shared, void* d_out, float* d_lse,
                                   int32_t* d_status, void* stream);
 
+/* Positions turn queries and keys: number pairs (x, y) of a head become gain (x cos a - y sin a, x sin a + y cos a), where pair i has
+ * the angle a = sum over the axes of (position + shift) d_freq[axis, i] radians.  Text has one axis; rows of pictures and clips have a time, a
+ * row and a column, and frequencies that are zero but for the axis that a pair turns with. */
+typedef struct graft_rope {
+    int32_t rot_dim;           /* the first rot_dim numbers of a head are turned, the others are not: a multiple of 16, at most head_dim */
+    int32_t interleaved;       /* 0: pair i is numbers i and i + rot_dim / 2; 1: numbers 2 i and 2 i + 1 */
+    int32_t axes;              /* 1 to 8 */
+    float gain;                /* 1 unless a model scales what it turns */
+    const float* d_freq;       /* [axes, rot_dim / 2] */
+    const int32_t* d_position; /* [batch, pos_rows, pos_axes], pos_rows >= rows; NULL: a row's position is its slot, d_prefix_len[b] - 1 + i */
+    int32_t pos_rows, pos_axes; /* pos_axes 1 (the same on all axes; d_position of graft_build_trees) or `axes` */
+    const int32_t* d_shift;    /* [batch] added to all of a sequence's positions, or NULL (pictures take fewer positions than slots) */
+} graft_rope;
+
+/* The new rows of one layer on their way to attention, in one call: queries and keys are turned by their positions, keys and values go into the
+ * cache as graft_cache_write does it.  d_q [batch, rows, q_heads, head_dim] bf16 with row stride q_stride, d_q_out with out_stride (the same array
+ * with the same stride, or one apart from all others); d_key, d_value as graft_cache_write's, kv_stride.  q_heads 0: no queries (d_q,
+ * d_q_out NULL).  Angles are worked out in fp64 and reduced before they are rounded to fp32; turned numbers are fp32 and rounded once: to bf16, or into
+ * an e4m3 cache by its rule applied to the fp32 numbers.  Rows behind the count, and sequences that are left out, are not touched.
+ * Strides are multiples of 8, rows 16-byte aligned. */
+graft_status graft_cache_append(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer, const graft_rope* rope, int32_t q_heads,
+                                const int32_t* d_prefix_len, const int32_t* d_count, int32_t rows, int64_t q_stride, const void* d_q,
+                                int64_t kv_stride, const void* d_key, const void* d_value, int64_t out_stride, void* d_q_out,
+                                int32_t* d_status, void* stream);
+
+/* graft_tree_attention for a layer whose rows see the last `window` positions and the first `sinks` only.
+ *   A slot before d_prefix_len[b] - 1 has its number as its position.  Row i's position is d_position[b, i] (d_position [batch, Nmax] as
+ *   graft_build_trees emits it, held to what a tree can have: d_prefix_len[b] - 1 up to i more) where there is a mask, else its slot; d_mask and
+ *   d_position are both given or both NULL.  Row i sees what graft_tree_attention lets it see, of that the positions from sinks on only
+ *   where they are less than `window` behind its own (window >= 1: its own is the first; sinks >= 0).
+ * Pages that hold no slot below `sinks` and none from d_prefix_len[b] - window on are not read, nor are their entries of the table:
+ * a server may take back what fell behind the window.  The other arguments, what is not a number, the scratch and the precision are as
+ * described there; behind many rows without a mask (prompts) each block of rows goes through its own slots alone. */
+graft_status graft_window_attention(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer, int32_t q_heads, int32_t rows,
+                                    int64_t q_stride, const void* d_q, float scale, const int32_t* d_prefix_len, const int32_t* d_count,
+                                    const uint32_t* d_mask, const int32_t* d_position, int32_t window, int32_t sinks, void* d_out,
+                                    float* d_lse, int32_t* d_status, void* stream);
+
 /* The acceptance walk for a target that samples (graft_accept is the one for a target that takes its likeliest token).  The tree's
  * tokens are the drafter's best, not draws, so a child is kept with the target's own probability and what is left of the target's
  * distribution is sampled when none is: the committed tokens are distributed as the target's, whatever the tree.

@@ -22,7 +22,8 @@ ENTRY_POINTS = [
     "graft_create", "graft_destroy", "graft_nmax", "graft_mask_words", "graft_set_saba", "graft_set_tdes_tables",
     "graft_tdes_precompute", "graft_build_trees", "graft_vocab_pass", "graft_vocab_pass_static", "graft_tdes_edges",
     "graft_accept", "graft_tdes_loss", "graft_saba_fit", "graft_set_edge_rows", "graft_edge_rows", "graft_set_hist_window", "graft_vocab_pass_partial", "graft_vocab_merge",
-    "graft_cache_write", "graft_cache_read", "graft_cache_keep", "graft_tree_attention", "graft_verify",
+    "graft_cache_write", "graft_cache_read", "graft_cache_keep", "graft_cache_append",
+    "graft_tree_attention", "graft_window_attention", "graft_verify",
     "graft_build_trees_host", "graft_launch_count", "graft_set_timing", "graft_read_timing", "graft_status_str",
     "graft_version",
 ]
@@ -70,6 +71,11 @@ class _Cache(C.Structure):
     _fields_ = [("layers", C.c_int32), ("n_pages", C.c_int32), ("kv_heads", C.c_int32), ("page_size", C.c_int32),
                 ("head_dim", C.c_int32), ("dtype", C.c_int), ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_exp", C.c_void_p),
                 ("d_v_exp", C.c_void_p), ("d_table", C.c_void_p), ("table_width", C.c_int32)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("axes", C.c_int32), ("gain", C.c_float), ("d_freq", C.c_void_p),
+                ("d_position", C.c_void_p), ("pos_rows", C.c_int32), ("pos_axes", C.c_int32), ("d_shift", C.c_void_p)]
 
 
 _lib = None
@@ -120,6 +126,8 @@ def load_library():
     lib.graft_cache_read.argtypes = [vp, i32, pc, i32, vp, vp, i32, vp, vp, vp, vp]
     lib.graft_cache_keep.argtypes = [vp, i32, pc, vp, vp, vp, vp, vp, vp]
     lib.graft_tree_attention.argtypes = [vp, i32, pc, i32, i32, i32, i64, vp, C.c_float, vp, vp, vp, i32, vp, vp, vp, vp]
+    lib.graft_cache_append.argtypes = [vp, i32, pc, i32, C.POINTER(_Rope), i32, vp, vp, i32, i64, vp, i64, vp, vp, i64, vp, vp, vp]
+    lib.graft_window_attention.argtypes = [vp, i32, pc, i32, i32, i32, i64, vp, C.c_float, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
     lib.graft_verify.argtypes = [vp, i32, C.POINTER(_TreeOut), i32, C.c_int, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.graft_launch_count.argtypes = [vp]
     lib.graft_launch_count.restype = C.c_uint64
@@ -234,6 +242,49 @@ class KVCache:
             ve = _shaped("v_exp", self.v_exp, torch.uint8, shape[:-1], dev)
         return _Cache(layers, n_pages, heads, page, dim, E4M3 if q8 else BF16, _shaped("k", k, dt, shape, dev),
                       _shaped("v", self.v, dt, shape, dev), ke, ve, _shaped("table", table, torch.int32, (batch, width), dev), width)
+
+
+@dataclass
+class Rope:
+    """How positions turn queries and keys (graft_rope in include/graft.h): freq [axes, pairs] float32, radians a position; pairs of numbers
+    of a head are i and i + pairs, or neighbours (interleaved); shift [batch] int32 is added to a sequence's positions."""
+    freq: torch.Tensor
+    interleaved: bool = False
+    gain: float = 1.0
+    shift: torch.Tensor | None = None
+
+    @classmethod
+    def of(cls, rot_dim, base=10000.0, sections=None, striped=False, interleaved=False, gain=1.0, shift=None, device="cuda"):
+        """Frequencies base ** (-2 i / rot_dim).  sections: how many pairs turn with each axis (time, row, column), side by side; striped: the
+        axes take turns pair by pair for as long as a section lasts, what is left over goes to the first."""
+        pairs = rot_dim // 2
+        f = torch.tensor([base ** (-i / pairs) for i in range(pairs)], dtype=torch.float64)
+        sections = [pairs] if sections is None else list(sections)
+        if rot_dim % 2 or sum(sections) != pairs or min(sections) < 0:
+            raise GraftError(f"sections must add up to rot_dim / 2 = {pairs}, got {sections}")
+        axes = len(sections)
+        if striped:
+            axis = [i % axes if i < axes * sections[i % axes] else 0 for i in range(pairs)]
+            if [axis.count(a) for a in range(axes)] != sections:
+                raise GraftError(f"{sections} pairs cannot take turns")
+        else:
+            axis = [a for a, n in enumerate(sections) for _ in range(n)]
+        rows = torch.arange(axes)[:, None] == torch.tensor(axis)[None, :]
+        return cls((rows * f).float().to(device), interleaved, gain, shift)
+
+    def _c(self, batch, rows, position, dev):
+        freq = self.freq
+        if freq.dim() != 2:
+            raise GraftError(f"freq must be [axes, pairs], got {tuple(freq.shape)}")
+        axes, pairs = freq.shape
+        at, pos_rows, pos_axes = None, 0, 0
+        if position is not None:
+            shape = position.shape
+            if len(shape) not in (2, 3) or shape[0] != batch or shape[1] < rows or (len(shape) == 3 and shape[2] not in (1, axes)):
+                raise GraftError(f"position must be [{batch}, {rows} or more] or [{batch}, {rows} or more, {axes}], got {tuple(shape)}")
+            at, pos_rows, pos_axes = _shaped("position", position, torch.int32, shape, dev), shape[1], 1 if len(shape) == 2 else shape[2]
+        return _Rope(2 * pairs, int(self.interleaved), axes, self.gain, _shaped("freq", freq, torch.float32, (axes, pairs), dev), at, pos_rows,
+                     pos_axes, _shaped("shift", self.shift, torch.int32, (batch,), dev))
 
 
 def vocab_pass_static(logits, K, topk_id, topk_lp, lse, row_status):
@@ -469,6 +520,56 @@ class Graft:
             self._ctx, batch, C.byref(cc), _shaped("prefix_len", prefix_len, i32, one, dev), _shaped("accept_len", accept_len, i32, one, dev),
             _shaped("accept_path", accept_path, i32, (batch, self.cfg.L), dev), _shaped("next_prefix", next_prefix, i32, one, dev),
             _shaped("status", status, i32, one, dev), _stream()), "graft_cache_keep")
+
+    def cache_append(self, cache: KVCache, layer, table, prefix_len, count, rope: Rope, q, key, value, q_out=None, position=None, status=None):
+        """q [batch, rows, q_heads, head_dim] turned by its positions into q_out (None: in place), key turned likewise and value into
+        the layer's slots as cache_write does it, in one launch.  position: [batch, rows or more] int32 (the trees' position), [batch, rows or
+        more, axes], or None (a row's slot).  q None: keys and values only."""
+        batch, i32, dev = key.shape[0], torch.int32, _device()
+        cc = cache._c(table, batch, dev)
+        kp, rows, stride = _token_rows("key", key, cc.kv_heads, cc.head_dim, dev)
+        vp, v_rows, v_stride = _token_rows("value", value, cc.kv_heads, cc.head_dim, dev)
+        if value.shape[0] != batch or v_rows != rows or v_stride != stride:
+            raise GraftError("key and value must be laid out alike")
+        qp = op = None
+        heads = q_stride = o_stride = 0
+        if q is not None:
+            if q.dim() != 4 or q.shape[:2] != key.shape[:2]:
+                raise GraftError(f"q must be [{batch}, {rows}, heads, {cc.head_dim}], got {tuple(q.shape)}")
+            heads = q.shape[2]
+            qp, _, q_stride = _token_rows("q", q, heads, cc.head_dim, dev)
+            op, o_stride = qp, q_stride
+            if q_out is not None:
+                if q_out.shape != q.shape:
+                    raise GraftError(f"q_out must have shape {tuple(q.shape)}, got {tuple(q_out.shape)}")
+                op, _, o_stride = _token_rows("q_out", q_out, heads, cc.head_dim, dev)
+        elif q_out is not None:
+            raise GraftError("q_out is given without q")
+        rc = rope._c(batch, rows, position, dev)
+        _check(self.lib, self.lib.graft_cache_append(
+            self._ctx, batch, C.byref(cc), int(layer), C.byref(rc), heads, _shaped("prefix_len", prefix_len, i32, (batch,), dev),
+            _shaped("count", count, i32, (batch,), dev), rows, q_stride, qp, stride, kp, vp, o_stride, op,
+            _shaped("status", status, i32, (batch,), dev), _stream()), "graft_cache_append")
+
+    def window_attention(self, cache: KVCache, layer, table, q, prefix_len, count, mask, position, window, sinks, out, lse=None, scale=None,
+                         status=None):
+        """tree_attention of rows that see the last `window` positions and the first `sinks`.  mask and position [batch, nmax] (the trees'): both or
+        neither (a chain).  Pages that hold nothing that is seen need not be there: their entries in the table are not looked at."""
+        batch, i32, dev = q.shape[0], torch.int32, _device()
+        cc = cache._c(table, batch, dev)
+        if q.dim() != 4:
+            raise GraftError(f"q must be [batch, rows, heads, {cc.head_dim}], got {tuple(q.shape)}")
+        if (mask is None) != (position is None):
+            raise GraftError("mask and position are both given or neither")
+        heads = q.shape[2]
+        qp, rows, stride = _token_rows("q", q, heads, cc.head_dim, dev)
+        _check(self.lib, self.lib.graft_window_attention(
+            self._ctx, batch, C.byref(cc), int(layer), heads, rows, stride, qp, cc.head_dim ** -0.5 if scale is None else scale,
+            _shaped("prefix_len", prefix_len, i32, (batch,), dev), _shaped("count", count, i32, (batch,), dev),
+            _shaped("mask", mask, i32, (batch, self.nmax, self.mask_words), dev), _shaped("position", position, i32, (batch, self.nmax), dev),
+            int(window), int(sinks), _shaped("out", out, torch.bfloat16, (batch, rows, heads, cc.head_dim), dev),
+            _shaped("lse", lse, torch.float32, (batch, rows, heads), dev), _shaped("status", status, i32, (batch,), dev), _stream()),
+            "graft_window_attention")
 
     def tree_attention(self, cache: KVCache, layer, table, q, prefix_len, count, mask, out, lse=None, scale=None, shared=0, status=None):
         """Attention of q [batch, rows, q_heads, head_dim] over one layer of the cache: the prefix, and of the rows' own entries those

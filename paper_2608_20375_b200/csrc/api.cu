@@ -561,6 +561,44 @@ graft_status graft_tree_attention(graft_ctx* ctx, int32_t batch, const graft_cac
                                      d_out, d_lse, d_status, scratch, (cudaStream_t)stream));
 }
 
+graft_status graft_cache_append(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer, const graft_rope* rope, int32_t q_heads,
+                                const int32_t* d_prefix_len, const int32_t* d_count, int32_t rows, int64_t q_stride, const void* d_q,
+                                int64_t kv_stride, const void* d_key, const void* d_value, int64_t out_stride, void* d_q_out,
+                                int32_t* d_status, void* stream) {
+    graft_status gs = check_cache(ctx, batch, cache, layer);
+    if (gs != GRAFT_OK) return gs;
+    if (!rope || !rope->d_freq || !d_prefix_len || !d_count || !d_key || !d_value || q_heads < 0) return GRAFT_ERR_INVALID_ARG;
+    if (q_heads > 0 && (!d_q || !d_q_out)) return GRAFT_ERR_INVALID_ARG;
+    if (((uintptr_t)d_q | (uintptr_t)d_q_out | (uintptr_t)d_key | (uintptr_t)d_value) & 15) return GRAFT_ERR_INVALID_ARG;
+    if (rope->rot_dim < 16 || rope->rot_dim > cache->head_dim || rope->rot_dim % 16 || rope->axes < 1 || rope->axes > 8)
+        return GRAFT_ERR_UNSUPPORTED;
+    if (!(fabsf(rope->gain) <= FLT_MAX)) return GRAFT_ERR_INVALID_ARG;
+    if (rope->d_position && (rope->pos_rows < rows || (rope->pos_axes != 1 && rope->pos_axes != rope->axes))) return GRAFT_ERR_INVALID_ARG;
+    if ((gs = check_rows(cache, rows, cache->kv_heads, kv_stride)) != GRAFT_OK) return gs;
+    if (q_heads > 0 && ((gs = check_rows(cache, rows, q_heads, q_stride)) != GRAFT_OK || (gs = check_rows(cache, rows, q_heads, out_stride)) != GRAFT_OK))
+        return gs;
+    // (a block's rows are counted in 32 bits)
+    if ((double)(q_heads + 2 * (double)cache->kv_heads) * 8 >= 2147483648.0 - 1024) return GRAFT_ERR_UNSUPPORTED;
+    if (q_heads > 0 && d_q == d_q_out && q_stride != out_stride) return GRAFT_ERR_INVALID_ARG;
+    return launched(cache_append_launch(ctx, batch, cache, layer, rope, q_heads, d_prefix_len, d_count, rows, q_stride, d_q, kv_stride, d_key,
+                                        d_value, out_stride, d_q_out, d_status, (cudaStream_t)stream));
+}
+
+graft_status graft_window_attention(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer, int32_t q_heads, int32_t rows,
+                                    int64_t q_stride, const void* d_q, float scale, const int32_t* d_prefix_len, const int32_t* d_count,
+                                    const uint32_t* d_mask, const int32_t* d_position, int32_t window, int32_t sinks, void* d_out,
+                                    float* d_lse, int32_t* d_status, void* stream) {
+    graft_status gs = check_cache(ctx, batch, cache, layer);
+    if (gs != GRAFT_OK) return gs;
+    if (!d_q || !d_prefix_len || !d_count || !d_out || (((uintptr_t)d_q | (uintptr_t)d_out) & 15)) return GRAFT_ERR_INVALID_ARG;
+    if (q_heads < 1 || q_heads % cache->kv_heads || !(fabs((double)scale) <= FLT_MAX / 1.5)) return GRAFT_ERR_INVALID_ARG;
+    if ((gs = check_rows(cache, rows, q_heads, q_stride)) != GRAFT_OK) return gs;
+    if ((d_mask == nullptr) != (d_position == nullptr) || (d_mask && rows > ctx->nmax)) return GRAFT_ERR_INVALID_ARG;
+    if (window < 1 || sinks < 0) return GRAFT_ERR_INVALID_ARG;
+    return launched(window_attn_launch(ctx, batch, cache, layer, q_heads, rows, q_stride, d_q, scale, d_prefix_len, d_count, d_mask, d_position,
+                                       window, sinks, d_out, d_lse, d_status, (cudaStream_t)stream));
+}
+
 graft_status graft_verify(graft_ctx* ctx, int32_t batch, const graft_tree_out* trees, int32_t rows, graft_dtype logits_dtype,
                           const void* d_target_logits, const float* d_temperature, const float* d_uniform, int32_t* d_accept_len,
                           int32_t* d_accept_path, int32_t* d_bonus_token, int32_t* d_status, void* stream) {

@@ -216,6 +216,14 @@ cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache
                              const void* d_q, float scale, const int32_t* d_prefix_len, const int32_t* d_count, const uint32_t* d_mask,
                              int shared, void* d_out, float* d_lse, int32_t* d_status, void* scratch, cudaStream_t st);
 size_t tree_attn_scratch_bytes(const graft_ctx* ctx, int batch, const graft_cache* cache, int q_heads, int rows, int shared);
+// (csrc/append.cu, csrc/window_attn.cu)
+cudaError_t cache_append_launch(graft_ctx* ctx, int batch, const graft_cache* cache, int layer, const graft_rope* rope, int q_heads,
+                                const int32_t* d_prefix_len, const int32_t* d_count, int rows, long long q_stride, const void* d_q,
+                                long long kv_stride, const void* d_key, const void* d_value, long long out_stride, void* d_q_out,
+                                int32_t* d_status, cudaStream_t st);
+cudaError_t window_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache, int layer, int q_heads, int rows, long long q_stride,
+                               const void* d_q, float scale, const int32_t* d_prefix_len, const int32_t* d_count, const uint32_t* d_mask,
+                               const int32_t* d_position, int window, int sinks, void* d_out, float* d_lse, int32_t* d_status, cudaStream_t st);
 cudaError_t verify_launch(graft_ctx* ctx, int batch, const graft_tree_out* trees, int rows, graft_dtype dt, const void* d_logits,
                           const float* d_temperature, const float* d_uniform, int32_t* d_accept_len, int32_t* d_accept_path,
                           int32_t* d_bonus, int32_t* d_status, cudaStream_t st);
