@@ -25,8 +25,8 @@ SOURCES = {
     "saba_fit.cu": ["common.cuh", "internal.h", GRAFT_H],
     "cache.cu": ["common.cuh", "internal.h", "cache.cuh", GRAFT_H],
     "append.cu": ["common.cuh", "internal.h", "cache.cuh", GRAFT_H],
-    "window_attn.cu": ["common.cuh", "internal.h", "cache.cuh", "umma.cuh", GRAFT_H],
-    "tree_attn.cu": ["common.cuh", "internal.h", "cache.cuh", "umma.cuh", GRAFT_H],
+    "window_attn.cu": ["common.cuh", "internal.h", "cache.cuh", "umma.cuh", "attn.cuh", GRAFT_H],
+    "tree_attn.cu": ["common.cuh", "internal.h", "cache.cuh", "umma.cuh", "attn.cuh", GRAFT_H],
     "verify.cu": ["common.cuh", "internal.h", "umma.cuh", GRAFT_H],
     "tables_mma.cu": ["common.cuh", "internal.h", "umma.cuh", GRAFT_H],
 }

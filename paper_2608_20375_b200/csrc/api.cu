@@ -595,8 +595,13 @@ graft_status graft_window_attention(graft_ctx* ctx, int32_t batch, const graft_c
     if ((gs = check_rows(cache, rows, q_heads, q_stride)) != GRAFT_OK) return gs;
     if ((d_mask == nullptr) != (d_position == nullptr) || (d_mask && rows > ctx->nmax)) return GRAFT_ERR_INVALID_ARG;
     if (window < 1 || sinks < 0) return GRAFT_ERR_INVALID_ARG;
+    if (cache->kv_heads > 65535) return GRAFT_ERR_UNSUPPORTED;
+    const size_t bytes = window_attn_scratch_bytes(ctx, batch, cache, q_heads, rows, d_mask != nullptr, window, sinks);
+    if (bytes == 0) return GRAFT_ERR_UNSUPPORTED;
+    void* scratch = grown(ctx->attn_scratch, bytes);
+    if (scratch == nullptr) return GRAFT_ERR_WORKSPACE;
     return launched(window_attn_launch(ctx, batch, cache, layer, q_heads, rows, q_stride, d_q, scale, d_prefix_len, d_count, d_mask, d_position,
-                                       window, sinks, d_out, d_lse, d_status, (cudaStream_t)stream));
+                                       window, sinks, d_out, d_lse, d_status, scratch, (cudaStream_t)stream));
 }
 
 graft_status graft_verify(graft_ctx* ctx, int32_t batch, const graft_tree_out* trees, int32_t rows, graft_dtype logits_dtype,

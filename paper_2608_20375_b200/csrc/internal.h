@@ -110,7 +110,7 @@ struct graft_ctx {
     // scratch that comes with the first call that needs it (api.cu, grown): of the tensor-core table precompute (pieces of split
     // tiles, W's parts, flags of rows) and of graft_tree_attention (the plan, pieces of units that were cut)
     graft::Grown tables_scratch, attn_scratch;
-    int attn_ready;  // variants of the attention kernel that may use their shared memory
+    uint32_t attn_ready, window_ready;  // variants of the attention kernels that may use their shared memory
     int* w_attn_n;   // graft_tree_attention: arrivals, zero between calls
     int verify_ready;  // variants of graft_verify's kernel that may be launched in clusters of 16
     // host-buffer staging (allocated on first use of graft_build_trees_host)
@@ -223,7 +223,9 @@ cudaError_t cache_append_launch(graft_ctx* ctx, int batch, const graft_cache* ca
                                 int32_t* d_status, cudaStream_t st);
 cudaError_t window_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache, int layer, int q_heads, int rows, long long q_stride,
                                const void* d_q, float scale, const int32_t* d_prefix_len, const int32_t* d_count, const uint32_t* d_mask,
-                               const int32_t* d_position, int window, int sinks, void* d_out, float* d_lse, int32_t* d_status, cudaStream_t st);
+                               const int32_t* d_position, int window, int sinks, void* d_out, float* d_lse, int32_t* d_status, void* scratch,
+                               cudaStream_t st);
+size_t window_attn_scratch_bytes(const graft_ctx* ctx, int batch, const graft_cache* cache, int q_heads, int rows, bool mask, int window, int sinks);
 cudaError_t verify_launch(graft_ctx* ctx, int batch, const graft_tree_out* trees, int rows, graft_dtype dt, const void* d_logits,
                           const float* d_temperature, const float* d_uniform, int32_t* d_accept_len, int32_t* d_accept_path,
                           int32_t* d_bonus, int32_t* d_status, cudaStream_t st);

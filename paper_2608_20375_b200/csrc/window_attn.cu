@@ -1,147 +1,203 @@
 // Attention over a paged cache of rows that see the last `window` positions and the first `sinks` (graft_window_attention).
-#include "cache.cuh"
+//
+// The kernels are those of graft_tree_attention (attn.cuh, kWin); what differs is what they go through.  A tree, or up to 256 / group rows of a
+// chain, is an entry of the plan with a line of slots of its own: the sinks, then the slots from the first row's window on up to the last row's
+// own, rounded to whole grains (16 slots for few rows, what a copy brings for others).  Rows see less than that at the line's borders alone: tiles
+// there are masked row by row, and V of places that only some rows see is looked at for what is not a number, as V of new rows is.
+#include "attn.cuh"
 
 namespace graft {
 
 namespace {
 
-constexpr int kThreads = 128;
+// Rows of a sequence that are an entry: a mask's all (they see one another by the mask), else as many as a unit holds.
+__device__ __forceinline__ int entries_of(const AttnParams& p, int n) { return n > 0 ? (n + p.block_rows - 1) / p.block_rows : 0; }
 
-struct WindowParams {
-    CacheView c;
-    const uint8_t* q;
-    long long q_stride;
-    const int32_t* prefix_len;
-    const int32_t* count;
-    const uint32_t* mask;
-    const int32_t* position;
-    __nv_bfloat16* out;
-    float* lse;
-    int32_t* status;
-    float scale;
-    int rows, q_heads, group, nmax, words, window, sinks;
-};
-
-__device__ __forceinline__ float entry_of(const CacheView& c, const uint8_t* x, const uint8_t* exps, size_t row, int d) {
-    if (!exps) return __uint_as_float((uint32_t)((const uint16_t*)x)[row * c.head_dim + d] << 16);
-    uint32_t f, more;
-    e4m3_factors(exps[row], f, more);
-    return __uint_as_float(e4m3x4_to_bf16(x[row * c.head_dim + d], f, more).x << 16);
-}
-
-// A block a row and head, four warps that take 32 slots in turn: a lane a slot for the scores, some numbers of the head for the sums.
-template <int D>
-__global__ void __launch_bounds__(kThreads) window_attn_kernel(const __grid_constant__ WindowParams p) {
-    constexpr int kWarps = kThreads / 32, kPer = D / 32;
-    __shared__ float q[D], sum[kWarps][D], sm[kWarps], sl[kWarps];
-    __shared__ int fine;
+__global__ void __launch_bounds__(kPlanThreads) window_plan_kernel(const __grid_constant__ AttnParams p) {
     pdl_launch_dependents();
     pdl_wait();
+    constexpr int kWarps = kPlanThreads / 32;
     const CacheView& c = p.c;
-    const int i = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int n = p.count[b], base = p.prefix_len[b] - 1, end = base + n, lo = max(0, base - p.window + 1), low = (1 << c.page_shift) - 1;
-    const int32_t* table = c.table + (size_t)b * c.width;
-    if (warp == 0) {
-        bool ok = n >= 0 && n <= p.rows && base >= 0 && (long long)base + n <= (long long)c.width << c.page_shift;
+    __shared__ int fine[kWarps], last;
+    __shared__ int scratch[3][kWarps];
+    __shared__ PlanSeq entries[kPlanSeqs + 1];
+    __shared__ int first_entry[kPlanSeqs];
+    __shared__ int2 uses[kPlanSeqs];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    {
+        const int b = blockIdx.x;
+        int n = p.count[b], base = p.prefix_len[b] - 1;
+        const int32_t* table = c.table + (size_t)b * c.width;
+        bool ok = n >= 0 && n <= p.rows && base >= 0 && (long long)base + n <= ((long long)c.width << c.page_shift);
         if (ok && n > 0) {
-            ok = cache_slots_ok(c, table, 0, min(p.sinks, end)) && cache_slots_ok(c, table, lo, end);
+            // pages of the sinks, and from the first row's window on
+            const int end = base + n, lo = max(0, base - p.window + 1), pages = (end - 1) >> c.page_shift;
+            const int sinks = p.sinks > 0 ? min((min(p.sinks, end) - 1) >> c.page_shift, pages) : -1;
+            for (int i = tid; i <= sinks; i += kPlanThreads) ok = ok && (unsigned)table[i] < (unsigned)c.n_pages;
+            for (int i = max(lo >> c.page_shift, sinks + 1) + tid; i <= pages; i += kPlanThreads) ok = ok && (unsigned)table[i] < (unsigned)c.n_pages;
         }
-        if (lane == 0) {
-            fine = ok;
-            if (p.status && i == 0 && h == 0) p.status[b] = ok ? 0 : GRAFT_ST_BAD_CACHE;
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (lane == 0) fine[warp] = ok;
+        __syncthreads();
+        for (int w = 0; w < kWarps; ++w) ok = ok && fine[w];
+        if (tid == 0) {
+            if (p.status) p.status[b] = ok ? 0 : GRAFT_ST_BAD_CACHE;
+            p.use[b] = make_int2(ok ? n : 0, base);
+            last = gridDim.x == 1 || atom_add_acq_rel(p.arrivals, 1) == (int)gridDim.x - 1;
         }
+        __syncthreads();
+        if (!last) return;
+    }
+    // the last block: where the sequences' entries begin, what every entry has, where it stands in the line
+    const int Hk = c.kv_heads;
+    const bool few_seqs = p.batch <= kPlanSeqs;
+    int n_entries = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += kPlanThreads) {
+        const int b = b0 + tid;
+        const int2 u = b < p.batch ? __ldcg(p.use + b) : make_int2(0, 0);
+        const int mine = entries_of(p, u.x);
+        const Sums s = block_sums(scratch, false, mine, 0, 0);
+        if (b < p.batch) {
+            if (few_seqs)
+                first_entry[b] = n_entries + s.before[0], uses[b] = u;
+            else
+                p.entry0[b] = n_entries + s.before[0];
+        }
+        n_entries += s.all[0];
     }
     __syncthreads();
-    if (!fine || i >= n) return;
-    const int kh = h / p.group;
-    for (int d = tid; d < D; d += kThreads)
-        q[d] = p.scale * __bfloat162float(((const __nv_bfloat16*)p.q)[((long long)b * p.rows + i) * p.q_stride + (long long)h * D + d]);
-    __syncthreads();
-    const int32_t* pos = p.mask ? p.position + (size_t)b * p.nmax : nullptr;
-    const uint32_t* bits = p.mask ? p.mask + ((size_t)b * p.nmax + i) * p.words : nullptr;
-    const auto position_of = [&](int j) { return pos ? min(max(pos[j], base), base + j) : base + j; };
-    const int mine = position_of(i);
-    const auto sees = [&](int s) {
-        const int j = s - base;
-        if (j >= 0 && !(bits ? j < 32 * p.words && (bits[j >> 5] >> (j & 31) & 1) : j <= i)) return false;
-        const int at = j < 0 ? s : position_of(j);
-        return mine - at < p.window || at < p.sinks;
+    const auto of = [&](int e, PlanSeq& q) {
+        q = {};
+        if (e >= n_entries) return;
+        int lo = 0, hi = p.batch - 1;  // the last sequence whose first entry is not behind e: it has some, as sequences without begin where the next does
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if ((few_seqs ? first_entry[mid] : p.entry0[mid]) <= e)
+                lo = mid;
+            else
+                hi = mid - 1;
+        }
+        const int2 u = few_seqs ? uses[lo] : __ldcg(p.use + lo);
+        q.b = lo;
+        q.node0 = (e - (few_seqs ? first_entry[lo] : p.entry0[lo])) * p.block_rows;
+        q.n = min(p.block_rows, u.x - q.node0);
+        q.base = u.y + q.node0;
+        q.gap = gap_of(p, q.base);
+        q.kt = (q.base + q.n - q.gap + kTile - 1) / kTile;
     };
-    float m = -INFINITY, l = 0.0f, o[kPer] = {};
-    const int first = min(p.sinks, lo), total = first + end - lo;
-    for (int x0 = warp * 32; x0 < total; x0 += kThreads) {
-        const int x = x0 + lane, s = x < first ? x : lo + x - first;
-        const bool see = x < total && sees(s);
-        float sc = -INFINITY;
-        if (see) {
-            const size_t row = cache_row(c, table[s >> c.page_shift], kh, s & low);
-            sc = 0.0f;
-            for (int d = 0; d < D; ++d) sc = fmaf(q[d], entry_of(c, c.k, c.k_exp, row, d), sc);
-            if (!(sc < INFINITY)) sc = __int_as_float(0x7FFFFFFF);
-        }
-        const bool nan = __any_sync(0xFFFFFFFFu, sc != sc);
-        float mx = sc;
-        for (int y = 16; y > 0; y >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, y));
-        const float now = fmaxf(m, mx), f = m > -INFINITY ? expf(m - now) : 0.0f;
-        const float w = sc > -INFINITY ? expf(sc - now) : 0.0f;
-        float ws = w;
-        for (int y = 16; y > 0; y >>= 1) ws += __shfl_xor_sync(0xFFFFFFFFu, ws, y);
-        l = nan ? __int_as_float(0x7FFFFFFF) : l * f + ws;
-        m = now;
-        for (int y = 0; y < kPer; ++y) o[y] *= f;
-        const unsigned who = __ballot_sync(0xFFFFFFFFu, see);
-        for (int y = 0; y < 32; ++y) {
-            if (!(who >> y & 1)) continue;
-            const float wy = __shfl_sync(0xFFFFFFFFu, w, y);
-            const int sy = __shfl_sync(0xFFFFFFFFu, s, y);
-            const size_t row = cache_row(c, table[sy >> c.page_shift], kh, sy & low);
-            for (int z = 0; z < kPer; ++z) o[z] += wy * entry_of(c, c.v, c.v_exp, row, z * 32 + lane);
-        }
+    const auto cost_of = [&](const PlanSeq& q, int chunk) { return Hk * head_cost(q.n * p.group, q.kt, chunk); };
+    const bool small = n_entries <= 32, held = n_entries <= kPlanSeqs;  // (few entries: every warp goes through them by itself)
+    const int me = small ? lane : tid;
+    PlanSeq q;
+    int total = 0, chunk = 1;
+    for (int e0 = 0; e0 < n_entries; e0 += kPlanThreads) {
+        of(e0 + me, q);
+        total += block_sums(scratch, small, cost_of(q, 1), 0, 0).all[0];
     }
-    if (lane == 0) sm[warp] = m, sl[warp] = l;
-    for (int z = 0; z < kPer; ++z) sum[warp][z * 32 + lane] = o[z];
+    // (short shares: as in attn_plan_kernel)
+    const int share = (total + p.ctas - 1) / p.ctas;
+    if (share > 1 && share <= p.most_share && n_entries <= kPlanThreads)
+        for (int c2 = (share + 5) / 6 * 6; c2 <= share + 11; c2 += 6)
+            if (block_sums(scratch, small, cost_of(q, c2) / c2, 0, 0).all[0] <= p.ctas) {
+                chunk = c2;
+                break;
+            }
+    int cost = 0;
+    if (tid == 0) {
+        const PlanSeq none = {};
+        p.seq[0] = none;
+        entries[0] = none;
+    }
+    for (int e0 = 0; e0 < n_entries; e0 += kPlanThreads) {
+        const int e = e0 + me;
+        if (n_entries > kPlanThreads) of(e, q);
+        const Sums s = block_sums(scratch, small, cost_of(q, chunk), 0, 0);
+        if (e < n_entries && (!small || warp == 0)) {
+            q.cost0 = cost + s.before[0];
+            p.seq[e + 1] = q;
+            if (held) entries[e + 1] = q;
+        }
+        cost += s.all[0];
+    }
+    total = cost;
+    const int parts = chunk > 1 ? total / chunk : min(p.ctas, total);
+    if (tid == 0) {
+        p.head->total = total;
+        p.head->parts = parts;
+        p.head->chunk = chunk;
+        p.head->entries = n_entries;
+        *p.arrivals = 0;
+    }
     __syncthreads();
-    float mm = -INFINITY, ll = 0.0f;
-    for (int w = 0; w < kWarps; ++w) mm = fmaxf(mm, sm[w]);
-    const auto weight = [&](int w) { return sm[w] > -INFINITY ? expf(sm[w] - mm) : 0.0f; };
-    for (int w = 0; w < kWarps; ++w) ll += sl[w] != sl[w] ? sl[w] : weight(w) * sl[w];
-    const size_t row = ((size_t)b * p.rows + i) * p.q_heads + h;
-    for (int d = tid; d < D; d += kThreads) {
-        float x = 0.0f;
-        for (int w = 0; w < kWarps; ++w) x += weight(w) * sum[w][d];
-        p.out[row * D + d] = __float2bfloat16(ll != 0.0f ? x / ll : x);
-    }
-    if (p.lse && tid == 0) p.lse[row] = ll == 0.0f ? -INFINITY : (mm > -INFINITY ? mm : 0.0f) + logf(ll);
+    plan_starts<true>(p, entries, held, n_entries, total, parts, chunk);
+}
+
+template <int D, bool Q8>
+cudaError_t launch_any(graft_ctx* ctx, const AttnParams& p, bool few, cudaStream_t st) {
+    const uint32_t bit = 1u << ((D == 128) + 2 * Q8);
+    if (few)
+        return launch_kernels(ctx, p, window_plan_kernel, few_attn_kernel<D, Q8, true>, FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kSmem,
+                              &ctx->window_ready, bit, [] { return cudaSuccess; }, st);
+    const auto join = [&] { return launch_join<D>(ctx, p, st); };
+    if ((long long)p.block_rows * p.group <= kTile)
+        return launch_kernels(ctx, p, window_plan_kernel, tree_attn_kernel<D, Q8, true, true>, Shape<D, Q8, true>::kThreads,
+                              Shape<D, Q8, true>::kSmem, &ctx->window_ready, bit << 4, join, st);
+    return launch_kernels(ctx, p, window_plan_kernel, tree_attn_kernel<D, Q8, false, true>, Shape<D, Q8, false>::kThreads,
+                          Shape<D, Q8, false>::kSmem, &ctx->window_ready, bit << 8, join, st);
+}
+
+struct WindowShape {
+    int ctas, block_rows;
+    long long entries;
+    AttnSizes z;
+};
+// block_rows: what a unit holds of a chain's rows; all of a tree's
+WindowShape window_shape(const graft_ctx* ctx, int batch, const graft_cache* cache, int q_heads, int rows, bool mask) {
+    const int group = q_heads / cache->kv_heads;
+    WindowShape w;
+    w.ctas = attn_ctas(ctx, cache->dtype == GRAFT_E4M3, cache->head_dim, group, rows, 0);
+    w.block_rows = mask || (long long)rows * group <= kUnitRows ? rows : group < kUnitRows ? kUnitRows / group : 1;
+    w.entries = (long long)batch * ((rows + w.block_rows - 1) / w.block_rows);
+    w.z = attn_sizes(w.ctas, batch, (int)w.entries, batch, cache->kv_heads, cache->head_dim, group, w.block_rows, 0);
+    return w;
 }
 
 }  // namespace
 
+// Bytes of scratch; 0: positions in the line of key tiles would not fit in 32 bits.
+size_t window_attn_scratch_bytes(const graft_ctx* ctx, int batch, const graft_cache* cache, int q_heads, int rows, bool mask, int window, int sinks) {
+    const WindowShape w = window_shape(ctx, batch, cache, q_heads, rows, mask);
+    const double all = (double)cache->table_width * cache->page_size, seen = (double)window + sinks + w.block_rows + 2 * kTile;
+    const double row_tiles = (double)w.entries * ((double)w.block_rows * (q_heads / cache->kv_heads) / 128 + 2);
+    if ((double)w.entries >= 2147483648.0 || 2 * row_tiles * cache->kv_heads * ((all < seen ? all : seen) / 128 + 2) >= 2147483648.0) return 0;
+    return w.z.total;
+}
+
 cudaError_t window_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache, int layer, int q_heads, int rows, long long q_stride,
                                const void* d_q, float scale, const int32_t* d_prefix_len, const int32_t* d_count, const uint32_t* d_mask,
-                               const int32_t* d_position, int window, int sinks, void* d_out, float* d_lse, int32_t* d_status, cudaStream_t st) {
-    WindowParams p;
-    p.c = cache_view(cache, layer);
-    p.q = (const uint8_t*)d_q;
-    p.q_stride = q_stride;
-    p.prefix_len = d_prefix_len;
-    p.count = d_count;
-    p.mask = d_mask;
+                               const int32_t* d_position, int window, int sinks, void* d_out, float* d_lse, int32_t* d_status, void* scratch,
+                               cudaStream_t st) {
+    const bool q8 = cache->dtype == GRAFT_E4M3, few = few_rows(q_heads / cache->kv_heads, rows, 0);
+    // (a copy brings no more than 32 slots, so that the line's borders are not rounded by more)
+    const int box_rows = cache->page_size < 32 ? cache->page_size : 32;
+    AttnParams p;
+    const cudaError_t e = attn_params(p, ctx, batch, cache, layer, q_heads, rows, q_stride, d_q, scale, d_prefix_len, d_count, d_mask, d_out, d_lse,
+                                      d_status, !few, box_rows);
+    if (e != cudaSuccess) return e;
+    const WindowShape w = window_shape(ctx, batch, cache, q_heads, rows, d_mask != nullptr);
+    p.ctas = w.ctas;
+    p.block_rows = w.block_rows;
+    attn_places(p, w.z, scratch);
+    p.most_share = few ? 0 : 128;
+    const int most = cache->table_width * cache->page_size;  // (below 2^31 - 65536)
     p.position = d_position;
-    p.out = (__nv_bfloat16*)d_out;
-    p.lse = d_lse;
-    p.status = d_status;
-    p.scale = scale;
-    p.rows = rows;
-    p.q_heads = q_heads;
-    p.group = q_heads / cache->kv_heads;
-    p.nmax = ctx->nmax;
-    p.words = ctx->mask_words;
-    p.window = window;
-    p.sinks = sinks;
-    const cudaError_t e = launch_pdl(cache->head_dim == 128 ? window_attn_kernel<128> : window_attn_kernel<64>, dim3(rows, q_heads, batch),
-                                     dim3(kThreads), 0, st, p);
-    ctx->launches += 1;
-    return e != cudaSuccess ? e : cudaGetLastError();
+    p.window = window < most ? window : most;  // (neither changes what is seen)
+    p.sinks = sinks < most ? sinks : most;
+    p.grain = few ? 16 : box_rows;
+    p.sink_pad = (p.sinks + p.grain - 1) / p.grain * p.grain;
+    const auto launch = cache->head_dim == 128 ? (q8 ? launch_any<128, true> : launch_any<128, false>)
+                                               : (q8 ? launch_any<64, true> : launch_any<64, false>);
+    return launch(ctx, p, few, st);
 }
 
 }  // namespace graft
