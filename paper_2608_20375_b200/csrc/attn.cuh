@@ -242,9 +242,19 @@ __device__ __forceinline__ void plan_starts(const AttnParams& p, const PlanSeq* 
 }
 
 // ---- walking along a CTA's stretch -----------------------------------------------------------------------------------
-// A bounded wait whose polls sleep: the polls of warps that wait would otherwise take the shared-memory pipe from those that work.
+// A bounded wait whose polls sleep: the polls of warps that wait would otherwise take the shared-memory pipe from those that work.  (mbar_wait_bounded_hint
+// with its loop kept small: unrolled, a wait is 2 KB of code, thirty of them are more than the instruction cache next to the cores, and the softmax
+// waited a quarter of its time for instructions.)
 __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int* gave_up) {
-    return mbar_wait_bounded_hint(bar, parity, gave_up, kWaitNs);
+    if (mbar_try_wait(bar, parity)) return true;
+    if (*gave_up) return false;
+#pragma unroll 1
+    for (uint32_t it = 0; it < GRAFT_SPIN_LIMIT; ++it) {
+        if (mbar_try_wait_hint(bar, parity, kWaitNs)) return true;
+        if ((it & 15u) == 15u && *gave_up) return false;
+    }
+    *gave_up = 1;
+    return false;
 }
 
 // What the warps of a CTA are told of a piece.
@@ -354,7 +364,7 @@ __device__ __forceinline__ void row_of(const AttnParams& p, const volatile Piece
 }
 
 // which of the 128 slots from `first` on row `node` sees; end: slots there are.  (Words of the mask are loaded without branches, all together.)
-__device__ __forceinline__ void seen_words(const uint32_t* mask_row, int words, int node, int base, int end, int first, uint32_t (&sees)[4]) {
+__device__ __noinline__ void seen_words(const uint32_t* mask_row, int words, int node, int base, int end, int first, uint32_t (&sees)[4]) {
     const int j0 = first - base, w0 = j0 >> 5;  // new row of the first slot (below 0: slots of the prefix) and its word
     uint32_t m[5] = {0, 0, 0, 0, 0};
     if (mask_row != nullptr)
@@ -373,7 +383,7 @@ __device__ __forceinline__ void seen_words(const uint32_t* mask_row, int words, 
 }
 
 // The same behind a window: of the 128 places from `first` on, for row i of a block (the sequence's row `node`) whose first row stands in place `base`.
-__device__ __forceinline__ void window_words(const AttnParams& p, int gap, int lo, int base, int end, int b, int node, int i, int first, uint32_t (&sees)[4]) {
+__device__ __noinline__ void window_words(const AttnParams& p, int gap, int lo, int base, int end, int b, int node, int i, int first, uint32_t (&sees)[4]) {
     const int j0 = first - base, w0 = j0 >> 5;
     const int32_t* position = p.mask != nullptr ? p.position + (size_t)b * p.nmax : nullptr;
     const int step = window_step(position, i, base + gap);  // (with a mask a block is a whole tree: i is its node)
@@ -408,6 +418,10 @@ constexpr int kPieces = 4;  // that are told ahead
 // warps' arrivals on q_full, which follow their test.
 constexpr int kSpoiltPieces = 2;
 
+// Tiles of V in a row that the first stream may have cleared before the second one asks whether: as many as the ring holds, and they come
+// by turns, so that a barrier's phase tells uses apart.
+constexpr int kCleared = 8;
+
 // kOne: no unit has more than one row tile, and there is room for more key tiles.
 template <int D, bool Q8, bool kOne>
 struct Shape {
@@ -423,8 +437,10 @@ struct Shape {
     // registers a thread: the softmax's eight warps take over what the others leave (of what the launch has)
     static constexpr int kRegsLaunch = Q8 ? 96 : 168;
     static constexpr int kRegsSoftmax = Q8 ? 168 : 224, kRegsOthers = Q8 ? 48 : 56;
+    static constexpr int kRegsSoftmaxHalves = Q8 ? 144 : 200, kRegsOthersHalves = Q8 ? 64 : 104;  // (scores of half a tile at a time)
     static constexpr int kCols = Q8 ? 64 : 128;  // scores that a softmax thread holds at a time
-    static_assert(256 * kRegsSoftmax + (kThreads - 256) * kRegsOthers <= kThreads * kRegsLaunch, "registers of a launch");
+    static_assert(256 * kRegsSoftmax + (kThreads - 256) * kRegsOthers <= kThreads * kRegsLaunch &&
+                  256 * kRegsSoftmaxHalves + (kThreads - 256) * kRegsOthersHalves <= kThreads * kRegsLaunch, "registers of a launch");
     static constexpr size_t kSmem = 1024 + kQTiles * kTileBytes + (size_t)kStages * kTileBytes + (size_t)kRaw * kRawBytes + 1024;
 };
 
@@ -484,6 +500,13 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 __device__ __forceinline__ bool not_finite2(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
 
+// the larger magnitudes of two pairs of bf16 (signs mean nothing), NaN where one is
+__device__ __forceinline__ uint32_t max_magnitude2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
 // log(2^m sum); m = -inf: nothing seen, or nothing but what is not a number
 __device__ __forceinline__ float log_sum(float m, float sum) {
     return sum == 0.0f ? -INFINITY : (m > -INFINITY ? m * 0.69314718f : 0.0f) + logf(sum);
@@ -536,8 +559,8 @@ __device__ __forceinline__ float max2(float a, float b) {
 }
 // kCols of the row's scores at tS, from x0 on, all asked for together (while the tensor cores work on the other stream, an answer takes
 // several hundred cycles), -inf in the place of those that `sees` leaves out, and their largest (NaN if one of them is).
-template <int kCols>
-__device__ __forceinline__ float scores(uint32_t tS, int x0, uint32_t (&u)[kCols], bool masked, const uint32_t (&sees)[4]) {
+template <int kCols, int kWords>
+__device__ __forceinline__ float scores(uint32_t tS, int x0, uint32_t (&u)[kCols], bool masked, const uint32_t (&sees)[kWords]) {
 #pragma unroll
     for (int x = 0; x < kCols; x += 32) tmem_ld_32x32(tS + x0 + x, *(uint32_t(*)[32]) & u[x]);
     tmem_arrived(u);
@@ -596,7 +619,7 @@ __device__ __forceinline__ float weigh(uint32_t* v, float c2, float off, uint32_
 template <int D>
 __device__ __forceinline__ void rescale(uint32_t tO, float f) {
     uint32_t u[32];
-#pragma unroll
+#pragma unroll 1
     for (int x = 0; x < D / 32; ++x) {
         tmem_ld_32x32(tO + 32 * x, u);
         tmem_arrived(u);
@@ -609,6 +632,34 @@ __device__ __forceinline__ void rescale(uint32_t tO, float f) {
 // Entries of the ring are used in the order K0 V0 K1 V1 ... (two row tiles against every key tile), or K0 K1 V0 K2 V1 K3 ... (one row tile:
 // a stream's product with K(t + 2) follows its product with V(t)); T key tiles are 2 T entries either way.
 __device__ __forceinline__ int v_entry(bool two, int T, int t) { return two ? 1 + 2 * t : t <= T - 2 ? 2 + 2 * t : 2 * T - 1; }
+
+// A row of V in its tile: cleared if it is to be, or holds what is not a number; whether it was.
+template <int D>
+__device__ __noinline__ bool clear_row(uint32_t at, int row, bool clear) {
+    constexpr uint32_t kHalf = kTile * 128;
+    if (!clear) {
+        uint32_t most = 0;  // magnitudes; NaN if one is
+#pragma unroll
+        for (int x0 = 0; x0 < D / 8; x0 += 4) {
+            uint32_t a[4][4];
+#pragma unroll
+            for (int x = x0; x < x0 + 4; ++x)  // (a row's pieces in an order of its own: eight rows then use all banks)
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(a[x - x0][0]), "=r"(a[x - x0][1]), "=r"(a[x - x0][2]), "=r"(a[x - x0][3])
+                             : "r"(at + (x >> 3) * kHalf + ((x + row) & 7) * 16)
+                             : "memory");
+#pragma unroll
+            for (int x = 0; x < 16; ++x) most = max_magnitude2(most, a[x >> 2][x & 3]);
+        }
+        clear = not_finite2(most);
+    }
+    if (clear) {
+#pragma unroll
+        for (int x = 0; x < D / 8; ++x)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + (x >> 3) * kHalf + ((x + row) & 7) * 16), "r"(0) : "memory");
+    }
+    return clear;
+}
 
 // What a row sees of new slots whose V is not a number, which was taken out of the products: added to its O in TMEM, with scores of
 // its own.  Key tiles t0, t0 + dt, .. of the piece; a whole warp calls it, `sums` are the rows that see anything, m their maxima.
@@ -634,6 +685,7 @@ __device__ __noinline__ void add_spoilt(const AttnParams& p, const Piece& pc, ui
                 return e4m3x4_to_bf16(*(const uint32_t*)(x + at * c.row_bytes + d), f, more);
             };
             bool bad = false;  // the same in all lanes: a piece's rows have one sequence where there are new slots
+#pragma unroll 1
             for (int d = 0; d < D; d += 4) {
                 const uint2 v = entry(c.v, c.v_exp, d);
                 bad = bad || not_finite2(v.x) || not_finite2(v.y);
@@ -649,6 +701,7 @@ __device__ __noinline__ void add_spoilt(const AttnParams& p, const Piece& pc, ui
                 mine = mine && (mask_row == nullptr ? j <= node : j < 32 * p.words && ((mask_row[j >> 5] >> (j & 31)) & 1));
             float s = 0.0f;
             if (mine)
+#pragma unroll 1
                 for (int d = 0; d < D; d += 4) {
                     const uint2 k = entry(c.k, c.k_exp, d);
                     for (int y = 0; y < 4; ++y) {
@@ -657,6 +710,7 @@ __device__ __noinline__ void add_spoilt(const AttnParams& p, const Piece& pc, ui
                     }
                 }
             const float e = mine ? ex2_approx((s - m) * p.c2) : 0.0f;
+#pragma unroll 1
             for (int d = 0; d < D; d += 4) {
                 const uint2 v = entry(c.v, c.v_exp, d);
                 const uint32_t v0 = v.x << 16, v1 = v.x & 0xFFFF0000u, v2 = v.y << 16, v3 = v.y & 0xFFFF0000u;
@@ -684,6 +738,12 @@ template <int D, bool Q8, bool kOne, bool kWin>
 __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_kernel(const __grid_constant__ AttnParams p) {
     using S = Shape<D, Q8, kOne>;
     constexpr int NS = S::kStages, NR = S::kRaw > 0 ? S::kRaw : 1;
+    // Slots whose scores a stream takes at a time.  Halves of a key tile have halves of the stream's 128 columns: while one half's
+    // exponentials are worked out, the products of the other (its weights' with V, then K of the next tile) run, and the softmax of either
+    // stream waits for nothing.  A whole tile's scores leave no room for the next ones, and a stream's softmax and products are one chain: 4000 cycles
+    // for a key tile and two row tiles, of which the tensor cores work for 2050.
+    constexpr int kSub = kWin && Q8 ? 64 : kTile, kSubs = kTile / kSub;
+    static_assert(NS / 2 < kCleared, "tiles that the streams may be apart");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base_addr = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* const smem = smem_raw + (base_addr - smem_u32(smem_raw));
@@ -695,13 +755,17 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
     const auto kv_empty = [&](int i) { return bar0 + 8 * (NS + i); };
     const auto raw_full = [&](int i) { return bar0 + 8 * (2 * NS + i); };
     const auto raw_empty = [&](int i) { return bar0 + 8 * (2 * NS + NR + i); };
-    const uint32_t q_full = bar0 + 8 * (2 * NS + 2 * NR), s_full0 = q_full + 8, p_full0 = q_full + 24, pair = q_full + 40, turn0 = q_full + 48;
-    const uint32_t piece_full0 = q_full + 64, piece_empty0 = piece_full0 + 8 * kPieces;
-    volatile int* const gave_up = (volatile int*)(bars + 2 * NS + 2 * NR + 8 + 2 * kPieces);
+    const uint32_t q_full = bar0 + 8 * (2 * NS + 2 * NR), pair = q_full + 8, turn0 = q_full + 16, cleared0 = q_full + 32;
+    const uint32_t s_full0 = cleared0 + 8 * kCleared, p_full0 = s_full0 + 32, o_done0 = p_full0 + 32, piece_full0 = o_done0 + 32, piece_empty0 = piece_full0 + 8 * kPieces;
+    const auto s_full = [&](int stream, int c) { return s_full0 + 8 * (2 * stream + c); };
+    const auto p_full = [&](int stream, int c) { return p_full0 + 8 * (2 * stream + c); };
+    const auto o_done = [&](int stream, int c) { return o_done0 + 8 * (2 * stream + c); };
+    constexpr int kBars = 2 * NS + 2 * NR + 16 + kCleared + 2 * kPieces;
+    volatile int* const gave_up = (volatile int*)(bars + kBars);
     volatile int* const spoilt = gave_up + 1;  // [kSpoiltPieces][2 streams] the last piece (counted from 1) with a row of V that was taken out
     uint32_t* const tmem_at = (uint32_t*)(gave_up + 1 + 2 * kSpoiltPieces);
     Piece* const pieces = (Piece*)(gave_up + 2 + 2 * kSpoiltPieces);  // [kPieces]
-    static_assert((2 * NS + 2 * NR + 8 + 2 * kPieces) * 8 + (2 + 2 * kSpoiltPieces) * 4 + kPieces * sizeof(Piece) <= 1024, "barriers and pieces");
+    static_assert(kBars * 8 + (2 + 2 * kSpoiltPieces) * 4 + kPieces * sizeof(Piece) <= 1024, "barriers and pieces");
     static_assert((2 + 2 * kSpoiltPieces) * 4 % 8 == 0, "pieces begin where they may be copied eight bytes at a time");
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -721,10 +785,14 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
         mbar_init(q_full, 10);
         mbar_init(pair, 8);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(s_full0 + 8 * i, 1);
-            mbar_init(p_full0 + 8 * i, 4);
+            for (int c = 0; c < kSubs; ++c) {
+                mbar_init(s_full(i, c), 1);
+                mbar_init(p_full(i, c), 4);
+                mbar_init(o_done(i, c), 1);
+            }
             mbar_init(turn0 + 8 * i, 1);
         }
+        for (int i = 0; i < kCleared; ++i) mbar_init(cleared0 + 8 * i, 4);
         *gave_up = 0;
         for (int i = 0; i < 2 * kSpoiltPieces; ++i) spoilt[i] = 0;
         mbar_fence_init();
@@ -747,12 +815,12 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
     };
 
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kRegsSoftmax));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSubs > 1 ? S::kRegsSoftmaxHalves : S::kRegsSoftmax));
         // ---- softmax: a thread a row
         const int i = warp >> 2, row_in_tile = tid & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the lanes
         const uint32_t tS = tmem + lanes + i * 128, tO = tmem + lanes + 256 + i * 128;
-        uint32_t it = 0, n_s = 0, n_piece = 0, n_pair = 0;
+        uint32_t it = 0, n_s = 0, n_piece = 0, n_pair = 0, n_cleared = 0;
         bool ok = true;
         const float c2 = p.c2;
         const auto both = [&]() {  // the two streams meet
@@ -762,9 +830,15 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
             n_pair += 1;
             return r;
         };
-        const auto wait_s = [&]() {
-            const bool r = wait_for(s_full0 + 8 * i, n_s & 1, gave_up);
-            n_s += 1;
+        const auto wait_s = [&](int c) {
+            const bool r = wait_for(s_full(i, c), n_s & 1, gave_up);
+            tc_fence_after();
+            return r;
+        };
+        // The stream's last product with V that it handed weights over for, ahead of part c of its tile n_s.  (The one before it with the same part is done:
+        // scores that have been waited for come from a product behind that.)
+        const auto wait_o = [&](int c) {
+            const bool r = wait_for(o_done(i, c == 0 ? kSubs - 1 : 0), c == 0 ? (n_s & 1) ^ 1 : n_s & 1, gave_up);
             tc_fence_after();
             return r;
         };
@@ -818,28 +892,9 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                 if (!wait_for(kv_full(entry % NS), (entry / NS) & 1, gave_up)) return false;
                 const int slot = first + row_in_tile, end = pc.end;
                 if (slot >= pc.base || (kWin && slot >= border0 && slot < border1)) {
-                    const uint32_t at = kv_addr + (entry % NS) * S::kTileBytes + row_in_tile * 128;
-                    bool clear = slot >= end;
                     const bool unseen = kWin && slot >= border0 && slot < min(pc.lo, pc.base);  // by all rows
-                    if (kWin) clear = clear || unseen;
-                    if (!clear)
-#pragma unroll
-                        for (int x = 0; x < D / 8; ++x) {  // (a row's pieces in an order of its own: eight rows then use all banks)
-                            uint32_t a0, a1, a2, a3;
-                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                         : "=r"(a0), "=r"(a1), "=r"(a2), "=r"(a3)
-                                         : "r"(at + (x >> 3) * S::kHalf + ((x + row_in_tile) & 7) * 16)
-                                         : "memory");
-                            clear = clear || not_finite2(a0) || not_finite2(a1) || not_finite2(a2) || not_finite2(a3);
-                        }
-                    if (clear) {
-#pragma unroll
-                        for (int x = 0; x < D / 8; ++x)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + (x >> 3) * S::kHalf + ((x + row_in_tile) & 7) * 16),
-                                         "r"(0)
-                                         : "memory");
-                        if (slot < end && !unseen) spoilt[2 * (n_piece % kSpoiltPieces) + i] = (int)n_piece + 1;
-                    }
+                    if (clear_row<D>(kv_addr + (entry % NS) * S::kTileBytes + row_in_tile * 128, row_in_tile, slot >= end || unseen) && slot < end && !unseen)
+                        spoilt[2 * (n_piece % kSpoiltPieces) + i] = (int)n_piece + 1;
                 }
                 fence_proxy_async();
                 return true;
@@ -859,46 +914,69 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                         seen_words(mask_row, p.words, node, pc.base, live ? pc.end : 0, first, sees);
                     }
                     // (with two row tiles every entry ahead of V's in the ring has been used by this stream, so its phase is certain: see `pass`)
-                    if (two && i == 0 && !(ok = clear_v(t, first))) break;
-                }
-                if (!(ok = wait_s())) break;
-                if (warp_live) {
-                    // (with fewer registers: the maximum first, then each half again)
-                    constexpr bool kAgain = S::kCols < kTile;
-                    uint32_t u[S::kCols], w[32];
-                    float mx = scores(tS, 0, u, masked, sees);
-                    if (kAgain) mx = max2(mx, scores(tS, 64, u, masked, sees));
-                    // (m = -inf: nothing seen so far, and what O holds is zero)
-                    const bool grown = mx > m && !((mx - m) * c2 <= kMostGrowth);
-                    if (__any_sync(0xFFFFFFFFu, grown)) {
-                        const float now = fmaxf(m, mx), f = m > -INFINITY ? ex2_approx((m - now) * c2) : 1.0f;
-                        if (any) rescale<D>(tO, f);
-                        l *= f;
-                        m = now;
+                    if (two && i == 0) {
+                        if (!(ok = clear_v(t, first))) break;
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(cleared0 + 8 * (n_cleared % kCleared));
                     }
-                    // (a score of NaN or +inf, which some of the exponentials below would lose: the row's sum is NaN from here on, and so is all that
-                    // is divided by it)
-                    if (!(mx < INFINITY)) l = __int_as_float(0x7FFFFFFF);
-                    const float off = m > -INFINITY ? -m * c2 : 0.0f;
-                    if (kAgain) scores(tS, 0, u, masked, sees);
-                    l += weigh(u, c2, off, w);
-                    tmem_st_32x32(tS, w);
-                    if (kAgain) scores(tS, 64, u, masked, sees);
-                    l += weigh(u + S::kCols - 64, c2, off, w);
-                    tmem_st_32x32(tS + 32, w);
-                    tmem_wait_st();
                 }
-                if (masked && !two && !(ok = clear_v(t, first))) break;
-                if (masked && two && !(ok = both())) break;  // (the first stream clears for both)
-                any = true;
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(p_full0 + 8 * i);
+#pragma unroll 1
+                for (int c = 0; c < kSubs; ++c) {
+                    if (!(ok = wait_s(c))) break;
+                    if (warp_live) {
+                        // (with fewer registers: the maximum first, then each half again)
+                        constexpr int kCols = S::kCols < kSub ? S::kCols : kSub;
+                        constexpr bool kAgain = kCols < kSub;
+                        uint32_t u[kCols], w[32];
+                        const uint32_t tSc = tS + c * kSub;
+                        uint32_t part[kSub / 32];
+#pragma unroll
+                        for (int x = 0; x < kSub / 32; ++x) part[x] = kSubs > 1 && c > 0 ? sees[(x + 2) & 3] : sees[x];
+                        float mx = scores(tSc, 0, u, masked, part);
+                        if (kAgain) mx = max2(mx, scores(tSc, 64, u, masked, part));
+                        // (m = -inf: nothing seen so far, and what O holds is zero)
+                        const bool grown = mx > m && !((mx - m) * c2 <= kMostGrowth);
+                        if (__any_sync(0xFFFFFFFFu, grown)) {
+                            const float now = fmaxf(m, mx), f = m > -INFINITY ? ex2_approx((m - now) * c2) : 1.0f;
+                            if (any) {
+                                if (kSubs > 1 && !(ok = wait_o(c))) break;
+                                rescale<D>(tO, f);
+                            }
+                            l *= f;
+                            m = now;
+                        }
+                        // (a score of NaN or +inf, which some of the exponentials below would lose: the row's sum is NaN from here on, and so is all that
+                        // is divided by it)
+                        if (!(mx < INFINITY)) l = __int_as_float(0x7FFFFFFF);
+                        const float off = m > -INFINITY ? -m * c2 : 0.0f;
+                        if (kAgain) scores(tSc, 0, u, masked, part);
+                        l += weigh(u, c2, off, w);
+                        tmem_st_32x32(tSc, w);
+                        if (kSub == kTile) {
+                            if (kAgain) scores(tSc, 64, u, masked, part);
+                            l += weigh(u + kCols - 64, c2, off, w);
+                            tmem_st_32x32(tSc + 32, w);
+                        }
+                        tmem_wait_st();
+                    }
+                    if (masked && c == 0) {
+                        if (!two && !(ok = clear_v(t, first))) break;
+                        // (the first stream clears for both)
+                        if (two && i == 1 && !(ok = wait_for(cleared0 + 8 * (n_cleared % kCleared), (n_cleared / kCleared) & 1, gave_up))) break;
+                        n_cleared += two ? 1 : 0;
+                    }
+                    any = true;
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_full(i, c));
+                }
+                if (!ok) break;
+                n_s += 1;
             }
             if (!ok) break;
             it += 2 * T;
             if (any)
-                ok = wait_s();  // the last product is done
+                ok = wait_o(0);
             else
                 ok = wait_for(q_full, n_piece & 1, gave_up);  // (nor does a stream without a tile run ahead)
             if (!ok) break;
@@ -944,11 +1022,46 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
             if (two || T == 1) {
                 if (two || i == 0) {
                     const float inv = l != 0.0f ? 1.0f / l : 1.0f;  // (a row that sees nothing: O is zero)
+                    if (!whole) {
+#pragma unroll 1
+                        for (int x = 0; x < D / 32; ++x) {
+                            tmem_ld_32x32(tO + 32 * x, u);
+                            tmem_arrived(u);
+                            put(32 * x, u, inv);
+                        }
+                    } else {
+                        // rows go through their own places in Q's tile, which nobody reads any more, so that a warp's stores are whole rows
+                        constexpr int kPer = D / 8, kRows = 32 / kPer;  // lanes a row, rows a store
+                        const uint32_t tile = q_addr + i * S::kTileBytes;
+                        const auto piece_at = [&](int row, int x) { return tile + row * 128 + (x >> 3) * S::kHalf + (((x & 7) ^ (row & 7)) << 4); };
+#pragma unroll 1
+                        for (int x = 0; x < D / 32; ++x) {
+                            tmem_ld_32x32(tO + 32 * x, u);
+                            tmem_arrived(u);
 #pragma unroll
-                    for (int x = 0; x < D / 32; ++x) {
-                        tmem_ld_32x32(tO + 32 * x, u);
-                        tmem_arrived(u);
-                        put(32 * x, u, inv);
+                            for (int y = 0; y < 4; ++y) {
+                                uint32_t w[4];
+#pragma unroll
+                                for (int z = 0; z < 4; ++z)
+                                    w[z] = pack_bf16(__uint_as_float(u[8 * y + 2 * z]) * inv, __uint_as_float(u[8 * y + 2 * z + 1]) * inv);
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(piece_at(row_in_tile, 4 * x + y)), "r"(w[0]),
+                                             "r"(w[1]), "r"(w[2]), "r"(w[3])
+                                             : "memory");
+                            }
+                        }
+                        __syncwarp();
+                        const long long mine = live ? (long long)(out_row * D) : -1;
+#pragma unroll
+                        for (int y = 0; y < 32 / kRows; ++y) {
+                            const int from = y * kRows + lane / kPer;
+                            const long long at = __shfl_sync(0xFFFFFFFFu, mine, from);
+                            uint4 v;
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                         : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                                         : "r"(piece_at((warp & 3) * 32 + from, lane % kPer))
+                                         : "memory");
+                            if (at >= 0) ((uint4*)(p.out + at))[lane % kPer] = v;
+                        }
                     }
                     put_sums(m, l);
                 }
@@ -956,7 +1069,7 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                 // the streams' halves are joined: the second one's goes through the shared memory of Q, which nobody reads any more
                 float* const tmp = (float*)smem;  // [D / 2 columns][128 rows]
                 float m1 = 0.0f, l1 = 0.0f, f0 = 1.0f, f1 = 0.0f, ms = 0.0f, ls = 0.0f, inv = 1.0f;
-#pragma unroll
+#pragma unroll 1
                 for (int half = 0; half < 2 && ok; ++half) {
                     // maximum and sum of the second stream go ahead of its sums
                     if (half == 0) {
@@ -978,7 +1091,7 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                         if (!(ok = both())) break;
                     }
                     if (i == 1) {
-#pragma unroll
+#pragma unroll 1
                         for (int x = 0; x < D / 64; ++x) {
                             const int d0 = half * (D / 2) + 32 * x;
                             tmem_ld_32x32(tO + d0, u);
@@ -989,7 +1102,7 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                     }
                     if (!(ok = both())) break;
                     if (i == 0) {
-#pragma unroll
+#pragma unroll 1
                         for (int x = 0; x < D / 64; ++x) {
                             const int d0 = half * (D / 2) + 32 * x;
                             tmem_ld_32x32(tO + d0, u);
@@ -1009,7 +1122,7 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
             piece_done(n_piece);
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kRegsOthers));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kSubs > 1 ? S::kRegsOthersHalves : S::kRegsOthers));
         uint32_t n_piece = 0;
         bool ok = true;
         if (warp == 11) {
@@ -1024,6 +1137,14 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                     pieces[n_piece % kPieces] = pc;
                     mbar_arrive(piece_full0 + 8 * (n_piece % kPieces));
                 }
+                if (more && pc.s > 0)  // its rows of Q come to L2 while the pieces ahead are worked on
+                    for (int r = lane; r < pc.rows; r += 32) {
+                        int b, node, g;
+                        row_of<kWin>(p, pc, pc.r0 + r, b, node, g);
+                        const uint8_t* at = p.q + 2 * (((long long)b * p.rows + node) * p.q_stride + (long long)(pc.h * p.group + g) * D);
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+                        if (D > 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + 128));
+                    }
             }
         } else if (warp == 9) {
             // ---- copies: K and V tiles page by page, into the ring (bf16) or to where the conversion takes them from (e4m3)
@@ -1085,29 +1206,30 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
             __syncwarp();
         } else if (warp == 8 || warp == 10) {
             // ---- products, a warp a stream: while one waits for weights or signals, the other's instructions keep the tensor cores busy
-            constexpr uint32_t id_s = umma_idesc(128, 128, true), id_o = umma_idesc(128, D, true) | (1u << 16);  // (V: head_dim is contiguous)
+            constexpr uint32_t id_s = umma_idesc(128, kSub, true), id_o = umma_idesc(128, D, true) | (1u << 16);  // (V: head_dim is contiguous)
             const uint32_t i = warp == 8 ? 0 : 1;
             uint32_t it = 0, n_p = 0, n_turn = 0;
             // (descriptors differ in their low words alone; the numbers that choose them are loaded, so the compiler is told that they are uniform)
             constexpr uint32_t kDescHi = (uint32_t)(umma_desc_sw128(0) >> 32);
             const uint32_t tS = uniform(tmem + i * 128), tO = uniform(tmem + 256 + i * 128);
             const uint32_t q_lo = uniform((uint32_t)umma_desc_sw128(q_addr)), kv_lo = uniform((uint32_t)umma_desc_sw128(kv_addr));
-            const auto qk = [&](uint32_t a, uint32_t b) {
+            const auto qk = [&](int c, uint32_t a, uint32_t b) {  // (rows of K: slots)
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
-                    const uint32_t at = ((ks >> 2) * S::kHalf + (ks & 3) * 32) / 16;
+                    const uint32_t at = ((ks >> 2) * S::kHalf + (ks & 3) * 32) / 16, row = c * (kSub * 128 / 16);
                     if (ks == 0)
-                        umma_ss<false>(tS, a + at, b + at, kDescHi, id_s);
+                        umma_ss<false>(tS + c * kSub, a + at, b + at + row, kDescHi, id_s);
                     else
-                        umma_ss<true>(tS, a + at, b + at, kDescHi, id_s);
+                        umma_ss<true>(tS + c * kSub, a + at, b + at + row, kDescHi, id_s);
                 }
             };
             // V as the second operand of P V: rows (slots) of 64 numbers of head_dim side by side, so head_dim is the contiguous direction.  In
             // the 128-byte swizzle: blocks of 64 numbers kHalf apart (a field that the other operands leave at 1), groups of eight slots 1024 bytes.
             constexpr uint32_t kHalfField = (uint32_t)(S::kHalf / 16) << 16, kOneField = 1u << 16;
-            const auto pv = [&](bool first, uint32_t b) {
+            const auto pv = [&](int c, bool first, uint32_t b) {
 #pragma unroll
-                for (int ks = 0; ks < kTile / 16; ++ks) umma_ts(tO, tS + ks * 8, kDescHi, b + ks * (2048 / 16), id_o, ks > 0 || !first);
+                for (int ks = 0; ks < kSub / 16; ++ks)
+                    umma_ts(tO, tS + c * kSub + ks * 8, kDescHi, b + (c * (kSub / 16) + ks) * (2048 / 16), id_o, c > 0 || ks > 0 || !first);
             };
             const auto at_entry = [&](uint32_t entry) { return uniform(kv_lo + (entry % NS) * (S::kTileBytes / 16)); };
             const auto wait_kv = [&](uint32_t entry) { return wait_for(kv_full(entry % NS), (entry / NS) & 1, gave_up); };
@@ -1121,10 +1243,10 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                 }
                 return true;
             };
-            // Two row tiles: the streams issue by turns.  Side by side, their instructions would share the tensor cores and both streams'
+            // Two row tiles, whole tiles' scores: the streams issue by turns.  Side by side, their instructions would share the tensor cores and both streams'
             // softmax would then share the rest of the time; by turns, one stream's softmax runs under the other's products.
             const auto my_turn = [&](bool two) {
-                if (!two) return true;
+                if (!two || kSubs > 1) return true;
                 const bool r = wait_for(turn0 + 8 * i, (n_turn & 1) ^ (1 - i), gave_up);
                 n_turn += 1;
                 return r;
@@ -1143,10 +1265,15 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                     tc_fence_after();
                     const uint32_t bk = at_entry(it);
                     if (elect_one()) {
-                        qk(a, bk);
-                        if (two) mbar_arrive(turn0 + 8 * (1 - i));
-                        umma_commit(kv_empty(it % NS));
-                        umma_commit(s_full0 + 8 * i);
+#pragma unroll
+                        for (int c = 0; c < kSubs; ++c) {
+                            qk(c, a, bk);
+                            if (c == kSubs - 1) {
+                                if (two && kSubs == 1) mbar_arrive(turn0 + 8 * (1 - i));
+                                umma_commit(kv_empty(it % NS));
+                            }
+                            umma_commit(s_full(i, c));
+                        }
                     }
                     __syncwarp();
                     it += 1;
@@ -1154,27 +1281,32 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                 // P V of a tile, then Q K of the next, which takes the weights' place
                 for (int t = t0; t < T; t += dt) {
                     const bool more = t + dt < T;
-                    ok = pass(it0 + v_entry(two, T, t)) && wait_kv(it) && wait_for(p_full0 + 8 * i, n_p & 1, gave_up) && my_turn(two);
+                    if (!(ok = pass(it0 + v_entry(two, T, t)) && wait_kv(it))) break;
+                    const uint32_t bv = uniform(at_entry(it) - kOneField + kHalfField), bk = at_entry(it + 1);
+#pragma unroll 1
+                    for (int c = 0; c < kSubs; ++c) {
+                        if (!(ok = wait_for(p_full(i, c), n_p & 1, gave_up) && my_turn(two))) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            pv(c, t == t0, bv);
+                            umma_commit(o_done(i, c));
+                            if (c == kSubs - 1) umma_commit(kv_empty(it % NS));
+                        }
+                        __syncwarp();
+                        if (more && c == 0) {
+                            if (!(ok = wait_kv(it + 1))) break;
+                            tc_fence_after();
+                        }
+                        if (elect_one()) {
+                            if (more) qk(c, a, bk);
+                            if (two && kSubs == 1) mbar_arrive(turn0 + 8 * (1 - i));
+                            if (more) umma_commit(s_full(i, c));
+                            if (more && c == kSubs - 1) umma_commit(kv_empty((it + 1) % NS));
+                        }
+                        __syncwarp();
+                    }
                     n_p += 1;
                     if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t bv = uniform(at_entry(it) - kOneField + kHalfField), bk = at_entry(it + 1);
-                    if (elect_one()) {
-                        pv(t == t0, bv);
-                        umma_commit(kv_empty(it % NS));
-                    }
-                    __syncwarp();
-                    if (more) {
-                        if (!(ok = wait_kv(it + 1))) break;
-                        tc_fence_after();
-                    }
-                    if (elect_one()) {
-                        if (more) qk(a, bk);
-                        if (two) mbar_arrive(turn0 + 8 * (1 - i));
-                        umma_commit(s_full0 + 8 * i);
-                        if (more) umma_commit(kv_empty((it + 1) % NS));
-                    }
-                    __syncwarp();
                     it += more ? 2 : 1;
                 }
                 ok = ok && pass(it0 + 2 * T);
