@@ -382,13 +382,14 @@ __device__ __noinline__ void seen_words(const uint32_t* mask_row, int words, int
     }
 }
 
-// The same behind a window: of the 128 places from `first` on, for row i of a block (the sequence's row `node`) whose first row stands in place `base`.
-__device__ __noinline__ void window_words(const AttnParams& p, int gap, int lo, int base, int end, int b, int node, int i, int first, uint32_t (&sees)[4]) {
+// The same behind a window: of the 128 places from `first` on, for row i of a block (the sequence's row `node`) whose first row stands in place
+// `base`; step: how far behind that one's position its own is.
+__device__ __noinline__ void window_words(const AttnParams& p, int gap, int lo, int base, int end, int b, int node, int i, int step, int first,
+                                          uint32_t (&sees)[4]) {
     const int j0 = first - base, w0 = j0 >> 5;
-    const int32_t* position = p.mask != nullptr ? p.position + (size_t)b * p.nmax : nullptr;
-    const int step = window_step(position, i, base + gap);  // (with a mask a block is a whole tree: i is its node)
+    const int32_t* position = p.mask != nullptr ? p.position + (size_t)b * p.nmax : nullptr;  // (with a mask a block is a whole tree: i is its node)
     uint32_t m[5] = {0, 0, 0, 0, 0};
-    if (p.mask != nullptr) {
+    if (p.mask != nullptr && first + kTile > base) {
         const uint32_t* mask_row = p.mask + ((size_t)b * p.nmax + node) * p.words;
 #pragma unroll
         for (int x = 0; x < 5; ++x) {
@@ -672,7 +673,9 @@ __device__ __noinline__ void add_spoilt(const AttnParams& p, const Piece& pc, ui
     for (int t = t0; t < pc.T; t += dt) {
         const int first = pc.first + t * kTile;
         uint32_t sees[4];
-        if (kWin) window_words(p, pc.gap, pc.lo, pc.base, pc.end, b, node, node - pc.node0, first, sees);
+        if (kWin)
+            window_words(p, pc.gap, pc.lo, pc.base, pc.end, b, node, node - pc.node0,
+                         window_step(p.mask ? p.position + (size_t)b * p.nmax : nullptr, node - pc.node0, pc.base + pc.gap), first, sees);
         for (int place = kWin ? first : max(first, pc.base); place < min(pc.end, first + kTile); ++place) {
             if (kWin && place < pc.base && !window_border(place, p.sinks, pc.lo, pc.n)) continue;
             const int slot = kWin ? slot_at(p, pc.gap, place) : place;
@@ -849,10 +852,12 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
             const bool two = !kOne && pc.rows > kTile;
             const int r = (two ? i * kTile : 0) + row_in_tile;  // row of the unit
             const bool live = r < pc.rows;
+            int row_b = 0, row_node = 0, row_step = 0;  // kWin: the row's sequence, its number there, and how far its position is behind the first row's
             if (two || i == 0) {
                 // a row's pieces side by side in a warp's load; where a row stands is worked out by the lane that has it
                 int b = 0, node = 0, g = 0;
                 if (live) row_of<kWin>(p, pc, pc.r0 + r, b, node, g);
+                if (kWin) row_b = live ? b : pc.b, row_node = live ? node : pc.node0;
                 const long long mine = live ? ((long long)b * p.rows + node) * p.q_stride + (long long)(pc.h * p.group + g) * D : -1;
                 constexpr int kPer = D / 8, kRows = 32 / kPer;  // lanes a row, rows a load
                 const int x = lane % kPer;
@@ -875,7 +880,12 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                                  : "memory");
                 }
                 fence_proxy_async();
+            } else if (kWin) {
+                int g = 0;
+                row_b = pc.b, row_node = pc.node0;
+                if (live) row_of<kWin>(p, pc, pc.r0 + r, row_b, row_node, g);
             }
+            if (kWin) row_step = window_step(p.mask ? p.position + (size_t)row_b * p.nmax : nullptr, row_node - pc.node0, pc.base + pc.gap);
             __syncwarp();
             if (lane == 0) mbar_arrive(q_full);
             const bool warp_live = __any_sync(0xFFFFFFFFu, live);
@@ -904,12 +914,11 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                 const bool masked = t >= t_masked || (kWin && first < border1 && first + kTile > border0 && border0 < border1);
                 uint32_t sees[4];
                 if (masked) {
-                    int b = 0, node = 0, g = 0;
-                    if (live) row_of<kWin>(p, pc, pc.r0 + r, b, node, g);
                     if (kWin) {
-                        const int node0 = pc.node0;
-                        window_words(p, pc.gap, pc.lo, pc.base, live ? pc.end : 0, live ? b : pc.b, live ? node : node0, live ? node - node0 : 0, first, sees);
+                        window_words(p, pc.gap, pc.lo, pc.base, live ? pc.end : 0, row_b, row_node, row_node - pc.node0, row_step, first, sees);
                     } else {
+                        int b = 0, node = 0, g = 0;
+                        if (live) row_of<kWin>(p, pc, pc.r0 + r, b, node, g);
                         const uint32_t* mask_row = p.mask ? p.mask + ((size_t)b * p.nmax + node) * p.words : nullptr;
                         seen_words(mask_row, p.words, node, pc.base, live ? pc.end : 0, first, sees);
                     }
@@ -924,16 +933,21 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                 for (int c = 0; c < kSubs; ++c) {
                     if (!(ok = wait_s(c))) break;
                     if (warp_live) {
-                        // (with fewer registers: the maximum first, then each half again)
+                        // (with fewer registers: the maximum first, then the scores again, 64 at a time; one piece of code for both halves, which has to stay
+                        // in the instruction cache beside that of the other warps: 32 trees behind 500 to 4096 e4m3 slots 160 -> 129 us)
                         constexpr int kCols = S::kCols < kSub ? S::kCols : kSub;
-                        constexpr bool kAgain = kCols < kSub;
-                        uint32_t u[kCols], w[32];
+                        uint32_t u[kCols], w[32], part[kCols / 32];
                         const uint32_t tSc = tS + c * kSub;
-                        uint32_t part[kSub / 32];
+                        const auto words = [&](int second) {
 #pragma unroll
-                        for (int x = 0; x < kSub / 32; ++x) part[x] = kSubs > 1 && c > 0 ? sees[(x + 2) & 3] : sees[x];
-                        float mx = scores(tSc, 0, u, masked, part);
-                        if (kAgain) mx = max2(mx, scores(tSc, 64, u, masked, part));
+                            for (int x = 0; x < kCols / 32; ++x) part[x] = second ? sees[(x + 2) & 3] : sees[x];
+                        };
+                        float mx = -INFINITY;
+#pragma unroll 1
+                        for (int h = 0; h < kSub / kCols; ++h) {
+                            words(kCols < kTile && c + h > 0);
+                            mx = max2(mx, scores(tSc + 64 * h, 0, u, masked, part));
+                        }
                         // (m = -inf: nothing seen so far, and what O holds is zero)
                         const bool grown = mx > m && !((mx - m) * c2 <= kMostGrowth);
                         if (__any_sync(0xFFFFFFFFu, grown)) {
@@ -949,13 +963,18 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                         // is divided by it)
                         if (!(mx < INFINITY)) l = __int_as_float(0x7FFFFFFF);
                         const float off = m > -INFINITY ? -m * c2 : 0.0f;
-                        if (kAgain) scores(tSc, 0, u, masked, part);
-                        l += weigh(u, c2, off, w);
-                        tmem_st_32x32(tSc, w);
-                        if (kSub == kTile) {
-                            if (kAgain) scores(tSc, 64, u, masked, part);
-                            l += weigh(u + kCols - 64, c2, off, w);
-                            tmem_st_32x32(tSc + 32, w);
+#pragma unroll 1
+                        for (int h = 0; h < kSub / kCols; ++h) {
+                            if (kCols < kSub) {
+                                words(h);
+                                scores(tSc + 64 * h, 0, u, masked, part);
+                            }
+                            l += weigh(u, c2, off, w);
+                            tmem_st_32x32(tSc + 32 * h, w);
+                            if (kCols == kTile) {
+                                l += weigh(u + kCols - 64, c2, off, w);
+                                tmem_st_32x32(tSc + 32, w);
+                            }
                         }
                         tmem_wait_st();
                     }
