@@ -161,7 +161,7 @@ graft_status graft_create(const graft_config* cfg, graft_ctx** out) {
     const size_t o_id = take(B * L * K * 4), o_lp = take(B * L * K * 4), o_lse = take(B * L * 4);
     const size_t o_rs = take(B * L * 4), o_edge = take(B * L * K * K * 4);
     const size_t o_es = take(B * L * K * K * 4), o_ei = take(B * L * K * K);
-    const size_t o_u = take(L * (size_t)cfg->m * 4), o_err = take(256), o_cos = take(B * L * 8), o_saba = take(B * sizeof(SabaResult)), o_fit = take(saba_fit_doubles() * 8), o_loss = take(tdes_loss_bytes(*cfg)), o_order = take(B * 4), o_ordn = take(256), o_attn = take(256);
+    const size_t o_u = take(L * (size_t)cfg->m * 4), o_err = take(256), o_cos = take(B * L * 8), o_saba = take(B * sizeof(SabaResult)), o_fit = take(saba_fit_doubles() * 8), o_loss = take(tdes_loss_bytes(*cfg)), o_order = take(B * 4), o_ordn = take(256), o_attn = take(256), o_window = take((size_t)ctx->num_sms * 2 * sizeof(int));
     ctx->ws_bytes = off;
     if (cudaMalloc(&ctx->ws, ctx->ws_bytes) != cudaSuccess) {
         cudaGetLastError();
@@ -207,6 +207,7 @@ graft_status graft_create(const graft_config* cfg, graft_ctx** out) {
     ctx->w_order = (int32_t*)(base + o_order);
     ctx->w_order_n = (int*)(base + o_ordn);
     ctx->w_attn_n = (int*)(base + o_attn);
+    ctx->w_window_n = (int*)(base + o_window);
     *out = ctx;
     return GRAFT_OK;
 }

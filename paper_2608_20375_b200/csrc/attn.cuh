@@ -84,6 +84,7 @@ struct __align__(64) AttnParams {
     int block_rows;      // nodes of an entry at most
     int2* use;           // [batch] rows in use and the slots before them
     int* entry0;         // [batch] entries before the sequence's
+    int self_plan;       // few rows: every CTA works out the plan by itself (`ready` is zero between calls then)
 };
 
 // ---- windows -------------------------------------------------------------------------------------------------------
@@ -274,18 +275,32 @@ struct Walk {
     int last_s, Hk, group, shared, window;
     int x, x1, chunk;
     int s, h, mt, k;
+    bool own;  // entries are in this CTA's shared memory
     PlanSeq q;
-    __device__ __forceinline__ void begin(const AttnParams& p, int cta) {
-        seq = p.seq;
-        last_s = kWin ? __ldcg(&p.head->entries) : p.batch;
+    __device__ __forceinline__ void of(const AttnParams& p) {
         Hk = p.c.kv_heads;
         group = p.group;
         shared = kWin ? 0 : p.shared;
         window = p.window;
+    }
+    __device__ __forceinline__ void begin(const AttnParams& p, int cta) {
+        seq = p.seq;
+        last_s = kWin ? __ldcg(&p.head->entries) : p.batch;
+        own = false;
+        of(p);
         const PlanStart* from = p.start + cta;
         const int4 st = __ldcg((const int4*)from), en = __ldcg((const int4*)from + 1);
         load_seq(q, &from->q);
         s = st.x, h = st.y, mt = st.z, k = st.w, x = en.x, x1 = en.y, chunk = en.z;
+    }
+    // the same from entries of its own and where its stretch begins
+    __device__ __forceinline__ void begin(const AttnParams& p, const PlanSeq* entries, const PlanStart& from) {
+        seq = entries;
+        last_s = p.batch;
+        own = true;
+        of(p);
+        q = entries[from.s];
+        s = from.s, h = from.h, mt = 0, k = from.k, x = from.x, x1 = from.x1, chunk = 1;
     }
     __device__ __forceinline__ bool next(Piece& pc) {
         if (x >= x1) return false;
@@ -304,7 +319,10 @@ struct Walk {
                     h = 0;
                     s += 1;
                     if (s > last_s) return false;
-                    load_seq(q, seq + s);
+                    if (kWin && own)
+                        q = seq[s];
+                    else
+                        load_seq(q, seq + s);
                     R = q.n * group;
                 }
             }
@@ -1530,6 +1548,67 @@ __device__ __forceinline__ uint4 load_once(const uint8_t* p) {
     asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
     return r;
 }
+// The plan of few rows behind a window, worked out by every CTA for itself: a launch ahead takes longer than two loads and a sum over the sequences.
+// Numbers that are wrong by themselves leave a sequence without rows; its pages are looked at with its pieces.
+constexpr int kSelfSeqs = 256;
+struct SelfPlan {
+    PlanSeq entry[kSelfSeqs + 1];
+    PlanStart start;
+    int sums[kSelfSeqs / 32];
+    int total;
+};
+__device__ __forceinline__ void self_plan(const AttnParams& p, SelfPlan& sm) {
+    const int b = threadIdx.x, lane = b & 31, warp = b >> 5;
+    PlanSeq q = {};
+    int cost = 0, before = 0;
+    if (b < kSelfSeqs) {
+        if (b < p.batch) {
+            const int n = p.count[b], base = p.prefix_len[b] - 1;
+            const bool fine = n >= 0 && n <= p.rows && base >= 0 && (long long)base + n <= (long long)p.c.width << p.c.page_shift;
+            if (p.status && blockIdx.x == 0 && (!fine || n == 0)) p.status[b] = fine ? 0 : GRAFT_ST_BAD_CACHE;
+            if (fine && n > 0) {
+                q.n = n, q.base = base, q.b = b;
+                q.gap = gap_of(p, base);
+                q.kt = (base + n - q.gap + kTile - 1) / kTile;
+                cost = p.c.kv_heads * padded(kOneTile * q.kt, 1);
+            }
+        }
+        before = cost;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xFFFFFFFFu, before, o);
+            if (lane >= o) before += y;
+        }
+        if (lane == 31) sm.sums[warp] = before;
+        before -= cost;
+    }
+    if (b == 0) sm.start = PlanStart{};
+    __syncthreads();
+    int total = 0;
+    for (int w = 0; w < kSelfSeqs / 32; ++w) {
+        if (w == warp) before += total;
+        total += sm.sums[w];
+    }
+    const int parts = min(p.ctas, total), i = blockIdx.x;
+    if (b < p.batch && b < kSelfSeqs) {
+        q.cost0 = before;
+        sm.entry[b + 1] = q;
+        if (i < parts) {
+            const int x = part_first(total, parts, i);
+            if (cost > 0 && before <= x && x < before + cost) {  // the stretch begins here
+                const int unit = padded(kOneTile * q.kt, 1), h = (x - before) / unit, rem = x - before - h * unit;
+                PlanStart st = {};
+                st.s = b + 1, st.h = h;
+                st.k = min((rem + kOneTile - 1) / kOneTile, q.kt);
+                st.x = x + st.k * kOneTile - rem;
+                st.x1 = part_first(total, parts, i + 1);
+                sm.start = st;
+            }
+        }
+    }
+    if (b == 0) sm.total = total, sm.entry[0] = PlanSeq{};
+    __syncthreads();
+}
+
 template <int D, bool Q8, bool kWin>
 __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kCtas) few_attn_kernel(const __grid_constant__ AttnParams p) {
     using S = FewShape<D, Q8>;
@@ -1547,8 +1626,17 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
     pdl_launch_dependents();
     pdl_wait();
     Walk<kWin> walk;
-    const int total = __ldcg(&p.head->total), parts = __ldcg(&p.head->parts);
-    if (tid == 0) walk.begin(p, blockIdx.x);
+    __shared__ uint4 self_sm[kWin ? (sizeof(SelfPlan) + 15) / 16 : 1];
+    SelfPlan* const self = (SelfPlan*)self_sm;
+    const bool selfish = kWin && p.self_plan;
+    if (selfish) self_plan(p, self[0]);
+    const int total = selfish ? self[0].total : __ldcg(&p.head->total), parts = selfish ? min(p.ctas, total) : __ldcg(&p.head->parts);
+    if (tid == 0) {
+        if (selfish)
+            walk.begin(p, self[0].entry, self[0].start);
+        else
+            walk.begin(p, blockIdx.x);
+    }
     for (;;) {
         if (tid == 0) {
             Piece x;
@@ -1571,7 +1659,10 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
         const int all = min(8 * T, (end - first0 + 15) / 16), steps = warp < all ? (all - warp + kWarps - 1) / kWarps : 0;
         const auto slot_of = [&](int step) { return first0 + (warp + step * kWarps) * 16; };  // (kWin: the place)
         const auto stored_at = [&](int step) { return kWin ? slot_at(p, gap, slot_of(step)) : slot_of(step); };
-        const auto page_of = [&](int step) { return __ldg(table + (stored_at(min(step, steps - 1)) >> shift)); };
+        const auto page_of = [&](int step) {
+            const int page = __ldg(table + (stored_at(min(step, steps - 1)) >> shift));
+            return kWin && (unsigned)page >= (unsigned)c.n_pages ? 0 : page;  // (what is read there is not used, see `fine`)
+        };
         const auto row_at = [&](int step, int page) { return cache_row(c, page, h, stored_at(step) & low); };
         uint4 kr[2][kK], k_exps = {}, v_exps = {};  // (exponents of all 16 slots)
         uint32_t vr[4][4 * kV];
@@ -1601,6 +1692,14 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
                 }
             if (Q8) v_exps = __ldg((const uint4*)(c.v_exp + row0));
         };
+        // Whether the sequence's pages are all there: this thread's share of them.
+        bool fine = true;
+        if (selfish) {
+            const int last_page = (end + gap - 1) >> shift, sinks = p.sinks > 0 ? min((p.sinks - 1) >> shift, last_page) : -1;
+            for (int i = tid; i <= sinks; i += S::kThreads) fine = fine && (unsigned)__ldg(table + i) < (unsigned)c.n_pages;
+            for (int i = max(max(lo + gap, 0) >> shift, sinks + 1) + tid; i <= last_page; i += S::kThreads)
+                fine = fine && (unsigned)__ldg(table + i) < (unsigned)c.n_pages;
+        }
         size_t row0 = 0;
         int page = 0;
         if (steps > 0) {
@@ -1836,7 +1935,15 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
             for (int y = 0; y < D / 16; ++y)
                 *(float2*)&few_sm[(warp * kFewRows + r) * D + 2 * y / kCv * (8 * kCv) + g * kCv + 2 * y % kCv] = make_float2(o[y][i], o[y][i + 2]);
         }
-        __syncthreads();
+        if (selfish) {
+            fine = __syncthreads_and(fine);
+            if (tid == 0 && h == 0 && pc.head && p.status) p.status[b] = fine ? 0 : GRAFT_ST_BAD_CACHE;
+            if (!fine) {  // (so it is for all CTAs that have pieces of the sequence: it is left out)
+                __syncthreads();
+                continue;
+            }
+        } else
+            __syncthreads();
         const bool whole = pc.whole;
         const size_t slot = 2 * (size_t)blockIdx.x + pc.head;
         for (int x = tid; x < R * (D / 4); x += S::kThreads) {
@@ -1872,7 +1979,10 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
             if (warp == 0) {
                 list_unit(list, {cut_x0, kOneTile, cut_kt}, cut_f, cta_of(cut_x0 + (cut_kt - 1) * kOneTile, total, parts), total, parts, -1, 0, 0,
                           kJoinRows);
-                if (lane == 0) last = atomicAdd(p.ready + cut_f, 1) == list.n - 1;
+                if (lane == 0) {
+                    last = atomicAdd(p.ready + cut_f, 1) == list.n - 1;
+                    if (selfish && last) p.ready[cut_f] = 0;  // (nobody else comes)
+                }
             }
             __syncthreads();
             if (last) {

@@ -112,6 +112,7 @@ struct graft_ctx {
     graft::Grown tables_scratch, attn_scratch;
     uint32_t attn_ready, window_ready;  // variants of the attention kernels that may use their shared memory
     int* w_attn_n;   // graft_tree_attention: arrivals, zero between calls
+    int* w_window_n; // graft_window_attention, few rows: pieces that are there of a CTA's cut unit [2 num_sms], zero between calls
     int verify_ready;  // variants of graft_verify's kernel that may be launched in clusters of 16
     // host-buffer staging (allocated on first use of graft_build_trees_host)
     void* stage;

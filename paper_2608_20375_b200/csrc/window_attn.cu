@@ -135,6 +135,15 @@ __global__ void __launch_bounds__(kPlanThreads) window_plan_kernel(const __grid_
 template <int D, bool Q8>
 cudaError_t launch_any(graft_ctx* ctx, const AttnParams& p, bool few, cudaStream_t st) {
     const uint32_t bit = 1u << ((D == 128) + 2 * Q8);
+    if (few && p.self_plan) {
+        if (!(ctx->window_ready & bit)) {
+            const cudaError_t e = allow_smem((const void*)few_attn_kernel<D, Q8, true>, FewShape<D, Q8>::kSmem);
+            if (e != cudaSuccess) return e;
+            ctx->window_ready |= bit;
+        }
+        ctx->launches += 1;
+        return launch_pdl(few_attn_kernel<D, Q8, true>, dim3(p.ctas), dim3(FewShape<D, Q8>::kThreads), FewShape<D, Q8>::kSmem, st, p);
+    }
     if (few)
         return launch_kernels(ctx, p, window_plan_kernel, few_attn_kernel<D, Q8, true>, FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kSmem,
                               &ctx->window_ready, bit, [] { return cudaSuccess; }, st);
@@ -189,6 +198,8 @@ cudaError_t window_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cac
     p.block_rows = w.block_rows;
     attn_places(p, w.z, scratch);
     p.most_share = few ? 0 : 128;
+    p.self_plan = few && batch <= kSelfSeqs;
+    if (p.self_plan) p.ready = ctx->w_window_n;
     const int most = cache->table_width * cache->page_size;  // (below 2^31 - 65536)
     p.position = d_position;
     p.window = window < most ? window : most;  // (neither changes what is seen)
