@@ -549,7 +549,7 @@ def run_verifier(args):
     """--verifier: rounds that build the workload's trees, write the nodes' entries into the target's cache, attend over it in every layer, walk
     the trees by sampling and move the accepted entries; each part and the round timed on the device.  Prints its own JSON line (not the
     benchmark's metric)."""
-    from paper_2608_20375_b200 import BF16, E4M3, Graft, KVCache, MicroBatch, Sampled, join, run_rounds
+    from paper_2608_20375_b200 import BF16, E4M3, Graft, KVCache, MicroBatch, Rope, Sampled, join, run_rounds
 
     w = gi.WORKLOADS[args.workload]
     dev = torch.device("cuda", 0)
@@ -579,6 +579,11 @@ def run_verifier(args):
     for b in range(w.batch):
         logits[b].normal_()
     uniform = torch.rand((w.batch, rows), device=dev)
+    how = {}
+    if args.rope:
+        how.update(rope=Rope.of(dim, 500000.0), q_out=torch.empty_like(q))
+    if args.window:
+        how.update(window=args.window, sinks=args.sinks)
     marks = [[torch.cuda.Event(enable_timing=True) for _ in range(4)] for _ in range(args.steps)]
     step = [0]
 
@@ -590,7 +595,7 @@ def run_verifier(args):
     def verify(i, r, trees):
         marks[step[0]][1].record()
         for layer in range(layers):
-            mb.attend(layer, q, key, value, out)
+            mb.attend(layer, q, key, value, out, **how)
         marks[step[0]][2].record()
         return Sampled(logits, uniform)
 
@@ -609,7 +614,8 @@ def run_verifier(args):
     nodes = mb.out.n_nodes.float()
     print(json.dumps({
         "kind": "rounds with the target's cache (median microseconds on the device)", "workload": args.workload, "batch": w.batch, "rounds": args.steps,
-        "layers": layers, "q_heads": q_heads, "kv_heads": kv_heads, "head_dim": dim, "prefix": prefix, "cache": args.verifier,
+        "layers": layers, "q_heads": q_heads, "kv_heads": kv_heads, "head_dim": dim, "prefix": prefix, "cache": args.verifier, "rope": args.rope,
+        "window": args.window, "sinks": args.sinks if args.window else None,
         "nodes_mean": round(float(nodes.mean()), 1), "nodes_max": int(nodes.max()), "build_us": part(0, 1),
         "write_and_attend_us_per_layer": round(part(1, 2) / layers, 2), "walk_and_move_us": part(2, 3), "round_us": part(0, 3),
     }))
@@ -931,6 +937,9 @@ def main():
                          "duration, sequential against overlapped schedule")
     ap.add_argument("--verifier", choices=["bf16", "e4m3"], default=None,
                     help="instead of the benchmark: rounds with the target's cache of this type, attention, sampled walk (own JSON line)")
+    ap.add_argument("--rope", action="store_true", help="with --verifier: queries and keys are turned by their positions on the way")
+    ap.add_argument("--window", type=int, default=None, help="with --verifier: nodes see that many of the last positions, and the first --sinks")
+    ap.add_argument("--sinks", type=int, default=4)
     ap.add_argument("--tdes-loss", action="store_true",
                     help="instead of the benchmark: time the TDES training objective (forward + backward)")
     ap.add_argument("--saba-fit", action="store_true",

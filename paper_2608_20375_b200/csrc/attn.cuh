@@ -23,7 +23,7 @@ struct __align__(16) PlanSeq {
     int n;       // rows in use (nodes); 0: none, or left out
     int base;    // slots before the first row's (shared prefix: its length)
     int node0;   // nodes of the sequences before (kWin: of the sequence, before the block)
-    int unit0;   // units before
+    int unit0;   // units before (kWin: how far behind the first row's position another row's is at most)
     int cost0;   // position in the line: lengths of the units before
     int kt;      // key tiles
     int b, gap;  // kWin: the sequence; slots that are left out
@@ -82,7 +82,7 @@ struct __align__(64) AttnParams {
     int grain;           // slots are left out in whole multiples of it, from `sink_pad` on
     int sink_pad;
     int block_rows;      // nodes of an entry at most
-    int2* use;           // [batch] rows in use and the slots before them
+    int4* use;           // [batch] rows in use, the slots before them, and unit0 of a tree
     int* entry0;         // [batch] entries before the sequence's
     int self_plan;       // few rows: every CTA works out the plan by itself (`ready` is zero between calls then)
 };
@@ -96,9 +96,9 @@ __device__ __forceinline__ int gap_of(const AttnParams& p, int base) {
     return max(0, (max(lo, 0) & ~(p.grain - 1)) - p.sink_pad);
 }
 __device__ __forceinline__ int slot_at(const AttnParams& p, int gap, int place) { return place + (place >= p.sink_pad ? gap : 0); }
-// Slots ahead of the new rows that some row of the block does not see: those behind the sinks and ahead of the last row's window.  (A node's
-// position is at most its number behind the root's.)
-__device__ __forceinline__ bool window_border(int place, int sinks, int lo, int n) { return place >= sinks && place < lo + n - 1; }
+// Slots ahead of the new rows that some row of the block does not see: those behind the sinks and ahead of the window of the row that is `reach`
+// positions behind the first.
+__device__ __forceinline__ bool window_border(int place, int sinks, int lo, int reach) { return place >= sinks && place < lo + reach; }
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1; }
 // how far behind the first row's slot row i's position is; base: that slot
 __device__ __forceinline__ int window_step(const int32_t* position, int i, int base) {
@@ -267,7 +267,8 @@ struct Piece {
     int r0, rows;   // first row of the unit among the entry's, rows of the unit
     int unit;       // number of the unit
     int head, whole;  // the piece begins with the unit's first tile; is all of it
-    int b, node0, gap, lo;  // kWin: the sequence, its nodes before the entry's, slots left out, the place that the first row's window begins at
+    int b, node0, gap, lo, reach;  // kWin: the sequence, its nodes before the entry's, slots left out, the place that the first row's window begins at, and
+                                   // how far behind it the last one begins
 };
 template <bool kWin>
 struct Walk {
@@ -339,7 +340,7 @@ struct Walk {
         pc.head = k == 0;
         pc.whole = k == 0 && pc.T == q.kt && shared == 0;
         if (kWin) {
-            pc.b = q.b, pc.node0 = q.node0, pc.gap = q.gap;
+            pc.b = q.b, pc.node0 = q.node0, pc.gap = q.gap, pc.reach = q.unit0;
             pc.lo = q.base - window + 1 - q.gap;
             pc.end -= q.gap, pc.base -= q.gap;
         }
@@ -695,7 +696,7 @@ __device__ __noinline__ void add_spoilt(const AttnParams& p, const Piece& pc, ui
             window_words(p, pc.gap, pc.lo, pc.base, pc.end, b, node, node - pc.node0,
                          window_step(p.mask ? p.position + (size_t)b * p.nmax : nullptr, node - pc.node0, pc.base + pc.gap), first, sees);
         for (int place = kWin ? first : max(first, pc.base); place < min(pc.end, first + kTile); ++place) {
-            if (kWin && place < pc.base && !window_border(place, p.sinks, pc.lo, pc.n)) continue;
+            if (kWin && place < pc.base && !window_border(place, p.sinks, pc.lo, pc.reach)) continue;
             const int slot = kWin ? slot_at(p, pc.gap, place) : place;
             const size_t at = cache_row(c, __ldg(c.table + (size_t)(kWin ? pc.b : pc.s - 1) * c.width + (slot >> c.page_shift)), pc.h,
                                         slot & ((1 << c.page_shift) - 1));
@@ -912,7 +913,7 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
             // from this tile on there are new slots, or slots that are not there (the shared prefix: base is its end)
             const int first0 = pc.first, to_base = pc.base - kTile - first0, t_masked = to_base < 0 ? 0 : to_base / kTile + 1;
             // (kWin: and tiles at the window's border, with places that some rows do not see)
-            const int border0 = kWin ? p.sinks : 0, border1 = kWin ? pc.lo + pc.n - 1 : 0;
+            const int border0 = kWin ? p.sinks : 0, border1 = kWin ? pc.lo + pc.reach : 0;
             // Slots that are not there hold anything, and new slots may hold what is not a number and is not for every row: weights of zero do
             // not keep it out of the sums.  Their rows of V are cleared (a thread a slot); rows that see such a slot get it in the end.
             const auto clear_v = [&](int t, int first) {
@@ -1568,6 +1569,7 @@ __device__ __forceinline__ void self_plan(const AttnParams& p, SelfPlan& sm) {
             if (p.status && blockIdx.x == 0 && (!fine || n == 0)) p.status[b] = fine ? 0 : GRAFT_ST_BAD_CACHE;
             if (fine && n > 0) {
                 q.n = n, q.base = base, q.b = b;
+                q.unit0 = n - 1;  // (at most eight rows)
                 q.gap = gap_of(p, base);
                 q.kt = (base + n - q.gap + kTile - 1) / kTile;
                 cost = p.c.kv_heads * padded(kOneTile * q.kt, 1);
@@ -1835,7 +1837,7 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
                         for (int x = 0; x < 4 * kV; ++x) bad = bad || not_finite2(vr[i][x]);
                     // (a slot's lanes differ in g: any of them)
                     const bool unseen = kWin && slot >= p.sinks && slot < min(lo, base);  // (by all rows)
-                    const unsigned who = __ballot_sync(0xFFFFFFFFu, bad && slot < end && (slot >= base || (kWin && !unseen && window_border(slot, p.sinks, lo, pc.n))));
+                    const unsigned who = __ballot_sync(0xFFFFFFFFu, bad && slot < end && (slot >= base || (kWin && !unseen && window_border(slot, p.sinks, lo, pc.n - 1))));
                     spoilt[i] = (who & (0x11111111u << q4)) != 0;
                     if (slot >= end || spoilt[i] || unseen) {
 #pragma unroll
@@ -2071,7 +2073,7 @@ AttnSizes attn_sizes(int ctas, int batch, int entries, int use, int kv_heads, in
     z.o_start = take((size_t)ctas * sizeof(PlanStart));
     z.o_join = take((size_t)(ctas + 1) * sizeof(PlanJoin));
     z.o_ready = take((size_t)ctas * sizeof(int));
-    z.o_use = take((size_t)use * sizeof(int2));
+    z.o_use = take((size_t)use * sizeof(int4));
     z.o_entry0 = take((size_t)use * sizeof(int));
     z.o_ml = take(slots * z.part_rows * sizeof(float2));
     z.o_o = take(slots * z.part_rows * head_dim * sizeof(float));
@@ -2147,7 +2149,7 @@ void attn_places(AttnParams& p, const AttnSizes& z, void* scratch) {
     p.start = (PlanStart*)(base + z.o_start);
     p.join = (PlanJoin*)(base + z.o_join);
     p.ready = (int*)(base + z.o_ready);
-    p.use = (int2*)(base + z.o_use);
+    p.use = (int4*)(base + z.o_use);
     p.entry0 = (int*)(base + z.o_entry0);
     p.part_ml = (float2*)(base + z.o_ml);
     p.part_o = (float*)(base + z.o_o);

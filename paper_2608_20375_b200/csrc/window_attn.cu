@@ -22,7 +22,7 @@ __global__ void __launch_bounds__(kPlanThreads) window_plan_kernel(const __grid_
     __shared__ int scratch[3][kWarps];
     __shared__ PlanSeq entries[kPlanSeqs + 1];
     __shared__ int first_entry[kPlanSeqs];
-    __shared__ int2 uses[kPlanSeqs];
+    __shared__ int4 uses[kPlanSeqs];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     {
         const int b = blockIdx.x;
@@ -36,13 +36,17 @@ __global__ void __launch_bounds__(kPlanThreads) window_plan_kernel(const __grid_
             for (int i = tid; i <= sinks; i += kPlanThreads) ok = ok && (unsigned)table[i] < (unsigned)c.n_pages;
             for (int i = max(lo >> c.page_shift, sinks + 1) + tid; i <= pages; i += kPlanThreads) ok = ok && (unsigned)table[i] < (unsigned)c.n_pages;
         }
+        int reach = 0;  // of a tree: the deepest node's, as the window's border is as wide as that
+        if (p.mask != nullptr && ok)
+            for (int i = tid; i < n; i += kPlanThreads) reach = max(reach, window_step(p.position + (size_t)b * p.nmax, i, base));
         ok = __all_sync(0xFFFFFFFFu, ok);
-        if (lane == 0) fine[warp] = ok;
+        reach = __reduce_max_sync(0xFFFFFFFFu, reach);
+        if (lane == 0) fine[warp] = ok ? reach : -1;
         __syncthreads();
-        for (int w = 0; w < kWarps; ++w) ok = ok && fine[w];
+        for (int w = 0; w < kWarps; ++w) ok = ok && fine[w] >= 0, reach = max(reach, fine[w]);
         if (tid == 0) {
             if (p.status) p.status[b] = ok ? 0 : GRAFT_ST_BAD_CACHE;
-            p.use[b] = make_int2(ok ? n : 0, base);
+            p.use[b] = make_int4(ok ? n : 0, base, reach, 0);
             last = gridDim.x == 1 || atom_add_acq_rel(p.arrivals, 1) == (int)gridDim.x - 1;
         }
         __syncthreads();
@@ -54,7 +58,7 @@ __global__ void __launch_bounds__(kPlanThreads) window_plan_kernel(const __grid_
     int n_entries = 0;
     for (int b0 = 0; b0 < p.batch; b0 += kPlanThreads) {
         const int b = b0 + tid;
-        const int2 u = b < p.batch ? __ldcg(p.use + b) : make_int2(0, 0);
+        const int4 u = b < p.batch ? __ldcg(p.use + b) : make_int4(0, 0, 0, 0);
         const int mine = entries_of(p, u.x);
         const Sums s = block_sums(scratch, false, mine, 0, 0);
         if (b < p.batch) {
@@ -77,11 +81,12 @@ __global__ void __launch_bounds__(kPlanThreads) window_plan_kernel(const __grid_
             else
                 hi = mid - 1;
         }
-        const int2 u = few_seqs ? uses[lo] : __ldcg(p.use + lo);
+        const int4 u = few_seqs ? uses[lo] : __ldcg(p.use + lo);
         q.b = lo;
         q.node0 = (e - (few_seqs ? first_entry[lo] : p.entry0[lo])) * p.block_rows;
         q.n = min(p.block_rows, u.x - q.node0);
         q.base = u.y + q.node0;
+        q.unit0 = p.mask != nullptr ? u.z : q.n - 1;
         q.gap = gap_of(p, q.base);
         q.kt = (q.base + q.n - q.gap + kTile - 1) / kTile;
     };

@@ -20,7 +20,7 @@ from typing import Callable, Sequence
 
 import torch
 
-from .binding import Graft, GraftError, KVCache, TreeOut
+from .binding import Graft, GraftError, KVCache, Rope, TreeOut
 
 
 @dataclass
@@ -80,12 +80,19 @@ class MicroBatch:
             self._rows().zero_()
             self._attended = set()
 
-    def attend(self, layer, q, key, value, out, lse=None, scale=None, shared=0):
+    def attend(self, layer, q, key, value, out, lse=None, scale=None, shared=0, rope: Rope = None, q_out=None, window=None, sinks=0):
         """One layer of the target over this round's trees: the nodes' new entries go into the cache, q [batch, rows, q_heads, head_dim]
-        sees the prefix and the nodes above its own.  Outside of a round (by hand, without begin_round) status
-        is this call's."""
+        sees the prefix and the nodes above its own.  rope: queries and keys are turned by the nodes' positions on the way, the queries into
+        q_out (None: in place).  window: rows see that many of the last positions, and the first `sinks`.  Outside of a round (by hand, without
+        begin_round) status is this call's."""
         if self.cache is None:
             raise GraftError("the micro-batch has no cache")
+        if window is not None and shared:
+            raise GraftError("a window and a shared prefix do not go together")
+        if window is None and sinks:
+            raise GraftError("sinks are given without a window")
+        if rope is None and q_out is not None:
+            raise GraftError("q_out is given without rope")
         if not 0 <= layer < self.cache.k.shape[0]:
             raise GraftError(f"layer must be below {self.cache.k.shape[0]}, got {layer}")
         calls = self._rows()
@@ -94,9 +101,17 @@ class MicroBatch:
             if layer in self._attended:
                 calls[-3].bitwise_or_(written | attended)
             self._attended.add(layer)
-        self.graft.cache_write(self.cache, layer, self.table, self.prefix_len, self.out.n_nodes, key, value, written)
-        self.graft.tree_attention(self.cache, layer, self.table, q, self.prefix_len, self.out.n_nodes, self.out.mask, out, lse, scale, shared,
-                                  attended)
+        g, o = self.graft, self.out
+        if rope is None:
+            g.cache_write(self.cache, layer, self.table, self.prefix_len, o.n_nodes, key, value, written)
+        else:
+            g.cache_append(self.cache, layer, self.table, self.prefix_len, o.n_nodes, rope, q, key, value, q_out, o.position, written)
+            q = q if q_out is None else q_out
+        if window is None:
+            g.tree_attention(self.cache, layer, self.table, q, self.prefix_len, o.n_nodes, o.mask, out, lse, scale, shared, attended)
+        else:
+            g.window_attention(self.cache, layer, self.table, q, self.prefix_len, o.n_nodes, o.mask, o.position, window, sinks, out, lse, scale,
+                               attended)
         if self._attended is None:
             torch.bitwise_or(written, attended, out=self.status)
 
