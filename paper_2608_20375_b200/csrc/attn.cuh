@@ -1223,15 +1223,11 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
                     it += 1;
                     return true;
                 };
-                if (two) {
-                    for (int t = 0; ok && t < T; ++t) ok = bring(t, false) && bring(t, true);
-                } else {
-                    ok = bring(0, false);
-                    if (T > 1) ok = ok && bring(1, false);
-                    for (int t = 0; ok && t < T; ++t) {
-                        ok = bring(t, true);
-                        if (t + 2 < T) ok = ok && bring(t + 2, false);
-                    }
+                // (in the order of the ring, see v_entry)
+#pragma unroll 1
+                for (int e = 0; ok && e < 2 * T; ++e) {
+                    const bool is_v = two ? e & 1 : e == 2 * T - 1 || (e > 0 && !(e & 1));
+                    ok = bring(two ? e >> 1 : e == 2 * T - 1 ? T - 1 : is_v ? (e - 2) >> 1 : (e + 1) >> 1, is_v);
                 }
                 if (!ok) break;
                 piece_done(n_piece);
