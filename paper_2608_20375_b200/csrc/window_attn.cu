@@ -152,12 +152,10 @@ cudaError_t launch_any(graft_ctx* ctx, const AttnParams& p, bool few, cudaStream
     if (few)
         return launch_kernels(ctx, p, window_plan_kernel, few_attn_kernel<D, Q8, true>, FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kSmem,
                               &ctx->window_ready, bit, [] { return cudaSuccess; }, st);
-    const auto join = [&] { return launch_join<D>(ctx, p, st); };
-    if ((long long)p.block_rows * p.group <= kTile)
-        return launch_kernels(ctx, p, window_plan_kernel, tree_attn_kernel<D, Q8, true, true>, Shape<D, Q8, true>::kThreads,
-                              Shape<D, Q8, true>::kSmem, &ctx->window_ready, bit << 4, join, st);
-    return launch_kernels(ctx, p, window_plan_kernel, tree_attn_kernel<D, Q8, false, true>, Shape<D, Q8, false>::kThreads,
-                          Shape<D, Q8, false>::kSmem, &ctx->window_ready, bit << 8, join, st);
+    const bool one = (long long)p.block_rows * p.group <= kTile;
+    const TilesKernel k = window_tiles_kernel(D, Q8, one);
+    return launch_kernels(ctx, p, window_plan_kernel, k.kernel, k.threads, k.smem, &ctx->window_ready, bit << (one ? 4 : 8),
+                          [&] { return launch_join<D>(ctx, p, st); }, st);
 }
 
 struct WindowShape {
