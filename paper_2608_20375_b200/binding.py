@@ -567,7 +567,7 @@ class Graft:
             self._ctx, batch, C.byref(cc), int(layer), heads, rows, stride, qp, cc.head_dim ** -0.5 if scale is None else scale,
             _shaped("prefix_len", prefix_len, i32, (batch,), dev), _shaped("count", count, i32, (batch,), dev),
             _shaped("mask", mask, i32, (batch, self.nmax, self.mask_words), dev), _shaped("position", position, i32, (batch, self.nmax), dev),
-            int(window), int(sinks), _shaped("out", out, torch.bfloat16, (batch, rows, heads, cc.head_dim), dev),
+            *(min(max(int(x), -1), 2 ** 31 - 1) for x in (window, sinks)), _shaped("out", out, torch.bfloat16, (batch, rows, heads, cc.head_dim), dev),
             _shaped("lse", lse, torch.float32, (batch, rows, heads), dev), _shaped("status", status, i32, (batch,), dev), _stream()),
             "graft_window_attention")
 
