@@ -107,7 +107,11 @@ __device__ __forceinline__ int slot_at(const AttnParams& p, int gap, int place) 
 // Slots ahead of the new rows that some row of the block does not see: those behind the sinks and ahead of the window of the row that is `reach`
 // positions behind the first.
 __device__ __forceinline__ bool window_border(int place, int sinks, int lo, int reach) { return place >= sinks && place < lo + reach; }
-__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1; }
+__device__ __forceinline__ uint32_t low_bits(int n) {  // (a shift by 32 or more leaves nothing)
+    uint32_t r;
+    asm("shl.b32 %0, %1, %2;" : "=r"(r) : "r"(1), "r"(max(n, 0)));
+    return r - 1;
+}
 // how far behind the first row's slot row i's position is; base: that slot
 __device__ __forceinline__ int window_step(const int32_t* position, int i, int base) {
     if (position == nullptr) return i;
@@ -409,12 +413,19 @@ __device__ __noinline__ void seen_words(const uint32_t* mask_row, int words, int
     }
 }
 
+// Of the new rows from j on that `tree` has, those that a row further than the window behind the first one sees, by their own positions.
+__device__ __noinline__ uint32_t near_rows(const AttnParams& p, const int32_t* position, uint32_t tree, int j, int at_base, int step) {
+    for (uint32_t left = tree; left != 0; left &= left - 1) {
+        const int y = __ffs(left) - 1, at = window_step(position, j + y, at_base);
+        if (step - at >= p.window && at + at_base >= p.sinks) tree &= ~(1u << y);
+    }
+    return tree;
+}
 // The same behind a window: of the 128 places from `first` on, for row i of a block (the sequence's row `node`) whose first row stands in place
 // `base`; step: how far behind that one's position its own is.
 __device__ __noinline__ void window_words(const AttnParams& p, int gap, int lo, int base, int end, int b, int node, int i, int step, int first,
                                           uint32_t (&sees)[4]) {
     const int j0 = first - base, w0 = j0 >> 5;
-    const int32_t* position = p.mask != nullptr ? p.position + (size_t)b * p.nmax : nullptr;  // (with a mask a block is a whole tree: i is its node)
     uint32_t m[5] = {0, 0, 0, 0, 0};
     if (p.mask != nullptr && first + kTile > base) {
         const uint32_t* mask_row = p.mask + ((size_t)b * p.nmax + node) * p.words;
@@ -430,11 +441,8 @@ __device__ __noinline__ void window_words(const AttnParams& p, int gap, int lo, 
         const uint32_t near = low_bits(p.sinks - place) | ~low_bits(lo + step - place);
         const uint32_t there = low_bits(end - place);
         uint32_t tree = __funnelshift_r(m[x], m[x + 1], j0 & 31) & there;
-        if (p.mask != nullptr && step >= p.window)  // (a path longer than the window: rows ahead of it by their own positions)
-            for (uint32_t left = tree; left != 0; left &= left - 1) {
-                const int y = __ffs(left) - 1, at = window_step(position, j + y, base + gap);
-                if (step - at >= p.window && at + base + gap >= p.sinks) tree &= ~(1u << y);
-            }
+        // (with a mask a block is a whole tree: i is its node; a path may be longer than the window)
+        if (p.mask != nullptr && step >= p.window) tree = near_rows(p, p.position + (size_t)b * p.nmax, tree, j, base + gap, step);
         sees[x] = (p.mask != nullptr ? (low_bits(-j) & near) | tree : low_bits(i - j + 1) & near) & there;
     }
 }

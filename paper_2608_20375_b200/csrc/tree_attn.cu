@@ -159,7 +159,10 @@ __device__ __forceinline__ float scores(uint32_t tS, int x0, uint32_t (&u)[kCols
     tmem_arrived(u);
     if (masked)
 #pragma unroll
-        for (int x = 0; x < kCols; ++x) u[x] = (sees[(x0 + x) / 32] >> (x % 32)) & 1 ? u[x] : 0xFF800000u;
+        for (int w = 0; w < kCols / 32; ++w)
+            if (__any_sync(0xFFFFFFFFu, sees[x0 / 32 + w] != 0xFFFFFFFFu))  // (borders cross few of a tile's columns)
+#pragma unroll
+                for (int x = 0; x < 32; ++x) u[32 * w + x] = (sees[x0 / 32 + w] >> x) & 1 ? u[32 * w + x] : 0xFF800000u;
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
     for (int x = 0; x < kCols; x += 2) mx[x / 2 % 4] = max3(mx[x / 2 % 4], __uint_as_float(u[x]), __uint_as_float(u[x + 1]));
