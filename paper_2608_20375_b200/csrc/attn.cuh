@@ -552,12 +552,13 @@ __device__ __forceinline__ void join_rows(const AttnParams& p, const JoinList& j
 // ---- few rows ----------------------------------------------------------------------------------------------------------
 // Single tokens (up to eight rows a sequence and key head) are bound by the bytes of K and V, and a tile of 128 rows would be nearly empty.
 // Here a warp takes 16 slots at a time into the fragments of m16n8k16 products, S^T = K Q^T and O^T = V^T P^T, with slots and head_dim in
-// the long directions and the rows in the short one; e4m3 entries become bf16 in registers.  The order of head_dim inside a product is free,
-// so a lane loads pieces of 16 bytes straight into what it multiplies: of K, a quarter of those of two slots; of V, an eighth of four.  The next
+// the long directions and the rows in the short one; e4m3 entries become f16 (K) and bf16 (V) in registers, their slots' powers of two go to scores
+// and weights.  The order of head_dim inside a product is free, so a lane loads pieces of 16 bytes straight into what it multiplies: of K, a quarter of those of two slots; of V, an eighth of four.  The next
 // step's K is asked for when this one's scores are done, and V when its products are: the warps of an SM then have 50 to 60 KB under way.
-// 64 sequences of 2000 to 16000 slots, 8 key heads of 128: bf16 354 us (6.6 TB/s; through the tiles of 128 rows 417), e4m3 274 us (4.3
-// TB/s; 553), which conversions bound: 500 instructions for 16 slots, three warps a scheduler to hide their latencies.  Before pieces' own cost
-// was counted (371 and 288): through a ring of cp.async in shared memory 543 and 295; with 8 warps of two steps 297, with 16 warps 294 (registers spill).
+// 64 sequences of 2000 to 16000 slots, 8 key heads of 128: bf16 354 us (6.6 TB/s; through the tiles of 128 rows 417), e4m3 224 us (5.3
+// TB/s; 553), which instructions bound, three warps a scheduler to hide their latencies.  With K and V turned into bf16 and multiplied by their slots'
+// powers: 500 instructions for 16 slots, 275 us.  Before pieces' own cost was counted (371 and 288): through a ring of cp.async in shared memory 543 and 295;
+// with 8 warps of two steps 297, with 16 warps 294 (registers spill).  Behind a window of 4096, 64 sequences: e4m3 120 us, 130 before.
 constexpr int kFewRows = 8;
 
 template <int D, bool Q8>
@@ -577,6 +578,18 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_16816_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// four e4m3 numbers as f16, which holds them all
+__device__ __forceinline__ uint2 e4m3x4_to_f16(uint32_t w) {
+    uint2 r;
+    asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %2;\n cvt.rn.f16x2.e4m3x2 %0, lo;\n cvt.rn.f16x2.e4m3x2 %1, hi;\n}" : "=r"(r.x), "=r"(r.y) : "r"(w));
+    return r;
+}
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }  // -126 .. 127
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
     uint32_t r;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
@@ -587,7 +600,8 @@ __device__ __forceinline__ uint4 load_once(const uint8_t* p) {
     asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
     return r;
 }
-// The plan of few rows behind a window, worked out by every CTA for itself: a launch ahead takes longer than two loads and a sum over the sequences.
+// The plan of few rows behind a window, worked out by every CTA for itself: a launch ahead takes longer than two loads and a sum over the sequences (one
+// token behind a window of 4096 18.4 -> 16.2 us, 64 of them, e4m3, 152 -> 130).  More sequences than this have a launch ahead, as their plan takes a block its time.
 // Numbers that are wrong by themselves leave a sequence without rows; its pages are looked at with its pieces.
 constexpr int kSelfSeqs = 256;
 struct SelfPlan {
@@ -764,6 +778,26 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
                 qf[4 * i] = u.x, qf[4 * i + 1] = u.y, qf[4 * i + 2] = u.z, qf[4 * i + 3] = u.w;
             }
         }
+        // Over e4m3 slots: f16 holds e4m3 numbers, and a row of Q when its largest number is brought to 2^14 by a power of two (what f16 then rounds is
+        // 2^-39 of that); scores take the powers of both back.
+        float q_down[2] = {1.0f, 1.0f};  // of rows 2 q4, 2 q4 + 1
+        bool q_far = false;
+        if (Q8) {
+            uint32_t most2 = 0;
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) most2 = max_magnitude2(most2, qf[i]);
+            uint32_t top = max(most2 & 0x7FFFu, most2 >> 16 & 0x7FFFu);
+            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            const int up = top == 0 ? 0 : min(127 + 14 - (int)(top >> 7), 126);  // (from -114 on)
+            const float f = power_of_two(up);
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i)
+                asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(qf[i]) : "f"(__uint_as_float(qf[i] & 0xFFFF0000u) * f), "f"(__uint_as_float(qf[i] << 16) * f));
+            q_far = __any_sync(0xFFFFFFFFu, up > 60 || up < -60);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) q_down[i] = power_of_two(-__shfl_sync(0xFFFFFFFFu, up, (2 * q4 + i) * 4));
+        }
         float o[D / 16][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, upto[2] = {-INFINITY, -INFINITY}, off[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
@@ -772,25 +806,11 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
             const bool more_steps = step + 1 < steps;
             const size_t row1 = row_at(step + 1, page);
             page = page_of(step + 2);
-            // factors of K's slots g, g + 8: 2^(e + 120), a second one where that is above bf16's largest (rare, and not numbers)
-            uint32_t f[2] = {0, 0}, ke[2] = {0, 0};
-            float more[2] = {1.0f, 1.0f};
-            bool large = false;
-            if (Q8) {
+            // powers of two of K's slots g, g + 8
+            uint32_t ke[2] = {0, 0};
+            if (Q8)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    ke[i] = __byte_perm(i ? k_exps.z : k_exps.x, i ? k_exps.w : k_exps.y, g) & 255;
-                    f[i] = (ke[i] + 120) * 0x00800080u;
-                }
-                large = __any_sync(0xFFFFFFFFu, max(ke[0], ke[1]) > 134);
-                if (large)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint32_t x;
-                        e4m3_factors(ke[i], f[i], x);
-                        more[i] = __uint_as_float(x << 16);
-                    }
-            }
+                for (int i = 0; i < 2; ++i) ke[i] = __byte_perm(i ? k_exps.z : k_exps.x, i ? k_exps.w : k_exps.y, g) & 255;
             // ---- scores: rows 2 q4, 2 q4 + 1 at slots g, g + 8
             float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s2[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -801,22 +821,32 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const uint32_t w[4] = {kr[i][y].x, kr[i][y].y, kr[i][y].z, kr[i][y].w};
-                        a[x][i] = Q8 ? make_uint2(bf16x2_mul(e4m3_pair_small(w[x], 0, 0, 1), f[i]), bf16x2_mul(e4m3_pair_small(w[x], 0, 2, 3), f[i]))
-                                     : make_uint2(w[2 * x & 3], w[(2 * x + 1) & 3]);
+                        a[x][i] = Q8 ? e4m3x4_to_f16(w[x]) : make_uint2(w[2 * x & 3], w[(2 * x + 1) & 3]);
                     }
 #pragma unroll
                 for (int x = 0; x < 4 / kBytes; ++x) {
                     const int ks = y * (4 / kBytes) + x;
-                    mma_16816(x & 1 ? s2 : s, a[x][0].x, a[x][1].x, a[x][0].y, a[x][1].y, qf[2 * ks], qf[2 * ks + 1]);
+                    const auto mma = Q8 ? mma_16816_f16 : mma_16816;
+                    mma(x & 1 ? s2 : s, a[x][0].x, a[x][1].x, a[x][0].y, a[x][1].y, qf[2 * ks], qf[2 * ks + 1]);
                 }
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[i] += s2[i];
-            if (Q8 && large)
+            if (Q8) {
+                if (q_far || __any_sync(0xFFFFFFFFu, max(ke[0] - 67, ke[1] - 67) > 120)) {  // (rare: in two steps, and what is not a number)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[i] *= more[i >> 1];
+                    for (int i = 0; i < 4; ++i) {
+                        const int e = (int)ke[i >> 1] - 127, d = (__float_as_int(q_down[i & 1]) >> 23) - 127, e1 = e >> 1, d1 = d >> 1;
+                        s[i] = ke[i >> 1] == 255 ? __int_as_float(0x7FFFFFFF) : s[i] * power_of_two(e1 + d1) * power_of_two(e - e1 + d - d1);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[i] *= q_down[i & 1] * __uint_as_float(ke[i >> 1] << 23);
+                }
+            }
             if (more_steps) bring_k(row1);
-            // the same for V's pairs of slots; second factors go to the weights (slots g, g + 8)
+            // What e4m3_pair_small makes of V lacks a power of two a slot, 2^(e + 120).  It goes to the slot's weights, where it changes no rounding, as long
+            // as those stay below 2^128; else (rare, and not numbers) to V, with what is above bf16's largest power going to the weights.
             uint32_t f2[2] = {0, 0}, x[2] = {0, 0};  // (x: the exponents of two slots)
             float big[2] = {1.0f, 1.0f};
             bool large_v = false;
@@ -824,9 +854,9 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     x[i] = __byte_perm(i ? v_exps.z : v_exps.x, i ? v_exps.w : v_exps.y, 2 * q4 | (2 * q4 + 1) << 8) & 0x00FF00FFu;
-                    f2[i] = (x[i] + 0x00780078u) << 7;
+                    big[i] = __uint_as_float(((__byte_perm(i ? v_exps.z : v_exps.x, i ? v_exps.w : v_exps.y, g) & 255) + 120) << 23);
                 }
-                large_v = __any_sync(0xFFFFFFFFu, ((x[0] + 0x00790079u) | (x[1] + 0x00790079u)) & 0x01000100u);  // (one above 134)
+                large_v = __any_sync(0xFFFFFFFFu, ((x[0] + 0x00810081u) | (x[1] + 0x00810081u)) & 0x01000100u);  // (one above 126: weights are up to 2^8)
                 if (large_v)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -907,7 +937,7 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
             }
             // P^T as the second operand: rows where the slots were
             float e[4] = {s[0], s[1], s[2], s[3]};
-            if (Q8 && large_v)
+            if (Q8)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) e[i] *= big[i >> 1];
             const uint32_t pb0 = transpose_8x8(pack_bf16(e[0], e[1])), pb1 = transpose_8x8(pack_bf16(e[2], e[3]));
@@ -923,10 +953,13 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
                         for (int z = 0; z < 2; ++z) {
                             const int y = y0 + x, byte = (2 * y + z) & 3;
                             if (Q8) {
-                                a[x][i][z] = bf16x2_mul(e4m3_pair_small(vr[2 * i][y / 2], vr[2 * i + 1][y / 2], byte, 4 + byte), f2[i]);
+                                a[x][i][z] = e4m3_pair_small(vr[2 * i][y / 2], vr[2 * i + 1][y / 2], byte, 4 + byte);
                             } else
                                 a[x][i][z] = __byte_perm(vr[2 * i][y], vr[2 * i + 1][y], z ? 0x7632 : 0x5410);
                         }
+                if (Q8 && large_v)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) a[x >> 2][x >> 1 & 1][x & 1] = bf16x2_mul(a[x >> 2][x >> 1 & 1][x & 1], f2[x >> 1 & 1]);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) mma_16816(o[y0 + x], a[x][0][0], a[x][0][1], a[x][1][0], a[x][1][1], pb0, pb1);
             }

@@ -138,3 +138,59 @@ def test_windows_and_sinks_beyond_32_bits():
         for window, sinks in ((0, 0), (-2 ** 32 + 5, 0), (5, -1), (5, -2 ** 32)):
             with pytest.raises(GraftError):
                 g.window_attention(c, 0, tb, q, _i32([400]), _i32([rows]), None, None, window, sinks, out)
+
+
+@pytest.mark.parametrize("dtype", [BF, Q8])
+@pytest.mark.parametrize("rows,heads", [(1, 8), (4, 2), (40, 4)])
+def test_powers_of_two_go_through(dtype, rows, heads):
+    """Queries times 2^a, keys times 2^-a and values times 2^b: the same scores, and the same result times 2^b, bit for bit."""
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    g = _graft(2, 2)
+    n, D = 300, 128
+    tb = torch.arange(2 * 6, dtype=torch.int32, device="cuda").view(2, 6)
+    key, value = (torch.randn((2, n, 1, D), generator=gen, device="cuda").to(BF) for _ in range(2))
+    q = torch.randn((2, rows, heads, D), generator=gen, device="cuda").to(BF)
+    q[:, 0, 0, 1:] *= 2.0 ** -20  # (numbers far below a row's largest)
+    want = None
+    for a, b in ((0, 0), (5, 9), (40, 20), (-40, 100), (75, -60), (-75, 7), (100, -100), (-100, 8)):
+        c = _cache(gen, (1, 12, 1, 64, D), dtype, garbage=False)
+        g.cache_write(c, 0, tb, _i32([1, 1]), _i32([n, n]), (key.float() * 2.0 ** -a).to(BF), (value.float() * 2.0 ** b).to(BF))
+        out, lse = torch.zeros_like(q), torch.zeros((2, rows, heads), device="cuda")
+        for call in ("window", "tree"):
+            args = c, 0, tb, (q.float() * 2.0 ** a).to(BF), _i32([n + 1 - rows, 100]), _i32([rows, rows])
+            if call == "window":
+                g.window_attention(*args, None, None, 200, 4, out, lse=lse)
+            else:
+                g.tree_attention(*args, None, out, lse=lse)
+            got = out.float() * 2.0 ** -b, lse.clone()
+            if (a, b) == (0, 0):
+                want = {**(want or {}), call: got}
+            assert torch.equal(got[0], want[call][0]) and torch.equal(got[1], want[call][1]), (call, a, b)
+    assert want["window"][0].abs().sum() > 0
+
+
+@pytest.mark.parametrize("rows,heads", [(1, 8), (4, 2)])
+def test_rows_of_queries_that_are_not_numbers(rows, heads):
+    """Over e4m3 slots: a query with an infinity or NaN makes its own row NaN and no other; a row of zeros weighs all alike."""
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    g = _graft(2, 1)
+    D, n = 64, 200
+    tb = _i32([list(range(4))])
+    c = _cache(gen, (1, 4, 1, 64, D), Q8, garbage=False)
+    key, value = (torch.randn((1, n, 1, D), generator=gen, device="cuda").to(BF) for _ in range(2))
+    g.cache_write(c, 0, tb, _i32([1]), _i32([n]), key, value)
+    q = torch.randn((1, rows, heads, D), generator=gen, device="cuda").to(BF)
+
+    def call(q):
+        out = torch.zeros_like(q)
+        g.window_attention(c, 0, tb, q, _i32([n + 1 - rows]), _i32([rows]), None, None, 90, 3, out)
+        return out.flatten(1, 2)[0]
+
+    want = call(q)
+    assert torch.isfinite(want).all()
+    bad = q.clone().flatten(1, 2)
+    bad[0, 1, 5], bad[0, 3, 7], bad[0, 5] = float("inf"), float("nan"), 0.0
+    got = call(bad.view_as(q))
+    assert got[1].isnan().all() and got[3].isnan().all()
+    others = [i for i in range(8) if i not in (1, 3, 5)]
+    assert torch.equal(got[others], want[others]) and torch.isfinite(got[5]).all()
