@@ -558,18 +558,21 @@ __device__ __forceinline__ void join_rows(const AttnParams& p, const JoinList& j
 // 64 sequences of 2000 to 16000 slots, 8 key heads of 128: bf16 354 us (6.6 TB/s; through the tiles of 128 rows 417), e4m3 224 us (5.3
 // TB/s; 553), which instructions bound, three warps a scheduler to hide their latencies.  With K and V turned into bf16 and multiplied by their slots'
 // powers: 500 instructions for 16 slots, 275 us.  Before pieces' own cost was counted (371 and 288): through a ring of cp.async in shared memory 543 and 295;
-// with 8 warps of two steps 297, with 16 warps 294 (registers spill).  Behind a window of 4096, 64 sequences: e4m3 120 us, 130 before.
+// with 8 warps of two steps 297, with 16 warps 294 (registers spill).  Behind a window of 4096, 64 sequences: e4m3 114 us.
 constexpr int kFewRows = 8;
 
-template <int D, bool Q8>
+template <int D, bool Q8, bool kWin>
 struct FewShape {
     static constexpr int kBytes = Q8 ? 1 : 2;
     static constexpr int kK = D / 4 * kBytes / 16;                                     // pieces of a slot's K that a lane has
     static constexpr int kPiece = D / 8 * kBytes < 16 ? D / 8 * kBytes : 16;           // bytes of a piece of V (D = 64, e4m3: 8)
     static constexpr int kV = D / 8 * kBytes / kPiece;                                 // pieces of a slot's V
-    // as many warps an SM as have room in registers for a step's K and V (16 to 64 of them) beside Q and O
-    static constexpr int kWarps = Q8 && D == 128 ? 12 : 8, kThreads = 32 * kWarps;
-    static constexpr int kCtas = D == 128 ? 1 : 2;
+    // As many warps an SM as have room in registers for a step's K and V (16 to 64 of them) beside Q and O.  In two CTAs one begins a piece while the
+    // other is under way: e4m3 slots behind a window, 12 warps an SM, 64 tokens 121 -> 114 us, 12 tokens 33.0 -> 29.9.  Over bf16 slots there are 8, whose
+    // loads fill the SM's share of the memory either way (64 tokens 168.0 and 168.8, 4 tokens 19.8 and 20.3).
+    static constexpr bool kPair = D == 64 || (Q8 && kWin);
+    static constexpr int kWarps = Q8 && D == 128 ? (kPair ? 6 : 12) : 8, kThreads = 32 * kWarps;
+    static constexpr int kCtas = kPair ? 2 : 1;
     static constexpr size_t kSmem = (size_t)kWarps * kFewRows * (D + 2) * sizeof(float);
 };
 
@@ -601,9 +604,9 @@ __device__ __forceinline__ uint4 load_once(const uint8_t* p) {
     return r;
 }
 // The plan of few rows behind a window, worked out by every CTA for itself: a launch ahead takes longer than two loads and a sum over the sequences (one
-// token behind a window of 4096 18.4 -> 16.2 us, 64 of them, e4m3, 152 -> 130).  More sequences than this have a launch ahead, as their plan takes a block its time.
+// token behind a window of 4096 18.4 -> 16.2 us, 64 of them, e4m3, 152 -> 130, before the steps below).  More sequences than this have a launch ahead, as their plan takes a block its time.
 // Numbers that are wrong by themselves leave a sequence without rows; its pages are looked at with its pieces.
-constexpr int kSelfSeqs = 256;
+constexpr int kSelfSeqs = 192;
 struct SelfPlan {
     PlanSeq entry[kSelfSeqs + 1];
     PlanStart start;
@@ -663,9 +666,73 @@ __device__ __forceinline__ void self_plan(const AttnParams& p, SelfPlan& sm) {
     __syncthreads();
 }
 
+// Up to eight rows of a unit from the pieces on the list, behind a window: a lane a row and every fourth piece, a warp some of the columns; the four
+// lanes of a row are added in the end, so results repeat.  Eight pieces are on their way at a time: one token behind a window of 4096, whose units
+// have 18 pieces, 16.2 -> 12.4 us beside a lane a row and four pieces at a time (sixteen at a time 12.6, registers spill).
+template <int D, int kWarps>
+__device__ __forceinline__ void join_few(const AttnParams& p, const JoinList& j, int R, size_t out_row0) {
+    constexpr int kQuads = (D / 4 + kWarps - 1) / kWarps, kEach = 2;
+    const int lane = lane_id(), warp = threadIdx.x >> 5, n = j.n, row = lane & 7, at = lane >> 3;
+    const int r = row < R ? row : 0;
+    float m = -INFINITY, l = 0.0f;
+    float o[4 * kQuads] = {};
+    for (int i0 = 0; i0 < n; i0 += 4 * kEach) {
+        float2 ml[kEach];
+        float4 v[kEach][kQuads];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int e = i0 + 4 * i + at;
+            const size_t slot = j.piece[min(e, n - 1)].slot;
+            ml[i] = make_float2(-INFINITY, 0.0f);
+            if (e < n) ml[i] = __ldcg(p.part_ml + slot * p.part_rows + r);
+#pragma unroll
+            for (int y = 0; y < kQuads; ++y) {
+                v[i][y] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (e < n && warp + y * kWarps < D / 4)
+                    v[i][y] = __ldcg((const float4*)p.part_o + (slot * (D / 4) + warp + y * kWarps) * p.part_rows + r);
+            }
+        }
+        float now = m;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) now = fmaxf(now, ml[i].x);
+        const float f0 = m > -INFINITY ? ex2_approx(m - now) : 0.0f;
+        m = now;
+        l *= f0;
+#pragma unroll
+        for (int x = 0; x < 4 * kQuads; ++x) o[x] *= f0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const float f = ml[i].x > -INFINITY ? ex2_approx(ml[i].x - m) : 0.0f;
+            l += f * ml[i].y;
+#pragma unroll
+            for (int y = 0; y < kQuads; ++y)
+                o[4 * y] += f * v[i][y].x, o[4 * y + 1] += f * v[i][y].y, o[4 * y + 2] += f * v[i][y].z, o[4 * y + 3] += f * v[i][y].w;
+        }
+    }
+    float all = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
+    all = fmaxf(all, __shfl_xor_sync(0xFFFFFFFFu, all, 16));
+    const float f = m > -INFINITY ? ex2_approx(m - all) : 0.0f;
+    const auto sum4 = [&](float x) {
+        x *= f;
+        x += __shfl_xor_sync(0xFFFFFFFFu, x, 8);
+        return x + __shfl_xor_sync(0xFFFFFFFFu, x, 16);
+    };
+    l = sum4(l);
+    const float inv = l != 0.0f ? 1.0f / l : 1.0f;
+#pragma unroll
+    for (int y = 0; y < kQuads; ++y) {
+        const float a = sum4(o[4 * y]), b = sum4(o[4 * y + 1]), c = sum4(o[4 * y + 2]), d = sum4(o[4 * y + 3]);
+        const int quad = warp + y * kWarps;
+        if (at == 0 && row < R && quad < D / 4)
+            ((uint2*)(p.out + (out_row0 + (row / p.group) * (size_t)p.q_heads + row % p.group) * D))[quad] =
+                make_uint2(pack_bf16(a * inv, b * inv), pack_bf16(c * inv, d * inv));
+    }
+    if (p.lse && warp == 0 && at == 0 && row < R) p.lse[out_row0 + (row / p.group) * (size_t)p.q_heads + row % p.group] = log_sum(all, l);
+}
+
 template <int D, bool Q8, bool kWin>
-__global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kCtas) few_attn_kernel(const __grid_constant__ AttnParams p) {
-    using S = FewShape<D, Q8>;
+__global__ void __launch_bounds__(FewShape<D, Q8, kWin>::kThreads, FewShape<D, Q8, kWin>::kCtas) few_attn_kernel(const __grid_constant__ AttnParams p) {
+    using S = FewShape<D, Q8, kWin>;
     constexpr int kBytes = S::kBytes, kK = S::kK, kV = S::kV, kPiece = S::kPiece, kWarps = S::kWarps;
     constexpr int kCk = 16 / kBytes, kCv = kPiece / kBytes;  // numbers of a piece
     extern __shared__ __align__(16) float few_sm[];  // [warps][rows][D], then [warps][rows][2]
@@ -1062,7 +1129,9 @@ __global__ void __launch_bounds__(FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kC
             if (last) {
                 __threadfence();
                 const int node = lane / p.group;
-                if (tid < kJoinThreads)
+                if (kWin)
+                    join_few<D, kWarps>(p, list, R, (size_t)b * p.rows * p.q_heads + h * p.group);
+                else if (tid < kJoinThreads)
                     join_rows<D>(p, list, lane < R, ((size_t)b * p.rows + node) * p.q_heads + h * p.group + (lane - node * p.group));
             }
             __syncthreads();
@@ -1119,9 +1188,10 @@ bool encode_map(CUtensorMap* map, const void* base, bool q8, int D, uint64_t row
 }
 
 bool few_rows(int group, int rows, int shared) { return shared == 0 && (long long)rows * group <= kFewRows; }
+template <bool kWin>
 int attn_ctas(const graft_ctx* ctx, bool q8, int head_dim, int group, int rows, int shared) {
-    const int ctas = head_dim == 128 ? (q8 ? FewShape<128, true>::kCtas : FewShape<128, false>::kCtas)
-                                     : (q8 ? FewShape<64, true>::kCtas : FewShape<64, false>::kCtas);
+    const int ctas = head_dim == 128 ? (q8 ? FewShape<128, true, kWin>::kCtas : FewShape<128, false, kWin>::kCtas)
+                                     : (q8 ? FewShape<64, true, kWin>::kCtas : FewShape<64, false, kWin>::kCtas);
     return ctx->num_sms * (few_rows(group, rows, shared) ? ctas : 1);
 }
 

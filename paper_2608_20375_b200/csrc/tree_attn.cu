@@ -18,11 +18,16 @@
 //
 // Sequences of up to eight rows a key head (single tokens) have a kernel of their own, on the same plan: see "few rows".
 //
-// What bounds it.  Large trees (16 of up to 513 nodes behind 6000 to 8192 slots, bf16, 717 GFLOP): 840 to 875 us, the tensor cores busy for 47 % of
-// the time, the exponentials' unit for 36 %: a stream's next product waits for all of a tile's weights, and two streams (TMEM holds
-// no more) do not fill the gaps; the clock falls to 1.3 GHz under that load in a long run (980 to 1060 us).  A tile of e4m3 slots is converted
-// once a unit, 0.5 to 0.6 us, and is as long on its way as the products: 823 us against 621 for 8 sequences of 512 nodes.  17 nodes (68 rows)
-// behind 4000 slots, bf16: 213 us, 0.78 of the copy's rate.  Small calls are latencies: one tree of 65 nodes behind 1500 slots 31 us, of
+// What bounds it.  Large trees (16 of up to 513 nodes behind 6000 to 8192 slots, bf16, 717 GFLOP): 805 to 850 us, the tensor cores busy for 52 % of
+// the time, the exponentials' unit for 39 %: a stream's next product waits for all of a tile's weights, and two streams (TMEM holds
+// no more) do not fill the gaps; the clock falls to 1.3 GHz under that load in a long run (960 to 1040 us).  A tile of e4m3 slots is converted
+// once a unit, 0.5 to 0.6 us: 32 trees of up to 65 nodes behind 500 to 4096 slots 131 us.  17 nodes (68 rows)
+// behind 4000 slots, bf16: 213 us, 0.78 of the copy's rate.  Small calls are latencies: one tree of 65 nodes behind 1500 slots 29.5 us, of
+// which the plan takes 4, the kernel 10 to 15 and the join 8.
+//
+// Code counts.  Four roles of warps run in four places of this kernel, and what they go through in a tile has to stay in the SM's instruction cache: with
+// every wait unrolled and a copy of the softmax for each half of e4m3 scores it was 185 KB, and the e4m3 case above 177 us (now 111 KB); so
+// waits, rescaling and walks along lists are rolled loops and rare paths are functions.
 #include "attn.cuh"
 
 namespace graft {
@@ -336,10 +341,13 @@ template <int D, bool Q8, bool kOne, bool kWin>
 __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_kernel(const __grid_constant__ AttnParams p) {
     using S = Shape<D, Q8, kOne>;
     constexpr int NS = S::kStages, NR = S::kRaw > 0 ? S::kRaw : 1;
-    // Slots whose scores a stream takes at a time.  Halves of a key tile have halves of the stream's 128 columns: while one half's
-    // exponentials are worked out, the products of the other (its weights' with V, then K of the next tile) run, and the softmax of either
-    // stream waits for nothing.  A whole tile's scores leave no room for the next ones, and a stream's softmax and products are one chain: 4000 cycles
-    // for a key tile and two row tiles, of which the tensor cores work for 2050.
+    // Slots whose scores a stream takes at a time.  Whole tiles' scores leave no room for the next ones, and a stream's softmax and products are one
+    // chain, two streams by turns: 3450 to 4100 cycles for a key tile and two row tiles, of which the tensor cores work for 1050 (head_dim 64) to 2050.
+    // Halves of a key tile have halves of the stream's 128 columns: while one half's exponentials are worked out, the products of the other
+    // (its weights' with V, then K of the next tile) run.  That is faster where tiles are converted and arrive late: e4m3 slots behind a window 580
+    // us against 600 for 16 trees of up to 513 nodes, 840 against 914 for a prompt of 12000.  It is slower over bf16, where turns do as well and products
+    // of 64 slots cost 48 cycles in place of 32: 521 against 490, 780 against 728.  Without a window scores of e4m3 slots are whole tiles' too, which keeps sums in
+    // the order that they have had.
     constexpr int kSub = kWin && Q8 ? 64 : kTile, kSubs = kTile / kSub;
     static_assert(NS / 2 < kCleared, "tiles that the streams may be apart");
     extern __shared__ uint8_t smem_raw[];
@@ -1164,7 +1172,7 @@ template <int D, bool Q8>
 cudaError_t launch_any(graft_ctx* ctx, const AttnParams& p, cudaStream_t st) {
     const long long rows = (long long)p.rows * p.group;
     if (few_rows(p.group, p.rows, p.shared))
-        return launch_tree<D>(ctx, p, few_attn_kernel<D, Q8, false>, FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kSmem,
+        return launch_tree<D>(ctx, p, few_attn_kernel<D, Q8, false>, FewShape<D, Q8, false>::kThreads, FewShape<D, Q8, false>::kSmem,
                                  256u << ((D == 128) + 2 * Q8), false, st);
     return p.shared == 0 && rows <= kTile ? launch_attn<D, Q8, true>(ctx, p, st) : launch_attn<D, Q8, false>(ctx, p, st);
 }
@@ -1186,7 +1194,7 @@ TilesKernel window_tiles_kernel(int head_dim, bool q8, bool one) {
 }
 
 size_t tree_attn_scratch_bytes(const graft_ctx* ctx, int batch, const graft_cache* cache, int q_heads, int rows, int shared) {
-    const int group = q_heads / cache->kv_heads, ctas = attn_ctas(ctx, cache->dtype == GRAFT_E4M3, cache->head_dim, group, rows, shared);
+    const int group = q_heads / cache->kv_heads, ctas = attn_ctas<false>(ctx, cache->dtype == GRAFT_E4M3, cache->head_dim, group, rows, shared);
     return attn_sizes(ctas, batch, batch, 0, cache->kv_heads, cache->head_dim, group, rows, shared).total;
 }
 
@@ -1199,7 +1207,7 @@ cudaError_t tree_attn_launch(graft_ctx* ctx, int batch, const graft_cache* cache
                                       d_status, !few, cache->page_size < kTile ? cache->page_size : kTile);
     if (e != cudaSuccess) return e;
     p.shared = shared;
-    p.ctas = attn_ctas(ctx, q8, cache->head_dim, p.group, rows, shared);
+    p.ctas = attn_ctas<false>(ctx, q8, cache->head_dim, p.group, rows, shared);
     attn_places(p, attn_sizes(p.ctas, batch, batch, 0, cache->kv_heads, cache->head_dim, p.group, rows, shared), scratch);
     p.most_share = few ? 0 : 128;
     const auto launch = cache->head_dim == 128 ? (q8 ? launch_any<128, true> : launch_any<128, false>)

@@ -4,6 +4,12 @@
 // chain, is an entry of the plan with a line of slots of its own: the sinks, then the slots from the first row's window on up to the last row's
 // own, rounded to whole grains (16 slots for few rows, what a copy brings for others).  Rows see less than that at the line's borders alone: tiles
 // there are masked row by row, and V of places that only some rows see is looked at for what is not a number, as V of new rows is.
+//
+// What bounds it.  One token behind a window of 4096: 12.4 us, latencies (the floor is 2.6); 64 of them over e4m3 slots 114 us, 0.73 of the copy's rate (83).
+// 32 trees of up to 65 nodes, window 1024: 75 us; 16 of up to 513, window 4096, e4m3, head_dim 64: 538; 4 prompts of up to 8192, window 1024: 505 to 530, tensor cores
+// busy for 36 %; a prompt of 12000, window 4001: 670 to 740 by the clock that power leaves.  Beside the chain of scores, exponentials and products that tree_attn.cu
+// describes it is the borders: masked tiles cost 9 to 17 % (three of ten tiles behind a window of 1024), and a unit's beginning and end as long as three tiles.
+// Chains go in blocks of as many rows as make a unit of 256: smaller blocks would mask less and bring K and V more often, at half-empty row tiles.
 #include "attn.cuh"
 
 namespace graft {
@@ -142,15 +148,15 @@ cudaError_t launch_any(graft_ctx* ctx, const AttnParams& p, bool few, cudaStream
     const uint32_t bit = 1u << ((D == 128) + 2 * Q8);
     if (few && p.self_plan) {
         if (!(ctx->window_ready & bit)) {
-            const cudaError_t e = allow_smem((const void*)few_attn_kernel<D, Q8, true>, FewShape<D, Q8>::kSmem);
+            const cudaError_t e = allow_smem((const void*)few_attn_kernel<D, Q8, true>, FewShape<D, Q8, true>::kSmem);
             if (e != cudaSuccess) return e;
             ctx->window_ready |= bit;
         }
         ctx->launches += 1;
-        return launch_pdl(few_attn_kernel<D, Q8, true>, dim3(p.ctas), dim3(FewShape<D, Q8>::kThreads), FewShape<D, Q8>::kSmem, st, p);
+        return launch_pdl(few_attn_kernel<D, Q8, true>, dim3(p.ctas), dim3(FewShape<D, Q8, true>::kThreads), FewShape<D, Q8, true>::kSmem, st, p);
     }
     if (few)
-        return launch_kernels(ctx, p, window_plan_kernel, few_attn_kernel<D, Q8, true>, FewShape<D, Q8>::kThreads, FewShape<D, Q8>::kSmem,
+        return launch_kernels(ctx, p, window_plan_kernel, few_attn_kernel<D, Q8, true>, FewShape<D, Q8, true>::kThreads, FewShape<D, Q8, true>::kSmem,
                               &ctx->window_ready, bit, [] { return cudaSuccess; }, st);
     const bool one = (long long)p.block_rows * p.group <= kTile;
     const TilesKernel k = window_tiles_kernel(D, Q8, one);
@@ -167,7 +173,7 @@ struct WindowShape {
 WindowShape window_shape(const graft_ctx* ctx, int batch, const graft_cache* cache, int q_heads, int rows, bool mask) {
     const int group = q_heads / cache->kv_heads;
     WindowShape w;
-    w.ctas = attn_ctas(ctx, cache->dtype == GRAFT_E4M3, cache->head_dim, group, rows, 0);
+    w.ctas = attn_ctas<true>(ctx, cache->dtype == GRAFT_E4M3, cache->head_dim, group, rows, 0);
     w.block_rows = mask || (long long)rows * group <= kUnitRows ? rows : group < kUnitRows ? kUnitRows / group : 1;
     w.entries = (long long)batch * ((rows + w.block_rows - 1) / w.block_rows);
     w.z = attn_sizes(w.ctas, batch, (int)w.entries, batch, cache->kv_heads, cache->head_dim, group, w.block_rows, 0);

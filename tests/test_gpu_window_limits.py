@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("dtype", [BF, Q8])
-@pytest.mark.parametrize("B", [255, 256, 257, 600])  # with a plan of their own from 257 on, that is not held on the chip from 513 on
+@pytest.mark.parametrize("B", [191, 192, 193, 256, 257, 600])  # with a launch for their plan from 193 on, that is not held on the chip from 513 on
 def test_many_single_tokens(dtype, B):
     lens, counts = [1 + 7 * i % 190 for i in range(B)], [int(i % 11 != 3) for i in range(B)]
     _attend(B, dtype, B, 1, 2, 1, 64, 16, lens, counts, 50, 3, None, calls=2)
