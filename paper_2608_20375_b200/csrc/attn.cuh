@@ -503,13 +503,12 @@ __device__ __forceinline__ void list_unit(JoinList& j, const UnitAt& u, int f, i
 }
 
 // 32 rows of a unit from the pieces on the list: a lane a row, a warp some of the columns.  Pieces are added in their order along the line, results repeat; four are on their way at a time.
-template <int D>
+template <int D, int kAhead>
 __device__ __forceinline__ void join_rows(const AttnParams& p, const JoinList& j, bool live, size_t out_row) {
     constexpr int kWarps = kJoinThreads / 32, kQuads = D / 4 / kWarps;  // groups of four columns a warp
     const int lane = lane_id(), warp = threadIdx.x >> 5, n = j.n;
     float m = -INFINITY, l = 0.0f;
     float o[4 * kQuads] = {};
-    constexpr int kAhead = 4;
     for (int i0 = 0; i0 < n; i0 += kAhead) {
         float2 ml[kAhead];
         float4 v[kAhead][kQuads];
@@ -1132,7 +1131,7 @@ __global__ void __launch_bounds__(FewShape<D, Q8, kWin>::kThreads, FewShape<D, Q
                 if (kWin)
                     join_few<D, kWarps>(p, list, R, (size_t)b * p.rows * p.q_heads + h * p.group);
                 else if (tid < kJoinThreads)
-                    join_rows<D>(p, list, lane < R, ((size_t)b * p.rows + node) * p.q_heads + h * p.group + (lane - node * p.group));
+                    join_rows<D, 4>(p, list, lane < R, ((size_t)b * p.rows + node) * p.q_heads + h * p.group + (lane - node * p.group));
             }
             __syncthreads();
         }
@@ -1141,7 +1140,7 @@ __global__ void __launch_bounds__(FewShape<D, Q8, kWin>::kThreads, FewShape<D, Q
 
 // Units that were cut, without a shared prefix: blocks for every boundary between CTAs; the first boundary inside a unit joins it.
 template <int D>
-__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_constant__ AttnParams p) {
+__global__ void __launch_bounds__(kJoinThreads, 4) attn_join_kernel(const __grid_constant__ AttnParams p) {
     pdl_launch_dependents();
     pdl_wait();
     __shared__ JoinList j;
@@ -1159,7 +1158,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_co
     __syncthreads();
     const int r = q.r0 + r0 + lane_id(), node = r / p.group;
     const bool live = r0 + lane_id() < q.rows;
-    join_rows<D>(p, j, live, ((size_t)(q.s - 1) * p.rows + q.node0 + node) * p.q_heads + q.h * p.group + (r - node * p.group));
+    join_rows<D, 2>(p, j, live, ((size_t)(q.s - 1) * p.rows + q.node0 + node) * p.q_heads + q.h * p.group + (r - node * p.group));
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,

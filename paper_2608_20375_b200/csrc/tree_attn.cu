@@ -1121,7 +1121,7 @@ __global__ void __launch_bounds__(kPlanThreads) attn_plan_kernel(const __grid_co
 
 // Behind a shared prefix every row has pieces of two units; 32 rows of a sequence may lie in two units of the prefix.
 template <int D>
-__global__ void __launch_bounds__(kJoinThreads) attn_join_shared_kernel(const __grid_constant__ AttnParams p) {
+__global__ void __launch_bounds__(kJoinThreads, 4) attn_join_shared_kernel(const __grid_constant__ AttnParams p) {
     pdl_launch_dependents();
     pdl_wait();
     __shared__ JoinList j;
@@ -1149,7 +1149,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_shared_kernel(const __
     }
     __syncthreads();
     const int r = r0 + lane_id(), node = r / p.group;
-    join_rows<D>(p, j, r < R, ((size_t)b * p.rows + node) * p.q_heads + h * p.group + (r - node * p.group));
+    join_rows<D, 2>(p, j, r < R, ((size_t)b * p.rows + node) * p.q_heads + h * p.group + (r - node * p.group));
 }
 
 template <int D, typename Kernel>
