@@ -502,7 +502,8 @@ __device__ __forceinline__ void list_unit(JoinList& j, const UnitAt& u, int f, i
     }
 }
 
-// 32 rows of a unit from the pieces on the list: a lane a row, a warp some of the columns.  Pieces are added in their order along the line, results repeat; four are on their way at a time.
+// 32 rows of a unit from the pieces on the list: a lane a row, a warp some of the columns.  Pieces are added in their order along the line, results
+// repeat; kAhead are on their way at a time (kernels that join have two, as most units were cut once, and four blocks an SM: trees behind a window 75.5 -> 73.1 us).
 template <int D, int kAhead>
 __device__ __forceinline__ void join_rows(const AttnParams& p, const JoinList& j, bool live, size_t out_row) {
     constexpr int kWarps = kJoinThreads / 32, kQuads = D / 4 / kWarps;  // groups of four columns a warp

@@ -21,7 +21,7 @@
 // What bounds it.  Large trees (16 of up to 513 nodes behind 6000 to 8192 slots, bf16, 717 GFLOP): 805 to 850 us, the tensor cores busy for 52 % of
 // the time, the exponentials' unit for 39 %: a stream's next product waits for all of a tile's weights, and two streams (TMEM holds
 // no more) do not fill the gaps; the clock falls to 1.3 GHz under that load in a long run (960 to 1040 us).  A tile of e4m3 slots is converted
-// once a unit, 0.5 to 0.6 us: 32 trees of up to 65 nodes behind 500 to 4096 slots 131 us.  17 nodes (68 rows)
+// once a unit, 0.5 to 0.6 us: 32 trees of up to 65 nodes behind 500 to 4096 slots 127 us.  17 nodes (68 rows)
 // behind 4000 slots, bf16: 213 us, 0.78 of the copy's rate.  Small calls are latencies: one tree of 65 nodes behind 1500 slots 29.5 us, of
 // which the plan takes 4, the kernel 10 to 15 and the join 8.
 //
