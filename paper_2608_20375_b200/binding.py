@@ -79,6 +79,7 @@ class _Rope(C.Structure):
 
 
 _lib = None
+_fast = None  # _marshal: the same checks and calls for calls of a few microseconds (without it they are made in Python)
 
 
 def library_path() -> str:
@@ -87,7 +88,7 @@ def library_path() -> str:
 
 def load_library():
     """Load libgraft.so (building it with nvcc first if it is missing or stale).  Raises if that fails."""
-    global _lib
+    global _lib, _fast
     if _lib is not None:
         return _lib
     path = _build.LIB
@@ -137,6 +138,12 @@ def load_library():
     lib.graft_status_str.argtypes = [C.c_int]
     lib.graft_status_str.restype = C.c_char_p
     lib.graft_version.restype = C.c_char_p
+    try:
+        from . import _marshal
+        _marshal.bind(C.cast(lib.graft_cache_append, vp).value, C.cast(lib.graft_window_attention, vp).value)
+        _fast = _marshal
+    except ImportError:  # (another torch than the one that it was built with)
+        _fast = None
     _lib = lib
     return lib
 
@@ -525,7 +532,13 @@ class Graft:
         """q [batch, rows, q_heads, head_dim] turned by its positions into q_out (None: in place), key turned likewise and value into
         the layer's slots as cache_write does it, in one launch.  position: [batch, rows or more] int32 (the trees' position), [batch, rows or
         more, axes], or None (a row's slot).  q None: keys and values only."""
-        batch, i32, dev = key.shape[0], torch.int32, _device()
+        dev = _device()
+        if _fast is not None and dev >= 0:
+            rc = _fast.cache_append(self._ctx.value, dev, _stream(), layer, cache.k, cache.v, cache.k_exp, cache.v_exp, table, prefix_len, count,
+                                    rope.freq, rope.interleaved, rope.gain, rope.shift, q, key, value, q_out, position, status)
+            if rc is not None:
+                return _check(self.lib, rc, "graft_cache_append")
+        batch, i32 = key.shape[0], torch.int32
         cc = cache._c(table, batch, dev)
         kp, rows, stride = _token_rows("key", key, cc.kv_heads, cc.head_dim, dev)
         vp, v_rows, v_stride = _token_rows("value", value, cc.kv_heads, cc.head_dim, dev)
@@ -555,7 +568,13 @@ class Graft:
                          status=None):
         """tree_attention of rows that see the last `window` positions and the first `sinks`.  mask and position [batch, nmax] (the trees'): both or
         neither (a chain).  Pages that hold nothing that is seen need not be there: their entries in the table are not looked at."""
-        batch, i32, dev = q.shape[0], torch.int32, _device()
+        dev = _device()
+        if _fast is not None and dev >= 0:
+            rc = _fast.window_attention(self._ctx.value, dev, _stream(), self.nmax, self.mask_words, layer, cache.k, cache.v, cache.k_exp, cache.v_exp,
+                                        table, q, prefix_len, count, mask, position, window, sinks, out, lse, scale, status)
+            if rc is not None:
+                return _check(self.lib, rc, "graft_window_attention")
+        batch, i32 = q.shape[0], torch.int32
         cc = cache._c(table, batch, dev)
         if q.dim() != 4:
             raise GraftError(f"q must be [batch, rows, heads, {cc.head_dim}], got {tuple(q.shape)}")

@@ -1,18 +1,20 @@
 """Build libgraft.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a.
 
 Every source becomes an object under _build/ (rebuilt when it or one of its headers is newer) and the objects are
-linked into libgraft.so.
+linked into libgraft.so.  _marshal.so, the binding's checks of tensors for calls of a few microseconds, is host code against torch's headers.
 """
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgraft.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 GRAFT_H = os.path.join("..", "..", "include", "graft.h")
 ALL_HEADERS = ["common.cuh", "internal.h", "edge_score.cuh", "cosine.cuh", "saba.cuh", GRAFT_H]
 # source -> headers it depends on
@@ -50,7 +52,20 @@ def needs_build() -> bool:
     for src, hdrs in SOURCES.items():
         if _stale(_obj(src), [os.path.join(CSRC, src)] + [os.path.join(CSRC, h) for h in hdrs]):
             return True
-    return _stale(LIB, [_obj(s) for s in SOURCES])
+    return _stale(LIB, [_obj(s) for s in SOURCES]) or _stale(MARSHAL, _marshal_deps())
+
+
+def _marshal_deps() -> list[str]:
+    return [os.path.join(CSRC, "marshal.cpp"), os.path.join(CSRC, GRAFT_H)]
+
+
+def _marshal_command() -> list[str]:
+    import torch
+    at = os.path.dirname(torch.__file__)
+    inc = [os.path.join(at, "include"), os.path.join(at, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"]]
+    return (["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] +
+            [f"-I{i}" for i in inc] + [os.path.join(CSRC, "marshal.cpp"), "-o", MARSHAL, "-L" + os.path.join(at, "lib"), "-ltorch_python",
+                                       "-ltorch_cpu", "-lc10"])
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -64,6 +79,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
             continue
         cmds.append([nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + inc +
                     ["-c", os.path.join(CSRC, src), "-o", _obj(src)])
+    if force or _stale(MARSHAL, _marshal_deps()):
+        cmds.append(_marshal_command())
     procs = [subprocess.Popen(c) for c in cmds]  # the sources compile side by side
     failed = [c for c, pr in zip(cmds, procs) if pr.wait() != 0]
     if failed:
