@@ -79,7 +79,7 @@ class _Rope(C.Structure):
 
 
 _lib = None
-_fast = None  # _marshal: the same checks and calls for calls of a few microseconds (without it they are made in Python)
+_fast = None  # _marshal: the same checks and calls for calls of a few microseconds on the GPU (without it they are made in Python)
 
 
 def library_path() -> str:
@@ -140,7 +140,7 @@ def load_library():
     lib.graft_version.restype = C.c_char_p
     try:
         from . import _marshal
-        _marshal.bind(C.cast(lib.graft_cache_append, vp).value, C.cast(lib.graft_window_attention, vp).value)
+        _marshal.bind(*(C.cast(f, vp).value for f in (lib.graft_cache_write, lib.graft_cache_read, lib.graft_cache_append, lib.graft_window_attention)))
         _fast = _marshal
     except ImportError:  # (another torch than the one that it was built with)
         _fast = None
@@ -495,7 +495,13 @@ class Graft:
     # ---- verification of the trees
     def cache_write(self, cache: KVCache, layer, table, prefix_len, count, key, value, status=None):
         """Row i < count[b] of key and value [batch, rows, kv_heads, head_dim] into slot prefix_len[b] - 1 + i of the layer."""
-        batch, i32, dev = key.shape[0], torch.int32, _device()
+        dev = _device()
+        if _fast is not None and dev >= 0:
+            rc = _fast.cache_write(self._ctx.value, dev, _stream(), layer, cache.k, cache.v, cache.k_exp, cache.v_exp, table, prefix_len, count, key,
+                                  value, status)
+            if rc is not None:
+                return _check(self.lib, rc, "graft_cache_write")
+        batch, i32 = key.shape[0], torch.int32
         cc = cache._c(table, batch, dev)
         kp, rows, stride = _token_rows("key", key, cc.kv_heads, cc.head_dim, dev)
         vp, v_rows, v_stride = _token_rows("value", value, cc.kv_heads, cc.head_dim, dev)
@@ -508,7 +514,13 @@ class Graft:
 
     def cache_read(self, cache: KVCache, layer, table, prefix_len, count, key, value, status=None):
         """The entries of the same slots back into dense key and value; rows behind the count are left as they were."""
-        batch, i32, dev = key.shape[0], torch.int32, _device()
+        dev = _device()
+        if _fast is not None and dev >= 0:
+            rc = _fast.cache_read(self._ctx.value, dev, _stream(), layer, cache.k, cache.v, cache.k_exp, cache.v_exp, table, prefix_len, count, key,
+                                  value, status)
+            if rc is not None:
+                return _check(self.lib, rc, "graft_cache_read")
+        batch, i32 = key.shape[0], torch.int32
         cc = cache._c(table, batch, dev)
         if key.dim() != 4:
             raise GraftError(f"key must be [batch, rows, {cc.kv_heads}, {cc.head_dim}], got {tuple(key.shape)}")

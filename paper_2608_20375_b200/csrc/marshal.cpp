@@ -10,6 +10,8 @@
 
 namespace {
 
+decltype(&graft_cache_write) call_write = nullptr;
+decltype(&graft_cache_read) call_read = nullptr;
 decltype(&graft_cache_append) call_append = nullptr;
 decltype(&graft_window_attention) call_window = nullptr;
 
@@ -78,13 +80,46 @@ PyObject* status(Call call) {
     return PyLong_FromLong((long)s);
 }
 
-// bind(address of graft_cache_append, of graft_window_attention)
+// bind(addresses of graft_cache_write, graft_cache_read, graft_cache_append, graft_window_attention)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 2) return none();
-    call_append = (decltype(call_append))PyLong_AsVoidPtr(a[0]);
-    call_window = (decltype(call_window))PyLong_AsVoidPtr(a[1]);
+    if (n != 4) return none();
+    call_write = (decltype(call_write))PyLong_AsVoidPtr(a[0]);
+    call_read = (decltype(call_read))PyLong_AsVoidPtr(a[1]);
+    call_append = (decltype(call_append))PyLong_AsVoidPtr(a[2]);
+    call_window = (decltype(call_window))PyLong_AsVoidPtr(a[3]);
     return PyErr_Occurred() ? nullptr : none();
 }
+
+// (context, device, stream, layer, k, v, k_exp, v_exp, table, prefix_len, count, key, value, status), written or read
+PyObject* cache_rows(bool write, PyObject* const* a, Py_ssize_t n) try {
+    if (n != 14 || !call_write || !call_read || !PyLong_Check(a[0]) || !PyLong_Check(a[2])) return none();
+    Checks x{0};
+    x.dev = x.number(a[1], INT32_MIN, INT32_MAX);
+    const int32_t layer = (int32_t)x.number(a[3], INT32_MIN, INT32_MAX);
+    const at::Tensor *key = tensor(a[11]), *value = tensor(a[12]);
+    if (!x.ok || !key || !value || key->dim() != 4 || value->sizes() != key->sizes()) return none();
+    const int64_t batch = key->size(0), rows = key->size(1);
+    if (batch > INT32_MAX || rows > INT32_MAX) return none();
+    const graft_cache c = x.cache(a + 4, batch);
+    int64_t k_stride = 0, v_stride = 0;
+    void* const kp = (void*)x.rows(key, c.kv_heads, c.head_dim, k_stride);
+    void* const vp = (void*)x.rows(value, c.kv_heads, c.head_dim, v_stride);
+    const int32_t* const prefix = x.dense<const int32_t>(a[9], at::kInt, {batch});
+    const int32_t* const count = x.dense<const int32_t>(a[10], at::kInt, {batch});
+    int32_t* const st = x.dense<int32_t>(a[13], at::kInt, {batch}, true);
+    if (!x.ok || k_stride != v_stride || (!write && !(key->is_contiguous() && value->is_contiguous()))) return none();
+    graft_ctx* const ctx = (graft_ctx*)PyLong_AsVoidPtr(a[0]);
+    void* const stream = PyLong_AsVoidPtr(a[2]);
+    if (PyErr_Occurred()) return nullptr;
+    return status([&] {
+        return write ? call_write(ctx, (int32_t)batch, &c, layer, prefix, count, (int32_t)rows, k_stride, kp, vp, st, stream)
+                     : call_read(ctx, (int32_t)batch, &c, layer, prefix, count, (int32_t)rows, kp, vp, st, stream);
+    });
+} catch (...) {
+    return none();
+}
+PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t n) { return cache_rows(true, a, n); }
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) { return cache_rows(false, a, n); }
 
 // (context, device, stream, layer, k, v, k_exp, v_exp, table, prefix_len, count, freq, interleaved, gain, shift, q, key, value, q_out, position, status)
 PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) try {
@@ -180,6 +215,8 @@ PyObject* window_attention(PyObject*, PyObject* const* a, Py_ssize_t n) try {
 }
 
 PyMethodDef methods[] = {{"bind", (PyCFunction)(void*)bind, METH_FASTCALL, nullptr},
+                         {"cache_write", (PyCFunction)(void*)cache_write, METH_FASTCALL, nullptr},
+                         {"cache_read", (PyCFunction)(void*)cache_read, METH_FASTCALL, nullptr},
                          {"cache_append", (PyCFunction)(void*)cache_append, METH_FASTCALL, nullptr},
                          {"window_attention", (PyCFunction)(void*)window_attention, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

@@ -1,4 +1,4 @@
-"""The compiled checks of cache_append and window_attention against the methods' own: the same results, the same refusals."""
+"""The compiled checks of the cache's calls and window_attention against the methods' own: the same results, the same refusals."""
 import pytest
 import torch
 
@@ -24,6 +24,7 @@ def _inputs(dtype):
 
 
 APPEND = "cache layer table prefix_len count rope q key value q_out position status".split()
+ROWS = "cache layer table prefix_len count key value status".split()
 ATTEND = "cache layer table q prefix_len count mask position window sinks out lse scale status".split()
 
 
@@ -40,6 +41,9 @@ def test_results_are_the_same(dtype, monkeypatch):
         a["cache"].k.zero_(), a["cache"].v.zero_()
         g.cache_append(*(a[x] for x in APPEND))
         a["status"].fill_(7)
+        g.cache_write(*((a | dict(prefix_len=_i32([60, 70])))[x] for x in ROWS))
+        back = torch.zeros((2, 9, 2, 64), dtype=BF, device="cuda")
+        g.cache_read(*((a | dict(key=back, value=torch.zeros_like(back), prefix_len=_i32([59, 70]), status=None))[x] for x in ROWS))
         g.window_attention(**{x: a["q_out"] if x == "q" else a[x] for x in ATTEND})
         for change in (dict(q=None, q_out=None), dict(position=None), dict(position=a["position"][:, :9, None].contiguous()), dict(q_out=None)):
             g.cache_append(*((a | change | dict(layer=0))[x] for x in APPEND))
@@ -47,7 +51,7 @@ def test_results_are_the_same(dtype, monkeypatch):
         for change in (dict(mask=None, position=None), dict(scale=0.3, lse=None), dict(status=None), dict(window=2 ** 40)):
             g.window_attention(**{x: (a | change)[x] for x in ATTEND})
             first = first + a["out"]
-        got.append([a["cache"].k, a["cache"].v, a["q_out"], first, a["lse"], a["status"], a["q"]])
+        got.append([a["cache"].k, a["cache"].v, a["q_out"], first, a["lse"], a["status"], a["q"], back])
     for x, y in zip(*got):
         assert torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8))
 
@@ -70,7 +74,12 @@ def test_refusals_are_the_same(monkeypatch):
               dict(rope=Rope(a["rope"].freq[0])), dict(rope=Rope(a["rope"].freq, gain=float("nan")))]
     attend = [dict(mask=None), dict(position=None), dict(window=0), dict(sinks=-1), dict(out=wide), dict(lse=a["lse"].double()), dict(mask=a["mask"][:, :3]),
               dict(scale=float("inf")), dict(scale=float("nan"))]
-    for call, names, changes in ((g.cache_append, APPEND, wrong + append), (g.window_attention, ATTEND, wrong + attend)):
+    rows = [dict(key=a["key"][:, :3]), dict(key=cpu), dict(value=wide), dict(key=a["key"].float()), dict(value=a["value"][0]), dict(value=a["value"][:1])]
+    shared = [c for c in wrong if not {"q", "position"} & set(c)]
+    dense = dict(key=a["key"].contiguous(), value=a["value"].contiguous())
+    for call, names, changes in ((g.cache_append, APPEND, wrong + append), (g.window_attention, ATTEND, wrong + attend),
+                                 (g.cache_write, ROWS, shared + rows + [dict(value=dense["value"])]),
+                                 (g.cache_read, ROWS, [dense | c for c in shared + rows] + [dict(key=a["key"])])):
         for change in changes:
             said = []
             for way in (fast, None):
