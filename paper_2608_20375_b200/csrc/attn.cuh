@@ -2,6 +2,7 @@
 // kernels and the line of key tiles that they share out are described in tree_attn.cu.
 #pragma once
 #include <cuda.h>
+#include <cuda_fp16.h>
 #include <float.h>
 #include <string.h>
 
@@ -14,6 +15,13 @@ constexpr int kTile = 128;      // slots of a key tile, rows of a row tile
 constexpr int kUnitRows = 256;
 constexpr uint32_t kWaitNs = 500;  // that a poll may sleep
 constexpr float kMostGrowth = 8.0f;  // (powers of two) of a row's maximum, before O is rescaled
+
+struct Yes {
+    static constexpr bool value = true;
+};
+struct No {
+    static constexpr bool value = false;
+};
 
 // What the plan says of a sequence (entry 0: the shared prefix with the rows of all of them; entry b + 1: sequence b).  Behind a window (kWin)
 // entries are blocks of a sequence's rows, entry 0 is empty, and slots are counted along what the block's rows see: see "windows".
@@ -555,7 +563,7 @@ __device__ __forceinline__ void join_rows(const AttnParams& p, const JoinList& j
 // the long directions and the rows in the short one; e4m3 entries become f16 (K) and bf16 (V) in registers, their slots' powers of two go to scores
 // and weights.  The order of head_dim inside a product is free, so a lane loads pieces of 16 bytes straight into what it multiplies: of K, a quarter of those of two slots; of V, an eighth of four.  The next
 // step's K is asked for when this one's scores are done, and V when its products are: the warps of an SM then have 50 to 60 KB under way.
-// 64 sequences of 2000 to 16000 slots, 8 key heads of 128: bf16 354 us (6.6 TB/s; through the tiles of 128 rows 417), e4m3 224 us (5.3
+// 64 sequences of 2000 to 16000 slots, 8 key heads of 128: bf16 354 us (6.6 TB/s; through the tiles of 128 rows 417), e4m3 226 us (5.3
 // TB/s; 553), which instructions bound, three warps a scheduler to hide their latencies.  With K and V turned into bf16 and multiplied by their slots'
 // powers: 500 instructions for 16 slots, 275 us.  Before pieces' own cost was counted (371 and 288): through a ring of cp.async in shared memory 543 and 295;
 // with 8 warps of two steps 297, with 16 warps 294 (registers spill).  Behind a window of 4096, 64 sequences: e4m3 114 us.
@@ -845,10 +853,11 @@ __global__ void __launch_bounds__(FewShape<D, Q8, kWin>::kThreads, FewShape<D, Q
                 qf[4 * i] = u.x, qf[4 * i + 1] = u.y, qf[4 * i + 2] = u.z, qf[4 * i + 3] = u.w;
             }
         }
-        // Over e4m3 slots: f16 holds e4m3 numbers, and a row of Q when its largest number is brought to 2^14 by a power of two (what f16 then rounds is
-        // 2^-39 of that); scores take the powers of both back.
+        // Over e4m3 slots: f16 holds e4m3 numbers, and a row of Q when its largest number is brought to 2^14 by a power of two, unless others are
+        // 2^31 times smaller; scores take the powers of both back.  With a row that f16 does not hold bit for bit, Q stays as it is and K becomes bf16
+        // (rare; 64 tokens behind a window of 4096 114 us, with such rows 122).
         float q_down[2] = {1.0f, 1.0f};  // of rows 2 q4, 2 q4 + 1
-        bool q_far = false;
+        bool q_far = false, q_wide = false;
         if (Q8) {
             uint32_t most2 = 0;
 #pragma unroll
@@ -857,211 +866,237 @@ __global__ void __launch_bounds__(FewShape<D, Q8, kWin>::kThreads, FewShape<D, Q
             top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
             top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
             const int up = top == 0 ? 0 : min(127 + 14 - (int)(top >> 7), 126);  // (from -114 on)
-            const float f = power_of_two(up);
+            const float f = power_of_two(up), down = power_of_two(-up);
+            uint32_t qh[D / 8];
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i)
-                asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(qf[i]) : "f"(__uint_as_float(qf[i] & 0xFFFF0000u) * f), "f"(__uint_as_float(qf[i] << 16) * f));
-            q_far = __any_sync(0xFFFFFFFFu, up > 60 || up < -60);
+            for (int i = 0; i < D / 8; ++i) {
+                const float lo = __uint_as_float(qf[i] << 16), hi = __uint_as_float(qf[i] & 0xFFFF0000u);
+                asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(qh[i]) : "f"(hi * f), "f"(lo * f));
+                const float2 back = __half22float2(*(const __half2*)&qh[i]);
+                const float2 again = make_float2(back.x * down, back.y * down);
+                q_wide = q_wide || again.x < lo || again.x > lo || again.y < hi || again.y > hi;  // (what is not a number is none in f16 either)
+            }
+            q_wide = __any_sync(0xFFFFFFFFu, q_wide);
+            if (!q_wide) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) q_down[i] = power_of_two(-__shfl_sync(0xFFFFFFFFu, up, (2 * q4 + i) * 4));
+                for (int i = 0; i < D / 8; ++i) qf[i] = qh[i];
+                q_far = __any_sync(0xFFFFFFFFu, up > 60 || up < -60);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) q_down[i] = power_of_two(-__shfl_sync(0xFFFFFFFFu, up, (2 * q4 + i) * 4));
+            }
         }
         float o[D / 16][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, upto[2] = {-INFINITY, -INFINITY}, off[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
-        for (int step = 0; step < steps; ++step) {
-            const int s0 = slot_of(step);
-            const bool more_steps = step + 1 < steps;
-            const size_t row1 = row_at(step + 1, page);
-            page = page_of(step + 2);
-            // powers of two of K's slots g, g + 8
-            uint32_t ke[2] = {0, 0};
-            if (Q8)
+        // (its steps with K as bf16 are code of their own: a branch inside of them costs 2 %)
+        const auto steps_of_piece = [&](auto wide) {
+            constexpr bool kF16 = Q8 && !decltype(wide)::value;
+            for (int step = 0; step < steps; ++step) {
+                const int s0 = slot_of(step);
+                const bool more_steps = step + 1 < steps;
+                const size_t row1 = row_at(step + 1, page);
+                page = page_of(step + 2);
+                // powers of two of K's slots g, g + 8
+                uint32_t ke[2] = {0, 0};
+                if (Q8)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) ke[i] = __byte_perm(i ? k_exps.z : k_exps.x, i ? k_exps.w : k_exps.y, g) & 255;
-            // ---- scores: rows 2 q4, 2 q4 + 1 at slots g, g + 8
-            float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s2[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    for (int i = 0; i < 2; ++i) ke[i] = __byte_perm(i ? k_exps.z : k_exps.x, i ? k_exps.w : k_exps.y, g) & 255;
+                // ---- scores: rows 2 q4, 2 q4 + 1 at slots g, g + 8
+                float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s2[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                uint32_t f[2] = {0, 0}, more[2] = {kOneBf16x2, kOneBf16x2};
+                if (Q8 && !kF16)
 #pragma unroll
-            for (int y = 0; y < kK; ++y) {
-                uint2 a[4 / kBytes][2];
+                    for (int i = 0; i < 2; ++i) e4m3_factors(ke[i], f[i], more[i]);
 #pragma unroll
-                for (int x = 0; x < 4 / kBytes; ++x)  // four numbers of the lane's a product
+                for (int y = 0; y < kK; ++y) {
+                    uint2 a[4 / kBytes][2];
+#pragma unroll
+                    for (int x = 0; x < 4 / kBytes; ++x)  // four numbers of the lane's a product
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t w[4] = {kr[i][y].x, kr[i][y].y, kr[i][y].z, kr[i][y].w};
+                            a[x][i] = kF16 ? e4m3x4_to_f16(w[x]) : Q8 ? e4m3x4_to_bf16(w[x], f[i], kOneBf16x2) : make_uint2(w[2 * x & 3], w[(2 * x + 1) & 3]);
+                        }
+#pragma unroll
+                    for (int x = 0; x < 4 / kBytes; ++x) {
+                        const int ks = y * (4 / kBytes) + x;
+                        const auto mma = kF16 ? mma_16816_f16 : mma_16816;
+                        mma(x & 1 ? s2 : s, a[x][0].x, a[x][1].x, a[x][0].y, a[x][1].y, qf[2 * ks], qf[2 * ks + 1]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[i] += s2[i];
+                    if (Q8 && !kF16) s[i] *= __uint_as_float(more[i >> 1] << 16);  // (what is above bf16's largest power)
+                }
+                if (kF16) {
+                    if (q_far || __any_sync(0xFFFFFFFFu, max(ke[0] - 67, ke[1] - 67) > 120)) {  // (rare: in two steps, and what is not a number)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int e = (int)ke[i >> 1] - 127, d = (__float_as_int(q_down[i & 1]) >> 23) - 127, e1 = e >> 1, d1 = d >> 1;
+                            s[i] = ke[i >> 1] == 255 ? __int_as_float(0x7FFFFFFF) : s[i] * power_of_two(e1 + d1) * power_of_two(e - e1 + d - d1);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[i] *= q_down[i & 1] * __uint_as_float(ke[i >> 1] << 23);
+                    }
+                }
+                if (more_steps) bring_k(row1);
+                // What e4m3_pair_small makes of V lacks a power of two a slot, 2^(e + 120).  It goes to the slot's weights, where it changes no rounding, as long
+                // as those stay below 2^128; else (rare, and not numbers) to V, with what is above bf16's largest power going to the weights.
+                uint32_t f2[2] = {0, 0}, x[2] = {0, 0};  // (x: the exponents of two slots)
+                float big[2] = {1.0f, 1.0f};
+                bool large_v = false;
+                if (Q8) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const uint32_t w[4] = {kr[i][y].x, kr[i][y].y, kr[i][y].z, kr[i][y].w};
-                        a[x][i] = Q8 ? e4m3x4_to_f16(w[x]) : make_uint2(w[2 * x & 3], w[(2 * x + 1) & 3]);
+                        x[i] = __byte_perm(i ? v_exps.z : v_exps.x, i ? v_exps.w : v_exps.y, 2 * q4 | (2 * q4 + 1) << 8) & 0x00FF00FFu;
+                        big[i] = __uint_as_float(((__byte_perm(i ? v_exps.z : v_exps.x, i ? v_exps.w : v_exps.y, g) & 255) + 120) << 23);
                     }
+                    large_v = __any_sync(0xFFFFFFFFu, ((x[0] + 0x00810081u) | (x[1] + 0x00810081u)) & 0x01000100u);  // (one above 126: weights are up to 2^8)
+                    if (large_v)
 #pragma unroll
-                for (int x = 0; x < 4 / kBytes; ++x) {
-                    const int ks = y * (4 / kBytes) + x;
-                    const auto mma = Q8 ? mma_16816_f16 : mma_16816;
-                    mma(x & 1 ? s2 : s, a[x][0].x, a[x][1].x, a[x][0].y, a[x][1].y, qf[2 * ks], qf[2 * ks + 1]);
+                        for (int i = 0; i < 2; ++i) {
+                            uint32_t fa, fb, y;
+                            e4m3_factors(x[i] & 255, fa, y), e4m3_factors(x[i] >> 16, fb, y);
+                            f2[i] = __byte_perm(fa, fb, 0x5410);
+                            const uint32_t pair = __shfl_sync(0xFFFFFFFFu, x[i], g >> 1);
+                            e4m3_factors(g & 1 ? pair >> 16 : pair & 255, fa, y);
+                            big[i] = __uint_as_float(y << 16);
+                        }
                 }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] += s2[i];
-            if (Q8) {
-                if (q_far || __any_sync(0xFFFFFFFFu, max(ke[0] - 67, ke[1] - 67) > 120)) {  // (rare: in two steps, and what is not a number)
+                const bool masked = s0 + 16 > base || (kWin && s0 < border1 && s0 + 16 > p.sinks);
+                bool spoilt[4] = {false, false, false, false};
+                uint32_t sees = 0;  // bit i: score i is of a slot that its row sees
+                if (masked) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int e = (int)ke[i >> 1] - 127, d = (__float_as_int(q_down[i & 1]) >> 23) - 127, e1 = e >> 1, d1 = d >> 1;
-                        s[i] = ke[i >> 1] == 255 ? __int_as_float(0x7FFFFFFF) : s[i] * power_of_two(e1 + d1) * power_of_two(e - e1 + d - d1);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[i] *= q_down[i & 1] * __uint_as_float(ke[i >> 1] << 23);
-                }
-            }
-            if (more_steps) bring_k(row1);
-            // What e4m3_pair_small makes of V lacks a power of two a slot, 2^(e + 120).  It goes to the slot's weights, where it changes no rounding, as long
-            // as those stay below 2^128; else (rare, and not numbers) to V, with what is above bf16's largest power going to the weights.
-            uint32_t f2[2] = {0, 0}, x[2] = {0, 0};  // (x: the exponents of two slots)
-            float big[2] = {1.0f, 1.0f};
-            bool large_v = false;
-            if (Q8) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    x[i] = __byte_perm(i ? v_exps.z : v_exps.x, i ? v_exps.w : v_exps.y, 2 * q4 | (2 * q4 + 1) << 8) & 0x00FF00FFu;
-                    big[i] = __uint_as_float(((__byte_perm(i ? v_exps.z : v_exps.x, i ? v_exps.w : v_exps.y, g) & 255) + 120) << 23);
-                }
-                large_v = __any_sync(0xFFFFFFFFu, ((x[0] + 0x00810081u) | (x[1] + 0x00810081u)) & 0x01000100u);  // (one above 126: weights are up to 2^8)
-                if (large_v)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint32_t fa, fb, y;
-                        e4m3_factors(x[i] & 255, fa, y), e4m3_factors(x[i] >> 16, fb, y);
-                        f2[i] = __byte_perm(fa, fb, 0x5410);
-                        const uint32_t pair = __shfl_sync(0xFFFFFFFFu, x[i], g >> 1);
-                        e4m3_factors(g & 1 ? pair >> 16 : pair & 255, fa, y);
-                        big[i] = __uint_as_float(y << 16);
-                    }
-            }
-            const bool masked = s0 + 16 > base || (kWin && s0 < border1 && s0 + 16 > p.sinks);
-            bool spoilt[4] = {false, false, false, false};
-            uint32_t sees = 0;  // bit i: score i is of a slot that its row sees
-            if (masked) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int slot = s0 + g + 8 * (i >> 1), r = 2 * q4 + (i & 1), j = slot - base, node = r / p.group;
-                    bool seen = slot < end && r < R;
-                    if (kWin) {
-                        if (seen) {
-                            const int32_t* position = p.mask != nullptr ? p.position + (size_t)b * p.nmax : nullptr;
-                            const int step = window_step(position, node, base + gap);
-                            if (j < 0 || p.mask == nullptr)
-                                seen = j <= node && (slot < p.sinks || slot >= lo + step);
-                            else {
-                                seen = j < 32 * p.words && ((p.mask[((size_t)b * p.nmax + node) * p.words + (j >> 5)] >> (j & 31)) & 1);
-                                if (seen && step >= p.window) {
-                                    const int at = window_step(position, j, base + gap);
-                                    seen = step - at < p.window || at + base + gap < p.sinks;
+                        const int slot = s0 + g + 8 * (i >> 1), r = 2 * q4 + (i & 1), j = slot - base, node = r / p.group;
+                        bool seen = slot < end && r < R;
+                        if (kWin) {
+                            if (seen) {
+                                const int32_t* position = p.mask != nullptr ? p.position + (size_t)b * p.nmax : nullptr;
+                                const int step = window_step(position, node, base + gap);
+                                if (j < 0 || p.mask == nullptr)
+                                    seen = j <= node && (slot < p.sinks || slot >= lo + step);
+                                else {
+                                    seen = j < 32 * p.words && ((p.mask[((size_t)b * p.nmax + node) * p.words + (j >> 5)] >> (j & 31)) & 1);
+                                    if (seen && step >= p.window) {
+                                        const int at = window_step(position, j, base + gap);
+                                        seen = step - at < p.window || at + base + gap < p.sinks;
+                                    }
                                 }
                             }
+                        } else if (seen && j >= 0)
+                            seen = p.mask == nullptr ? j <= node
+                                                     : j < 32 * p.words && ((p.mask[((size_t)b * p.nmax + node) * p.words + (j >> 5)] >> (j & 31)) & 1);
+                        s[i] = seen ? s[i] : -INFINITY;
+                        sees |= (seen ? 1u : 0u) << i;
+                    }
+                    // V of slots that are not there is taken out, and of new slots that are not numbers: what of those is seen is added in the end
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int slot = s0 + 2 * q4 + (i & 1) + 8 * (i >> 1);
+                        bool bad = Q8 && (x[i >> 1] >> (16 * (i & 1)) & 255) > 246;  // (up to 480 2^119 is below 2^128)
+                        if (!Q8)
+#pragma unroll
+                            for (int x = 0; x < 4 * kV; ++x) bad = bad || not_finite2(vr[i][x]);
+                        // (a slot's lanes differ in g: any of them)
+                        const bool unseen = kWin && slot >= p.sinks && slot < min(lo, base);  // (by all rows)
+                        const unsigned who = __ballot_sync(0xFFFFFFFFu, bad && slot < end && (slot >= base || (kWin && !unseen && window_border(slot, p.sinks, lo, pc.n - 1))));
+                        spoilt[i] = (who & (0x11111111u << q4)) != 0;
+                        if (slot >= end || spoilt[i] || unseen) {
+#pragma unroll
+                            for (int x = 0; x < 4 * kV; ++x) vr[i][x] = 0;
+                            f2[i >> 1] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
                         }
-                    } else if (seen && j >= 0)
-                        seen = p.mask == nullptr ? j <= node
-                                                 : j < 32 * p.words && ((p.mask[((size_t)b * p.nmax + node) * p.words + (j >> 5)] >> (j & 31)) & 1);
-                    s[i] = seen ? s[i] : -INFINITY;
-                    sees |= (seen ? 1u : 0u) << i;
+                    }
                 }
-                // V of slots that are not there is taken out, and of new slots that are not numbers: what of those is seen is added in the end
+                // ---- weights, against the maximum known before as long as it has not grown by more than 2^8
+                if (__any_sync(0xFFFFFFFFu, fmaxf(s[0], s[2]) > upto[0] || fmaxf(s[1], s[3]) > upto[1])) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float x = fmaxf(s[i], s[i + 2]);
+                        for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, d));
+                        const float now = fmaxf(m[i], x), k = m[i] > -INFINITY ? ex2_approx((m[i] - now) * c2) : 1.0f;
+                        m[i] = now;
+                        upto[i] = now + most;
+                        off[i] = now > -INFINITY ? -now * c2 : 0.0f;
+                        l[i] *= k;
+#pragma unroll
+                        for (int y = 0; y < D / 16; ++y) o[y][i] *= k, o[y][i + 2] *= k;
+                    }
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int slot = s0 + 2 * q4 + (i & 1) + 8 * (i >> 1);
-                    bool bad = Q8 && (x[i >> 1] >> (16 * (i & 1)) & 255) > 246;  // (up to 480 2^119 is below 2^128)
-                    if (!Q8)
-#pragma unroll
-                        for (int x = 0; x < 4 * kV; ++x) bad = bad || not_finite2(vr[i][x]);
-                    // (a slot's lanes differ in g: any of them)
-                    const bool unseen = kWin && slot >= p.sinks && slot < min(lo, base);  // (by all rows)
-                    const unsigned who = __ballot_sync(0xFFFFFFFFu, bad && slot < end && (slot >= base || (kWin && !unseen && window_border(slot, p.sinks, lo, pc.n - 1))));
-                    spoilt[i] = (who & (0x11111111u << q4)) != 0;
-                    if (slot >= end || spoilt[i] || unseen) {
-#pragma unroll
-                        for (int x = 0; x < 4 * kV; ++x) vr[i][x] = 0;
-                        f2[i >> 1] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-                    }
+                    s[i] = ex2_approx(fmaf(s[i], c2, off[i & 1]));
+                    l[i & 1] += s[i];
                 }
-            }
-            // ---- weights, against the maximum known before as long as it has not grown by more than 2^8
-            if (__any_sync(0xFFFFFFFFu, fmaxf(s[0], s[2]) > upto[0] || fmaxf(s[1], s[3]) > upto[1])) {
+                // P^T as the second operand: rows where the slots were
+                float e[4] = {s[0], s[1], s[2], s[3]};
+                if (Q8)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float x = fmaxf(s[i], s[i + 2]);
-                    for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, d));
-                    const float now = fmaxf(m[i], x), k = m[i] > -INFINITY ? ex2_approx((m[i] - now) * c2) : 1.0f;
-                    m[i] = now;
-                    upto[i] = now + most;
-                    off[i] = now > -INFINITY ? -now * c2 : 0.0f;
-                    l[i] *= k;
+                    for (int i = 0; i < 4; ++i) e[i] *= big[i >> 1];
+                const uint32_t pb0 = transpose_8x8(pack_bf16(e[0], e[1])), pb1 = transpose_8x8(pack_bf16(e[2], e[3]));
+                // ---- O^T += V^T P^T: rows of the first operand are head_dim, two numbers of the lane's D / 8 a product
 #pragma unroll
-                    for (int y = 0; y < D / 16; ++y) o[y][i] *= k, o[y][i + 2] *= k;
+                for (int y0 = 0; y0 < D / 16; y0 += 4) {
+                    uint32_t a[4][2][2];  // [product][slot pair][number]
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int z = 0; z < 2; ++z) {
+                                const int y = y0 + x, byte = (2 * y + z) & 3;
+                                if (Q8) {
+                                    a[x][i][z] = e4m3_pair_small(vr[2 * i][y / 2], vr[2 * i + 1][y / 2], byte, 4 + byte);
+                                } else
+                                    a[x][i][z] = __byte_perm(vr[2 * i][y], vr[2 * i + 1][y], z ? 0x7632 : 0x5410);
+                            }
+                    if (Q8 && large_v)
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) a[x >> 2][x >> 1 & 1][x & 1] = bf16x2_mul(a[x >> 2][x >> 1 & 1][x & 1], f2[x >> 1 & 1]);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) mma_16816(o[y0 + x], a[x][0][0], a[x][0][1], a[x][1][0], a[x][1][1], pb0, pb1);
                 }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s[i] = ex2_approx(fmaf(s[i], c2, off[i & 1]));
-                l[i & 1] += s[i];
-            }
-            // P^T as the second operand: rows where the slots were
-            float e[4] = {s[0], s[1], s[2], s[3]};
-            if (Q8)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] *= big[i >> 1];
-            const uint32_t pb0 = transpose_8x8(pack_bf16(e[0], e[1])), pb1 = transpose_8x8(pack_bf16(e[2], e[3]));
-            // ---- O^T += V^T P^T: rows of the first operand are head_dim, two numbers of the lane's D / 8 a product
-#pragma unroll
-            for (int y0 = 0; y0 < D / 16; y0 += 4) {
-                uint32_t a[4][2][2];  // [product][slot pair][number]
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int z = 0; z < 2; ++z) {
-                            const int y = y0 + x, byte = (2 * y + z) & 3;
-                            if (Q8) {
-                                a[x][i][z] = e4m3_pair_small(vr[2 * i][y / 2], vr[2 * i + 1][y / 2], byte, 4 + byte);
-                            } else
-                                a[x][i][z] = __byte_perm(vr[2 * i][y], vr[2 * i + 1][y], z ? 0x7632 : 0x5410);
-                        }
-                if (Q8 && large_v)
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) a[x >> 2][x >> 1 & 1][x & 1] = bf16x2_mul(a[x >> 2][x >> 1 & 1][x & 1], f2[x >> 1 & 1]);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) mma_16816(o[y0 + x], a[x][0][0], a[x][0][1], a[x][1][0], a[x][1][1], pb0, pb1);
-            }
-            if (more_steps) bring_v(row1);
-            // number y of the lane's of V: o[y / 2][..], [rows + 2 (y & 1)]
-            const auto dim = [&](int y) { return y / kCv * (8 * kCv) + g * kCv + y % kCv; };
-            // ---- new slots whose V is not a number: to the rows that see them
-            if (masked && __any_sync(0xFFFFFFFFu, spoilt[0] || spoilt[1] || spoilt[2] || spoilt[3])) {
+                if (more_steps) bring_v(row1);
+                // number y of the lane's of V: o[y / 2][..], [rows + 2 (y & 1)]
+                const auto dim = [&](int y) { return y / kCv * (8 * kCv) + g * kCv + y % kCv; };
+                // ---- new slots whose V is not a number: to the rows that see them
+                if (masked && __any_sync(0xFFFFFFFFu, spoilt[0] || spoilt[1] || spoilt[2] || spoilt[3])) {
 #pragma unroll 1
-                for (int i = 0; i < 16; ++i) {
-                    const int owner = (i & 7) >> 1, which = (i & 1) + 2 * (i >> 3);
-                    const bool bad = __shfl_sync(0xFFFFFFFFu, which == 0 ? spoilt[0] : which == 1 ? spoilt[1] : which == 2 ? spoilt[2] : spoilt[3], owner);
-                    if (!bad) continue;
-                    const size_t r = row0 + i;
-                    uint32_t fv = 0, mv = kOneBf16x2;
-                    if (Q8) e4m3_factors(__ldg(c.v_exp + r), fv, mv);
-                    const float w0 = __shfl_sync(0xFFFFFFFFu, i < 8 ? s[0] : s[2], (i & 7) * 4 + q4);
-                    const float w1 = __shfl_sync(0xFFFFFFFFu, i < 8 ? s[1] : s[3], (i & 7) * 4 + q4);
-                    // (a weight of a slot that is seen may be too small for fp32 and 0: what it stands before is not a number all the same)
-                    const uint32_t see = __shfl_sync(0xFFFFFFFFu, sees >> (i < 8 ? 0 : 2), (i & 7) * 4 + q4);
+                    for (int i = 0; i < 16; ++i) {
+                        const int owner = (i & 7) >> 1, which = (i & 1) + 2 * (i >> 3);
+                        const bool bad = __shfl_sync(0xFFFFFFFFu, which == 0 ? spoilt[0] : which == 1 ? spoilt[1] : which == 2 ? spoilt[2] : spoilt[3], owner);
+                        if (!bad) continue;
+                        const size_t r = row0 + i;
+                        uint32_t fv = 0, mv = kOneBf16x2;
+                        if (Q8) e4m3_factors(__ldg(c.v_exp + r), fv, mv);
+                        const float w0 = __shfl_sync(0xFFFFFFFFu, i < 8 ? s[0] : s[2], (i & 7) * 4 + q4);
+                        const float w1 = __shfl_sync(0xFFFFFFFFu, i < 8 ? s[1] : s[3], (i & 7) * 4 + q4);
+                        // (a weight of a slot that is seen may be too small for fp32 and 0: what it stands before is not a number all the same)
+                        const uint32_t see = __shfl_sync(0xFFFFFFFFu, sees >> (i < 8 ? 0 : 2), (i & 7) * 4 + q4);
 #pragma unroll
-                    for (int y = 0; y < D / 8; ++y) {
-                        const uint8_t* from = c.v + (r * D + dim(y)) * kBytes;
-                        float v;
-                        if (Q8)
-                            v = __uint_as_float(e4m3x4_to_bf16(*from, fv, mv).x << 16);
-                        else
-                            v = __uint_as_float((uint32_t) * (const uint16_t*)from << 16);
-                        if (see & 1) o[y / 2][2 * (y & 1)] += w0 * v;
-                        if (see & 2) o[y / 2][2 * (y & 1) + 1] += w1 * v;
+                        for (int y = 0; y < D / 8; ++y) {
+                            const uint8_t* from = c.v + (r * D + dim(y)) * kBytes;
+                            float v;
+                            if (Q8)
+                                v = __uint_as_float(e4m3x4_to_bf16(*from, fv, mv).x << 16);
+                            else
+                                v = __uint_as_float((uint32_t) * (const uint16_t*)from << 16);
+                            if (see & 1) o[y / 2][2 * (y & 1)] += w0 * v;
+                            if (see & 2) o[y / 2][2 * (y & 1) + 1] += w1 * v;
+                        }
                     }
                 }
+                row0 = row1;
             }
-            row0 = row1;
-        }
+        };
+        if (Q8 && q_wide)
+            steps_of_piece(Yes());
+        else
+            steps_of_piece(No());
         // ---- the warps' sums are joined
 #pragma unroll
         for (int i = 0; i < 2; ++i) {

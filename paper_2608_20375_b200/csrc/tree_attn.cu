@@ -116,12 +116,6 @@ __device__ __forceinline__ void tmem_arrived(uint32_t (&r)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
 }
-struct Yes {
-    static constexpr bool value = true;
-};
-struct No {
-    static constexpr bool value = false;
-};
 // two fp32 numbers in a 64-bit register
 __device__ __forceinline__ uint64_t two(float lo, float hi) {
     uint64_t r;
