@@ -8,7 +8,9 @@ missing or a call fails, a GraftError is raised.
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
+import warnings
 from dataclasses import dataclass
 
 import torch
@@ -138,14 +140,25 @@ def load_library():
     lib.graft_status_str.argtypes = [C.c_int]
     lib.graft_status_str.restype = C.c_char_p
     lib.graft_version.restype = C.c_char_p
-    try:
-        from . import _marshal
-        _marshal.bind(*(C.cast(f, vp).value for f in (lib.graft_cache_write, lib.graft_cache_read, lib.graft_cache_append, lib.graft_window_attention)))
-        _fast = _marshal
-    except ImportError:  # (another torch than the one that it was built with)
-        _fast = None
+    _fast = _load_marshal(lib)
     _lib = lib
     return lib
+
+
+def _load_marshal(lib):
+    path = _build.build_marshal()
+    if path is None:
+        return None
+    try:
+        spec = importlib.util.spec_from_file_location(f"{__package__}._marshal", path)
+        marshal = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(marshal)
+    except ImportError as e:
+        warnings.warn(f"the binding's compiled checks could not be loaded, calls check their arguments in Python: {e}")
+        return None
+    marshal.bind(*(C.cast(f, C.c_void_p).value
+                   for f in (lib.graft_cache_write, lib.graft_cache_read, lib.graft_cache_append, lib.graft_window_attention)))
+    return marshal
 
 
 def _check(lib, rc, what):
