@@ -60,10 +60,8 @@ struct Shape {
     // registers a thread: the softmax's eight warps take over what the others leave (of what the launch has)
     static constexpr int kRegsLaunch = Q8 ? 96 : 168;
     static constexpr int kRegsSoftmax = Q8 ? 168 : 224, kRegsOthers = Q8 ? 48 : 56;
-    static constexpr int kRegsSoftmaxHalves = Q8 ? 144 : 200, kRegsOthersHalves = Q8 ? 64 : 104;  // (scores of half a tile at a time)
     static constexpr int kCols = Q8 ? 64 : 128;  // scores that a softmax thread holds at a time
-    static_assert(256 * kRegsSoftmax + (kThreads - 256) * kRegsOthers <= kThreads * kRegsLaunch &&
-                  256 * kRegsSoftmaxHalves + (kThreads - 256) * kRegsOthersHalves <= kThreads * kRegsLaunch, "registers of a launch");
+    static_assert(256 * kRegsSoftmax + (kThreads - 256) * kRegsOthers <= kThreads * kRegsLaunch, "registers of a launch");
     static constexpr size_t kSmem = 1024 + kQTiles * kTileBytes + (size_t)kStages * kTileBytes + (size_t)kRaw * kRawBytes + 1024;
 };
 
@@ -343,6 +341,8 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
     // of 64 slots cost 48 cycles in place of 32: 521 against 490, 780 against 728.  Without a window scores of e4m3 slots are whole tiles' too, which keeps sums in
     // the order that they have had.
     constexpr int kSub = kWin && Q8 ? 64 : kTile, kSubs = kTile / kSub;
+    constexpr int kRegsSoftmax = kSubs > 1 ? 144 : S::kRegsSoftmax, kRegsOthers = kSubs > 1 ? 64 : S::kRegsOthers;
+    static_assert(256 * kRegsSoftmax + (S::kThreads - 256) * kRegsOthers <= S::kThreads * S::kRegsLaunch, "registers of a launch");
     static_assert(NS / 2 < kCleared, "tiles that the streams may be apart");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base_addr = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
     };
 
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSubs > 1 ? S::kRegsSoftmaxHalves : S::kRegsSoftmax));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
         // ---- softmax: a thread a row
         const int i = warp >> 2, row_in_tile = tid & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the lanes
@@ -738,7 +738,7 @@ __global__ void __launch_bounds__(Shape<D, Q8, kOne>::kThreads, 1) tree_attn_ker
             piece_done(n_piece);
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kSubs > 1 ? S::kRegsOthersHalves : S::kRegsOthers));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOthers));
         uint32_t n_piece = 0;
         bool ok = true;
         if (warp == 11) {
