@@ -354,7 +354,7 @@ graft_status graft_cache_append(graft_ctx* ctx, int32_t batch, const graft_cache
  *   d_position are both given or both NULL.  Row i sees what graft_tree_attention lets it see, of that the positions from sinks on only
  *   where they are less than `window` behind its own (window >= 1: its own is the first; sinks >= 0).
  * Pages that hold no slot below `sinks` and none from d_prefix_len[b] - window on are not read, nor are their entries of the table:
- * a server may take back what fell behind the window.  The other arguments, what is not a number, the scratch and the precision are as
+ * a server may take back what fell behind the window.  The other arguments, what is not a number, the scratch (and 32 bytes a block of rows) and the precision are as
  * described there; behind many rows without a mask (prompts) each block of rows goes through its own slots alone. */
 graft_status graft_window_attention(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer, int32_t q_heads, int32_t rows,
                                     int64_t q_stride, const void* d_q, float scale, const int32_t* d_prefix_len, const int32_t* d_count,

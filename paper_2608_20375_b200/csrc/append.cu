@@ -7,9 +7,9 @@
 // tokens' pairs once, into shared memory, for all of their heads.  Rotated numbers are fp32 and are rounded once: to bf16, or, into an e4m3
 // cache, to e4m3 with the row's exponent taken from the fp32 numbers.
 //
-// What bounds it.  Every number is read and written once: 8 prompts of up to 8192 rows, 32 query heads on 8 of 128, 904 MB, 162 us: 5.6 TB/s, 0.85 of a plain copy's rate,
+// What bounds it.  Every number is read and written once: 8 prompts of up to 8192 rows, 32 query heads on 8 of 128, 904 MB, 162 us: 5.6 TB/s, 0.85 of a plain copy's rate (into an e4m3 cache 829 MB, 159 us),
 // with two rows a thread under way (one row a thread that was asked for behind the table and the angles: 209 us).  Clips of three axes 47 us (68 before).  64 trees'
-// rows into an e4m3 cache and back 25 us, one tree 3.4: chains of loads (count, table, rows).
+// rows into an e4m3 cache 15.4 us (bytes: 9.0), one tree 3.4: blocks of four tokens, two and a half to a place on an SM, each behind its chain of count, table and angles.
 #include <cuda_bf16.h>
 
 #include "cache.cuh"

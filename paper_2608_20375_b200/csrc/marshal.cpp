@@ -1,5 +1,5 @@
-// Arguments of the calls whose checks and conversions in Python would take longer than their work on the GPU (one tree's append: 3.4 us there, 9 in
-// Python).  Each function takes what the binding's method of the same name takes, checks it as the method does and makes the call: the call's status, or
+// Arguments of the calls whose checks and conversions in Python take longer than their work on the GPU.  One tree's append, 3.4 us on the GPU: 15.1 us a call
+// in a loop with the checks in Python, 4.2 with these.  Each function takes what the binding's method of the same name takes, checks it as the method does and makes the call: the call's status, or
 // None when a check fails (nothing has been done then, and the method finds the reason).
 #include <torch/csrc/autograd/python_variable.h>
 

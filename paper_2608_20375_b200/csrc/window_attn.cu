@@ -6,9 +6,9 @@
 // there are masked row by row, and V of places that only some rows see is looked at for what is not a number, as V of new rows is.
 //
 // What bounds it.  One token behind a window of 4096: 12.4 us, latencies (the floor is 2.6); 64 of them over e4m3 slots 114 us, 0.73 of the copy's rate (83).
-// 32 trees of up to 65 nodes, window 1024: 73 us (10 of them this plan's launch, 9 the join); 16 of up to 513, window 4096, e4m3, head_dim 64: 538; 4 prompts of up to 8192, window 1024: 505 to 530, tensor cores
-// busy for 36 %; a prompt of 12000, window 4001: 670 to 740 by the clock that power leaves.  Beside the chain of scores, exponentials and products that tree_attn.cu
-// describes it is the borders: masked tiles cost 9 to 17 % (three of ten tiles behind a window of 1024), and a unit's beginning and end as long as three tiles.
+// 32 trees of up to 65 nodes, window 1024: 73 us (10 of them this plan's launch, 9 the join); 16 of up to 513, window 4096, e4m3, head_dim 64: 538; 4 prompts of up to 8192, window 1024: 505 to 550, tensor cores
+// busy for 36 %, over e4m3 slots 630; a prompt of 12000, window 4001: 670 to 740 by the clock that power leaves, over e4m3 slots 885 (tiles are converted for every unit of 36 rows).  Beside the chain of scores, exponentials and products that tree_attn.cu
+// describes it is the borders: masked tiles cost 9 to 17 % (two of nine tiles behind a window of 1024, four to six of 35 to 37 of a tree of 257 to 513), and a unit's beginning and end as long as three tiles.
 // Chains go in blocks of as many rows as make a unit of 256: smaller blocks would mask less and bring K and V more often, at half-empty row tiles.
 #include "attn.cuh"
 
