@@ -340,7 +340,7 @@ typedef struct graft_rope {
 /* The new rows of one layer on their way to attention, in one call: queries and keys are turned by their positions, keys and values go into the
  * cache as graft_cache_write does it.  d_q [batch, rows, q_heads, head_dim] bf16 with row stride q_stride, d_q_out with out_stride (the same array
  * with the same stride, or one apart from all others); d_key, d_value as graft_cache_write's, kv_stride.  q_heads 0: no queries (d_q,
- * d_q_out NULL).  Angles are worked out in fp64 and reduced before they are rounded to fp32; turned numbers are fp32 and rounded once: to bf16, or into
+ * d_q_out NULL).  Angles, cosines and sines are worked out in fp64, the latter rounded to fp32; turned numbers are fp32 and rounded once: to bf16, or into
  * an e4m3 cache by its rule applied to the fp32 numbers.  Rows behind the count, and of sequences that are left out, are in no result and nothing of theirs
  * is written.  Strides are multiples of 8, rows 16-byte aligned. */
 graft_status graft_cache_append(graft_ctx* ctx, int32_t batch, const graft_cache* cache, int32_t layer, const graft_rope* rope, int32_t q_heads,

@@ -2,8 +2,9 @@
 // and values go into the paged cache.
 //
 // Pair i of a head, (x, y), becomes gain (x cos a - y sin a, x sin a + y cos a) with a = sum over axes of (position + shift) freq[axis, i].
-// A position may be far out and a frequency is up to a turn a step, so angles are worked out in fp64 and taken modulo a turn before
-// they become fp32: a position of 2^24 then costs no more precision than position 1.  A block works out the cosines and sines of its
+// A position may be far out and a frequency is up to a turn a step, so angles, their cosines and sines are worked out in fp64, modulo a turn: a
+// position of 2^24 costs no more precision than position 1.  (Turns in fp32 into sincospif: twice as many results rounded to the other side as
+// with cosines and sines that are right to half a step of fp32; the fp64 pair costs 0.5 % of a prompt's time.)  A block works out the cosines and sines of its
 // tokens' pairs once, into shared memory, for all of their heads.  Rotated numbers are fp32 and are rounded once: to bf16, or, into an e4m3
 // cache, to e4m3 with the row's exponent taken from the fp32 numbers.
 //
@@ -112,9 +113,9 @@ __global__ void __launch_bounds__(kThreads, 3) cache_append_kernel(const __grid_
             angle += (double)at * (double)p.freq[a * p.pairs + i];
         }
         const double turns = angle * 0.15915494309189535;  // 1 / (2 pi)
-        float s, co;
-        sincospif(2.0f * (float)(turns - rint(turns)), &s, &co);
-        ((float2*)&turn[t][(i >> 1) & 3][i >> 3])[i & 1] = make_float2(co * p.gain, s * p.gain);
+        double s, co;
+        sincospi(2.0 * (turns - rint(turns)), &s, &co);
+        ((float2*)&turn[t][(i >> 1) & 3][i >> 3])[i & 1] = make_float2((float)co * p.gain, (float)s * p.gain);
     }
     if (tid < tokens) {
         const int slot = base + first + tid;
